@@ -1,0 +1,655 @@
+// Attention of one new token per sequence over a paged cache (stom_kv_attend).
+//
+//   out = sum_t exp(x_t) V_t / sum_t exp(x_t),  x_t = scale <q, K_t>, capped if asked for, t over the sequence's tokens.
+//
+// What bounds it: every key and value row is read once and takes part in 4 * (query heads per kv head) flops per
+// element, 14 flops per byte at 7 heads: memory, by a wide margin, as long as the products run on the tensor cores
+// (the scalar units would need 45 of their 75 TFLOP/s).  The kernel is therefore built around keeping loads in flight.
+//
+// Split.  The work is one line of TILES of 16 tokens: sequence by sequence, within one head by head (a UNIT is one
+// (sequence, kv head)), within one along the tokens.  Every warp of a grid of one block per multiprocessor takes an
+// equal, contiguous stretch of that line, so unequal lengths need no planning on the host and a single long stream uses
+// the whole device.  A warp is alone with its stretch: its own ring of tiles in shared memory, filled by 16-byte
+// asynchronous copies (any page size, any strides; a tile's rows may lie in 16 pages), its own running maximum and sum,
+// no barrier between warps.  A unit that a warp holds whole goes straight to the output.  Pieces of a unit are joined
+// first within the block (shared memory), then, for the at most one unit that crosses each block's end, by a second
+// small kernel over a workspace of two partial results per block.
+//
+// Products.  Transposed, so that the up to 8 query heads of a kv head are the 8 columns of an m16n8k16 product and
+// the 16 tokens, respectively 16 channels, its rows: S^T = K q^T with K as stored, O^T = V^T P^T with V transposed on
+// the way out of shared memory (ldmatrix.trans).  Scores and accumulators then have their head in the same thread, so
+// that rescaling needs no exchange.  The softmax weights go into the second product as a high and a low 16-bit part
+// (2^-17 relative at bf16): one part alone would add an error of the size of the output's own rounding, and the
+// second costs nothing in a kernel that waits for memory.
+#include "stom_kv.cuh"
+
+namespace stom {
+
+namespace {
+
+constexpr int kTile = 16;         // tokens per tile
+constexpr int kMaxBlocks = 256;   // blocks of the grid the workspace has room for
+
+struct KvAttendParams {
+    const char *k, *v;            // at the layer
+    int64_t stride_page, stride_token, stride_head;
+    const int32_t *table;
+    const int32_t *len;
+    int64_t table_stride;
+    int32_t n_seqs, n_pages, max_tokens;
+    FastDiv page;
+    int32_t n_kv_heads, group;    // query heads per kv head
+    int32_t blocks_per_head;      // blocks of 8 * NT query heads a kv head's group is cut into
+    const char *q;
+    int64_t q_stride_seq, q_stride_head;
+    float scale, cap;             // softmax scale; cap <= 0: none
+    int32_t window;
+    char *out;
+    int64_t out_stride_seq, out_stride_head;
+    float *lse;
+    float *part_o;                // [blocks][2][8 NT][d]
+    float2 *part_ml;              // [blocks][2][8 NT]: maximum and sum
+    int32_t *open_unit;           // [blocks]: unit that begins in the block and goes on behind it, or -1
+    int32_t *goes_on;             // [blocks]: the unit that came in from the block before goes on behind this one too
+    uint32_t *flags;
+};
+
+template <int D, int NT>
+struct Shape {
+    static constexpr int kHeads = 8 * NT;
+    static constexpr int kWarps = D == 64 ? (NT == 1 ? 16 : 12) : D == 128 ? (NT == 1 ? 8 : 6) : 4;
+    static constexpr int kStages = 3;
+    static constexpr int kRow = D * 2;                       // bytes of a row
+    static constexpr int kTileBytes = kTile * kRow;          // of keys or of values
+    static constexpr int kRing = kStages * 2 * kTileBytes;   // per warp
+    static constexpr int kPiece = kHeads * D * 4;            // a partial result
+    static constexpr int kPieces = 2 * kWarps;
+    static constexpr int kSmem = kWarps * (kRing + kPiece) + kPieces * (kHeads * 8 + 8);
+    static_assert(kPiece <= kRing, "a warp's last piece lies in its ring");
+    static_assert(kSmem <= 227 * 1024, "shared memory");
+};
+
+__device__ __forceinline__ void span_of(const KvAttendParams &p, int b, int &first, int &end) {
+    end = min(max(p.len[b], 0), p.max_tokens);
+    first = p.window > 0 ? max(0, end - p.window) : 0;
+}
+__device__ __forceinline__ int tiles_of(const KvAttendParams &p, int b) {
+    int first, end;
+    span_of(p, b, first, end);
+    return (end - first + kTile - 1) / kTile;
+}
+
+// A place on the line of tiles.
+struct Cursor {
+    int b, hu;          // sequence, head block
+    int tile, tiles;    // within the unit
+    int first, end;     // token range of the sequence
+};
+
+__device__ __forceinline__ void next_seq(const KvAttendParams &p, Cursor &c) {
+    c.tiles = 0;
+    while (c.tiles == 0 && ++c.b < p.n_seqs) {
+        span_of(p, c.b, c.first, c.end);
+        c.tiles = (c.end - c.first + kTile - 1) / kTile;
+    }
+}
+__device__ __forceinline__ void advance(const KvAttendParams &p, int units, Cursor &c) {
+    if (++c.tile < c.tiles) return;
+    c.tile = 0;
+    if (++c.hu < units) return;
+    c.hu = 0;
+    next_seq(p, c);
+}
+
+// Output rows of unit (b, hu): query head and count of heads.
+__device__ __forceinline__ int heads_of(const KvAttendParams &p, int hu, int per, int &head0) {
+    const int h = hu / p.blocks_per_head, j = hu - h * p.blocks_per_head;
+    head0 = h * p.group + j * per;
+    return min(per, p.group - j * per);
+}
+
+template <typename T, int D, int NT>
+__global__ void __launch_bounds__(Shape<D, NT>::kWarps * 32, 1) kv_attend_kernel(const __grid_constant__ KvAttendParams p) {
+    using S = Shape<D, NT>;
+    constexpr int kWarps = S::kWarps, kHeads = S::kHeads, kStages = S::kStages;
+    constexpr int kKs = D / 16;                      // steps of the first product, row blocks of the second
+    constexpr int kChunks = D / 8;                   // 16-byte chunks of a row
+    constexpr int kRowsPerCopy = 32 / kChunks;       // rows one warp-wide copy covers
+    extern __shared__ __align__(16) uint8_t smem[];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    uint8_t *ring = smem + warp * S::kRing;
+    float *first_piece = reinterpret_cast<float *>(smem + kWarps * S::kRing + warp * S::kPiece);
+    float2 *piece_ml = reinterpret_cast<float2 *>(smem + kWarps * (S::kRing + S::kPiece));  // [2 kWarps][kHeads]
+    int *piece_unit = reinterpret_cast<int *>(piece_ml + S::kPieces * kHeads);              // [2 kWarps], -1: none
+    int *piece_ends = piece_unit + S::kPieces;  // bit 0: holds the unit's first tile, bit 1: its last
+
+    if (lane < 2) piece_unit[2 * warp + lane] = -1;
+    grid_dependency_wait();
+
+    // ---- the stretch of this warp
+    const int units = p.n_kv_heads * p.blocks_per_head;   // per sequence
+    const int seg = (p.n_seqs + 31) / 32;                 // sequences a lane adds up
+    long long mine = 0;
+    for (int b = lane * seg; b < min(p.n_seqs, (lane + 1) * seg); ++b) mine += tiles_of(p, b);
+    mine *= units;
+    long long upto = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const long long v = __shfl_up_sync(~0u, upto, o);
+        if (lane >= o) upto += v;
+    }
+    const long long total = __shfl_sync(~0u, upto, 31);
+    const long long warps = (long long)gridDim.x * kWarps;
+    const long long per = max(1ll, (total + warps - 1) / warps);
+    const long long f0 = min(total, ((long long)blockIdx.x * kWarps + warp) * per), f1 = min(total, f0 + per);
+    int left = (int)(f1 - f0);
+
+    // the empty sequences: zeros
+    for (int b = blockIdx.x * kWarps + warp; b < p.n_seqs; b += gridDim.x * kWarps) {
+        if (tiles_of(p, b)) continue;
+        const int heads = p.n_kv_heads * p.group;
+        for (int h = 0; h < heads; ++h) {
+            T *o = reinterpret_cast<T *>(p.out) + b * p.out_stride_seq + h * p.out_stride_head;
+            for (int c = lane; c < D / 2; c += 32) reinterpret_cast<uint32_t *>(o)[c] = 0u;
+            if (p.lse && lane == 0) p.lse[(int64_t)b * heads + h] = -INFINITY;
+        }
+    }
+
+    int pieces = 0;   // partial results this warp leaves in shared memory
+    if (left > 0) {
+        // the sequence, head block and tile of f0
+        Cursor cur;
+        {
+            const uint32_t past = __ballot_sync(~0u, upto > f0);
+            const int at = __ffs(past) - 1;                       // the lane whose sequences hold it
+            long long before = __shfl_sync(~0u, upto - mine, at);
+            int b = at * seg;
+            const int end = min(p.n_seqs, b + seg);
+            for (;; b += 32) {                                    // 32 of them at a time
+                const int t = b + lane < end ? tiles_of(p, b + lane) : 0;
+                long long sum = (long long)t * units;
+                const long long own = sum;
+#pragma unroll
+                for (int o = 1; o < 32; o <<= 1) {
+                    const long long v = __shfl_up_sync(~0u, sum, o);
+                    if (lane >= o) sum += v;
+                }
+                const uint32_t hit = __ballot_sync(~0u, before + sum > f0);
+                if (hit || b + 32 >= end) {
+                    const int j = hit ? __ffs(hit) - 1 : 0;
+                    before += __shfl_sync(~0u, sum - own, j);
+                    cur.b = b + j;
+                    break;
+                }
+                before += __shfl_sync(~0u, sum, 31);
+            }
+            span_of(p, cur.b, cur.first, cur.end);
+            cur.tiles = (cur.end - cur.first + kTile - 1) / kTile;
+            const long long in = f0 - before;
+            cur.hu = (int)(in / cur.tiles);
+            cur.tile = (int)(in - (long long)cur.hu * cur.tiles);
+        }
+
+        // ---- loads.  Lane r (and r + 16) looks up the page of row r one tile ahead of the copies.
+        Cursor ld = cur;
+        int ld_left = left;
+        int page_id = -1, page_off = 0;
+        auto look_up = [&]() {
+            const int t = ld.first + ld.tile * kTile + (lane & 15);
+            page_id = -1;
+            if (ld_left > 0 && t < ld.end) {
+                const uint32_t pg = div_by(p.page, (uint32_t)t);
+                page_off = t - (int)(pg * p.page.d);
+                page_id = p.table[ld.b * p.table_stride + pg];
+            } else {
+                page_id = -2;   // not a token
+            }
+        };
+        uint64_t seen = 0;       // 16 bits per tile in flight, oldest lowest: which rows are tokens
+        int in_flight = 0;
+        const uint32_t ring_u = smem_u32(ring);
+        auto issue = [&](int stage) {
+            if (ld_left > 0) {
+                const bool ok = (uint32_t)page_id < (uint32_t)p.n_pages;
+                if (page_id != -2 && !ok && p.flags) atomicOr(p.flags, STOM_FLAG_BAD_INDEX);
+                const uint32_t m = __ballot_sync(~0u, ok) & 0xffffu;
+                seen |= (uint64_t)m << (16 * in_flight);
+                ++in_flight;
+                const int64_t off = ok ? 2 * (page_id * p.stride_page + page_off * p.stride_token +
+                                              (ld.hu / p.blocks_per_head) * p.stride_head)
+                                       : -1;
+                const uint32_t dst = ring_u + stage * (2 * S::kTileBytes);
+                const int sub = lane / kChunks, chunk = lane % kChunks;
+#pragma unroll
+                for (int i = 0; i < kTile / kRowsPerCopy; ++i) {
+                    const int row = i * kRowsPerCopy + sub;
+                    const int64_t o = __shfl_sync(~0u, off, row);
+                    const uint32_t d = dst + row * S::kRow + ((chunk ^ (row & 7)) << 4);
+                    const int64_t at = (o < 0 ? 0 : o) + chunk * 16;
+                    copy16_async(d, p.k + at, o < 0 ? 0u : 16u);
+                    copy16_async(d + S::kTileBytes, p.v + at, o < 0 ? 0u : 16u);
+                }
+                --ld_left;
+                if (ld_left > 0) advance(p, units, ld);
+                look_up();
+            }
+            copy_commit();
+        };
+        look_up();
+#pragma unroll
+        for (int i = 0; i < kStages - 1; ++i) issue(i);
+
+        // ---- per-unit state
+        uint32_t qf[kKs][NT][2];
+        float o_acc[kKs][NT][4];
+        float m_run[NT][2], l_run[NT][2];
+        bool fresh = true, whole_from = false;
+        const float log2e = 1.4426950408889634f;
+        const float s1 = p.cap > 0.f ? p.scale / p.cap : p.scale * log2e;
+        const float s2 = p.cap * log2e;
+        int stage = 0;
+
+        while (left > 0) {
+            if (fresh) {
+                int head0;
+                const int nh = heads_of(p, cur.hu, kHeads, head0);
+                const T *q = reinterpret_cast<const T *>(p.q) + cur.b * p.q_stride_seq;
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    const int h = n * 8 + (lane >> 2);
+                    const T *row = q + (head0 + (h < nh ? h : 0)) * p.q_stride_head + (lane & 3) * 2;
+#pragma unroll
+                    for (int ks = 0; ks < kKs; ++ks) {
+                        qf[ks][n][0] = h < nh ? *reinterpret_cast<const uint32_t *>(row + ks * 16) : 0u;
+                        qf[ks][n][1] = h < nh ? *reinterpret_cast<const uint32_t *>(row + ks * 16 + 8) : 0u;
+                    }
+#pragma unroll
+                    for (int ks = 0; ks < kKs; ++ks)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) o_acc[ks][n][e] = 0.f;
+                    m_run[n][0] = m_run[n][1] = -INFINITY;
+                    l_run[n][0] = l_run[n][1] = 0.f;
+                }
+                whole_from = cur.tile == 0;
+                fresh = false;
+            }
+
+            copy_wait<kStages - 2>();
+            __syncwarp();
+            issue(stage == 0 ? kStages - 1 : stage - 1);   // into the slot the tile before this one has left
+
+            const uint32_t kt = ring_u + stage * (2 * S::kTileBytes), vt = kt + S::kTileBytes;
+            const uint32_t rows = (uint32_t)seen & 0xffffu;
+            seen >>= 16;
+            --in_flight;
+
+            // S^T = K q^T, in two chains of products
+            float s[NT][2][4];
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[n][0][e] = s[n][1][e] = 0.f;
+            {
+                const int row = (lane & 7) + ((lane >> 3) & 1) * 8;
+#pragma unroll
+                for (int ks = 0; ks < kKs; ++ks) {
+                    uint32_t a[4];
+                    ldsm4(a, kt + row * S::kRow + (((2 * ks + (lane >> 4)) ^ (row & 7)) << 4));
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) mma16x8x16<T>(s[n][ks & 1], a, qf[ks][n][0], qf[ks][n][1]);
+                }
+            }
+            const bool in0 = (rows >> (lane >> 2)) & 1u, in1 = (rows >> ((lane >> 2) + 8)) & 1u;
+            float alpha[NT][2];
+            uint32_t ph[NT][2], pl[NT][2];
+            bool moved = false;
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                float x[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    x[e] = (s[n][0][e] + s[n][1][e]) * s1;
+                    if (p.cap > 0.f) x[e] = s2 * tanhf(x[e]);
+                    if (!(e < 2 ? in0 : in1)) x[e] = -INFINITY;
+                }
+                float top[2] = {fmaxf(x[0], x[2]), fmaxf(x[1], x[3])};
+#pragma unroll
+                for (int o = 4; o < 32; o <<= 1) {
+                    top[0] = fmaxf(top[0], __shfl_xor_sync(~0u, top[0], o));
+                    top[1] = fmaxf(top[1], __shfl_xor_sync(~0u, top[1], o));
+                }
+                float w[4];
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    const float m = fmaxf(m_run[n][c], top[c]);
+                    const float base = m == -INFINITY ? 0.f : m;
+                    moved |= m > m_run[n][c];
+                    alpha[n][c] = exp2f(m_run[n][c] - base);
+                    m_run[n][c] = m;
+                    w[c] = exp2f(x[c] - base);
+                    w[c + 2] = exp2f(x[c + 2] - base);
+                    l_run[n][c] = l_run[n][c] * alpha[n][c] + w[c] + w[c + 2];
+                }
+#pragma unroll
+                for (int r = 0; r < 2; ++r) {
+                    const uint32_t hi = pack2<T>(w[2 * r], w[2 * r + 1]);
+                    float h0, h1;
+                    unpack2<T>(hi, h0, h1);
+                    ph[n][r] = transpose8x8(hi);
+                    pl[n][r] = transpose8x8(pack2<T>(w[2 * r] - h0, w[2 * r + 1] - h1));
+                }
+            }
+            if (__any_sync(~0u, moved)) {
+#pragma unroll
+                for (int ks = 0; ks < kKs; ++ks)
+#pragma unroll
+                    for (int n = 0; n < NT; ++n)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) o_acc[ks][n][e] *= alpha[n][e & 1];
+            }
+            // O^T += V^T P^T
+            {
+                const int row = (lane & 7) + (lane >> 4) * 8;
+#pragma unroll
+                for (int ks = 0; ks < kKs; ++ks) {
+                    uint32_t a[4];
+                    ldsm4_trans(a, vt + row * S::kRow + (((2 * ks + ((lane >> 3) & 1)) ^ (row & 7)) << 4));
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) {
+                        mma16x8x16<T>(o_acc[ks][n], a, ph[n][0], ph[n][1]);
+                        mma16x8x16<T>(o_acc[ks][n], a, pl[n][0], pl[n][1]);
+                    }
+                }
+            }
+            stage = stage + 1 == kStages ? 0 : stage + 1;
+            --left;
+
+            const bool last = cur.tile + 1 == cur.tiles;
+            if (last || left == 0) {
+                // the unit's end, or the stretch's
+                int head0;
+                const int nh = heads_of(p, cur.hu, kHeads, head0);
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int c = 0; c < 2; ++c)
+#pragma unroll
+                        for (int o = 4; o < 32; o <<= 1) l_run[n][c] += __shfl_xor_sync(~0u, l_run[n][c], o);
+                if (last && whole_from) {
+#pragma unroll
+                    for (int n = 0; n < NT; ++n)
+#pragma unroll
+                        for (int c = 0; c < 2; ++c) {
+                            const int h = n * 8 + (lane & 3) * 2 + c;
+                            if (h >= nh) continue;
+                            T *o = reinterpret_cast<T *>(p.out) + cur.b * p.out_stride_seq +
+                                   (head0 + h) * p.out_stride_head + (lane >> 2);
+                            const float inv = l_run[n][c] > 0.f ? 1.f / l_run[n][c] : l_run[n][c] == 0.f ? 0.f : l_run[n][c];
+#pragma unroll
+                            for (int ks = 0; ks < kKs; ++ks) {
+                                o[ks * 16] = from_float<T>(o_acc[ks][n][c] * inv);
+                                o[ks * 16 + 8] = from_float<T>(o_acc[ks][n][c + 2] * inv);
+                            }
+                            if (p.lse && lane < 4)
+                                p.lse[(int64_t)cur.b * (p.n_kv_heads * p.group) + head0 + h] =
+                                    l_run[n][c] == 0.f ? -INFINITY : 0.6931471805599453f * m_run[n][c] + logf(l_run[n][c]);
+                        }
+                } else {
+                    // a piece: a warp's first in its own place, its last (if it has two) in its ring, which no copy
+                    // is on its way to any more
+                    const int slot = 2 * warp + pieces;
+                    float *dst = pieces ? reinterpret_cast<float *>(ring) : first_piece;
+                    __syncwarp();
+#pragma unroll
+                    for (int n = 0; n < NT; ++n)
+#pragma unroll
+                        for (int c = 0; c < 2; ++c) {
+                            const int h = n * 8 + (lane & 3) * 2 + c;
+#pragma unroll
+                            for (int ks = 0; ks < kKs; ++ks) {
+                                dst[h * D + ks * 16 + (lane >> 2)] = o_acc[ks][n][c];
+                                dst[h * D + ks * 16 + 8 + (lane >> 2)] = o_acc[ks][n][c + 2];
+                            }
+                            if (lane < 4) piece_ml[slot * kHeads + h] = make_float2(m_run[n][c], l_run[n][c]);
+                        }
+                    if (lane == 0) {
+                        piece_unit[slot] = cur.b * units + cur.hu;
+                        piece_ends[slot] = (whole_from ? 1 : 0) | (last ? 2 : 0);
+                    }
+                    ++pieces;
+                }
+                fresh = true;
+            }
+            if (left > 0) advance(p, units, cur);
+        }
+        copy_wait<0>();
+    }
+    __syncthreads();
+
+    // ---- join the block's pieces, unit by unit; they stand in the order of the line
+    int open_unit = -1, goes_on = 0;
+    for (int i = 0; i < S::kPieces;) {
+        const int unit = piece_unit[i];
+        if (unit < 0) {
+            ++i;
+            continue;
+        }
+        int ends = 0, n = 0, e = i;
+        for (; e < S::kPieces && (piece_unit[e] == unit || piece_unit[e] < 0); ++e) {
+            if (piece_unit[e] < 0) continue;
+            if (n == 0) ends |= piece_ends[e] & 1;
+            ends = (ends & 1) | (piece_ends[e] & 2);
+            ++n;
+        }
+        const int b = unit / units, hu = unit - b * units;
+        int head0;
+        const int nh = heads_of(p, hu, kHeads, head0);
+        const int slot = ends & 1 ? 1 : 0;   // of the workspace: a unit that came in, or one that goes out
+        if (!(ends & 2)) {
+            if (ends & 1) open_unit = unit;
+            else goes_on = 1;
+        }
+        for (int at = threadIdx.x; at < nh * D; at += kWarps * 32) {
+            const int h = at / D, c = at % D;
+            float m = -INFINITY;
+            for (int j = i; j < e; ++j)
+                if (piece_unit[j] >= 0) m = fmaxf(m, piece_ml[j * kHeads + h].x);
+            const float base = m == -INFINITY ? 0.f : m;
+            float l = 0.f, o = 0.f;
+            for (int j = i; j < e; ++j) {
+                if (piece_unit[j] < 0) continue;
+                const float2 ml = piece_ml[j * kHeads + h];
+                const float f = exp2f(ml.x - base);
+                const uint8_t *src = j & 1 ? smem + (j >> 1) * S::kRing : smem + kWarps * S::kRing + (j >> 1) * S::kPiece;
+                l += f * ml.y;
+                o += f * reinterpret_cast<const float *>(src)[h * D + c];
+            }
+            if (ends == 3) {
+                reinterpret_cast<T *>(p.out)[b * p.out_stride_seq + (head0 + h) * p.out_stride_head + c] =
+                    from_float<T>(l == 0.f ? 0.f : o / l);
+                if (p.lse && c == 0)
+                    p.lse[(int64_t)b * (p.n_kv_heads * p.group) + head0 + h] =
+                        l == 0.f ? -INFINITY : 0.6931471805599453f * m + logf(l);
+            } else {
+                const int64_t w = ((int64_t)blockIdx.x * 2 + slot) * kHeads + h;
+                p.part_o[w * D + c] = o;
+                if (c == 0) p.part_ml[w] = make_float2(m, l);
+            }
+        }
+        i = e;
+    }
+    if (threadIdx.x == 0) {
+        p.open_unit[blockIdx.x] = open_unit;
+        p.goes_on[blockIdx.x] = goes_on;
+    }
+}
+
+// Joins the partial results of the units that cross a block's end: block (x, h) of this grid takes query head h of the
+// unit that begins in block x of the kernel above and goes on behind it, if there is one.
+template <typename T, int D, int NT>
+__global__ void __launch_bounds__(D) kv_attend_join_kernel(const __grid_constant__ KvAttendParams p) {
+    constexpr int kHeads = 8 * NT;
+    __shared__ float weight[kMaxBlocks];
+    __shared__ float head_m[32], head_l[32];
+    grid_dependency_wait();
+    const int first = blockIdx.x, h = blockIdx.y, blocks = gridDim.x;
+    const int unit = p.open_unit[first];
+    if (unit < 0) return;
+    const int units = p.n_kv_heads * p.blocks_per_head;
+    const int b = unit / units, hu = unit - b * units;
+    int head0;
+    if (h >= heads_of(p, hu, kHeads, head0)) return;
+    // the blocks it goes through: first, first + 1, ..., end - 1
+    __shared__ int end_s;
+    if (threadIdx.x == 0) end_s = blocks;
+    __syncthreads();
+    for (int j = first + 1 + threadIdx.x; j < blocks; j += D)
+        if (!p.goes_on[j]) atomicMin(&end_s, j + 1);
+    __syncthreads();
+    const int n = end_s - first;
+    auto row_of = [&](int j) { return ((int64_t)(first + j) * 2 + (j == 0 ? 1 : 0)) * kHeads + h; };
+    float m = -INFINITY;
+    for (int j = threadIdx.x; j < n; j += D) {
+        const float2 ml = p.part_ml[row_of(j)];
+        weight[j] = ml.x;
+        m = fmaxf(m, ml.x);
+    }
+#pragma unroll
+    for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(~0u, m, o));
+    if ((threadIdx.x & 31) == 0) head_m[threadIdx.x >> 5] = m;
+    __syncthreads();
+    m = -INFINITY;
+    for (int j = 0; j < D / 32; ++j) m = fmaxf(m, head_m[j]);
+    const float base = m == -INFINITY ? 0.f : m;
+    float l = 0.f;
+    for (int j = threadIdx.x; j < n; j += D) {
+        const float f = exp2f(weight[j] - base);
+        weight[j] = f;
+        l += f * p.part_ml[row_of(j)].y;
+    }
+#pragma unroll
+    for (int o = 16; o; o >>= 1) l += __shfl_xor_sync(~0u, l, o);
+    if ((threadIdx.x & 31) == 0) head_l[threadIdx.x >> 5] = l;
+    __syncthreads();
+    l = 0.f;
+    for (int j = 0; j < D / 32; ++j) l += head_l[j];
+    const int c = threadIdx.x;
+    float o = 0.f;
+#pragma unroll 8
+    for (int j = 0; j < n; ++j) o += weight[j] * p.part_o[row_of(j) * D + c];
+    reinterpret_cast<T *>(p.out)[b * p.out_stride_seq + (head0 + h) * p.out_stride_head + c] =
+        from_float<T>(l == 0.f ? 0.f : o / l);
+    if (p.lse && c == 0)
+        p.lse[(int64_t)b * (p.n_kv_heads * p.group) + head0 + h] =
+            l == 0.f ? -INFINITY : 0.6931471805599453f * m + logf(l);
+}
+
+// Query heads per product: 8, or 16 where a kv head has more than 8 and the accumulators fit (head_dim <= 128); a
+// larger group is cut into blocks of that many, which read the keys and values again, from L2.
+int heads_per_unit(int group, int head_dim) { return group > 8 && head_dim <= 128 ? 16 : 8; }
+
+int64_t round16(int64_t x) { return (x + 15) & ~(int64_t)15; }
+
+template <typename T, int D, int NT>
+int32_t launch(const KvAttendParams &p, int sms, cudaStream_t stream) {
+    using S = Shape<D, NT>;
+    cudaError_t e = cudaFuncSetAttribute(kv_attend_kernel<T, D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem);
+    if (e == cudaSuccess)
+        e = launch_after_producer(kv_attend_kernel<T, D, NT>, dim3(sms), dim3(S::kWarps * 32), S::kSmem, stream, p);
+    if (e == cudaSuccess)
+        e = launch_after_producer(kv_attend_join_kernel<T, D, NT>, dim3(sms, min(p.group, 8 * NT)), dim3(D), 0, stream, p);
+    if (e != cudaSuccess) {
+        set_last_cuda_error(e);
+        return STOM_ERR_CUDA;
+    }
+    return finish_launch();
+}
+
+template <typename T>
+int32_t dispatch(const KvAttendParams &p, int head_dim, int sms, cudaStream_t stream) {
+    const bool two = heads_per_unit(p.group, head_dim) == 16;
+    if (head_dim == 64) return two ? launch<T, 64, 2>(p, sms, stream) : launch<T, 64, 1>(p, sms, stream);
+    if (head_dim == 128) return two ? launch<T, 128, 2>(p, sms, stream) : launch<T, 128, 1>(p, sms, stream);
+    return launch<T, 256, 1>(p, sms, stream);
+}
+
+}  // namespace
+
+}  // namespace stom
+
+using namespace stom;
+
+extern "C" int64_t stom_kv_attend_workspace_bytes(const stom_kv_pool *pool, const stom_kv_seqs *seqs, int32_t n_q_heads) {
+    int32_t rc = check_pool(pool);
+    if (!rc) rc = check_seqs(pool, seqs, false);
+    if (rc) return rc;
+    if (n_q_heads < 1 || n_q_heads % pool->n_kv_heads) return STOM_ERR_SHAPE;
+    const int64_t rows = (int64_t)kMaxBlocks * 2 * heads_per_unit(n_q_heads / pool->n_kv_heads, pool->head_dim);
+    return rows * pool->head_dim * 4 + rows * 8 + round16(kMaxBlocks * 8);
+}
+
+extern "C" int32_t stom_kv_attend(const stom_kv_pool *pool, const stom_kv_seqs *seqs, int32_t layer, int32_t n_q_heads,
+                                  const void *q, int64_t q_stride_seq, int64_t q_stride_head, float softmax_scale,
+                                  float softcap, int32_t window, void *out, int64_t out_stride_seq,
+                                  int64_t out_stride_head, float *lse, void *workspace, int64_t workspace_bytes,
+                                  uint32_t *dev_flags, void *stream) {
+    int32_t rc = check_pool(pool);
+    if (!rc) rc = check_seqs(pool, seqs, false);
+    if (rc) return rc;
+    if (layer < 0 || layer >= pool->n_layers || n_q_heads < 1 || window < 0) return STOM_ERR_INVALID_ARG;
+    if (!(softcap >= 0.f) || !(softcap <= 3.0e38f) || !(softmax_scale >= -3.0e38f && softmax_scale <= 3.0e38f))
+        return STOM_ERR_INVALID_ARG;
+    if (n_q_heads % pool->n_kv_heads || n_q_heads / pool->n_kv_heads > 64) return STOM_ERR_SHAPE;
+    if (seqs->n_seqs == 0) return STOM_OK;
+    if (!q || !out) return STOM_ERR_INVALID_ARG;
+    if (!aligned16(q) || !aligned16(out) || !stride_ok(q_stride_seq, pool->dtype) || !stride_ok(q_stride_head, pool->dtype) ||
+        !stride_ok(out_stride_seq, pool->dtype) || !stride_ok(out_stride_head, pool->dtype))
+        return STOM_ERR_ALIGNMENT;
+    const int32_t d = pool->head_dim, group = n_q_heads / pool->n_kv_heads;
+    if (n_q_heads > 1 && (out_stride_head < d || q_stride_head < 0)) return STOM_ERR_INVALID_ARG;
+    if (seqs->n_seqs > 1 && (out_stride_seq < d || q_stride_seq < 0)) return STOM_ERR_INVALID_ARG;
+    const int64_t need = stom_kv_attend_workspace_bytes(pool, seqs, n_q_heads);
+    if (!workspace || !aligned16(workspace) || workspace_bytes < need) return STOM_ERR_WORKSPACE;
+    const int per = heads_per_unit(group, d);
+    const int64_t units = (int64_t)pool->n_kv_heads * ((group + per - 1) / per);
+    if (units * seqs->n_seqs > INT32_MAX) return STOM_ERR_SHAPE;
+    int sms = sm_count();
+    if (!sms) return STOM_ERR_CUDA;
+    if (sms > kMaxBlocks) sms = kMaxBlocks;
+
+    KvAttendParams p = {};
+    p.k = static_cast<const char *>(pool->k) + 2 * layer * pool->stride_layer;
+    p.v = static_cast<const char *>(pool->v) + 2 * layer * pool->stride_layer;
+    p.stride_page = pool->stride_page;
+    p.stride_token = pool->stride_token;
+    p.stride_head = pool->stride_head;
+    p.table = seqs->table;
+    p.len = seqs->len;
+    p.table_stride = seqs->table_stride;
+    p.n_seqs = seqs->n_seqs;
+    p.n_pages = pool->n_pages;
+    const int64_t most = (int64_t)seqs->max_pages * pool->page_tokens;
+    p.max_tokens = (int32_t)(most < 0x7fffffe0 ? most : 0x7fffffe0);
+    p.page = fast_div((uint32_t)pool->page_tokens);
+    p.n_kv_heads = pool->n_kv_heads;
+    p.group = group;
+    p.blocks_per_head = (group + per - 1) / per;
+    p.q = static_cast<const char *>(q);
+    p.q_stride_seq = q_stride_seq;
+    p.q_stride_head = q_stride_head;
+    p.scale = softmax_scale;
+    p.cap = softcap;
+    p.window = window;
+    p.out = static_cast<char *>(out);
+    p.out_stride_seq = out_stride_seq;
+    p.out_stride_head = out_stride_head;
+    p.lse = lse;
+    const int64_t rows = (int64_t)kMaxBlocks * 2 * per;
+    p.part_o = static_cast<float *>(workspace);
+    p.part_ml = reinterpret_cast<float2 *>(p.part_o + rows * d);
+    p.open_unit = reinterpret_cast<int32_t *>(p.part_ml + rows);
+    p.goes_on = p.open_unit + kMaxBlocks;
+    p.flags = dev_flags;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    return pool->dtype == STOM_BF16 ? dispatch<__nv_bfloat16>(p, d, sms, s) : dispatch<__half>(p, d, sms, s);
+}

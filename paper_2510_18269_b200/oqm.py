@@ -19,6 +19,11 @@ PER_LAYER, PER_HEAD = 0, 1
 FLAG_BAD_INDEX = 1
 FLAG_TIMEOUT = 2
 FLAG_DIRTY_WORKSPACE = 4
+FLAG_NO_PAGE = 8
+FLAG_BAD_VALUE = 16
+
+ROPE_HALF, ROPE_PAIRS = 0, 1
+ROPE_PLAIN, ROPE_LINEAR, ROPE_BASE, ROPE_WAVES = 0, 1, 2, 3
 
 _TORCH_DTYPE = {BF16: torch.bfloat16, FP16: torch.float16, FP32: torch.float32}
 _DTYPE_CODE = {v: k for k, v in _TORCH_DTYPE.items()}
@@ -32,6 +37,8 @@ EXPORTS = (
     "stom_oqm_score_groups_noalloc", "stom_oqm_attend_workspace_bytes", "stom_oqm_attend",
     "stom_oqm_retrieve_workspace_bytes",
     "stom_ctr_similarity", "stom_ctr_select", "stom_ctr_reduce", "stom_ctr_merge", "stom_ctr_reduce_tokens",
+    "stom_kv_frequencies", "stom_kv_attend_workspace_bytes", "stom_kv_attend",
+    "stom_kv_rotate", "stom_kv_append",
 )
 
 
@@ -52,12 +59,38 @@ class Layout(C.Structure):
         "off_rep_key", "off_rep_norm2", "bytes_codes", "bytes_meta", "bytes_norm2")]
 
 
+class KvPoolDesc(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p)] + [(n, C.c_int32) for n in (
+        "dtype", "n_layers", "n_pages", "page_tokens", "n_kv_heads", "head_dim")] + [(n, C.c_int64) for n in (
+            "stride_layer", "stride_page", "stride_token", "stride_head")]
+
+
+class KvSeqsDesc(C.Structure):
+    _fields_ = [("table", C.c_void_p), ("len", C.c_void_p), ("refs", C.c_void_p), ("n_seqs", C.c_int32),
+                ("max_pages", C.c_int32), ("table_stride", C.c_int64)]
+
+
+class RopeDesc(C.Structure):
+    _fields_ = [("freq", C.c_void_p), ("rot_dim", C.c_int32), ("layout", C.c_int32), ("magnitude", C.c_float)]
+
+
 class StomError(RuntimeError):
     def __init__(self, code: int, where: str):
         self.code = code
         msg = lib().stom_status_string(code).decode()
         super().__init__(f"{where}: {msg} (status {code}, cuda error {lib().stom_last_cuda_error()})")
 
+
+# Signatures of the calls that are made once per token: p pointer, i int32, l int64, f float, d double.  With them the
+# arguments go as plain numbers, which costs a call half of what wrapped ones do.
+_CTYPE = {"p": C.c_void_p, "i": C.c_int32, "l": C.c_int64, "f": C.c_float, "d": C.c_double}
+_SIGNATURES = {
+    "stom_kv_frequencies": (C.c_int32, "ididdddp"),
+    "stom_kv_attend_workspace_bytes": (C.c_int64, "ppi"),
+    "stom_kv_attend": (C.c_int32, "ppiipllffipllpplpp"),
+    "stom_kv_rotate": (C.c_int32, "piiip" + 2 * "pillpllp" + "fp"),
+    "stom_kv_append": (C.c_int32, "ppipippp" + "pillpllp" + "pllp" + "pll" + "fpp"),
+}
 
 _lib = None
 
@@ -80,6 +113,9 @@ def lib():
         L.stom_oqm_retrieve_workspace_bytes.restype = C.c_int64
         L.stom_oqm_quantize_host_scratch_bytes.restype = C.c_int64
         L.stom_oqm_retrieve_host_scratch_bytes.restype = C.c_int64
+        for name, (res, args) in _SIGNATURES.items():
+            fn = getattr(L, name)
+            fn.restype, fn.argtypes = res, [_CTYPE[a] for a in args]
         for name in EXPORTS:
             fn = getattr(L, name)
             if fn.restype is C.c_int:
@@ -335,3 +371,154 @@ def stom_ctr_reduce_tokens(F, prev, T, N, D, strides, alpha, G, tau_c, knn, sim,
                                         C.c_float(tau_c), C.c_int32(knn), _ptr(sim), _ptr(k_s), _ptr(k_d),
                                         _ptr(static_idx), _ptr(dyn_idx), _ptr(retained), _ptr(retained_pos),
                                         _ptr(dev_flags), _stream(stream)), "stom_ctr_reduce_tokens")
+
+
+# ---------------------------------------------------------------- paged cache (include/stom_kv.h)
+
+def _addr(t):
+    return None if t is None else t.data_ptr()
+
+
+class _On:
+    """Current device and stream for the tensors of a call: the stream given, else the current one of their device."""
+
+    def __init__(self, t, stream):
+        self.dev, self.stream = t.device, stream
+
+    def __call__(self, fn, *args):
+        if self.dev.type != "cuda":
+            raise ValueError("the tensors of a call lie on a CUDA device")
+        s = (torch.cuda.current_stream(self.dev) if self.stream is None else self.stream).cuda_stream
+        if self.dev.index == torch.cuda.current_device():
+            return fn(*args, s)
+        with torch.cuda.device(self.dev):
+            return fn(*args, s)
+
+
+def _dense(t, dtype, shape, name, device=None):
+    """A contiguous tensor of this type and shape on this device (or None)."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous() or (device is not None and t.device != device):
+        raise ValueError(f"{name}: a contiguous {dtype} tensor of shape {tuple(shape)}" +
+                         (f" on {device}" if device is not None else "") +
+                         f" is needed, not {t.dtype} {tuple(t.shape)} on {t.device}")
+    return t.data_ptr()
+
+
+def _rows3(t, dtype, n, heads, d, name, device):
+    """(address, stride of a row, stride of a head) of an [n][heads][d] tensor with adjacent channels."""
+    if t.dtype is not dtype or t.shape != (n, heads, d) or t.stride(2) != 1 or t.device != device:
+        raise ValueError(f"{name}: a {dtype} tensor of shape {(n, heads, d)} with adjacent channels on {device} is "
+                         f"needed, not {t.dtype} {tuple(t.shape)} with strides {t.stride()} on {t.device}")
+    sn, sh, _ = t.stride()
+    return t.data_ptr(), sn, sh
+
+
+class KvPool:
+    """Pages of keys and values: two tensors [layers][pages][page_tokens][kv heads][d] of the same strides."""
+
+    def __init__(self, k, v):
+        if k.shape != v.shape or k.stride() != v.stride() or k.dtype != v.dtype or k.device != v.device or k.dim() != 5:
+            raise ValueError("k and v are two [layers][pages][page_tokens][heads][d] tensors of the same type and strides")
+        if k.stride(4) != 1:
+            raise ValueError("the channels of a head are adjacent")
+        self.k, self.v, self.device, self.dtype = k, v, k.device, k.dtype
+        L, P, n, H, d = k.shape
+        self.n_layers, self.n_pages, self.page_tokens, self.n_kv_heads, self.head_dim = L, P, n, H, d
+        self.desc = KvPoolDesc(k.data_ptr(), v.data_ptr(), dtype_code(k.dtype), L, P, n, H, d, *k.stride()[:4])
+        self.ref = C.addressof(self.desc)
+
+
+class KvSeqs:
+    """The sequences of a pool: table [n_seqs][max_pages], len [n_seqs] and refs [pages], all int32."""
+
+    def __init__(self, table, len, refs=None):
+        n, width = table.shape
+        if table.dtype is not torch.int32 or (width > 1 and table.stride(1) != 1):
+            raise ValueError("table: int32 [n_seqs][max_pages] with adjacent entries")
+        _dense(len, torch.int32, (n,), "len", table.device)
+        if refs is not None:
+            _dense(refs, torch.int32, (refs.numel(),), "refs", table.device)
+        self.table, self.len, self.refs, self.n_seqs, self.max_pages = table, len, refs, n, width
+        stride = table.stride(0) if n > 1 else width
+        self.desc = KvSeqsDesc(_addr(table), _addr(len), _addr(refs), n, width, stride)
+        self.ref = C.addressof(self.desc)
+
+
+class Rope:
+    """Rotation of the first 2 * freq.numel() channels; freq: float64 tensor of radians per position."""
+
+    def __init__(self, freq=None, layout=ROPE_HALF, magnitude=1.0):
+        if freq is not None:
+            _dense(freq, torch.float64, (freq.numel(),), "freq")
+        self.freq, self.rot_dim = freq, 0 if freq is None else 2 * freq.numel()
+        self.desc = RopeDesc(_addr(freq), self.rot_dim, layout, magnitude)
+        self.ref = C.addressof(self.desc)
+
+
+def stom_kv_frequencies(rot_dim, theta=1.0e6, scaling=ROPE_PLAIN, factor=1.0, trained=0.0, low=1.0, high=4.0):
+    """Radians per position of every rotated pair, as a float64 CPU tensor (move it to the device once)."""
+    out = torch.empty(max(rot_dim // 2, 0), dtype=torch.float64)
+    _check(lib().stom_kv_frequencies(rot_dim, theta, scaling, factor, trained, low, high, out.data_ptr()),
+           "stom_kv_frequencies")
+    return out
+
+
+def stom_kv_attend_workspace_bytes(pool: KvPool, seqs: KvSeqs, n_q_heads: int) -> int:
+    n = lib().stom_kv_attend_workspace_bytes(pool.ref, seqs.ref, n_q_heads)
+    if n < 0:
+        _check(int(n), "stom_kv_attend_workspace_bytes")
+    return int(n)
+
+
+def stom_kv_attend(pool: KvPool, seqs: KvSeqs, layer, q, out, softmax_scale, workspace, lse=None, softcap=0.0, window=0,
+                   dev_flags=None, stream=None):
+    """q, out: [n_seqs][query heads][d] of the pool's type; lse: [n_seqs][query heads] float32 or None."""
+    n, hq, d = q.shape
+    qa, qs, qh = _rows3(q, pool.dtype, seqs.n_seqs, hq, pool.head_dim, "q", pool.device)
+    oa, os_, oh = _rows3(out, pool.dtype, n, hq, d, "out", pool.device)
+    la = _dense(lse, torch.float32, (n, hq), "lse", pool.device)
+    _check(_On(q, stream)(lib().stom_kv_attend, pool.ref, seqs.ref, layer, hq, qa, qs, qh, softmax_scale, softcap, window,
+                          oa, os_, oh, la, workspace.data_ptr(), workspace.numel() * workspace.element_size(),
+                          _addr(dev_flags)), "stom_kv_attend")
+
+
+def stom_kv_rotate(rope: Rope, pos, q=None, q_out=None, k=None, k_out=None, q_weight=None, k_weight=None, eps=1e-6,
+                   stream=None):
+    """q, k and their outputs: [n][heads][d], each with its own strides (an output may be its input); pos: int32 [n];
+    weights: float32 [d] or None (no norm)."""
+    x = q if q is not None else k
+    n, _, d = x.shape
+    dt, dev = x.dtype, x.device
+    qa = (None, 0, 0, 0, None, 0, 0, None)
+    ka = qa
+    if q is not None:
+        h = q.shape[1]
+        a, b = _rows3(q, dt, n, h, d, "q", dev), _rows3(q_out, dt, n, h, d, "q_out", dev)
+        qa = (a[0], h, a[1], a[2], b[0], b[1], b[2], _dense(q_weight, torch.float32, (d,), "q_weight", dev))
+    if k is not None:
+        h = k.shape[1]
+        a, b = _rows3(k, dt, n, h, d, "k", dev), _rows3(k_out, dt, n, h, d, "k_out", dev)
+        ka = (a[0], h, a[1], a[2], b[0], b[1], b[2], _dense(k_weight, torch.float32, (d,), "k_weight", dev))
+    _check(_On(x, stream)(lib().stom_kv_rotate, rope.ref, dtype_code(dt), d, n, _dense(pos, torch.int32, (n,), "pos", dev),
+                          *qa, *ka, eps), "stom_kv_rotate")
+
+
+def stom_kv_append(pool: KvPool, seqs: KvSeqs, layer, rope: Rope, pos, slot, k, v, q=None, q_out=None, seq=None,
+                   q_weight=None, k_weight=None, eps=1e-6, dev_flags=None, stream=None):
+    """k, v: [n][kv heads][d] of the pool's type; slot, pos, seq: int32 [n]; q and q_out: [n][query heads][d] or None."""
+    n, hk, d = k.shape
+    dt, dev = pool.dtype, pool.device
+    ka, ks, kh = _rows3(k, dt, n, pool.n_kv_heads, pool.head_dim, "k", dev)
+    va, vs, vh = _rows3(v, dt, n, hk, d, "v", dev)
+    qa = (None, 0, 0, 0, None, 0, 0, None)
+    if q is not None:
+        h = q.shape[1]
+        a, b = _rows3(q, dt, n, h, d, "q", dev), _rows3(q_out, dt, n, h, d, "q_out", dev)
+        qa = (a[0], h, a[1], a[2], b[0], b[1], b[2], _dense(q_weight, torch.float32, (d,), "q_weight", dev))
+    _check(_On(k, stream)(lib().stom_kv_append, pool.ref, seqs.ref, layer, rope.ref, n,
+                          _dense(pos, torch.int32, (n,), "pos", dev), _dense(slot, torch.int32, (n,), "slot", dev),
+                          _dense(seq, torch.int32, (n,), "seq", dev), *qa, ka, ks, kh,
+                          _dense(k_weight, torch.float32, (d,), "k_weight", dev), va, vs, vh, eps, _addr(dev_flags)),
+           "stom_kv_append")

@@ -1,0 +1,154 @@
+"""CPU-only checks of the paged cache and of the token choice: what the host refuses before any launch, the workspace
+sizes, the rotation frequencies, and the arithmetic identity the page lookup relies on.  No kernel is launched here:
+the addresses are never dereferenced."""
+import ctypes as C
+import math
+
+import numpy as np
+import pytest
+import torch
+
+P = 0x7f1000000000
+
+
+@pytest.fixture(scope="module")
+def oqm():
+    from paper_2510_18269_b200 import build, oqm as m
+    build.build()
+    m.lib()
+    return m
+
+
+def pool_of(oqm, **kw):
+    a = dict(k=P, v=P + (1 << 30), dtype=oqm.BF16, n_layers=2, n_pages=10, page_tokens=50, n_kv_heads=4, head_dim=128,
+             stride_layer=10 * 50 * 512, stride_page=50 * 512, stride_token=512, stride_head=128)
+    a.update(kw)
+    return oqm.KvPoolDesc(*[a[n] for n, _ in oqm.KvPoolDesc._fields_])
+
+
+def seqs_of(oqm, **kw):
+    a = dict(table=P, len=P, refs=P, n_seqs=3, max_pages=5, table_stride=5)
+    a.update(kw)
+    return oqm.KvSeqsDesc(*[a[n] for n, _ in oqm.KvSeqsDesc._fields_])
+
+
+BAD_POOLS = [(dict(k=None), -1), (dict(v=None), -1), (dict(k=P + 8), -3), (dict(dtype=2), -6), (dict(dtype=9), -6),
+             (dict(head_dim=96), -2), (dict(n_layers=0), -1), (dict(n_pages=0), -1), (dict(page_tokens=0), -1),
+             (dict(n_kv_heads=0), -1), (dict(stride_token=516), -3), (dict(stride_head=64), -1),
+             (dict(stride_page=-512), -1), (dict(stride_layer=0), -1)]
+BAD_SEQS = [(dict(table=None), -1), (dict(len=None), -1), (dict(n_seqs=-1), -1), (dict(max_pages=0), -1),
+            (dict(table_stride=4), -1), (dict(len=P + 2), -3)]
+
+
+def attend(oqm, pool=None, seqs=None, **kw):
+    pool, seqs = pool or pool_of(oqm), seqs or seqs_of(oqm)
+    a = dict(layer=0, hq=28, q=P, qs=28 * 128, qh=128, scale=0.1, cap=0.0, window=0, out=P, os=28 * 128, oh=128, lse=None,
+             ws=P, nb=1 << 40)
+    a.update(kw)
+    return oqm.lib().stom_kv_attend(C.addressof(pool), C.addressof(seqs), a["layer"], a["hq"], a["q"], a["qs"], a["qh"],
+                                    a["scale"], a["cap"], a["window"], a["out"], a["os"], a["oh"], a["lse"], a["ws"],
+                                    a["nb"], None, None)
+
+
+@pytest.mark.parametrize("kw,code", BAD_POOLS)
+def test_attend_refuses_bad_pools(oqm, kw, code):
+    assert attend(oqm, pool=pool_of(oqm, **kw)) == code
+    assert oqm.lib().stom_kv_attend_workspace_bytes(C.addressof(pool_of(oqm, **kw)), C.addressof(seqs_of(oqm)), 28) == code
+
+
+@pytest.mark.parametrize("kw,code", BAD_SEQS)
+def test_attend_refuses_bad_sequences(oqm, kw, code):
+    assert attend(oqm, seqs=seqs_of(oqm, **kw)) == code
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(layer=2), -1), (dict(layer=-1), -1), (dict(hq=0), -1), (dict(hq=30), -2), (dict(hq=260), -2),
+    (dict(window=-1), -1), (dict(cap=-1.0), -1), (dict(cap=math.nan), -1), (dict(cap=math.inf), -1),
+    (dict(scale=math.nan), -1), (dict(scale=math.inf), -1), (dict(q=None), -1), (dict(out=None), -1), (dict(q=P + 2), -3),
+    (dict(qh=100), -3), (dict(os=28 * 128 + 4), -3), (dict(oh=64), -1), (dict(ws=None), -8), (dict(ws=P + 4), -8),
+    (dict(nb=1000), -8),
+])
+def test_attend_refuses(oqm, kw, code):
+    assert attend(oqm, **kw) == code
+
+
+def test_attend_of_no_sequence_is_nothing(oqm):
+    assert attend(oqm, seqs=seqs_of(oqm, n_seqs=0)) == 0
+    assert attend(oqm, seqs=seqs_of(oqm, refs=None, n_seqs=0)) == 0            # counts are not needed here
+
+
+def test_attend_workspace_is_enough_for_two_rows_of_partial_results_per_block(oqm):
+    for hq, d, per in ((28, 128, 8), (40, 64, 16), (128, 256, 8)):
+        pool = pool_of(oqm, head_dim=d, stride_head=d, stride_token=4 * d, stride_page=200 * d, stride_layer=2000 * d)
+        n = oqm.lib().stom_kv_attend_workspace_bytes(C.addressof(pool), C.addressof(seqs_of(oqm)), hq)
+        assert n >= 148 * 2 * per * (d + 2) * 4 + 148 * 8
+
+
+def test_page_of_a_token_by_multiplication_equals_the_division():
+    """floor(x / d) = (mulhi(x, m) + x) >> s with s = ceil(log2 d), m = floor(2^32 (2^s - d) / d) + 1, for x < 2^31."""
+    rng = np.random.default_rng(1)
+    for d in list(range(1, 260)) + [1000, 4095, 4096, 4097, 65535, 10 ** 6, 2 ** 30, 2 ** 31 - 1]:
+        s = (d - 1).bit_length()
+        m = ((1 << 32) * ((1 << s) - d)) // d + 1
+        assert m < 1 << 32
+        x = np.concatenate([rng.integers(0, 1 << 31, 2000), np.arange(64), (1 << 31) - 1 - np.arange(64),
+                            np.minimum(d * rng.integers(0, max(1, (1 << 31) // d), 500), (1 << 31) - 1)])
+        x = np.concatenate([x, np.maximum(x - 1, 0)]).astype(np.uint64)
+        total = ((x * np.uint64(m)) >> np.uint64(32)) + x
+        assert (total < 1 << 32).all()
+        assert np.array_equal(total >> np.uint64(s), x // np.uint64(d)), d
+
+
+def test_frequencies(oqm):
+    i = np.arange(64)
+    plain = 1.0e6 ** (-2 * i / 128.0)
+    near = lambda a, b: np.allclose(a.numpy(), b, rtol=1e-14, atol=0)  # noqa: E731
+    assert near(oqm.stom_kv_frequencies(128), plain)
+    assert near(oqm.stom_kv_frequencies(128, scaling=oqm.ROPE_LINEAR, factor=4.0), plain / 4)
+    assert near(oqm.stom_kv_frequencies(128, scaling=oqm.ROPE_BASE, factor=8.0),
+                (1.0e6 * 8.0 ** (128 / 126)) ** (-2 * i / 128.0))
+    # the slowest pair of a raised base covers `factor` times the positions
+    assert math.isclose(oqm.stom_kv_frequencies(128, scaling=oqm.ROPE_BASE, factor=8.0)[-1], plain[-1] / 8, rel_tol=1e-12)
+    waves = oqm.stom_kv_frequencies(128, scaling=oqm.ROPE_WAVES, factor=8.0, trained=8192.0, low=1.0, high=4.0).numpy()
+    turns = 8192.0 * plain / (2 * math.pi)
+    assert np.allclose(waves[turns > 4], plain[turns > 4], rtol=1e-14)
+    assert np.allclose(waves[turns < 1], plain[turns < 1] / 8, rtol=1e-14)
+    between = (turns >= 1) & (turns <= 4)
+    assert between.any() and (waves[between] <= plain[between]).all() and (waves[between] >= plain[between] / 8).all()
+    assert oqm.stom_kv_frequencies(0).numel() == 0
+
+
+@pytest.mark.parametrize("kw", [dict(rot_dim=24), dict(rot_dim=-16), dict(rot_dim=64, theta=0.0),
+                                dict(rot_dim=64, scaling=7), dict(rot_dim=64, scaling=1, factor=0.0),
+                                dict(rot_dim=64, scaling=3, factor=2.0, trained=0.0),
+                                dict(rot_dim=64, scaling=3, factor=2.0, trained=9.0, low=4.0, high=4.0),
+                                dict(rot_dim=64, theta=math.nan), dict(rot_dim=64, scaling=2, factor=math.inf)])
+def test_frequencies_refuse(oqm, kw):
+    with pytest.raises(oqm.StomError):
+        oqm.stom_kv_frequencies(**kw)
+
+
+def test_bindings_refuse_tensors_that_do_not_fit(oqm):
+    k = torch.zeros(1, 4, 16, 2, 64, dtype=torch.bfloat16)
+    with pytest.raises(ValueError):
+        oqm.KvPool(k, k.half())
+    with pytest.raises(ValueError):
+        oqm.KvPool(k, torch.zeros(1, 4, 16, 4, 64, dtype=torch.bfloat16)[:, :, :, ::2])   # other strides
+    with pytest.raises(ValueError):
+        oqm.KvPool(k[..., ::2], k[..., ::2])
+    table, n = torch.zeros(3, 2, dtype=torch.int32), torch.zeros(3, dtype=torch.int32)
+    for bad in (dict(table=table.long(), len=n), dict(table=table, len=n[:2]), dict(table=table, len=n.long()),
+                dict(table=torch.zeros(3, 4, dtype=torch.int32)[:, ::2], len=n), dict(table=table, len=n, refs=n.float())):
+        with pytest.raises(ValueError):
+            oqm.KvSeqs(**bad)
+    pool, seqs = oqm.KvPool(k, k.clone()), oqm.KvSeqs(table, n)
+    q = torch.zeros(3, 4, 64, dtype=torch.bfloat16)
+    ws = torch.empty(1 << 20, dtype=torch.uint8)
+    for bad in (dict(q=q.half()), dict(q=q[:2]), dict(out=q[:, :2]), dict(q=torch.zeros(3, 4, 128, dtype=q.dtype)[..., ::2]),
+                dict(lse=torch.zeros(3, 4, dtype=torch.float64)), dict()):                  # the last: on the CPU
+        a = dict(q=q, out=q.clone(), lse=None)
+        a.update(bad)
+        with pytest.raises(ValueError):
+            oqm.stom_kv_attend(pool, seqs, 0, a["q"], a["out"], 0.1, ws, lse=a["lse"])
+    with pytest.raises(ValueError):
+        oqm.Rope(torch.zeros(8))
