@@ -145,6 +145,47 @@ int32_t stom_kv_attend(const stom_kv_pool *pool, const stom_kv_seqs *seqs, int32
                        int32_t window, void *out, int64_t out_stride_seq, int64_t out_stride_head, float *lse,
                        void *workspace, int64_t workspace_bytes, uint32_t *dev_flags, void *stream);
 
+/* ---- pages: reserve, fork, free, compact -----------------------------------
+ * All need seqs->refs and act on all layers.  Page ids outside [0, n_pages)
+ * are skipped and set STOM_FLAG_BAD_INDEX.
+ */
+
+/* Sequence i grows to want[i] tokens (want[i] <= len[i]: it stays).  Pages are
+ * taken lowest id first, rows in ascending order.  If the sequence's last page
+ * is partly filled and other rows hold it too, the tokens in use are copied to
+ * a page of its own; of several growing rows that share a page with nobody
+ * else the last keeps it.  If there are not enough free pages for all rows,
+ * nothing changes and STOM_FLAG_NO_PAGE is set.  A want[i] beyond
+ * max_pages*page_tokens is skipped and sets STOM_FLAG_BAD_INDEX.
+ * n_seqs <= STOM_KV_MAX_SEQS.  workspace: 16-byte aligned, of at least
+ * stom_kv_pages_workspace_bytes() bytes.  Errors as for stom_kv_attend. */
+#define STOM_KV_MAX_SEQS 8192
+int64_t stom_kv_pages_workspace_bytes(const stom_kv_pool *pool, const stom_kv_seqs *seqs);
+int32_t stom_kv_reserve(const stom_kv_pool *pool, const stom_kv_seqs *seqs, const int32_t *want, void *workspace,
+                        int64_t workspace_bytes, uint32_t *dev_flags, void *stream);
+
+/* Every empty sequence i with parent[i] >= 0 becomes a sharer of all pages of
+ * sequence parent[i] and takes its length (parent[i] == -1: not forked).
+ * Nothing is copied until one of them grows.  Skipped, with
+ * STOM_FLAG_BAD_INDEX: a parent out of range, a parent that is itself forked
+ * in this call, a row i that is not empty. */
+int32_t stom_kv_fork(const stom_kv_pool *pool, const stom_kv_seqs *seqs, const int32_t *parent, uint32_t *dev_flags,
+                     void *stream);
+
+/* Every sequence i with drop[i] != 0 gives its pages back: its row becomes -1,
+ * its length 0. */
+int32_t stom_kv_free(const stom_kv_pool *pool, const stom_kv_seqs *seqs, const int32_t *drop, uint32_t *dev_flags,
+                     void *stream);
+
+/* Moves the live pages to the front of the pool: with n live pages, the k-th
+ * live page of id >= n goes to the k-th free page of id < n, whole.  table_out
+ * [n_seqs][table_stride] gets the rows with their new ids (-1 behind the pages
+ * of a row), refs_out [n_pages] the counts, *n_live the number n (n_live may
+ * be NULL).  table_out and refs_out may be seqs->table and seqs->refs, or
+ * separate arrays, in which case the old ones stay as they were. */
+int32_t stom_kv_compact(const stom_kv_pool *pool, const stom_kv_seqs *seqs, int32_t *table_out, int32_t *refs_out,
+                        int32_t *n_live, void *workspace, int64_t workspace_bytes, uint32_t *dev_flags, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -38,7 +38,8 @@ EXPORTS = (
     "stom_oqm_retrieve_workspace_bytes",
     "stom_ctr_similarity", "stom_ctr_select", "stom_ctr_reduce", "stom_ctr_merge", "stom_ctr_reduce_tokens",
     "stom_kv_frequencies", "stom_kv_attend_workspace_bytes", "stom_kv_attend",
-    "stom_kv_rotate", "stom_kv_append",
+    "stom_kv_rotate", "stom_kv_append", "stom_kv_pages_workspace_bytes", "stom_kv_reserve", "stom_kv_fork",
+    "stom_kv_free", "stom_kv_compact",
 )
 
 
@@ -90,6 +91,11 @@ _SIGNATURES = {
     "stom_kv_attend": (C.c_int32, "ppiipllffipllpplpp"),
     "stom_kv_rotate": (C.c_int32, "piiip" + 2 * "pillpllp" + "fp"),
     "stom_kv_append": (C.c_int32, "ppipippp" + "pillpllp" + "pllp" + "pll" + "fpp"),
+    "stom_kv_pages_workspace_bytes": (C.c_int64, "pp"),
+    "stom_kv_reserve": (C.c_int32, "pppplpp"),
+    "stom_kv_fork": (C.c_int32, "ppppp"),
+    "stom_kv_free": (C.c_int32, "ppppp"),
+    "stom_kv_compact": (C.c_int32, "ppppppl" + "pp"),
 }
 
 _lib = None
@@ -522,3 +528,52 @@ def stom_kv_append(pool: KvPool, seqs: KvSeqs, layer, rope: Rope, pos, slot, k, 
                           _dense(seq, torch.int32, (n,), "seq", dev), *qa, ka, ks, kh,
                           _dense(k_weight, torch.float32, (d,), "k_weight", dev), va, vs, vh, eps, _addr(dev_flags)),
            "stom_kv_append")
+
+
+def stom_kv_pages_workspace_bytes(pool: KvPool, seqs: KvSeqs) -> int:
+    n = lib().stom_kv_pages_workspace_bytes(pool.ref, seqs.ref)
+    if n < 0:
+        _check(int(n), "stom_kv_pages_workspace_bytes")
+    return int(n)
+
+
+def _counts_of(pool, seqs):
+    if seqs.refs is None or seqs.refs.numel() != pool.n_pages:
+        raise ValueError("the sequences need refs, one count for each page of the pool")
+    if seqs.table.device != pool.device:
+        raise ValueError("table and pool lie on the same device")
+
+
+def stom_kv_reserve(pool: KvPool, seqs: KvSeqs, want, workspace, dev_flags=None, stream=None):
+    """want: int32 [n_seqs], the length each sequence grows to (at most its length: it stays)."""
+    _counts_of(pool, seqs)
+    w = _dense(want, torch.int32, (seqs.n_seqs,), "want", pool.device)
+    _check(_On(pool.k, stream)(lib().stom_kv_reserve, pool.ref, seqs.ref, w, workspace.data_ptr(),
+                               workspace.numel() * workspace.element_size(), _addr(dev_flags)), "stom_kv_reserve")
+
+
+def stom_kv_fork(pool: KvPool, seqs: KvSeqs, parent, dev_flags=None, stream=None):
+    """parent: int32 [n_seqs], the sequence an empty one shares from now on, or -1."""
+    _counts_of(pool, seqs)
+    w = _dense(parent, torch.int32, (seqs.n_seqs,), "parent", pool.device)
+    _check(_On(pool.k, stream)(lib().stom_kv_fork, pool.ref, seqs.ref, w, _addr(dev_flags)), "stom_kv_fork")
+
+
+def stom_kv_free(pool: KvPool, seqs: KvSeqs, drop, dev_flags=None, stream=None):
+    """drop: int32 [n_seqs], not 0 for the sequences that give their pages back."""
+    _counts_of(pool, seqs)
+    w = _dense(drop, torch.int32, (seqs.n_seqs,), "drop", pool.device)
+    _check(_On(pool.k, stream)(lib().stom_kv_free, pool.ref, seqs.ref, w, _addr(dev_flags)), "stom_kv_free")
+
+
+def stom_kv_compact(pool: KvPool, seqs: KvSeqs, table_out, refs_out, n_live, workspace, dev_flags=None, stream=None):
+    """table_out, refs_out: like seqs.table and seqs.refs (or those themselves); n_live: int32 [1] or None."""
+    _counts_of(pool, seqs)
+    t = seqs.table
+    if table_out.dtype is not torch.int32 or table_out.shape != t.shape or table_out.stride() != t.stride() \
+            or table_out.device != pool.device:
+        raise ValueError("table_out: a tensor like seqs.table")
+    r = _dense(refs_out, torch.int32, (pool.n_pages,), "refs_out", pool.device)
+    c = _dense(n_live, torch.int32, (1,), "n_live", pool.device)
+    _check(_On(pool.k, stream)(lib().stom_kv_compact, pool.ref, seqs.ref, table_out.data_ptr(), r, c, workspace.data_ptr(),
+                               workspace.numel() * workspace.element_size(), _addr(dev_flags)), "stom_kv_compact")

@@ -81,3 +81,68 @@ def turned(x, pos, freq, layout, weight=None, eps=1e-6, magnitude=1.0):
     m = abs(magnitude) * (np.abs(a) + np.abs(b))
     mag[..., ia], mag[..., ib] = m, m
     return y, mag
+
+
+class Book:
+    """The pages of a cache kept in Python, one rule after the other, for what the device decides in parallel."""
+
+    def __init__(self, table, lens, refs, page, k, v):
+        self.table, self.len, self.refs, self.page = table.copy(), list(lens), refs.copy(), page
+        self.k, self.v = k.clone(), v.clone()
+
+    def held(self, n):
+        return -(-n // self.page)
+
+    def free(self, drop):
+        for i, gone in enumerate(drop):
+            if gone:
+                for j in range(self.held(self.len[i])):
+                    self.refs[self.table[i, j]] -= 1
+                self.table[i], self.len[i] = -1, 0
+
+    def fork(self, parent):
+        before = list(self.len)
+        for i, f in enumerate(parent):
+            if f >= 0 and parent[f] == -1 and before[i] == 0:
+                m = self.held(before[f])
+                self.table[i] = -1
+                self.table[i, :m] = self.table[f, :m]
+                self.len[i] = before[f]
+                for j in range(m):
+                    self.refs[self.table[f, j]] += 1
+
+    def reserve(self, want):
+        keep = (self.table.copy(), list(self.len), self.refs.copy(), self.k.clone(), self.v.clone())
+        free = [p for p, r in enumerate(self.refs) if r == 0]
+        try:
+            for i, w in enumerate(want):
+                n = self.len[i]
+                if w <= n or w > self.table.shape[1] * self.page:
+                    continue
+                m = self.held(n)
+                if n % self.page and self.refs[self.table[i, m - 1]] > 1:
+                    old, new = self.table[i, m - 1], free.pop(0)
+                    self.refs[old] -= 1
+                    self.refs[new], self.table[i, m - 1] = 1, new
+                    for x in (self.k, self.v):
+                        x[:, new, :n % self.page] = x[:, old, :n % self.page]
+                for j in range(m, self.held(w)):
+                    self.table[i, j] = free.pop(0)
+                    self.refs[self.table[i, j]] = 1
+                self.len[i] = w
+            return True
+        except IndexError:                                       # out of pages: as if nothing had been asked
+            self.table, self.len, self.refs, self.k, self.v = keep
+            return False
+
+    def compact(self):
+        live = int((self.refs > 0).sum())
+        holes = [p for p in range(live) if self.refs[p] <= 0]
+        for p in range(live, len(self.refs)):
+            if self.refs[p] > 0:
+                to = holes.pop(0)
+                for x in (self.k, self.v):
+                    x[:, to] = x[:, p]
+                self.refs[to], self.refs[p] = self.refs[p], 0
+                self.table[self.table == p] = to
+        return live

@@ -45,7 +45,7 @@ def attend(oqm, pool=None, seqs=None, **kw):
     a = dict(layer=0, hq=28, q=P, qs=28 * 128, qh=128, scale=0.1, cap=0.0, window=0, out=P, os=28 * 128, oh=128, lse=None,
              ws=P, nb=1 << 40)
     a.update(kw)
-    return oqm.lib().stom_kv_attend(C.addressof(pool), C.addressof(seqs), a["layer"], a["hq"], a["q"], a["qs"], a["qh"],
+    return oqm.lib().stom_kv_attend(C.byref(pool), C.byref(seqs), a["layer"], a["hq"], a["q"], a["qs"], a["qh"],
                                     a["scale"], a["cap"], a["window"], a["out"], a["os"], a["oh"], a["lse"], a["ws"],
                                     a["nb"], None, None)
 
@@ -53,7 +53,7 @@ def attend(oqm, pool=None, seqs=None, **kw):
 @pytest.mark.parametrize("kw,code", BAD_POOLS)
 def test_attend_refuses_bad_pools(oqm, kw, code):
     assert attend(oqm, pool=pool_of(oqm, **kw)) == code
-    assert oqm.lib().stom_kv_attend_workspace_bytes(C.addressof(pool_of(oqm, **kw)), C.addressof(seqs_of(oqm)), 28) == code
+    assert oqm.lib().stom_kv_attend_workspace_bytes(C.byref(pool_of(oqm, **kw)), C.byref(seqs_of(oqm)), 28) == code
 
 
 @pytest.mark.parametrize("kw,code", BAD_SEQS)
@@ -80,7 +80,7 @@ def test_attend_of_no_sequence_is_nothing(oqm):
 def test_attend_workspace_is_enough_for_two_rows_of_partial_results_per_block(oqm):
     for hq, d, per in ((28, 128, 8), (40, 64, 16), (128, 256, 8)):
         pool = pool_of(oqm, head_dim=d, stride_head=d, stride_token=4 * d, stride_page=200 * d, stride_layer=2000 * d)
-        n = oqm.lib().stom_kv_attend_workspace_bytes(C.addressof(pool), C.addressof(seqs_of(oqm)), hq)
+        n = oqm.lib().stom_kv_attend_workspace_bytes(C.byref(pool), C.byref(seqs_of(oqm)), hq)
         assert n >= 148 * 2 * per * (d + 2) * 4 + 148 * 8
 
 
