@@ -39,7 +39,7 @@ EXPORTS = (
     "stom_ctr_similarity", "stom_ctr_select", "stom_ctr_reduce", "stom_ctr_merge", "stom_ctr_reduce_tokens",
     "stom_kv_frequencies", "stom_kv_attend_workspace_bytes", "stom_kv_attend",
     "stom_kv_rotate", "stom_kv_append", "stom_kv_pages_workspace_bytes", "stom_kv_reserve", "stom_kv_fork",
-    "stom_kv_free", "stom_kv_compact",
+    "stom_kv_free", "stom_kv_compact", "stom_sample_tokens",
 )
 
 
@@ -96,6 +96,7 @@ _SIGNATURES = {
     "stom_kv_fork": (C.c_int32, "ppppp"),
     "stom_kv_free": (C.c_int32, "ppppp"),
     "stom_kv_compact": (C.c_int32, "ppppppl" + "pp"),
+    "stom_sample_tokens": (C.c_int32, "piiil" + "ppppp" + "ppp" + "pp"),
 }
 
 _lib = None
@@ -577,3 +578,20 @@ def stom_kv_compact(pool: KvPool, seqs: KvSeqs, table_out, refs_out, n_live, wor
     c = _dense(n_live, torch.int32, (1,), "n_live", pool.device)
     _check(_On(pool.k, stream)(lib().stom_kv_compact, pool.ref, seqs.ref, table_out.data_ptr(), r, c, workspace.data_ptr(),
                                workspace.numel() * workspace.element_size(), _addr(dev_flags)), "stom_kv_compact")
+
+
+# ---------------------------------------------------------------- choice of the next token (include/stom_sample.h)
+
+def stom_sample_tokens(logits, u, token, temperature=None, top_k=None, top_p=None, min_p=None, logprob=None, kept=None,
+                       dev_flags=None, stream=None):
+    """logits: [rows][n]; u, temperature, top_p, min_p, logprob: float32 [rows]; token, kept, top_k: int32 [rows]."""
+    rows, n = logits.shape
+    if n > 1 and logits.stride(1) != 1:
+        raise ValueError("logits: the entries of a row are adjacent")
+    dev, one, f, i = logits.device, (rows,), torch.float32, torch.int32
+    _check(_On(logits, stream)(
+        lib().stom_sample_tokens, logits.data_ptr(), dtype_code(logits.dtype), rows, n, logits.stride(0),
+        _dense(temperature, f, one, "temperature", dev), _dense(top_k, i, one, "top_k", dev),
+        _dense(top_p, f, one, "top_p", dev), _dense(min_p, f, one, "min_p", dev), _dense(u, f, one, "u", dev),
+        _dense(token, i, one, "token", dev), _dense(kept, i, one, "kept", dev), _dense(logprob, f, one, "logprob", dev),
+        _addr(dev_flags)), "stom_sample_tokens")

@@ -146,3 +146,45 @@ class Book:
                 self.refs[to], self.refs[p] = self.refs[p], 0
                 self.table[self.table == p] = to
         return live
+
+
+def choose(x, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
+    """(acceptable tokens, acceptable counts, {token: logprob}) of one row by sorting it, in 64 bits.  More than one is
+    acceptable only where a mass comes within NEAR of the border asked for."""
+    x = np.asarray(x, np.float64)
+    order = np.argsort(-np.where(np.isnan(x), -np.inf, x) + 0.0, kind="stable")
+    order = order[~np.isnan(x[order]) & (x[order] > -np.inf)]
+    if not len(order):
+        return {-1}, {0}, {-1: -np.inf}
+    if temperature <= 0:
+        return {int(order[0])}, {1}, {int(order[0]): 0.0}
+    with np.errstate(invalid="ignore", over="ignore", under="ignore"):
+        y = np.where(x[order] == x[order[0]], 0.0, (x[order] - x[order[0]]) / temperature)
+        w = np.where(y < -700.0, 0.0, np.exp(y))
+    order, w = order[w > 0], w[w > 0]
+    if top_k > 0:
+        order, w = order[:top_k], w[:top_k]
+    upto = np.cumsum(w)
+    near = NEAR * upto[-1]
+    counts = {len(w)}
+    if top_p < 1:
+        aim = max(top_p, 0.0) * upto[-1]
+        counts = {int(np.searchsorted(upto, aim + s * near, side="left")) + 1 for s in (-1, 0, 1)}
+        exact = aim == upto
+        if exact.any():                                          # a tie that both sides can form exactly
+            counts = {int(np.argmax(exact)) + 1}
+    stay = int((w >= min(min_p, 1.0)).sum())
+    counts = {max(1, min(c, stay, len(w))) for c in counts}
+    tokens, logprobs = set(), {}
+    for c in counts:
+        for s in (0,) if (u * upto[c - 1] == upto[:c]).any() else (-1, 0, 1):
+            j = int(np.searchsorted(upto[:c], u * upto[c - 1] + s * near * (u > 0), side="right"))
+            j = min(j, c - 1)
+            tokens.add(int(order[j]))
+            logprobs[int(order[j])] = math.log(w[j]) - math.log(upto[c - 1])
+    return tokens, counts, logprobs
+
+
+#: relative error of the masses: 4 096 ranges of masses rounded to 2^-45 of the largest weight, or 131 072 logits each
+#: rounded so whose errors add up at random (factor 4 * 362 * 2^-45 = 4e-11), against 150 000 binary64 additions here
+NEAR = 1e-10
