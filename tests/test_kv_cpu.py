@@ -84,6 +84,133 @@ def test_attend_workspace_is_enough_for_two_rows_of_partial_results_per_block(oq
         assert n >= 148 * 2 * per * (d + 2) * 4 + 148 * 8
 
 
+def rope_of(oqm, **kw):
+    a = dict(freq=P, rot_dim=64, layout=0, magnitude=1.0)
+    a.update(kw)
+    return oqm.RopeDesc(*[a[n] for n, _ in oqm.RopeDesc._fields_])
+
+
+def rotate(oqm, rope=None, **kw):
+    a = dict(dt=0, d=128, n=5, pos=P, q=P, hq=4, qt=512, qh=128, qo=P, qot=512, qoh=128, qw=P, k=P, hk=2, kt=256, kh=128,
+             ko=P, kot=256, koh=128, kw=P, eps=1e-6)
+    a.update(kw)
+    return oqm.lib().stom_kv_rotate(
+        C.byref(rope or rope_of(oqm)), a["dt"], a["d"], a["n"], a["pos"], a["q"], a["hq"], a["qt"], a["qh"], a["qo"], a["qot"],
+        a["qoh"], a["qw"], a["k"], a["hk"], a["kt"], a["kh"], a["ko"], a["kot"], a["koh"], a["kw"], a["eps"], None)
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(n=-1), -1), (dict(dt=3), -6), (dict(d=96), -2), (dict(pos=None), -1), (dict(pos=P + 2), -3), (dict(q=None, k=None), -1),
+    (dict(qo=None), -1), (dict(ko=None), -1), (dict(hq=0), -1), (dict(hk=-1), -1), (dict(hq=70000), -2), (dict(q=P + 8), -3),
+    (dict(qo=P + 4), -3), (dict(ko=P + 4), -3), (dict(qw=P + 4), -3), (dict(kw=P + 8), -3), (dict(qt=516), -3),
+    (dict(koh=124), -3), (dict(qot=64), -1), (dict(kot=120), -1), (dict(koh=64), -1), (dict(qt=-512), -1), (dict(eps=-1.0), -1),
+    (dict(eps=math.nan), -1), (dict(eps=math.inf), -1),
+])
+def test_rotate_refuses(oqm, kw, code):
+    assert rotate(oqm, **kw) == code
+
+
+@pytest.mark.parametrize("kw,code", [(dict(freq=None), -1), (dict(freq=P + 4), -3), (dict(rot_dim=24), -2), (dict(rot_dim=-16), -2),
+                                     (dict(rot_dim=144), -2), (dict(layout=2), -6), (dict(magnitude=math.nan), -1)])
+def test_rotate_refuses_bad_ropes(oqm, kw, code):
+    assert rotate(oqm, rope=rope_of(oqm, **kw)) == code
+    assert append(oqm, rope=rope_of(oqm, **kw)) == code
+
+
+def test_rotate_of_nothing_is_nothing(oqm):
+    assert rotate(oqm, n=0) == 0
+    assert rotate(oqm, n=0, q=None, hq=0, qo=None) == 0 and rotate(oqm, n=0, k=None, hk=0, ko=None) == 0
+    assert rotate(oqm, rope=rope_of(oqm, rot_dim=0, freq=None), n=0, pos=None) == 0
+
+
+def append(oqm, pool=None, seqs=None, rope=None, **kw):
+    a = dict(layer=1, n=3, pos=P, slot=P, seq=None, q=P, hq=28, qt=28 * 128, qh=128, qo=P, qot=28 * 128, qoh=128, qw=None, k=P,
+             kt=512, kh=128, kw=None, v=P, vt=512, vh=128, eps=1e-6)
+    a.update(kw)
+    return oqm.lib().stom_kv_append(
+        C.byref(pool or pool_of(oqm)), C.byref(seqs or seqs_of(oqm)), a["layer"], C.byref(rope or rope_of(oqm)), a["n"],
+        a["pos"], a["slot"], a["seq"], a["q"], a["hq"], a["qt"], a["qh"], a["qo"], a["qot"], a["qoh"], a["qw"], a["k"], a["kt"],
+        a["kh"], a["kw"], a["v"], a["vt"], a["vh"], a["eps"], None, None)
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(layer=2), -1), (dict(layer=-1), -1), (dict(n=-1), -1), (dict(slot=None), -1), (dict(slot=P + 1), -3), (dict(k=None), -1),
+    (dict(v=None), -1), (dict(v=P + 8), -3), (dict(vt=516), -3), (dict(vh=-128), -1), (dict(n=4), -1), (dict(seq=P + 2, n=4), -3),
+    (dict(pos=None), -1), (dict(qo=None), -1),
+])
+def test_append_refuses(oqm, kw, code):
+    assert append(oqm, **kw) == code
+
+
+def test_append_and_pages_refuse_bad_pools_and_sequences(oqm):
+    for kw, code in BAD_POOLS:
+        assert append(oqm, pool=pool_of(oqm, **kw)) == code
+        for call in (reserve, fork, free, compact):
+            assert call(oqm, pool=pool_of(oqm, **kw)) == code
+    for kw, code in BAD_SEQS:
+        assert append(oqm, seqs=seqs_of(oqm, **kw)) == code
+        for call in (reserve, fork, free, compact):
+            assert call(oqm, seqs=seqs_of(oqm, **kw)) == code
+    assert append(oqm, n=0) == 0
+
+
+def _pages(oqm, name, pool, seqs, *args):
+    return getattr(oqm.lib(), name)(C.byref(pool or pool_of(oqm)), C.byref(seqs or seqs_of(oqm)), *args)
+
+
+def reserve(oqm, pool=None, seqs=None, want=P, ws=P, nb=1 << 30):
+    return _pages(oqm, "stom_kv_reserve", pool, seqs, want, ws, nb, None, None)
+
+
+def fork(oqm, pool=None, seqs=None, wish=P):
+    return _pages(oqm, "stom_kv_fork", pool, seqs, wish, None, None)
+
+
+def free(oqm, pool=None, seqs=None, wish=P):
+    return _pages(oqm, "stom_kv_free", pool, seqs, wish, None, None)
+
+
+def compact(oqm, pool=None, seqs=None, t=P, r=P, n=None, ws=P, nb=1 << 30):
+    return _pages(oqm, "stom_kv_compact", pool, seqs, t, r, n, ws, nb, None, None)
+
+
+def test_pages_refuse(oqm):
+    for call in (reserve, fork, free, compact):
+        assert call(oqm, seqs=seqs_of(oqm, refs=None)) == -1
+    assert reserve(oqm, want=None) == -1 and fork(oqm, wish=None) == -1 and free(oqm, wish=None) == -1
+    assert reserve(oqm, want=P + 1) == -3 and fork(oqm, wish=P + 2) == -3 and free(oqm, wish=P + 2) == -3
+    need = oqm.lib().stom_kv_pages_workspace_bytes(C.byref(pool_of(oqm)), C.byref(seqs_of(oqm)))
+    assert need >= 256 + 10 * 4 + 10 * 16
+    for call in (reserve, compact):
+        assert call(oqm, ws=None) == -8 and call(oqm, ws=P + 8) == -8 and call(oqm, nb=need - 1) == -8
+    assert reserve(oqm, seqs=seqs_of(oqm, n_seqs=8193)) == -2                      # more rows than a plan holds
+    assert compact(oqm, t=None) == -1 and compact(oqm, r=None) == -1 and compact(oqm, r=P + 2) == -3 and compact(oqm, n=P + 1) == -3
+    for call in (reserve, fork, free):
+        assert call(oqm, seqs=seqs_of(oqm, n_seqs=0)) == 0
+    assert reserve(oqm, pool=pool_of(oqm, page_tokens=1 << 25)) == -2              # a page's 16-byte chunks pass 2^30
+
+
+def sample(oqm, **kw):
+    a = dict(x=P, dt=0, rows=4, n=100, stride=100, t=P, k=P, p=P, m=P, u=P, token=P, kept=P, lp=P)
+    a.update(kw)
+    return oqm.lib().stom_sample_tokens(a["x"], a["dt"], a["rows"], a["n"], a["stride"], a["t"], a["k"], a["p"], a["m"], a["u"],
+                                        a["token"], a["kept"], a["lp"], None, None)
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(rows=-1), -1), (dict(n=0), -1), (dict(dt=3), -6), (dict(n=500001, stride=500001), -2), (dict(x=None), -1),
+    (dict(token=None), -1), (dict(u=None, t=None), -1), (dict(stride=99), -1), (dict(stride=-100), -1), (dict(x=P + 1), -3),
+    (dict(x=P + 2, dt=2), -3), (dict(t=P + 2), -3), (dict(k=P + 1), -3), (dict(p=P + 2), -3), (dict(m=P + 2), -3),
+    (dict(u=P + 2), -3), (dict(token=P + 2), -3), (dict(kept=P + 2), -3), (dict(lp=P + 2), -3),
+])
+def test_sample_refuses(oqm, kw, code):
+    assert sample(oqm, **kw) == code
+
+
+def test_sample_of_no_row_is_nothing(oqm):
+    assert sample(oqm, rows=0) == 0 and sample(oqm, rows=0, x=None, token=None) == 0
+
+
 def test_page_of_a_token_by_multiplication_equals_the_division():
     """floor(x / d) = (mulhi(x, m) + x) >> s with s = ceil(log2 d), m = floor(2^32 (2^s - d) / d) + 1, for x < 2^31."""
     rng = np.random.default_rng(1)
