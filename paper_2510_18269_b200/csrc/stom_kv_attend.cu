@@ -125,11 +125,13 @@ __global__ void __launch_bounds__(Shape<D, NT>::kWarps * 32, 1) kv_attend_kernel
 
     if (lane < 2) piece_unit[2 * warp + lane] = -1;
     grid_dependency_wait();
+    grid_launch_dependents();   // the joining kernel may take its places now; it waits for this grid's end
 
     // ---- the stretch of this warp
     const int units = p.n_kv_heads * p.blocks_per_head;   // per sequence
     const int seg = (p.n_seqs + 31) / 32;                 // sequences a lane adds up
     long long mine = 0;
+#pragma unroll 4
     for (int b = lane * seg; b < min(p.n_seqs, (lane + 1) * seg); ++b) mine += tiles_of(p, b);
     mine *= units;
     long long upto = mine;
@@ -140,20 +142,9 @@ __global__ void __launch_bounds__(Shape<D, NT>::kWarps * 32, 1) kv_attend_kernel
     }
     const long long total = __shfl_sync(~0u, upto, 31);
     const long long warps = (long long)gridDim.x * kWarps;
-    const long long per = max(1ll, (total + warps - 1) / warps);
+    const long long per = total >> 31 ? (total + warps - 1) / warps : max(1u, ((uint32_t)total + (uint32_t)warps - 1) / (uint32_t)warps);
     const long long f0 = min(total, ((long long)blockIdx.x * kWarps + warp) * per), f1 = min(total, f0 + per);
     int left = (int)(f1 - f0);
-
-    // the empty sequences: zeros
-    for (int b = blockIdx.x * kWarps + warp; b < p.n_seqs; b += gridDim.x * kWarps) {
-        if (tiles_of(p, b)) continue;
-        const int heads = p.n_kv_heads * p.group;
-        for (int h = 0; h < heads; ++h) {
-            T *o = reinterpret_cast<T *>(p.out) + b * p.out_stride_seq + h * p.out_stride_head;
-            for (int c = lane; c < D / 2; c += 32) reinterpret_cast<uint32_t *>(o)[c] = 0u;
-            if (p.lse && lane == 0) p.lse[(int64_t)b * heads + h] = -INFINITY;
-        }
-    }
 
     int pieces = 0;   // partial results this warp leaves in shared memory
     if (left > 0) {
@@ -164,8 +155,9 @@ __global__ void __launch_bounds__(Shape<D, NT>::kWarps * 32, 1) kv_attend_kernel
             const int at = __ffs(past) - 1;                       // the lane whose sequences hold it
             long long before = __shfl_sync(~0u, upto - mine, at);
             int b = at * seg;
+            cur.b = b;
             const int end = min(p.n_seqs, b + seg);
-            for (;; b += 32) {                                    // 32 of them at a time
+            for (; seg > 1; b += 32) {                                    // 32 of them at a time
                 const int t = b + lane < end ? tiles_of(p, b + lane) : 0;
                 long long sum = (long long)t * units;
                 const long long own = sum;
@@ -186,38 +178,45 @@ __global__ void __launch_bounds__(Shape<D, NT>::kWarps * 32, 1) kv_attend_kernel
             span_of(p, cur.b, cur.first, cur.end);
             cur.tiles = (cur.end - cur.first + kTile - 1) / kTile;
             const long long in = f0 - before;
-            cur.hu = (int)(in / cur.tiles);
+            cur.hu = in >> 31 ? (int)(in / cur.tiles) : (int)((uint32_t)in / (uint32_t)cur.tiles);
             cur.tile = (int)(in - (long long)cur.hu * cur.tiles);
         }
 
-        // ---- loads.  Lane r (and r + 16) looks up the page of row r one tile ahead of the copies.
+        // ---- loads.  Lane r (and r + 16) looks up the page of row r two tiles ahead of the copies.
         Cursor ld = cur;
-        int ld_left = left;
-        int page_id = -1, page_off = 0;
-        auto look_up = [&]() {
-            const int t = ld.first + ld.tile * kTile + (lane & 15);
-            page_id = -1;
-            if (ld_left > 0 && t < ld.end) {
-                const uint32_t pg = div_by(p.page, (uint32_t)t);
-                page_off = t - (int)(pg * p.page.d);
-                page_id = p.table[ld.b * p.table_stride + pg];
-            } else {
-                page_id = -2;   // not a token
+        int to_look = left;          // tiles not looked up yet
+        struct Row {
+            int page;                // id; kNone: not a token
+            int64_t rest;            // offset within a page, in elements
+        };
+        constexpr int kNone = INT32_MIN;
+        Row ahead[2];
+        auto look_up = [&](Row &r) {
+            r.page = kNone;
+            if (to_look > 0) {
+                const int t = ld.first + ld.tile * kTile + (lane & 15);
+                if (t < ld.end) {
+                    const uint32_t pg = div_by(p.page, (uint32_t)t);
+                    r.rest = (int64_t)(t - (int)(pg * p.page.d)) * p.stride_token + (ld.hu / p.blocks_per_head) * p.stride_head;
+                    r.page = p.table[ld.b * p.table_stride + pg];
+                    if (r.page == kNone) r.page = -1;
+                }
+                if (--to_look > 0) advance(p, units, ld);
             }
         };
         uint64_t seen = 0;       // 16 bits per tile in flight, oldest lowest: which rows are tokens
-        int in_flight = 0;
+        int in_flight = 0, to_issue = left;
         const uint32_t ring_u = smem_u32(ring);
         auto issue = [&](int stage) {
-            if (ld_left > 0) {
-                const bool ok = (uint32_t)page_id < (uint32_t)p.n_pages;
-                if (page_id != -2 && !ok && p.flags) atomicOr(p.flags, STOM_FLAG_BAD_INDEX);
+            if (to_issue > 0) {
+                --to_issue;
+                const Row r = ahead[0];
+                const bool ok = (uint32_t)r.page < (uint32_t)p.n_pages;
+                if (r.page != kNone && !ok && p.flags) atomicOr(p.flags, STOM_FLAG_BAD_INDEX);
                 const uint32_t m = __ballot_sync(~0u, ok) & 0xffffu;
                 seen |= (uint64_t)m << (16 * in_flight);
                 ++in_flight;
-                const int64_t off = ok ? 2 * (page_id * p.stride_page + page_off * p.stride_token +
-                                              (ld.hu / p.blocks_per_head) * p.stride_head)
-                                       : -1;
+                const int64_t off = ok ? 2 * (r.page * p.stride_page + r.rest) : -1;
                 const uint32_t dst = ring_u + stage * (2 * S::kTileBytes);
                 const int sub = lane / kChunks, chunk = lane % kChunks;
 #pragma unroll
@@ -229,13 +228,13 @@ __global__ void __launch_bounds__(Shape<D, NT>::kWarps * 32, 1) kv_attend_kernel
                     copy16_async(d, p.k + at, o < 0 ? 0u : 16u);
                     copy16_async(d + S::kTileBytes, p.v + at, o < 0 ? 0u : 16u);
                 }
-                --ld_left;
-                if (ld_left > 0) advance(p, units, ld);
-                look_up();
+                ahead[0] = ahead[1];
+                look_up(ahead[1]);
             }
             copy_commit();
         };
-        look_up();
+        look_up(ahead[0]);
+        look_up(ahead[1]);
 #pragma unroll
         for (int i = 0; i < kStages - 1; ++i) issue(i);
 
@@ -426,71 +425,96 @@ __global__ void __launch_bounds__(Shape<D, NT>::kWarps * 32, 1) kv_attend_kernel
     }
     __syncthreads();
 
-    // ---- join the block's pieces, unit by unit; they stand in the order of the line
+    // ---- join the block's pieces, unit by unit; they stand in the order of the line.  A thread has four channels of a
+    // head and walks the pieces with a running maximum; with more threads than that takes, teams take units in turn.
     int open_unit = -1, goes_on = 0;
-    for (int i = 0; i < S::kPieces;) {
-        const int unit = piece_unit[i];
-        if (unit < 0) {
-            ++i;
-            continue;
-        }
-        int ends = 0, n = 0, e = i;
-        for (; e < S::kPieces && (piece_unit[e] == unit || piece_unit[e] < 0); ++e) {
-            if (piece_unit[e] < 0) continue;
-            if (n == 0) ends |= piece_ends[e] & 1;
-            ends = (ends & 1) | (piece_ends[e] & 2);
-            ++n;
-        }
-        const int b = unit / units, hu = unit - b * units;
-        int head0;
-        const int nh = heads_of(p, hu, kHeads, head0);
-        const int slot = ends & 1 ? 1 : 0;   // of the workspace: a unit that came in, or one that goes out
-        if (!(ends & 2)) {
-            if (ends & 1) open_unit = unit;
-            else goes_on = 1;
-        }
-        for (int at = threadIdx.x; at < nh * D; at += kWarps * 32) {
-            const int h = at / D, c = at % D;
-            float m = -INFINITY;
-            for (int j = i; j < e; ++j)
-                if (piece_unit[j] >= 0) m = fmaxf(m, piece_ml[j * kHeads + h].x);
-            const float base = m == -INFINITY ? 0.f : m;
-            float l = 0.f, o = 0.f;
-            for (int j = i; j < e; ++j) {
-                if (piece_unit[j] < 0) continue;
-                const float2 ml = piece_ml[j * kHeads + h];
-                const float f = exp2f(ml.x - base);
-                const uint8_t *src = j & 1 ? smem + (j >> 1) * S::kRing : smem + kWarps * S::kRing + (j >> 1) * S::kPiece;
-                l += f * ml.y;
-                o += f * reinterpret_cast<const float *>(src)[h * D + c];
+    constexpr int kCols = kHeads * D / 4, kThreads = kWarps * 32, kTeams = kThreads > kCols ? kThreads / kCols : 1;
+    const int team = kTeams > 1 ? threadIdx.x / kCols : 0;
+    for (int at = threadIdx.x - team * kCols; at < kCols; at += kThreads) {
+        const int h = at / (D / 4), c = at % (D / 4) * 4;
+        int unit = -1, ends = 0, turn = -1;
+        float m = -INFINITY, l = 0.f;
+        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+        auto finish = [&]() {
+            if (!(ends & 2)) {
+                if (ends & 1) open_unit = unit;
+                else goes_on = 1;
             }
+            if (turn % kTeams != team) return;
+            const int b = unit / units, hu = unit - b * units;
+            int head0;
+            if (h >= heads_of(p, hu, kHeads, head0)) return;
             if (ends == 3) {
-                reinterpret_cast<T *>(p.out)[b * p.out_stride_seq + (head0 + h) * p.out_stride_head + c] =
-                    from_float<T>(l == 0.f ? 0.f : o / l);
+                const float inv = l == 0.f ? 0.f : 1.f / l;
+                T *dst = reinterpret_cast<T *>(p.out) + b * p.out_stride_seq + (head0 + h) * p.out_stride_head + c;
+                *reinterpret_cast<uint2 *>(dst) = make_uint2(pack2<T>(o.x * inv, o.y * inv), pack2<T>(o.z * inv, o.w * inv));
                 if (p.lse && c == 0)
                     p.lse[(int64_t)b * (p.n_kv_heads * p.group) + head0 + h] =
                         l == 0.f ? -INFINITY : 0.6931471805599453f * m + logf(l);
             } else {
-                const int64_t w = ((int64_t)blockIdx.x * 2 + slot) * kHeads + h;
-                p.part_o[w * D + c] = o;
+                // of the workspace: slot 1 for a unit that begins here, slot 0 for one that came in
+                const int64_t w = ((int64_t)blockIdx.x * 2 + (ends & 1)) * kHeads + h;
+                *reinterpret_cast<float4 *>(p.part_o + w * D + c) = o;
                 if (c == 0) p.part_ml[w] = make_float2(m, l);
             }
+        };
+        for (int j = 0; j < S::kPieces; ++j) {
+            const int u = piece_unit[j];
+            if (u < 0) continue;
+            if (u != unit) {
+                if (unit >= 0) finish();
+                unit = u;
+                ends = piece_ends[j] & 1;
+                ++turn;
+                m = -INFINITY;
+                l = 0.f;
+                o = make_float4(0.f, 0.f, 0.f, 0.f);
+            }
+            ends = (ends & 1) | (piece_ends[j] & 2);
+            if (turn % kTeams != team) continue;
+            const float2 ml = piece_ml[j * kHeads + h];
+            const uint8_t *src = j & 1 ? smem + (j >> 1) * S::kRing : smem + kWarps * S::kRing + (j >> 1) * S::kPiece;
+            const float4 v = *reinterpret_cast<const float4 *>(src + (h * D + c) * 4);
+            const float top = fmaxf(m, ml.x), base = top == -INFINITY ? 0.f : top;
+            const float fa = exp2f(m - base), fb = exp2f(ml.x - base);
+            m = top;
+            l = l * fa + ml.y * fb;
+            o.x = o.x * fa + v.x * fb;
+            o.y = o.y * fa + v.y * fb;
+            o.z = o.z * fa + v.z * fb;
+            o.w = o.w * fa + v.w * fb;
         }
-        i = e;
+        if (unit >= 0) finish();
     }
     if (threadIdx.x == 0) {
         p.open_unit[blockIdx.x] = open_unit;
         p.goes_on[blockIdx.x] = goes_on;
     }
+
+    // the empty sequences: zeros
+    for (int b = blockIdx.x * kWarps + warp; b < p.n_seqs; b += gridDim.x * kWarps) {
+        if (tiles_of(p, b)) continue;
+        const int heads = p.n_kv_heads * p.group;
+        for (int h = 0; h < heads; ++h) {
+            T *o = reinterpret_cast<T *>(p.out) + b * p.out_stride_seq + h * p.out_stride_head;
+            for (int c = lane; c < D / 2; c += 32) reinterpret_cast<uint32_t *>(o)[c] = 0u;
+            if (p.lse && lane == 0) p.lse[(int64_t)b * heads + h] = -INFINITY;
+        }
+    }
 }
 
 // Joins the partial results of the units that cross a block's end: block (x, h) of this grid takes query head h of the
-// unit that begins in block x of the kernel above and goes on behind it, if there is one.
+// unit that begins in block x of the kernel above and goes on behind it, if there is one.  Thread (g, c) adds up every
+// kJoin-th partial result of four channels.
+constexpr int kJoin = 8;
 template <typename T, int D, int NT>
-__global__ void __launch_bounds__(D) kv_attend_join_kernel(const __grid_constant__ KvAttendParams p) {
-    constexpr int kHeads = 8 * NT;
+__global__ void __launch_bounds__(D / 4 * kJoin) kv_attend_join_kernel(const __grid_constant__ KvAttendParams p) {
+    constexpr int kHeads = 8 * NT, kThreads = D / 4 * kJoin;
     __shared__ float weight[kMaxBlocks];
-    __shared__ float head_m[32], head_l[32];
+    __shared__ float warp_m[32], warp_l[32];
+    __shared__ float4 sum[kJoin][D / 4];
+    __shared__ int end_s;
+    if (threadIdx.x == 0) end_s = gridDim.x;
     grid_dependency_wait();
     const int first = blockIdx.x, h = blockIdx.y, blocks = gridDim.x;
     const int unit = p.open_unit[first];
@@ -500,45 +524,71 @@ __global__ void __launch_bounds__(D) kv_attend_join_kernel(const __grid_constant
     int head0;
     if (h >= heads_of(p, hu, kHeads, head0)) return;
     // the blocks it goes through: first, first + 1, ..., end - 1
-    __shared__ int end_s;
-    if (threadIdx.x == 0) end_s = blocks;
     __syncthreads();
-    for (int j = first + 1 + threadIdx.x; j < blocks; j += D)
-        if (!p.goes_on[j]) atomicMin(&end_s, j + 1);
+    for (int j = first + 1 + threadIdx.x; j < blocks; j += kThreads)
+        if (!p.goes_on[j]) {
+            atomicMin(&end_s, j + 1);
+            break;
+        }
     __syncthreads();
     const int n = end_s - first;
     auto row_of = [&](int j) { return ((int64_t)(first + j) * 2 + (j == 0 ? 1 : 0)) * kHeads + h; };
+    float2 ml[kMaxBlocks / kThreads + 1];
     float m = -INFINITY;
-    for (int j = threadIdx.x; j < n; j += D) {
-        const float2 ml = p.part_ml[row_of(j)];
-        weight[j] = ml.x;
-        m = fmaxf(m, ml.x);
+#pragma unroll
+    for (int k = 0; k <= kMaxBlocks / kThreads; ++k) {
+        const int j = threadIdx.x + k * kThreads;
+        ml[k] = j < n ? p.part_ml[row_of(j)] : make_float2(-INFINITY, 0.f);
+        m = fmaxf(m, ml[k].x);
     }
 #pragma unroll
     for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(~0u, m, o));
-    if ((threadIdx.x & 31) == 0) head_m[threadIdx.x >> 5] = m;
+    if ((threadIdx.x & 31) == 0) warp_m[threadIdx.x >> 5] = m;
     __syncthreads();
     m = -INFINITY;
-    for (int j = 0; j < D / 32; ++j) m = fmaxf(m, head_m[j]);
+#pragma unroll
+    for (int j = 0; j < kThreads / 32; ++j) m = fmaxf(m, warp_m[j]);
     const float base = m == -INFINITY ? 0.f : m;
     float l = 0.f;
-    for (int j = threadIdx.x; j < n; j += D) {
-        const float f = exp2f(weight[j] - base);
-        weight[j] = f;
-        l += f * p.part_ml[row_of(j)].y;
+#pragma unroll
+    for (int k = 0; k <= kMaxBlocks / kThreads; ++k) {
+        const int j = threadIdx.x + k * kThreads;
+        const float f = exp2f(ml[k].x - base);
+        if (j < n) weight[j] = f;
+        l += f * ml[k].y;
     }
 #pragma unroll
     for (int o = 16; o; o >>= 1) l += __shfl_xor_sync(~0u, l, o);
-    if ((threadIdx.x & 31) == 0) head_l[threadIdx.x >> 5] = l;
+    if ((threadIdx.x & 31) == 0) warp_l[threadIdx.x >> 5] = l;
     __syncthreads();
     l = 0.f;
-    for (int j = 0; j < D / 32; ++j) l += head_l[j];
-    const int c = threadIdx.x;
-    float o = 0.f;
-#pragma unroll 8
-    for (int j = 0; j < n; ++j) o += weight[j] * p.part_o[row_of(j) * D + c];
-    reinterpret_cast<T *>(p.out)[b * p.out_stride_seq + (head0 + h) * p.out_stride_head + c] =
-        from_float<T>(l == 0.f ? 0.f : o / l);
+#pragma unroll
+    for (int j = 0; j < kThreads / 32; ++j) l += warp_l[j];
+    const int c = threadIdx.x % (D / 4), g = threadIdx.x / (D / 4);
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+    for (int j = g; j < n; j += kJoin) {
+        const float4 v = *reinterpret_cast<const float4 *>(p.part_o + row_of(j) * D + c * 4);
+        const float f = weight[j];
+        o.x += f * v.x;
+        o.y += f * v.y;
+        o.z += f * v.z;
+        o.w += f * v.w;
+    }
+    sum[g][c] = o;
+    __syncthreads();
+    if (g) return;
+#pragma unroll
+    for (int k = 1; k < kJoin; ++k) {
+        const float4 v = sum[k][c];
+        o.x += v.x;
+        o.y += v.y;
+        o.z += v.z;
+        o.w += v.w;
+    }
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    T *dst = reinterpret_cast<T *>(p.out) + b * p.out_stride_seq + (head0 + h) * p.out_stride_head + c * 4;
+    *reinterpret_cast<uint2 *>(dst) = make_uint2(pack2<T>(o.x * inv, o.y * inv), pack2<T>(o.z * inv, o.w * inv));
     if (p.lse && c == 0)
         p.lse[(int64_t)b * (p.n_kv_heads * p.group) + head0 + h] =
             l == 0.f ? -INFINITY : 0.6931471805599453f * m + logf(l);
@@ -557,7 +607,8 @@ int32_t launch(const KvAttendParams &p, int sms, cudaStream_t stream) {
     if (e == cudaSuccess)
         e = launch_after_producer(kv_attend_kernel<T, D, NT>, dim3(sms), dim3(S::kWarps * 32), S::kSmem, stream, p);
     if (e == cudaSuccess)
-        e = launch_after_producer(kv_attend_join_kernel<T, D, NT>, dim3(sms, min(p.group, 8 * NT)), dim3(D), 0, stream, p);
+        e = launch_after_producer(kv_attend_join_kernel<T, D, NT>, dim3(sms, min(p.group, 8 * NT)), dim3(D / 4 * kJoin), 0, stream,
+                                  p);
     if (e != cudaSuccess) {
         set_last_cuda_error(e);
         return STOM_ERR_CUDA;

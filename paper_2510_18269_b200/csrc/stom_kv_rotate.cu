@@ -7,7 +7,9 @@
 // decode step (a few kilobytes) the launch.  One pass, all loads and stores 16 bytes wide.  A row (one head of one token)
 // belongs to d/16 adjacent threads; a thread owns the two 16-byte chunks that rotate with one another (half layout: the
 // chunk and the one rot_dim/2 channels on; pairs: two adjacent chunks), so a rotation needs no exchange and a norm a few
-// shuffles.  The sines and cosines of a token are worked out once per block, in shared memory, and serve all its heads.
+// shuffles.  A warp works on one token at a time, on several of its rows at once and on the others after them: its sines
+// and cosines, and the norm's weights, are then the same for all its rows and stay in registers, and warps need no
+// barrier.  A token with few companions is cut into parts, one warp each, down to one round of rows.
 // Angles: pos * freq is formed and reduced to [-pi, pi] in binary64 (at position 10^6 a binary32 product would be off by
 // 0.03 radians); the sine and cosine of the reduced angle are taken in binary32 with a first-order correction for the
 // part of the angle that its rounding to binary32 lost.
@@ -27,10 +29,10 @@ struct RowSet {
 };
 
 struct RotateParams {
-    RowSet set[3];              // queries, keys, values (values are only copied)
-    int32_t first_k, first_v;   // rows of a token: [0, first_k) queries, [first_k, first_v) keys, then values
-    FastDiv rows;
-    int32_t n_tokens, tokens_per_block;
+    RowSet set[3];              // queries, keys, values (values are only copied; src NULL: none)
+    int32_t n_q, n_k, n_tokens;
+    FastDiv parts;              // warps a token is cut into
+    int32_t steps_per_part;     // of a warp's rows: first those of the keys and values, then those of the queries
     const int32_t *pos;
     const double *freq;
     int32_t half;               // rotated pairs = rot_dim / 2
@@ -46,201 +48,318 @@ struct RotateParams {
     uint32_t *flags;
 };
 
-// Eight adjacent values as floats, and back
+// Two binary32 numbers in one 64-bit register: one instruction works on both
+struct Pair {
+    uint64_t v;
+};
+__device__ __forceinline__ Pair pair_of(float a, float b) {
+    Pair r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ float2 split(Pair a) {
+    float2 f;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(f.x), "=f"(f.y) : "l"(a.v));
+    return f;
+}
+__device__ __forceinline__ Pair mul(Pair a, Pair b) {
+    Pair r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+    return r;
+}
+__device__ __forceinline__ Pair fma(Pair a, Pair b, Pair c) {
+    Pair r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+    return r;
+}
+__device__ __forceinline__ Pair swapped(Pair a) {
+    const float2 f = split(a);
+    return pair_of(f.y, f.x);
+}
+
+// Eight adjacent values: as stored, and as pairs
 template <typename T>
 struct Chunk {
     uint4 v;
-    __device__ __forceinline__ void load(const T *p) { v = *reinterpret_cast<const uint4 *>(p); }
-    __device__ __forceinline__ void store(T *p) const { *reinterpret_cast<uint4 *>(p) = v; }
-    __device__ __forceinline__ void get(float (&f)[8]) const {
-        unpack2<T>(v.x, f[0], f[1]);
-        unpack2<T>(v.y, f[2], f[3]);
-        unpack2<T>(v.z, f[4], f[5]);
-        unpack2<T>(v.w, f[6], f[7]);
+    __device__ __forceinline__ void load(const char *p) { v = *reinterpret_cast<const uint4 *>(p); }
+    __device__ __forceinline__ void store(char *p) const { *reinterpret_cast<uint4 *>(p) = v; }
+    __device__ __forceinline__ void get(Pair (&f)[4]) const {
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            float lo, hi;
+            unpack2<T>(w[e], lo, hi);
+            f[e] = pair_of(lo, hi);
+        }
     }
-    __device__ __forceinline__ void set(const float (&f)[8]) {
-        v = make_uint4(pack2<T>(f[0], f[1]), pack2<T>(f[2], f[3]), pack2<T>(f[4], f[5]), pack2<T>(f[6], f[7]));
+    __device__ __forceinline__ void set(const Pair (&f)[4]) {
+        uint32_t w[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float2 x = split(f[e]);
+            w[e] = pack2<T>(x.x, x.y);
+        }
+        v = make_uint4(w[0], w[1], w[2], w[3]);
     }
 };
 template <>
 struct Chunk<float> {
     float4 a, b;
-    __device__ __forceinline__ void load(const float *p) {
+    __device__ __forceinline__ void load(const char *p) {
         a = reinterpret_cast<const float4 *>(p)[0];
         b = reinterpret_cast<const float4 *>(p)[1];
     }
-    __device__ __forceinline__ void store(float *p) const {
+    __device__ __forceinline__ void store(char *p) const {
         reinterpret_cast<float4 *>(p)[0] = a;
         reinterpret_cast<float4 *>(p)[1] = b;
     }
-    __device__ __forceinline__ void get(float (&f)[8]) const {
-        f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w; f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
+    __device__ __forceinline__ void get(Pair (&f)[4]) const {
+        f[0] = pair_of(a.x, a.y);
+        f[1] = pair_of(a.z, a.w);
+        f[2] = pair_of(b.x, b.y);
+        f[3] = pair_of(b.z, b.w);
     }
-    __device__ __forceinline__ void set(const float (&f)[8]) {
-        a = make_float4(f[0], f[1], f[2], f[3]);
-        b = make_float4(f[4], f[5], f[6], f[7]);
+    __device__ __forceinline__ void set(const Pair (&f)[4]) {
+        const float2 x0 = split(f[0]), x1 = split(f[1]), x2 = split(f[2]), x3 = split(f[3]);
+        a = make_float4(x0.x, x0.y, x1.x, x1.y);
+        b = make_float4(x2.x, x2.y, x3.x, x3.y);
     }
 };
 
+// The rows of one kind as a lane meets them, step by step
 template <typename T, int D>
-__global__ void __launch_bounds__(kThreads) kv_rotate_kernel(const __grid_constant__ RotateParams p) {
-    constexpr int kPerRow = D / 16;                 // threads of a row
-    constexpr int kRowsAtOnce = kThreads / kPerRow;
-    extern __shared__ __align__(16) float2 turn[];  // [tokens of the block][half]: cosine and sine
-    __shared__ int64_t place[32];                   // of a token in the pool, in elements; -1: not stored
-
-    const int token0 = blockIdx.x * p.tokens_per_block;
-    const int tokens = min(p.tokens_per_block, p.n_tokens - token0);
-    const int items = tokens * (int)p.rows.d;
-    const int t = threadIdx.x % kPerRow, h2 = p.half >> 3;
-    const bool turns = t < h2;
-    int ca, cb;                                     // this thread's chunks of a row
-    if (p.layout == STOM_ROPE_PAIRS) {
-        ca = 2 * t;
-        cb = 2 * t + 1;
-    } else if (turns) {
-        ca = t;
-        cb = t + h2;
-    } else {
-        ca = 2 * t;                                 // 2 h2 + 2 (t - h2)
-        cb = 2 * t + 1;
+struct Walk {
+    const char *src;
+    char *dst;
+    int64_t src_step, dst_step;   // bytes
+    int left;                     // rows from this lane's next one on
+    __device__ __forceinline__ Walk(const RowSet &s, int tok, int head, int n, int64_t dst_at, int rows) {
+        const int64_t e = sizeof(T);
+        src = s.src + e * (tok * s.src_token + head * s.src_head);
+        dst = s.dst + e * (dst_at + head * s.dst_head);
+        src_step = e * rows * s.src_head;
+        dst_step = e * rows * s.dst_head;
+        left = n - head;
     }
+};
 
-    // item -> token of the block and row; the loads of one item are on their way while the one before is worked on
-    struct Item {
-        int tok, row, kind;                         // kind: 0 query, 1 key, 2 value, -1 none
-    };
-    auto item_at = [&](int i) {
-        Item it;
-        it.kind = -1;
-        if (i < items) {
-            it.tok = (int)div_by(p.rows, (uint32_t)i);
-            it.row = i - it.tok * (int)p.rows.d;
-            it.kind = it.row < p.first_k ? 0 : it.row < p.first_v ? 1 : 2;
-            it.row -= it.kind == 0 ? 0 : it.kind == 1 ? p.first_k : p.first_v;
-        }
-        return it;
-    };
-    auto fetch = [&](const Item &it, Chunk<T> &a, Chunk<T> &b) {
-        if (it.kind < 0) return;
-        const RowSet &s = p.set[it.kind];
-        const T *x = reinterpret_cast<const T *>(s.src) + (token0 + it.tok) * s.src_token + it.row * s.src_head;
-        a.load(x + ca * 8);
-        b.load(x + cb * 8);
-    };
+// PAIRS: channels 2i and 2i + 1 rotate with one another; otherwise i and i + rot_dim / 2.
+template <typename T, int D, bool NORM, bool PAIRS>
+__global__ void __launch_bounds__(kThreads, NORM ? 2 : 3) kv_rotate_kernel(const __grid_constant__ RotateParams p) {
+    constexpr int kPerRow = D / 16;                 // threads of a row
+    constexpr int kRows = 32 / kPerRow;             // rows of a warp's step
+    constexpr int kE = sizeof(T);
+    __shared__ float2 turn_smem[kThreads / 32][D / 2];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    float2 *turn = turn_smem[warp];                 // cosine and sine of the token's angles
+    const uint32_t unit = blockIdx.x * (kThreads / 32) + warp;
+    const int tok = (int)div_by(p.parts, unit), part = (int)(unit - tok * p.parts.d);
+    if (tok >= p.n_tokens) return;
+    const int t = lane % kPerRow, sub = lane / kPerRow, h2 = p.half >> 3;
+    const bool turns = t < h2;
+    const bool across = !PAIRS && turns;
+    const int ca = (across ? t : 2 * t) * 8 * kE, cb = (across ? t + h2 : 2 * t + 1) * 8 * kE;
+
+    // steps of this part: [s0, s1), those below kv_steps with keys and values
+    const int kv_steps = (p.n_k + kRows - 1) / kRows, q_steps = (p.n_q + kRows - 1) / kRows;
+    const int s0 = part * p.steps_per_part, s1 = min(s0 + p.steps_per_part, kv_steps + q_steps);
+    const int k0 = min(s0, kv_steps), k1 = min(s1, kv_steps), q0 = max(s0, kv_steps) - kv_steps, q1 = max(s1, kv_steps) - kv_steps;
 
     grid_dependency_wait();
-    int i = threadIdx.x / kPerRow;
-    Item it = item_at(i);
-    Chunk<T> a, b;
-    fetch(it, a, b);
 
-    for (int j = threadIdx.x; j < tokens * p.half; j += kThreads) {
-        const int tok = j / p.half, pair = j - tok * p.half;
-        const double angle = (double)p.pos[token0 + tok] * p.freq[pair];
-        const double n = rint(angle * 0.15915494309189535);
-        double r = fma(-n, 6.283185307179586, angle);
-        r = fma(-n, 2.4492935982947064e-16, r);     // what 2 pi has beyond its binary64 value
-        const float rf = (float)r, rest = (float)(r - (double)rf);
-        float s, c;
-        sincosf(rf, &s, &c);
-        turn[j] = make_float2(p.magnitude * fmaf(-rest, s, c), p.magnitude * fmaf(rest, c, s));
-    }
-    if (p.table && threadIdx.x < tokens) {
-        const int tok = token0 + threadIdx.x;
+    // the token's place in the pool, in elements; -1: it is not stored
+    int64_t place = tok * p.set[1].dst_token;
+    if (p.table) {
         const int sl = p.slot[tok], sq = p.seq ? p.seq[tok] : tok;
-        int64_t at = -1;
+        place = -1;
         if (sl != -1) {
             bool ok = (uint32_t)sl < (uint32_t)p.max_tokens && (uint32_t)sq < (uint32_t)p.n_seqs;
             if (ok) {
                 const uint32_t pg = div_by(p.page, (uint32_t)sl);
                 const int id = p.table[sq * p.table_stride + pg];
                 ok = (uint32_t)id < (uint32_t)p.n_pages;
-                if (ok) at = id * p.stride_page + (int64_t)(sl - pg * p.page.d) * p.stride_token;
+                if (ok) place = id * p.stride_page + (int64_t)(sl - pg * p.page.d) * p.stride_token;
             }
-            if (!ok && p.flags) atomicOr(p.flags, STOM_FLAG_BAD_INDEX);
+            if (!ok && p.flags && lane == 0) atomicOr(p.flags, STOM_FLAG_BAD_INDEX);
         }
-        place[threadIdx.x] = at;
     }
-    __syncthreads();
+    // the first rows are on their way before the angles are worked out
+    Walk<T, D> k(p.set[1], tok, k0 * kRows + sub, min(p.n_k, k1 * kRows), place, kRows);
+    Walk<T, D> v(p.set[2], tok, k0 * kRows + sub, p.set[2].src ? min(p.n_k, k1 * kRows) : 0, place, kRows);
+    Chunk<T> qa[2], qb[2], ka, kb, va, vb;
+    auto fetch = [&](Walk<T, D> &w, Chunk<T> &a, Chunk<T> &b, int ahead) {
+        if (w.left > ahead * kRows) {
+            a.load(w.src + ahead * w.src_step + ca);
+            b.load(w.src + ahead * w.src_step + cb);
+        }
+    };
+    auto queries = [&]() {
+        return Walk<T, D>(p.set[0], tok, q0 * kRows + sub, min(p.n_q, q1 * kRows), tok * p.set[0].dst_token, kRows);
+    };
+    fetch(k, ka, kb, 0);
+    fetch(v, va, vb, 0);
+    {
+        Walk<T, D> q = queries();
+        fetch(q, qa[0], qb[0], 0);
+        fetch(q, qa[1], qb[1], 1);
+    }
 
-    for (int round = 0; round < items; round += kRowsAtOnce) {   // the same number for every thread: shuffles below
-        const int ahead = i + kRowsAtOnce;
-        const Item next = item_at(ahead);
-        Chunk<T> na, nb;
-        fetch(next, na, nb);
-        const RowSet &set = p.set[it.kind < 0 ? 0 : it.kind];
-        const bool works = it.kind == 0 || it.kind == 1;
-        float x[8], y[8];
-        if (works) {
-            a.get(x);
-            b.get(y);
-        }
-        if (p.set[0].weight || p.set[1].weight) {
-            float sum = 0.f;
-            if (works)
+    for (int j = lane; j < p.half; j += 32) {
+        const double angle = (double)p.pos[tok] * p.freq[j];
+        const double n = rint(angle * 0.15915494309189535);
+        double r = ::fma(-n, 6.283185307179586, angle);
+        r = ::fma(-n, 2.4492935982947064e-16, r);   // what 2 pi has beyond its binary64 value
+        const float rf = (float)r, rest = (float)(r - (double)rf);
+        float s, c;
+        sincosf(rf, &s, &c);
+        turn[j] = make_float2(p.magnitude * fmaf(-rest, s, c), p.magnitude * fmaf(rest, c, s));
+    }
+    __syncwarp();
+
+    // x' = x xx + (y, or x's neighbour) xy,  y' = y yy + (x, or y's neighbour) yx, four pairs each; with a norm its
+    // weights are in the factors and the row's scale comes after them
+    // (without a norm all of them follow from the cosines and sines, half the registers)
+    Pair xx[NORM ? 4 : 1], xy[NORM ? 4 : 1], yx[NORM ? 4 : 1], yy[NORM ? 4 : 1];
+    float2 cs[NORM ? 1 : 8];
+    auto factors = [&](const float *weight) {
+        if constexpr (!NORM) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) sum += x[e] * x[e] + y[e] * y[e];
+            for (int e = 0; e < 8; ++e) cs[e] = turns ? turn[t * 8 + e] : make_float2(1.f, 0.f);
+        } else {
+            float wx[8], wy[8];
 #pragma unroll
-            for (int o = 1; o < kPerRow; o <<= 1) sum += __shfl_xor_sync(~0u, sum, o);
-            if (works && set.weight) {
-                const float inv = 1.f / sqrtf(sum * (1.f / D) + p.eps);
-                const float4 *wa = reinterpret_cast<const float4 *>(set.weight + ca * 8);
-                const float4 *wb = reinterpret_cast<const float4 *>(set.weight + cb * 8);
+            for (int e = 0; e < 8; ++e) wx[e] = wy[e] = 1.f;
+            if (weight) {
+                const float *a = weight + ca / kE, *b = weight + cb / kE;
 #pragma unroll
-                for (int q = 0; q < 2; ++q) {
-                    const float4 u = wa[q], v = wb[q];
-                    x[4 * q] *= inv * u.x; x[4 * q + 1] *= inv * u.y; x[4 * q + 2] *= inv * u.z; x[4 * q + 3] *= inv * u.w;
-                    y[4 * q] *= inv * v.x; y[4 * q + 1] *= inv * v.y; y[4 * q + 2] *= inv * v.z; y[4 * q + 3] *= inv * v.w;
-                }
+                for (int e = 0; e < 8; ++e) wx[e] = a[e], wy[e] = b[e];
             }
-        }
-        if (works) {
-            if (turns) {
-                const float2 *cs = turn + it.tok * p.half;
-                if (p.layout == STOM_ROPE_PAIRS) {
 #pragma unroll
-                    for (int e = 0; e < 8; e += 2) {
-                        const float2 u = cs[ca * 4 + (e >> 1)], v = cs[cb * 4 + (e >> 1)];
-                        const float x0 = x[e], y0 = y[e];
-                        x[e] = x0 * u.x - x[e + 1] * u.y;
-                        x[e + 1] = x0 * u.y + x[e + 1] * u.x;
-                        y[e] = y0 * v.x - y[e + 1] * v.y;
-                        y[e + 1] = y0 * v.y + y[e + 1] * v.x;
-                    }
+            for (int e = 0; e < 4; ++e) {
+                if (PAIRS) {
+                    const float2 u = turns ? turn[t * 8 + e] : make_float2(1.f, 0.f);
+                    const float2 w = turns ? turn[t * 8 + 4 + e] : make_float2(1.f, 0.f);
+                    xx[e] = pair_of(wx[2 * e] * u.x, wx[2 * e + 1] * u.x);
+                    xy[e] = pair_of(-wx[2 * e + 1] * u.y, wx[2 * e] * u.y);
+                    yy[e] = pair_of(wy[2 * e] * w.x, wy[2 * e + 1] * w.x);
+                    yx[e] = pair_of(-wy[2 * e + 1] * w.y, wy[2 * e] * w.y);
                 } else {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const float2 u = cs[t * 8 + e];
-                        const float x0 = x[e];
-                        x[e] = x0 * u.x - y[e] * u.y;
-                        y[e] = x0 * u.y + y[e] * u.x;
-                    }
+                    const float2 u = turns ? turn[t * 8 + 2 * e] : make_float2(1.f, 0.f);
+                    const float2 w = turns ? turn[t * 8 + 2 * e + 1] : make_float2(1.f, 0.f);
+                    xx[e] = pair_of(wx[2 * e] * u.x, wx[2 * e + 1] * w.x);
+                    xy[e] = pair_of(-wy[2 * e] * u.y, -wy[2 * e + 1] * w.y);
+                    yy[e] = pair_of(wy[2 * e] * u.x, wy[2 * e + 1] * w.x);
+                    yx[e] = pair_of(wx[2 * e] * u.y, wx[2 * e + 1] * w.y);
                 }
             }
-            a.set(x);
-            b.set(y);
         }
-        if (it.kind >= 0) {
-            int64_t at = it.kind > 0 && p.table ? place[it.tok] : (token0 + it.tok) * set.dst_token;
-            if (at >= 0) {
-                T *o = reinterpret_cast<T *>(set.dst) + at + it.row * set.dst_head;
-                a.store(o + ca * 8);
-                b.store(o + cb * 8);
+    };
+    // norm and rotation of the two chunks of a row; all lanes of the warp take part
+    auto work = [&](Pair (&x)[4], Pair (&y)[4], bool norm) {
+        if constexpr (!NORM) {
+            if (!turns) return;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float2 a = split(x[e]), b = split(y[e]);
+                if (PAIRS) {
+                    const float2 u = cs[e], w = cs[4 + e];
+                    x[e] = pair_of(a.x * u.x - a.y * u.y, a.x * u.y + a.y * u.x);
+                    y[e] = pair_of(b.x * w.x - b.y * w.y, b.x * w.y + b.y * w.x);
+                } else {
+                    const float2 u = cs[2 * e], w = cs[2 * e + 1];
+                    x[e] = pair_of(a.x * u.x - b.x * u.y, a.y * w.x - b.y * w.y);
+                    y[e] = pair_of(a.x * u.y + b.x * u.x, a.y * w.y + b.y * w.x);
+                }
+            }
+        } else {
+            Pair scale = pair_of(1.f, 1.f);
+            if (norm) {
+                Pair sum = mul(x[0], x[0]);
+#pragma unroll
+                for (int e = 1; e < 4; ++e) sum = fma(x[e], x[e], sum);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) sum = fma(y[e], y[e], sum);
+                const float2 f = split(sum);
+                float all = f.x + f.y;
+#pragma unroll
+                for (int o = 1; o < kPerRow; o <<= 1) all += __shfl_xor_sync(~0u, all, o);
+                const float inv = rsqrtf(fmaf(all, 1.f / D, p.eps));
+                scale = pair_of(inv, inv);
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                Pair a = x[e], b = y[e];
+                if (turns) {
+                    const Pair xo = PAIRS ? swapped(a) : b, yo = PAIRS ? swapped(b) : a;
+                    a = fma(xo, xy[e], mul(a, xx[e]));
+                    b = fma(yo, yx[e], mul(b, yy[e]));
+                } else {
+                    a = mul(a, xx[e]);
+                    b = mul(b, yy[e]);
+                }
+                x[e] = mul(a, scale);
+                y[e] = mul(b, scale);
             }
         }
-        it = next;
-        a = na;
-        b = nb;
-        i = ahead;
+    };
+    // one step of rows: takes the chunks, sends for the rows `ahead` steps on, works and stores
+    auto step = [&](Walk<T, D> &w, Chunk<T> &a, Chunk<T> &b, int ahead, bool norm, bool stored) {
+        Pair x[4], y[4];
+        a.get(x);
+        b.get(y);
+        fetch(w, a, b, ahead);
+        work(x, y, norm);
+        if (w.left > 0 && stored) {
+            Chunk<T> o;
+            o.set(x);
+            o.store(w.dst + ca);
+            o.set(y);
+            o.store(w.dst + cb);
+        }
+        w.src += w.src_step;
+        w.dst += w.dst_step;
+        w.left -= kRows;
+    };
+
+    const bool stored = place >= 0;
+    if (k1 > k0) {
+        factors(p.set[1].weight);
+        for (int s = k0; s < k1; ++s) {
+            const Chunk<T> ca_v = va, cb_v = vb;
+            fetch(v, va, vb, 1);
+            if (v.left > 0 && stored) {
+                ca_v.store(v.dst + ca);
+                cb_v.store(v.dst + cb);
+            }
+            v.src += v.src_step;
+            v.dst += v.dst_step;
+            v.left -= kRows;
+            step(k, ka, kb, 1, p.set[1].weight != nullptr, stored);
+        }
+    }
+    if (q1 > q0) {
+        if (k1 == k0 || NORM) factors(p.set[0].weight);
+        Walk<T, D> q = queries();
+        for (int s = q0; s < q1; s += 2) {
+            step(q, qa[0], qb[0], 2, p.set[0].weight != nullptr, true);
+            if (s + 1 < q1) step(q, qa[1], qb[1], 2, p.set[0].weight != nullptr, true);
+        }
     }
 }
 
-template <typename T, int D>
-int32_t launch(const RotateParams &p, cudaStream_t stream) {
-    const size_t smem = (size_t)p.tokens_per_block * p.half * sizeof(float2);
-    const int blocks = (p.n_tokens + p.tokens_per_block - 1) / p.tokens_per_block;
-    cudaError_t e = launch_after_producer(kv_rotate_kernel<T, D>, dim3(blocks), dim3(kThreads), smem, stream, p);
+template <typename T, int D, bool NORM, bool PAIRS>
+int32_t launch(RotateParams &p, int sms, cudaStream_t stream) {
+    // Few tokens are cut into parts of whole steps, as long as all parts are on the device at once; a part works the
+    // token's angles out again.
+    constexpr int kRows = 32 / (D / 16);
+    const int steps = (p.n_k + kRows - 1) / kRows + (p.n_q + kRows - 1) / kRows;
+    int parts = 1;
+    while (parts < steps && (int64_t)p.n_tokens * (parts + 1) <= (NORM ? 2 : 3) * (kThreads / 32) * sms) ++parts;
+    p.steps_per_part = (steps + parts - 1) / parts;
+    p.parts = fast_div((uint32_t)((steps + p.steps_per_part - 1) / p.steps_per_part));
+    const int64_t warps = (int64_t)p.n_tokens * p.parts.d;
+    const int blocks = (int)((warps + kThreads / 32 - 1) / (kThreads / 32));
+    cudaError_t e = launch_after_producer(kv_rotate_kernel<T, D, NORM, PAIRS>, dim3(blocks), dim3(kThreads), 0, stream, p);
     if (e != cudaSuccess) {
         set_last_cuda_error(e);
         return STOM_ERR_CUDA;
@@ -248,9 +367,16 @@ int32_t launch(const RotateParams &p, cudaStream_t stream) {
     return finish_launch();
 }
 
+template <typename T, int D>
+int32_t by_kind(RotateParams &p, int sms, cudaStream_t s) {
+    const bool norm = p.set[0].weight || p.set[1].weight, pairs = p.layout == STOM_ROPE_PAIRS;
+    if (norm) return pairs ? launch<T, D, true, true>(p, sms, s) : launch<T, D, true, false>(p, sms, s);
+    return pairs ? launch<T, D, false, true>(p, sms, s) : launch<T, D, false, false>(p, sms, s);
+}
+
 template <typename T>
-int32_t by_width(const RotateParams &p, int d, cudaStream_t s) {
-    return d == 64 ? launch<T, 64>(p, s) : d == 128 ? launch<T, 128>(p, s) : launch<T, 256>(p, s);
+int32_t by_width(RotateParams &p, int d, int sms, cudaStream_t s) {
+    return d == 64 ? by_kind<T, 64>(p, sms, s) : d == 128 ? by_kind<T, 128>(p, sms, s) : by_kind<T, 256>(p, sms, s);
 }
 
 // Common checks of both calls; fills all but the destination of keys and values.
@@ -278,13 +404,12 @@ int32_t prepare(RotateParams &p, const stom_kv_rope *rope, int32_t dtype, int32_
     if (k && (k_tok < 0 || k_head < 0)) return STOM_ERR_INVALID_ARG;
     if (!q) n_q = 0;
     if (!k) n_k = 0;
-    if (n_q > 65536 || n_k > 65536) return STOM_ERR_SHAPE;
+    if (n_q > 65536 || n_k > 65536 || n > (1 << 30)) return STOM_ERR_SHAPE;
     p = RotateParams{};
     p.set[0] = RowSet{static_cast<const char *>(q), static_cast<char *>(q_out), q_tok, q_head, qo_tok, qo_head, q ? q_weight : nullptr};
     p.set[1] = RowSet{static_cast<const char *>(k), nullptr, k_tok, k_head, 0, 0, k ? k_weight : nullptr};
-    p.first_k = n_q;
-    p.first_v = n_q + n_k;
-    p.rows = fast_div((uint32_t)(n_q + n_k));
+    p.n_q = n_q;
+    p.n_k = n_k;
     p.n_tokens = n;
     p.pos = pos;
     p.freq = rope->freq;
@@ -296,15 +421,12 @@ int32_t prepare(RotateParams &p, const stom_kv_rope *rope, int32_t dtype, int32_
 }
 
 int32_t run(RotateParams &p, int32_t dtype, int32_t d, void *stream) {
-    // One token per block while that leaves multiprocessors with fewer than four blocks; four after that, so that the
-    // set-up of a block is shared by more rows.
     const int sms = sm_count();
     if (!sms) return STOM_ERR_CUDA;
-    p.tokens_per_block = p.n_tokens >= 16 * sms ? 4 : 1;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    if (dtype == STOM_BF16) return by_width<__nv_bfloat16>(p, d, s);
-    if (dtype == STOM_FP16) return by_width<__half>(p, d, s);
-    return by_width<float>(p, d, s);
+    if (dtype == STOM_BF16) return by_width<__nv_bfloat16>(p, d, sms, s);
+    if (dtype == STOM_FP16) return by_width<__half>(p, d, sms, s);
+    return by_width<float>(p, d, sms, s);
 }
 
 }  // namespace
@@ -366,7 +488,6 @@ extern "C" int32_t stom_kv_append(const stom_kv_pool *pool, const stom_kv_seqs *
     p.set[1].dst = at_k;
     p.set[1].dst_head = pool->stride_head;
     p.set[2] = RowSet{static_cast<const char *>(v), at_v, v_stride_token, v_stride_head, 0, pool->stride_head, nullptr};
-    p.rows = fast_div((uint32_t)(p.first_v + pool->n_kv_heads));
     p.table = seqs->table;
     p.table_stride = seqs->table_stride;
     p.slot = slot;

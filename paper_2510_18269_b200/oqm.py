@@ -386,40 +386,60 @@ def _addr(t):
     return None if t is None else t.data_ptr()
 
 
-class _On:
-    """Current device and stream for the tensors of a call: the stream given, else the current one of their device."""
-
-    def __init__(self, t, stream):
-        self.dev, self.stream = t.device, stream
-
-    def __call__(self, fn, *args):
-        if self.dev.type != "cuda":
-            raise ValueError("the tensors of a call lie on a CUDA device")
-        s = (torch.cuda.current_stream(self.dev) if self.stream is None else self.stream).cuda_stream
-        if self.dev.index == torch.cuda.current_device():
-            return fn(*args, s)
-        with torch.cuda.device(self.dev):
-            return fn(*args, s)
+# The checks and look-ups of the calls that are made once per token cost as much as a small kernel runs, so they ask
+# torch in the cheapest ways there are (get_device() in the place of device, one stride() instead of several).
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_current_device = getattr(torch._C, "_cuda_getDevice", None)
 
 
-def _dense(t, dtype, shape, name, device=None):
-    """A contiguous tensor of this type and shape on this device (or None)."""
+def _launch(dev, stream, fn, *args):
+    """fn(*args, stream) with `dev` as the current device; stream None: the current one of that device."""
+    if dev < 0:
+        raise ValueError("the tensors of a call lie on a CUDA device")
+    if stream is not None:
+        s = stream.cuda_stream
+    elif _raw_stream is not None:
+        s = _raw_stream(dev)
+    else:
+        s = torch.cuda.current_stream(dev).cuda_stream
+    if (_current_device() if _current_device is not None else torch.cuda.current_device()) == dev:
+        return fn(*args, s)
+    with torch.cuda.device(dev):
+        return fn(*args, s)
+
+
+def _dense(t, dtype, shape, name, dev):
+    """Address of a contiguous tensor of this type and shape on device number `dev` (-1: the CPU), or None."""
     if t is None:
         return None
-    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous() or (device is not None and t.device != device):
-        raise ValueError(f"{name}: a contiguous {dtype} tensor of shape {tuple(shape)}" +
-                         (f" on {device}" if device is not None else "") +
-                         f" is needed, not {t.dtype} {tuple(t.shape)} on {t.device}")
-    return t.data_ptr()
+    if t.dtype is dtype and t.shape == shape and t.get_device() == dev and t.is_contiguous():
+        return t.data_ptr()
+    raise ValueError(f"{name}: a contiguous {dtype} tensor of shape {tuple(shape)} on device {dev} is needed, not "
+                     f"{t.dtype} {tuple(t.shape)} with strides {t.stride()} on {t.device}")
 
 
-def _rows3(t, dtype, n, heads, d, name, device):
+def _rows3(t, dtype, shape, name, dev):
     """(address, stride of a row, stride of a head) of an [n][heads][d] tensor with adjacent channels."""
-    if t.dtype is not dtype or t.shape != (n, heads, d) or t.stride(2) != 1 or t.device != device:
-        raise ValueError(f"{name}: a {dtype} tensor of shape {(n, heads, d)} with adjacent channels on {device} is "
-                         f"needed, not {t.dtype} {tuple(t.shape)} with strides {t.stride()} on {t.device}")
-    sn, sh, _ = t.stride()
-    return t.data_ptr(), sn, sh
+    if t.dtype is dtype and t.shape == shape and t.get_device() == dev:
+        sn, sh, one = t.stride()
+        if one == 1:
+            return t.data_ptr(), sn, sh
+    raise ValueError(f"{name}: a {dtype} tensor of shape {tuple(shape)} with adjacent channels on device {dev} is needed, "
+                     f"not {t.dtype} {tuple(t.shape)} with strides {t.stride()} on {t.device}")
+
+
+def _workspace(t, dev):
+    if t.get_device() != dev or not t.is_contiguous():
+        raise ValueError("workspace: a contiguous tensor on the device of the call is needed")
+    return t.data_ptr(), t.nbytes
+
+
+def _flags(t, dev):
+    if t is None:
+        return None
+    if t.get_device() != dev or t.element_size() != 4 or t.numel() < 1:
+        raise ValueError("dev_flags: one 32-bit word on the device of the call is needed")
+    return t.data_ptr()
 
 
 class KvPool:
@@ -430,7 +450,7 @@ class KvPool:
             raise ValueError("k and v are two [layers][pages][page_tokens][heads][d] tensors of the same type and strides")
         if k.stride(4) != 1:
             raise ValueError("the channels of a head are adjacent")
-        self.k, self.v, self.device, self.dtype = k, v, k.device, k.dtype
+        self.k, self.v, self.dev, self.dtype = k, v, k.get_device(), k.dtype
         L, P, n, H, d = k.shape
         self.n_layers, self.n_pages, self.page_tokens, self.n_kv_heads, self.head_dim = L, P, n, H, d
         self.desc = KvPoolDesc(k.data_ptr(), v.data_ptr(), dtype_code(k.dtype), L, P, n, H, d, *k.stride()[:4])
@@ -444,9 +464,10 @@ class KvSeqs:
         n, width = table.shape
         if table.dtype is not torch.int32 or (width > 1 and table.stride(1) != 1):
             raise ValueError("table: int32 [n_seqs][max_pages] with adjacent entries")
-        _dense(len, torch.int32, (n,), "len", table.device)
+        self.dev = table.get_device()
+        _dense(len, torch.int32, (n,), "len", self.dev)
         if refs is not None:
-            _dense(refs, torch.int32, (refs.numel(),), "refs", table.device)
+            _dense(refs, torch.int32, (refs.numel(),), "refs", self.dev)
         self.table, self.len, self.refs, self.n_seqs, self.max_pages = table, len, refs, n, width
         stride = table.stride(0) if n > 1 else width
         self.desc = KvSeqsDesc(_addr(table), _addr(len), _addr(refs), n, width, stride)
@@ -458,8 +479,9 @@ class Rope:
 
     def __init__(self, freq=None, layout=ROPE_HALF, magnitude=1.0):
         if freq is not None:
-            _dense(freq, torch.float64, (freq.numel(),), "freq")
+            _dense(freq, torch.float64, (freq.numel(),), "freq", freq.get_device())
         self.freq, self.rot_dim = freq, 0 if freq is None else 2 * freq.numel()
+        self.dev = None if freq is None else freq.get_device()
         self.desc = RopeDesc(_addr(freq), self.rot_dim, layout, magnitude)
         self.ref = C.addressof(self.desc)
 
@@ -479,16 +501,32 @@ def stom_kv_attend_workspace_bytes(pool: KvPool, seqs: KvSeqs, n_q_heads: int) -
     return int(n)
 
 
+def _same_device(pool, seqs, rope=None):
+    if seqs.dev != pool.dev or (rope is not None and rope.dev is not None and rope.dev != pool.dev):
+        raise ValueError("pool, table and frequencies lie on the same device")
+
+
 def stom_kv_attend(pool: KvPool, seqs: KvSeqs, layer, q, out, softmax_scale, workspace, lse=None, softcap=0.0, window=0,
                    dev_flags=None, stream=None):
     """q, out: [n_seqs][query heads][d] of the pool's type; lse: [n_seqs][query heads] float32 or None."""
-    n, hq, d = q.shape
-    qa, qs, qh = _rows3(q, pool.dtype, seqs.n_seqs, hq, pool.head_dim, "q", pool.device)
-    oa, os_, oh = _rows3(out, pool.dtype, n, hq, d, "out", pool.device)
-    la = _dense(lse, torch.float32, (n, hq), "lse", pool.device)
-    _check(_On(q, stream)(lib().stom_kv_attend, pool.ref, seqs.ref, layer, hq, qa, qs, qh, softmax_scale, softcap, window,
-                          oa, os_, oh, la, workspace.data_ptr(), workspace.numel() * workspace.element_size(),
-                          _addr(dev_flags)), "stom_kv_attend")
+    dt, dev = pool.dtype, pool.dev
+    _same_device(pool, seqs)
+    hq = q.shape[1]
+    shape = (seqs.n_seqs, hq, pool.head_dim)
+    _check(_launch(dev, stream, lib().stom_kv_attend, pool.ref, seqs.ref, layer, hq, *_rows3(q, dt, shape, "q", dev),
+                   softmax_scale, softcap, window, *_rows3(out, dt, shape, "out", dev),
+                   _dense(lse, torch.float32, shape[:2], "lse", dev), *_workspace(workspace, dev), _flags(dev_flags, dev)),
+           "stom_kv_attend")
+
+
+_NO_ROWS = (None, 0, 0, 0, None, 0, 0, None)
+
+
+def _turned(x, out, weight, name, dt, n, d, dev):
+    """The arguments of one of the tensors that are rotated."""
+    shape = (n, x.shape[1], d)
+    a, sn, sh = _rows3(x, dt, shape, name, dev)
+    return (a, shape[1], sn, sh, *_rows3(out, dt, shape, name + "_out", dev), _dense(weight, torch.float32, (d,), name + "_weight", dev))
 
 
 def stom_kv_rotate(rope: Rope, pos, q=None, q_out=None, k=None, k_out=None, q_weight=None, k_weight=None, eps=1e-6,
@@ -497,38 +535,26 @@ def stom_kv_rotate(rope: Rope, pos, q=None, q_out=None, k=None, k_out=None, q_we
     weights: float32 [d] or None (no norm)."""
     x = q if q is not None else k
     n, _, d = x.shape
-    dt, dev = x.dtype, x.device
-    qa = (None, 0, 0, 0, None, 0, 0, None)
-    ka = qa
-    if q is not None:
-        h = q.shape[1]
-        a, b = _rows3(q, dt, n, h, d, "q", dev), _rows3(q_out, dt, n, h, d, "q_out", dev)
-        qa = (a[0], h, a[1], a[2], b[0], b[1], b[2], _dense(q_weight, torch.float32, (d,), "q_weight", dev))
-    if k is not None:
-        h = k.shape[1]
-        a, b = _rows3(k, dt, n, h, d, "k", dev), _rows3(k_out, dt, n, h, d, "k_out", dev)
-        ka = (a[0], h, a[1], a[2], b[0], b[1], b[2], _dense(k_weight, torch.float32, (d,), "k_weight", dev))
-    _check(_On(x, stream)(lib().stom_kv_rotate, rope.ref, dtype_code(dt), d, n, _dense(pos, torch.int32, (n,), "pos", dev),
-                          *qa, *ka, eps), "stom_kv_rotate")
+    dt, dev = x.dtype, x.get_device()
+    if rope.dev is not None and rope.dev != dev:
+        raise ValueError("the frequencies lie on the device of the tensors")
+    _check(_launch(dev, stream, lib().stom_kv_rotate, rope.ref, dtype_code(dt), d, n, _dense(pos, torch.int32, (n,), "pos", dev),
+                   *(_NO_ROWS if q is None else _turned(q, q_out, q_weight, "q", dt, n, d, dev)),
+                   *(_NO_ROWS if k is None else _turned(k, k_out, k_weight, "k", dt, n, d, dev)), eps), "stom_kv_rotate")
 
 
 def stom_kv_append(pool: KvPool, seqs: KvSeqs, layer, rope: Rope, pos, slot, k, v, q=None, q_out=None, seq=None,
                    q_weight=None, k_weight=None, eps=1e-6, dev_flags=None, stream=None):
     """k, v: [n][kv heads][d] of the pool's type; slot, pos, seq: int32 [n]; q and q_out: [n][query heads][d] or None."""
-    n, hk, d = k.shape
-    dt, dev = pool.dtype, pool.device
-    ka, ks, kh = _rows3(k, dt, n, pool.n_kv_heads, pool.head_dim, "k", dev)
-    va, vs, vh = _rows3(v, dt, n, hk, d, "v", dev)
-    qa = (None, 0, 0, 0, None, 0, 0, None)
-    if q is not None:
-        h = q.shape[1]
-        a, b = _rows3(q, dt, n, h, d, "q", dev), _rows3(q_out, dt, n, h, d, "q_out", dev)
-        qa = (a[0], h, a[1], a[2], b[0], b[1], b[2], _dense(q_weight, torch.float32, (d,), "q_weight", dev))
-    _check(_On(k, stream)(lib().stom_kv_append, pool.ref, seqs.ref, layer, rope.ref, n,
-                          _dense(pos, torch.int32, (n,), "pos", dev), _dense(slot, torch.int32, (n,), "slot", dev),
-                          _dense(seq, torch.int32, (n,), "seq", dev), *qa, ka, ks, kh,
-                          _dense(k_weight, torch.float32, (d,), "k_weight", dev), va, vs, vh, eps, _addr(dev_flags)),
-           "stom_kv_append")
+    dt, dev, d = pool.dtype, pool.dev, pool.head_dim
+    _same_device(pool, seqs, rope)
+    n = k.shape[0]
+    shape, one, i32 = (n, pool.n_kv_heads, d), (n,), torch.int32
+    _check(_launch(dev, stream, lib().stom_kv_append, pool.ref, seqs.ref, layer, rope.ref, n, _dense(pos, i32, one, "pos", dev),
+                   _dense(slot, i32, one, "slot", dev), _dense(seq, i32, one, "seq", dev),
+                   *(_NO_ROWS if q is None else _turned(q, q_out, q_weight, "q", dt, n, d, dev)),
+                   *_rows3(k, dt, shape, "k", dev), _dense(k_weight, torch.float32, (d,), "k_weight", dev),
+                   *_rows3(v, dt, shape, "v", dev), eps, _flags(dev_flags, dev)), "stom_kv_append")
 
 
 def stom_kv_pages_workspace_bytes(pool: KvPool, seqs: KvSeqs) -> int:
@@ -541,43 +567,40 @@ def stom_kv_pages_workspace_bytes(pool: KvPool, seqs: KvSeqs) -> int:
 def _counts_of(pool, seqs):
     if seqs.refs is None or seqs.refs.numel() != pool.n_pages:
         raise ValueError("the sequences need refs, one count for each page of the pool")
-    if seqs.table.device != pool.device:
-        raise ValueError("table and pool lie on the same device")
+    _same_device(pool, seqs)
+
+
+def _wish(call, pool, seqs, wish, name, rest, dev_flags, stream):
+    _counts_of(pool, seqs)
+    w = _dense(wish, torch.int32, (seqs.n_seqs,), name, pool.dev)
+    _check(_launch(pool.dev, stream, getattr(lib(), call), pool.ref, seqs.ref, w, *rest, _flags(dev_flags, pool.dev)), call)
 
 
 def stom_kv_reserve(pool: KvPool, seqs: KvSeqs, want, workspace, dev_flags=None, stream=None):
     """want: int32 [n_seqs], the length each sequence grows to (at most its length: it stays)."""
-    _counts_of(pool, seqs)
-    w = _dense(want, torch.int32, (seqs.n_seqs,), "want", pool.device)
-    _check(_On(pool.k, stream)(lib().stom_kv_reserve, pool.ref, seqs.ref, w, workspace.data_ptr(),
-                               workspace.numel() * workspace.element_size(), _addr(dev_flags)), "stom_kv_reserve")
+    _wish("stom_kv_reserve", pool, seqs, want, "want", _workspace(workspace, pool.dev), dev_flags, stream)
 
 
 def stom_kv_fork(pool: KvPool, seqs: KvSeqs, parent, dev_flags=None, stream=None):
     """parent: int32 [n_seqs], the sequence an empty one shares from now on, or -1."""
-    _counts_of(pool, seqs)
-    w = _dense(parent, torch.int32, (seqs.n_seqs,), "parent", pool.device)
-    _check(_On(pool.k, stream)(lib().stom_kv_fork, pool.ref, seqs.ref, w, _addr(dev_flags)), "stom_kv_fork")
+    _wish("stom_kv_fork", pool, seqs, parent, "parent", (), dev_flags, stream)
 
 
 def stom_kv_free(pool: KvPool, seqs: KvSeqs, drop, dev_flags=None, stream=None):
     """drop: int32 [n_seqs], not 0 for the sequences that give their pages back."""
-    _counts_of(pool, seqs)
-    w = _dense(drop, torch.int32, (seqs.n_seqs,), "drop", pool.device)
-    _check(_On(pool.k, stream)(lib().stom_kv_free, pool.ref, seqs.ref, w, _addr(dev_flags)), "stom_kv_free")
+    _wish("stom_kv_free", pool, seqs, drop, "drop", (), dev_flags, stream)
 
 
 def stom_kv_compact(pool: KvPool, seqs: KvSeqs, table_out, refs_out, n_live, workspace, dev_flags=None, stream=None):
     """table_out, refs_out: like seqs.table and seqs.refs (or those themselves); n_live: int32 [1] or None."""
     _counts_of(pool, seqs)
-    t = seqs.table
+    t, dev = seqs.table, pool.dev
     if table_out.dtype is not torch.int32 or table_out.shape != t.shape or table_out.stride() != t.stride() \
-            or table_out.device != pool.device:
+            or table_out.get_device() != dev:
         raise ValueError("table_out: a tensor like seqs.table")
-    r = _dense(refs_out, torch.int32, (pool.n_pages,), "refs_out", pool.device)
-    c = _dense(n_live, torch.int32, (1,), "n_live", pool.device)
-    _check(_On(pool.k, stream)(lib().stom_kv_compact, pool.ref, seqs.ref, table_out.data_ptr(), r, c, workspace.data_ptr(),
-                               workspace.numel() * workspace.element_size(), _addr(dev_flags)), "stom_kv_compact")
+    _check(_launch(dev, stream, lib().stom_kv_compact, pool.ref, seqs.ref, table_out.data_ptr(),
+                   _dense(refs_out, torch.int32, (pool.n_pages,), "refs_out", dev), _dense(n_live, torch.int32, (1,), "n_live", dev),
+                   *_workspace(workspace, dev), _flags(dev_flags, dev)), "stom_kv_compact")
 
 
 # ---------------------------------------------------------------- choice of the next token (include/stom_sample.h)
@@ -586,12 +609,12 @@ def stom_sample_tokens(logits, u, token, temperature=None, top_k=None, top_p=Non
                        dev_flags=None, stream=None):
     """logits: [rows][n]; u, temperature, top_p, min_p, logprob: float32 [rows]; token, kept, top_k: int32 [rows]."""
     rows, n = logits.shape
-    if n > 1 and logits.stride(1) != 1:
+    stride, one = logits.stride()
+    if n > 1 and one != 1:
         raise ValueError("logits: the entries of a row are adjacent")
-    dev, one, f, i = logits.device, (rows,), torch.float32, torch.int32
-    _check(_On(logits, stream)(
-        lib().stom_sample_tokens, logits.data_ptr(), dtype_code(logits.dtype), rows, n, logits.stride(0),
-        _dense(temperature, f, one, "temperature", dev), _dense(top_k, i, one, "top_k", dev),
-        _dense(top_p, f, one, "top_p", dev), _dense(min_p, f, one, "min_p", dev), _dense(u, f, one, "u", dev),
-        _dense(token, i, one, "token", dev), _dense(kept, i, one, "kept", dev), _dense(logprob, f, one, "logprob", dev),
-        _addr(dev_flags)), "stom_sample_tokens")
+    dev, of, f, i = logits.get_device(), (rows,), torch.float32, torch.int32
+    _check(_launch(dev, stream, lib().stom_sample_tokens, logits.data_ptr(), dtype_code(logits.dtype), rows, n, stride,
+                   _dense(temperature, f, of, "temperature", dev), _dense(top_k, i, of, "top_k", dev),
+                   _dense(top_p, f, of, "top_p", dev), _dense(min_p, f, of, "min_p", dev), _dense(u, f, of, "u", dev),
+                   _dense(token, i, of, "token", dev), _dense(kept, i, of, "kept", dev),
+                   _dense(logprob, f, of, "logprob", dev), _flags(dev_flags, dev)), "stom_sample_tokens")
