@@ -40,6 +40,7 @@ struct KvAttendParams {
     FastDiv page;
     int32_t n_kv_heads, group;    // query heads per kv head
     int32_t blocks_per_head;      // blocks of 8 * NT query heads a kv head's group is cut into
+    FastDiv by_blocks, by_units;  // division by that, and by n_kv_heads * blocks_per_head
     const char *q;
     int64_t q_stride_seq, q_stride_head;
     float scale, cap;             // softmax scale; cap <= 0: none
@@ -65,6 +66,8 @@ struct Shape {
     static constexpr int kPiece = kHeads * D * 4;            // a partial result
     static constexpr int kPieces = 2 * kWarps;
     static constexpr int kSmem = kWarps * (kRing + kPiece) + kPieces * (kHeads * 8 + 8);
+    static_assert(kPiece + kPieces * kHeads * 4 <= kRing, "the units' maxima lie behind the first warp's last piece");
+    static_assert(kPieces * kHeads <= 32 * kWarps, "a thread for each head of each piece");
     static_assert(kPiece <= kRing, "a warp's last piece lies in its ring");
     static_assert(kSmem <= 227 * 1024, "shared memory");
 };
@@ -103,7 +106,7 @@ __device__ __forceinline__ void advance(const KvAttendParams &p, int units, Curs
 
 // Output rows of unit (b, hu): query head and count of heads.
 __device__ __forceinline__ int heads_of(const KvAttendParams &p, int hu, int per, int &head0) {
-    const int h = hu / p.blocks_per_head, j = hu - h * p.blocks_per_head;
+    const int h = (int)div_by(p.by_blocks, (uint32_t)hu), j = hu - h * p.blocks_per_head;
     head0 = h * p.group + j * per;
     return min(per, p.group - j * per);
 }
@@ -190,14 +193,14 @@ __global__ void __launch_bounds__(Shape<D, NT>::kWarps * 32, 1) kv_attend_kernel
             int64_t rest;            // offset within a page, in elements
         };
         constexpr int kNone = INT32_MIN;
-        Row ahead[2];
+        Row ahead[2] = {{kNone, 0}, {kNone, 0}};
         auto look_up = [&](Row &r) {
             r.page = kNone;
             if (to_look > 0) {
                 const int t = ld.first + ld.tile * kTile + (lane & 15);
                 if (t < ld.end) {
                     const uint32_t pg = div_by(p.page, (uint32_t)t);
-                    r.rest = (int64_t)(t - (int)(pg * p.page.d)) * p.stride_token + (ld.hu / p.blocks_per_head) * p.stride_head;
+                    r.rest = (int64_t)(t - (int)(pg * p.page.d)) * p.stride_token + (int64_t)div_by(p.by_blocks, (uint32_t)ld.hu) * p.stride_head;
                     r.page = p.table[ld.b * p.table_stride + pg];
                     if (r.page == kNone) r.page = -1;
                 }
@@ -425,64 +428,107 @@ __global__ void __launch_bounds__(Shape<D, NT>::kWarps * 32, 1) kv_attend_kernel
     }
     __syncthreads();
 
-    // ---- join the block's pieces, unit by unit; they stand in the order of the line.  A thread has four channels of a
-    // head and walks the pieces with a running maximum; with more threads than that takes, teams take units in turn.
+    // ---- join the block's pieces, unit by unit; they stand in the order of the line.  First a thread for each head of
+    // each piece: what the piece counts for beside the unit's largest maximum.
+    float *piece_top = reinterpret_cast<float *>(smem + S::kPiece);   // [2 kWarps][kHeads], in a ring that is no more used
+    {
+        const int j = threadIdx.x / kHeads, h = threadIdx.x % kHeads;
+        float2 mine = make_float2(-INFINITY, 0.f);
+        float top = -INFINITY;
+        if (j < S::kPieces && piece_unit[j] >= 0) {
+            const int u = piece_unit[j];
+            mine = piece_ml[j * kHeads + h];
+#pragma unroll 8
+            for (int k = 0; k < S::kPieces; ++k)
+                if (piece_unit[k] == u) top = fmaxf(top, piece_ml[k * kHeads + h].x);
+        }
+        __syncthreads();
+        const float f = exp2f(mine.x - (top == -INFINITY ? 0.f : top));
+        if (j < S::kPieces) piece_ml[j * kHeads + h] = make_float2(f, f * mine.y);
+        if (j < S::kPieces) piece_top[j * kHeads + h] = top;
+    }
+    __syncthreads();
+    // Then a thread has four channels of a head (or several times four) and walks the pieces; with more threads than that
+    // takes, teams take units in turn.
     int open_unit = -1, goes_on = 0;
-    constexpr int kCols = kHeads * D / 4, kThreads = kWarps * 32, kTeams = kThreads > kCols ? kThreads / kCols : 1;
-    const int team = kTeams > 1 ? threadIdx.x / kCols : 0;
-    for (int at = threadIdx.x - team * kCols; at < kCols; at += kThreads) {
-        const int h = at / (D / 4), c = at % (D / 4) * 4;
+    constexpr int kThreads = kWarps * 32, kPer = kHeads * D / 4 <= kThreads ? 1 : kHeads * D / 4 <= 2 * kThreads ? 2 : 4;
+    constexpr int kAcross = D / 4 / kPer, kCols = kHeads * kAcross, kTeams = kThreads / kCols;
+    static_assert(kTeams >= 1, "a thread for each column");
+    const int team = threadIdx.x / kCols, h = threadIdx.x % kCols / kAcross, c0 = threadIdx.x % kAcross * 4;
+    if (team < kTeams) {
         int unit = -1, ends = 0, turn = -1;
         float m = -INFINITY, l = 0.f;
-        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+        float4 o[kPer];
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) o[i] = make_float4(0.f, 0.f, 0.f, 0.f);
         auto finish = [&]() {
             if (!(ends & 2)) {
                 if (ends & 1) open_unit = unit;
                 else goes_on = 1;
             }
-            if (turn % kTeams != team) return;
-            const int b = unit / units, hu = unit - b * units;
+            if (kTeams > 1 && turn % kTeams != team) return;
+            const int b = (int)div_by(p.by_units, (uint32_t)unit), hu = unit - b * units;
             int head0;
             if (h >= heads_of(p, hu, kHeads, head0)) return;
             if (ends == 3) {
                 const float inv = l == 0.f ? 0.f : 1.f / l;
-                T *dst = reinterpret_cast<T *>(p.out) + b * p.out_stride_seq + (head0 + h) * p.out_stride_head + c;
-                *reinterpret_cast<uint2 *>(dst) = make_uint2(pack2<T>(o.x * inv, o.y * inv), pack2<T>(o.z * inv, o.w * inv));
-                if (p.lse && c == 0)
+                T *dst = reinterpret_cast<T *>(p.out) + b * p.out_stride_seq + (head0 + h) * p.out_stride_head + c0;
+#pragma unroll
+                for (int i = 0; i < kPer; ++i)
+                    *reinterpret_cast<uint2 *>(dst + i * kAcross * 4) =
+                        make_uint2(pack2<T>(o[i].x * inv, o[i].y * inv), pack2<T>(o[i].z * inv, o[i].w * inv));
+                if (p.lse && c0 == 0)
                     p.lse[(int64_t)b * (p.n_kv_heads * p.group) + head0 + h] =
                         l == 0.f ? -INFINITY : 0.6931471805599453f * m + logf(l);
             } else {
                 // of the workspace: slot 1 for a unit that begins here, slot 0 for one that came in
                 const int64_t w = ((int64_t)blockIdx.x * 2 + (ends & 1)) * kHeads + h;
-                *reinterpret_cast<float4 *>(p.part_o + w * D + c) = o;
-                if (c == 0) p.part_ml[w] = make_float2(m, l);
+#pragma unroll
+                for (int i = 0; i < kPer; ++i) *reinterpret_cast<float4 *>(p.part_o + w * D + c0 + i * kAcross * 4) = o[i];
+                if (c0 == 0) p.part_ml[w] = make_float2(m, l);
             }
         };
-        for (int j = 0; j < S::kPieces; ++j) {
-            const int u = piece_unit[j];
-            if (u < 0) continue;
-            if (u != unit) {
-                if (unit >= 0) finish();
-                unit = u;
-                ends = piece_ends[j] & 1;
-                ++turn;
-                m = -INFINITY;
-                l = 0.f;
-                o = make_float4(0.f, 0.f, 0.f, 0.f);
+        constexpr int kBatch = kPer == 4 ? 2 : 4;
+        static_assert(S::kPieces % kBatch == 0, "pieces");
+        for (int j0 = 0; j0 < S::kPieces; j0 += kBatch) {
+            int u[kBatch], e[kBatch];
+            float2 f[kBatch];
+            float4 v[kBatch][kPer];
+            float t[kBatch];
+#pragma unroll
+            for (int k = 0; k < kBatch; ++k) {
+                const int j = j0 + k;
+                u[k] = piece_unit[j];
+                e[k] = piece_ends[j];
+                f[k] = piece_ml[j * kHeads + h];
+                t[k] = piece_top[j * kHeads + h];
+                const uint8_t *src = j & 1 ? smem + (j >> 1) * S::kRing : smem + kWarps * S::kRing + (j >> 1) * S::kPiece;
+#pragma unroll
+                for (int i = 0; i < kPer; ++i) v[k][i] = *reinterpret_cast<const float4 *>(src + (h * D + c0 + i * kAcross * 4) * 4);
             }
-            ends = (ends & 1) | (piece_ends[j] & 2);
-            if (turn % kTeams != team) continue;
-            const float2 ml = piece_ml[j * kHeads + h];
-            const uint8_t *src = j & 1 ? smem + (j >> 1) * S::kRing : smem + kWarps * S::kRing + (j >> 1) * S::kPiece;
-            const float4 v = *reinterpret_cast<const float4 *>(src + (h * D + c) * 4);
-            const float top = fmaxf(m, ml.x), base = top == -INFINITY ? 0.f : top;
-            const float fa = exp2f(m - base), fb = exp2f(ml.x - base);
-            m = top;
-            l = l * fa + ml.y * fb;
-            o.x = o.x * fa + v.x * fb;
-            o.y = o.y * fa + v.y * fb;
-            o.z = o.z * fa + v.z * fb;
-            o.w = o.w * fa + v.w * fb;
+#pragma unroll
+            for (int k = 0; k < kBatch; ++k) {
+                if (u[k] < 0) continue;
+                if (u[k] != unit) {
+                    if (unit >= 0) finish();
+                    unit = u[k];
+                    ends = e[k] & 1;
+                    ++turn;
+                    m = t[k];
+                    l = 0.f;
+#pragma unroll
+                    for (int i = 0; i < kPer; ++i) o[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+                }
+                ends = (ends & 1) | (e[k] & 2);
+                l += f[k].y;
+#pragma unroll
+                for (int i = 0; i < kPer; ++i) {
+                    o[i].x += v[k][i].x * f[k].x;
+                    o[i].y += v[k][i].y * f[k].x;
+                    o[i].z += v[k][i].z * f[k].x;
+                    o[i].w += v[k][i].w * f[k].x;
+                }
+            }
         }
         if (unit >= 0) finish();
     }
@@ -514,31 +560,37 @@ __global__ void __launch_bounds__(D / 4 * kJoin) kv_attend_join_kernel(const __g
     __shared__ float warp_m[32], warp_l[32];
     __shared__ float4 sum[kJoin][D / 4];
     __shared__ int end_s;
+    constexpr int kOwn = (kMaxBlocks + kThreads - 1) / kThreads;   // blocks a thread looks at
     if (threadIdx.x == 0) end_s = gridDim.x;
     grid_dependency_wait();
     const int first = blockIdx.x, h = blockIdx.y, blocks = gridDim.x;
+    auto row_of = [&](int j) { return ((int64_t)(first + j) * 2 + (j == 0 ? 1 : 0)) * kHeads + h; };
+    // all that may be needed is asked for at once: what turns out not to belong to the unit is not used
     const int unit = p.open_unit[first];
+    int on[kOwn];
+    float2 ml[kOwn];
+#pragma unroll
+    for (int k = 0; k < kOwn; ++k) {
+        const int j = threadIdx.x + k * kThreads;
+        on[k] = first + j < blocks && j ? p.goes_on[first + j] : 1;
+        ml[k] = first + j < blocks ? p.part_ml[row_of(j)] : make_float2(-INFINITY, 0.f);
+    }
     if (unit < 0) return;
     const int units = p.n_kv_heads * p.blocks_per_head;
-    const int b = unit / units, hu = unit - b * units;
+    const int b = (int)div_by(p.by_units, (uint32_t)unit), hu = unit - b * units;
     int head0;
     if (h >= heads_of(p, hu, kHeads, head0)) return;
     // the blocks it goes through: first, first + 1, ..., end - 1
     __syncthreads();
-    for (int j = first + 1 + threadIdx.x; j < blocks; j += kThreads)
-        if (!p.goes_on[j]) {
-            atomicMin(&end_s, j + 1);
-            break;
-        }
+#pragma unroll
+    for (int k = 0; k < kOwn; ++k)
+        if (!on[k]) atomicMin(&end_s, first + (int)threadIdx.x + k * kThreads + 1);
     __syncthreads();
     const int n = end_s - first;
-    auto row_of = [&](int j) { return ((int64_t)(first + j) * 2 + (j == 0 ? 1 : 0)) * kHeads + h; };
-    float2 ml[kMaxBlocks / kThreads + 1];
     float m = -INFINITY;
 #pragma unroll
-    for (int k = 0; k <= kMaxBlocks / kThreads; ++k) {
-        const int j = threadIdx.x + k * kThreads;
-        ml[k] = j < n ? p.part_ml[row_of(j)] : make_float2(-INFINITY, 0.f);
+    for (int k = 0; k < kOwn; ++k) {
+        if ((int)threadIdx.x + k * kThreads >= n) ml[k] = make_float2(-INFINITY, 0.f);
         m = fmaxf(m, ml[k].x);
     }
 #pragma unroll
@@ -551,7 +603,7 @@ __global__ void __launch_bounds__(D / 4 * kJoin) kv_attend_join_kernel(const __g
     const float base = m == -INFINITY ? 0.f : m;
     float l = 0.f;
 #pragma unroll
-    for (int k = 0; k <= kMaxBlocks / kThreads; ++k) {
+    for (int k = 0; k < kOwn; ++k) {
         const int j = threadIdx.x + k * kThreads;
         const float f = exp2f(ml[k].x - base);
         if (j < n) weight[j] = f;
@@ -685,6 +737,8 @@ extern "C" int32_t stom_kv_attend(const stom_kv_pool *pool, const stom_kv_seqs *
     p.n_kv_heads = pool->n_kv_heads;
     p.group = group;
     p.blocks_per_head = (group + per - 1) / per;
+    p.by_blocks = fast_div((uint32_t)p.blocks_per_head);
+    p.by_units = fast_div((uint32_t)units);
     p.q = static_cast<const char *>(q);
     p.q_stride_seq = q_stride_seq;
     p.q_stride_head = q_stride_head;
