@@ -1,4 +1,5 @@
-"""Builds libstom_oqm.so (sm_100a only) next to this file with nvcc.
+"""Builds libstom_oqm.so (sm_100a only) next to this file with nvcc, and _stom_bind.so, the Python binding of the
+calls that are made once per token, with g++ against torch's headers.
 
     python -m paper_2510_18269_b200.build [--force] [--verbose]
 
@@ -10,6 +11,7 @@ from __future__ import annotations
 import os
 import subprocess
 import sys
+import sysconfig
 from concurrent.futures import ThreadPoolExecutor
 from pathlib import Path
 
@@ -18,6 +20,7 @@ CSRC = PKG / "csrc"
 INCLUDE = PKG.parent / "include"
 OBJ = PKG / "_build"
 LIB = PKG / "libstom_oqm.so"
+BIND = PKG / "_stom_bind.so"
 
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
@@ -37,12 +40,27 @@ def sources():
 
 
 def _deps_mtime() -> float:
-    files = list(CSRC.glob("*.cu")) + list(CSRC.glob("*.cuh")) + list(INCLUDE.glob("*.h")) + [Path(__file__)]
+    files = list(CSRC.glob("*.cu")) + list(CSRC.glob("*.cuh")) + list(CSRC.glob("*.cpp")) + list(INCLUDE.glob("*.h")) + [Path(__file__)]
     return max(f.stat().st_mtime for f in files)
 
 
+def _build_binding() -> None:
+    import torch
+
+    at = Path(torch.__file__).parent
+    cuda = Path(_nvcc()).parent.parent if "/" in _nvcc() else Path("/usr/local/cuda")
+    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+           "-I", sysconfig.get_paths()["include"], "-I", str(at / "include"), "-I",
+           str(at / "include/torch/csrc/api/include"), "-I", str(cuda / "include"), "-I", str(INCLUDE),
+           str(CSRC / "stom_bind.cpp"), "-o", str(BIND), "-L", str(at / "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10",
+           "-lc10_cuda", f"-Wl,-rpath,{at / 'lib'}"]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode:
+        raise RuntimeError(f"g++ failed for stom_bind.cpp:\n{r.stdout}\n{r.stderr}")
+
+
 def build(force: bool = False, verbose: bool = False) -> Path:
-    if not force and LIB.exists() and LIB.stat().st_mtime >= _deps_mtime():
+    if not force and all(f.exists() and f.stat().st_mtime >= _deps_mtime() for f in (LIB, BIND)):
         return LIB
     OBJ.mkdir(exist_ok=True)
     nvcc = _nvcc()
@@ -59,7 +77,9 @@ def build(force: bool = False, verbose: bool = False) -> Path:
         return obj
 
     with ThreadPoolExecutor(max_workers=min(8, os.cpu_count() or 1)) as ex:
+        binding = ex.submit(_build_binding)
         objs = list(ex.map(compile_one, sources()))
+        binding.result()
     link = [nvcc, "-shared", "-gencode", "arch=compute_100a,code=sm_100a", "-o", str(LIB), *map(str, objs)]
     r = subprocess.run(link, capture_output=True, text=True)
     if r.returncode:

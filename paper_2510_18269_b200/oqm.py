@@ -82,8 +82,8 @@ class StomError(RuntimeError):
         super().__init__(f"{where}: {msg} (status {code}, cuda error {lib().stom_last_cuda_error()})")
 
 
-# Signatures of the calls that are made once per token: p pointer, i int32, l int64, f float, d double.  With them the
-# arguments go as plain numbers, which costs a call half of what wrapped ones do.
+# Result and argument types of the calls for the paged cache and the next token, for those who make them through ctypes:
+# p pointer, i int32, l int64, f float, d double.
 _CTYPE = {"p": C.c_void_p, "i": C.c_int32, "l": C.c_int64, "f": C.c_float, "d": C.c_double}
 _SIGNATURES = {
     "stom_kv_frequencies": (C.c_int32, "ididdddp"),
@@ -100,11 +100,14 @@ _SIGNATURES = {
 }
 
 _lib = None
+_bind = None   # the binding of the calls that are made once per token, set with the library
+_BOUND = ("stom_kv_attend", "stom_kv_rotate", "stom_kv_append", "stom_kv_reserve", "stom_kv_fork", "stom_kv_free",
+          "stom_kv_compact", "stom_sample_tokens")
 
 
 def lib():
     """The loaded C-ABI library.  Fails loudly when it has not been built."""
-    global _lib
+    global _lib, _bind
     if _lib is None:
         if not LIB_PATH.exists():
             raise ImportError(
@@ -123,6 +126,13 @@ def lib():
         for name, (res, args) in _SIGNATURES.items():
             fn = getattr(L, name)
             fn.restype, fn.argtypes = res, [_CTYPE[a] for a in args]
+        try:
+            from . import _stom_bind
+        except ImportError as e:
+            raise ImportError(f"{_PKG / '_stom_bind.so'} is missing or does not fit: build it with "
+                              "`python -m paper_2510_18269_b200.build`") from e
+        _stom_bind.use(*(C.cast(getattr(L, n), C.c_void_p).value for n in _BOUND))
+        _bind = _stom_bind
         for name in EXPORTS:
             fn = getattr(L, name)
             if fn.restype is C.c_int:
@@ -386,28 +396,6 @@ def _addr(t):
     return None if t is None else t.data_ptr()
 
 
-# The checks and look-ups of the calls that are made once per token cost as much as a small kernel runs, so they ask
-# torch in the cheapest ways there are (get_device() in the place of device, one stride() instead of several).
-_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-_current_device = getattr(torch._C, "_cuda_getDevice", None)
-
-
-def _launch(dev, stream, fn, *args):
-    """fn(*args, stream) with `dev` as the current device; stream None: the current one of that device."""
-    if dev < 0:
-        raise ValueError("the tensors of a call lie on a CUDA device")
-    if stream is not None:
-        s = stream.cuda_stream
-    elif _raw_stream is not None:
-        s = _raw_stream(dev)
-    else:
-        s = torch.cuda.current_stream(dev).cuda_stream
-    if (_current_device() if _current_device is not None else torch.cuda.current_device()) == dev:
-        return fn(*args, s)
-    with torch.cuda.device(dev):
-        return fn(*args, s)
-
-
 def _dense(t, dtype, shape, name, dev):
     """Address of a contiguous tensor of this type and shape on device number `dev` (-1: the CPU), or None."""
     if t is None:
@@ -418,28 +406,15 @@ def _dense(t, dtype, shape, name, dev):
                      f"{t.dtype} {tuple(t.shape)} with strides {t.stride()} on {t.device}")
 
 
-def _rows3(t, dtype, shape, name, dev):
-    """(address, stride of a row, stride of a head) of an [n][heads][d] tensor with adjacent channels."""
-    if t.dtype is dtype and t.shape == shape and t.get_device() == dev:
-        sn, sh, one = t.stride()
-        if one == 1:
-            return t.data_ptr(), sn, sh
-    raise ValueError(f"{name}: a {dtype} tensor of shape {tuple(shape)} with adjacent channels on device {dev} is needed, "
-                     f"not {t.dtype} {tuple(t.shape)} with strides {t.stride()} on {t.device}")
+def _binding():
+    if _bind is None:
+        lib()
+    return _bind
 
 
-def _workspace(t, dev):
-    if t.get_device() != dev or not t.is_contiguous():
-        raise ValueError("workspace: a contiguous tensor on the device of the call is needed")
-    return t.data_ptr(), t.nbytes
-
-
-def _flags(t, dev):
-    if t is None:
-        return None
-    if t.get_device() != dev or t.element_size() != 4 or t.numel() < 1:
-        raise ValueError("dev_flags: one 32-bit word on the device of the call is needed")
-    return t.data_ptr()
+def _handle(stream):
+    """What the binding takes for a stream: its handle, or None for the current one of the call's device."""
+    return None if stream is None else stream.cuda_stream
 
 
 class KvPool:
@@ -469,6 +444,7 @@ class KvSeqs:
         if refs is not None:
             _dense(refs, torch.int32, (refs.numel(),), "refs", self.dev)
         self.table, self.len, self.refs, self.n_seqs, self.max_pages = table, len, refs, n, width
+        self.n_refs = 0 if refs is None else refs.numel()
         stride = table.stride(0) if n > 1 else width
         self.desc = KvSeqsDesc(_addr(table), _addr(len), _addr(refs), n, width, stride)
         self.ref = C.addressof(self.desc)
@@ -509,52 +485,30 @@ def _same_device(pool, seqs, rope=None):
 def stom_kv_attend(pool: KvPool, seqs: KvSeqs, layer, q, out, softmax_scale, workspace, lse=None, softcap=0.0, window=0,
                    dev_flags=None, stream=None):
     """q, out: [n_seqs][query heads][d] of the pool's type; lse: [n_seqs][query heads] float32 or None."""
-    dt, dev = pool.dtype, pool.dev
     _same_device(pool, seqs)
-    hq = q.shape[1]
-    shape = (seqs.n_seqs, hq, pool.head_dim)
-    _check(_launch(dev, stream, lib().stom_kv_attend, pool.ref, seqs.ref, layer, hq, *_rows3(q, dt, shape, "q", dev),
-                   softmax_scale, softcap, window, *_rows3(out, dt, shape, "out", dev),
-                   _dense(lse, torch.float32, shape[:2], "lse", dev), *_workspace(workspace, dev), _flags(dev_flags, dev)),
-           "stom_kv_attend")
-
-
-_NO_ROWS = (None, 0, 0, 0, None, 0, 0, None)
-
-
-def _turned(x, out, weight, name, dt, n, d, dev):
-    """The arguments of one of the tensors that are rotated."""
-    shape = (n, x.shape[1], d)
-    a, sn, sh = _rows3(x, dt, shape, name, dev)
-    return (a, shape[1], sn, sh, *_rows3(out, dt, shape, name + "_out", dev), _dense(weight, torch.float32, (d,), name + "_weight", dev))
+    rc = _binding().attend(pool.ref, seqs.ref, pool.dev, layer, q, out, softmax_scale, softcap, window, lse, workspace,
+                           dev_flags, _handle(stream))
+    if rc:
+        _check(rc, "stom_kv_attend")
 
 
 def stom_kv_rotate(rope: Rope, pos, q=None, q_out=None, k=None, k_out=None, q_weight=None, k_weight=None, eps=1e-6,
                    stream=None):
     """q, k and their outputs: [n][heads][d], each with its own strides (an output may be its input); pos: int32 [n];
     weights: float32 [d] or None (no norm)."""
-    x = q if q is not None else k
-    n, _, d = x.shape
-    dt, dev = x.dtype, x.get_device()
-    if rope.dev is not None and rope.dev != dev:
-        raise ValueError("the frequencies lie on the device of the tensors")
-    _check(_launch(dev, stream, lib().stom_kv_rotate, rope.ref, dtype_code(dt), d, n, _dense(pos, torch.int32, (n,), "pos", dev),
-                   *(_NO_ROWS if q is None else _turned(q, q_out, q_weight, "q", dt, n, d, dev)),
-                   *(_NO_ROWS if k is None else _turned(k, k_out, k_weight, "k", dt, n, d, dev)), eps), "stom_kv_rotate")
+    rc = _binding().rotate(rope.ref, pos, q, q_out, k, k_out, q_weight, k_weight, eps, _handle(stream), rope.dev)
+    if rc:
+        _check(rc, "stom_kv_rotate")
 
 
 def stom_kv_append(pool: KvPool, seqs: KvSeqs, layer, rope: Rope, pos, slot, k, v, q=None, q_out=None, seq=None,
                    q_weight=None, k_weight=None, eps=1e-6, dev_flags=None, stream=None):
     """k, v: [n][kv heads][d] of the pool's type; slot, pos, seq: int32 [n]; q and q_out: [n][query heads][d] or None."""
-    dt, dev, d = pool.dtype, pool.dev, pool.head_dim
     _same_device(pool, seqs, rope)
-    n = k.shape[0]
-    shape, one, i32 = (n, pool.n_kv_heads, d), (n,), torch.int32
-    _check(_launch(dev, stream, lib().stom_kv_append, pool.ref, seqs.ref, layer, rope.ref, n, _dense(pos, i32, one, "pos", dev),
-                   _dense(slot, i32, one, "slot", dev), _dense(seq, i32, one, "seq", dev),
-                   *(_NO_ROWS if q is None else _turned(q, q_out, q_weight, "q", dt, n, d, dev)),
-                   *_rows3(k, dt, shape, "k", dev), _dense(k_weight, torch.float32, (d,), "k_weight", dev),
-                   *_rows3(v, dt, shape, "v", dev), eps, _flags(dev_flags, dev)), "stom_kv_append")
+    rc = _binding().append(pool.ref, seqs.ref, pool.dev, layer, rope.ref, pos, slot, k, v, q, q_out, seq, q_weight, k_weight,
+                           eps, dev_flags, _handle(stream))
+    if rc:
+        _check(rc, "stom_kv_append")
 
 
 def stom_kv_pages_workspace_bytes(pool: KvPool, seqs: KvSeqs) -> int:
@@ -565,42 +519,34 @@ def stom_kv_pages_workspace_bytes(pool: KvPool, seqs: KvSeqs) -> int:
 
 
 def _counts_of(pool, seqs):
-    if seqs.refs is None or seqs.refs.numel() != pool.n_pages:
+    if seqs.refs is None or seqs.n_refs != pool.n_pages:
         raise ValueError("the sequences need refs, one count for each page of the pool")
     _same_device(pool, seqs)
 
 
-def _wish(call, pool, seqs, wish, name, rest, dev_flags, stream):
-    _counts_of(pool, seqs)
-    w = _dense(wish, torch.int32, (seqs.n_seqs,), name, pool.dev)
-    _check(_launch(pool.dev, stream, getattr(lib(), call), pool.ref, seqs.ref, w, *rest, _flags(dev_flags, pool.dev)), call)
-
-
 def stom_kv_reserve(pool: KvPool, seqs: KvSeqs, want, workspace, dev_flags=None, stream=None):
     """want: int32 [n_seqs], the length each sequence grows to (at most its length: it stays)."""
-    _wish("stom_kv_reserve", pool, seqs, want, "want", _workspace(workspace, pool.dev), dev_flags, stream)
+    _counts_of(pool, seqs)
+    _check(_binding().reserve(pool.ref, seqs.ref, pool.dev, want, workspace, dev_flags, _handle(stream)), "stom_kv_reserve")
 
 
 def stom_kv_fork(pool: KvPool, seqs: KvSeqs, parent, dev_flags=None, stream=None):
     """parent: int32 [n_seqs], the sequence an empty one shares from now on, or -1."""
-    _wish("stom_kv_fork", pool, seqs, parent, "parent", (), dev_flags, stream)
+    _counts_of(pool, seqs)
+    _check(_binding().fork(pool.ref, seqs.ref, pool.dev, parent, dev_flags, _handle(stream)), "stom_kv_fork")
 
 
 def stom_kv_free(pool: KvPool, seqs: KvSeqs, drop, dev_flags=None, stream=None):
     """drop: int32 [n_seqs], not 0 for the sequences that give their pages back."""
-    _wish("stom_kv_free", pool, seqs, drop, "drop", (), dev_flags, stream)
+    _counts_of(pool, seqs)
+    _check(_binding().free(pool.ref, seqs.ref, pool.dev, drop, dev_flags, _handle(stream)), "stom_kv_free")
 
 
 def stom_kv_compact(pool: KvPool, seqs: KvSeqs, table_out, refs_out, n_live, workspace, dev_flags=None, stream=None):
     """table_out, refs_out: like seqs.table and seqs.refs (or those themselves); n_live: int32 [1] or None."""
     _counts_of(pool, seqs)
-    t, dev = seqs.table, pool.dev
-    if table_out.dtype is not torch.int32 or table_out.shape != t.shape or table_out.stride() != t.stride() \
-            or table_out.get_device() != dev:
-        raise ValueError("table_out: a tensor like seqs.table")
-    _check(_launch(dev, stream, lib().stom_kv_compact, pool.ref, seqs.ref, table_out.data_ptr(),
-                   _dense(refs_out, torch.int32, (pool.n_pages,), "refs_out", dev), _dense(n_live, torch.int32, (1,), "n_live", dev),
-                   *_workspace(workspace, dev), _flags(dev_flags, dev)), "stom_kv_compact")
+    _check(_binding().compact(pool.ref, seqs.ref, pool.dev, table_out, refs_out, n_live, workspace, dev_flags,
+                              _handle(stream)), "stom_kv_compact")
 
 
 # ---------------------------------------------------------------- choice of the next token (include/stom_sample.h)
@@ -608,13 +554,6 @@ def stom_kv_compact(pool: KvPool, seqs: KvSeqs, table_out, refs_out, n_live, wor
 def stom_sample_tokens(logits, u, token, temperature=None, top_k=None, top_p=None, min_p=None, logprob=None, kept=None,
                        dev_flags=None, stream=None):
     """logits: [rows][n]; u, temperature, top_p, min_p, logprob: float32 [rows]; token, kept, top_k: int32 [rows]."""
-    rows, n = logits.shape
-    stride, one = logits.stride()
-    if n > 1 and one != 1:
-        raise ValueError("logits: the entries of a row are adjacent")
-    dev, of, f, i = logits.get_device(), (rows,), torch.float32, torch.int32
-    _check(_launch(dev, stream, lib().stom_sample_tokens, logits.data_ptr(), dtype_code(logits.dtype), rows, n, stride,
-                   _dense(temperature, f, of, "temperature", dev), _dense(top_k, i, of, "top_k", dev),
-                   _dense(top_p, f, of, "top_p", dev), _dense(min_p, f, of, "min_p", dev), _dense(u, f, of, "u", dev),
-                   _dense(token, i, of, "token", dev), _dense(kept, i, of, "kept", dev),
-                   _dense(logprob, f, of, "logprob", dev), _flags(dev_flags, dev)), "stom_sample_tokens")
+    rc = _binding().sample(logits, u, token, temperature, top_k, top_p, min_p, logprob, kept, dev_flags, _handle(stream))
+    if rc:
+        _check(rc, "stom_sample_tokens")
