@@ -5,6 +5,8 @@
 #include "stom_internal.cuh"
 #include "stom_kv.h"
 
+#include <atomic>
+
 namespace stom {
 
 // ---------------------------------------------------------------- host
@@ -15,6 +17,17 @@ int32_t check_pool(const stom_kv_pool *p);
 int32_t check_seqs(const stom_kv_pool *p, const stom_kv_seqs *s, bool need_refs);
 // Multiprocessors of the current device, or 0 with the CUDA error recorded.
 int32_t sm_count();
+
+// Allows a kernel `bytes` of dynamic shared memory on the current device; `done` (a static of the caller's, one per
+// kernel) remembers the devices where that has been set.
+inline cudaError_t allow_shared(const void *kernel, int bytes, std::atomic<uint64_t> &done) {
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess || (dev < 64 && (done.load(std::memory_order_acquire) >> dev & 1u))) return e;
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e == cudaSuccess && dev < 64) done.fetch_or(1ull << dev, std::memory_order_release);
+    return e;
+}
 
 // x / d for 0 <= x < 2^31 by a multiplication (round-up method: m = floor(2^32 (2^s - d) / d) + 1 with
 // s = ceil(log2 d); then floor((mulhi(x, m) + x) / 2^s) = floor(x / d), and the sum stays below 2^32).

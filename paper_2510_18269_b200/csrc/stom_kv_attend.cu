@@ -655,7 +655,8 @@ int64_t round16(int64_t x) { return (x + 15) & ~(int64_t)15; }
 template <typename T, int D, int NT>
 int32_t launch(const KvAttendParams &p, int sms, cudaStream_t stream) {
     using S = Shape<D, NT>;
-    cudaError_t e = cudaFuncSetAttribute(kv_attend_kernel<T, D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem);
+    static std::atomic<uint64_t> allowed{0};
+    cudaError_t e = allow_shared(reinterpret_cast<const void *>(kv_attend_kernel<T, D, NT>), S::kSmem, allowed);
     if (e == cudaSuccess)
         e = launch_after_producer(kv_attend_kernel<T, D, NT>, dim3(sms), dim3(S::kWarps * 32), S::kSmem, stream, p);
     if (e == cudaSuccess)

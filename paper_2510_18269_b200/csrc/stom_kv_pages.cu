@@ -420,8 +420,8 @@ extern "C" int32_t stom_kv_reserve(const stom_kv_pool *pool, const stom_kv_seqs 
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     const size_t smem = (size_t)seqs->n_seqs * 8;
     cudaError_t e = cudaSuccess;
-    if (smem > 48 * 1024 - 1024)
-        e = cudaFuncSetAttribute(kv_reserve_plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, STOM_KV_MAX_SEQS * 8);
+    static std::atomic<uint64_t> allowed{0};
+    if (smem > 47 * 1024) e = allow_shared(reinterpret_cast<const void *>(kv_reserve_plan_kernel), STOM_KV_MAX_SEQS * 8, allowed);
     if (e == cudaSuccess) e = launch_after_producer(kv_reserve_plan_kernel, dim3(1), dim3(kPlanThreads), smem, s, p);
     if (e == cudaSuccess) e = launch_after_producer(kv_move_kernel<false>, dim3(sms * 8), dim3(256), 0, s, p);
     return e == cudaSuccess ? finish_launch() : failed(e);
