@@ -90,7 +90,7 @@ struct Plan {
     static constexpr int kThreads = kHalf ? 1024 : 512;
     static constexpr int kRaw = kHalf ? 65536 * 2 : kRanges * 16;     // counters
     // behind them: the list of ranges that are not empty (16 bits); the keys gathered, ranked, their sums (binary32)
-    static constexpr int kList = kHalf ? kRanges * 2 : kGather * (4 + 4 + 4 + 8) + 16;
+    static constexpr int kList = kHalf ? kRanges * 2 : kGather * (4 + 4 + 4 + 4 + 8);
     static int share(int cluster) { return ((kRanges + cluster - 1) / cluster + 31) & ~31; }   // whole words of bits
     static int smem(int cluster) { return kRaw + kList + (kHalf ? 1 : 2) * share(cluster) * 12; }
 };
@@ -465,7 +465,7 @@ struct Row {
             while (cell.count > kGather && low_key != high_key) {
                 const uint32_t span = high_key - low_key;
                 shift = max(0, 21 - __clz(span));                      // span >> shift < kRanges = 2^11
-                tally<1>();
+                tally<1, true>();
                 cell = find(1, q, cell.before, cell.mass_before);
                 high_key -= cell.range << shift;
                 low_key = max(low_key, high_key - min(high_key, (1u << shift) - 1));
@@ -504,7 +504,8 @@ struct Row {
     }
 
     // Counts and masses of a level (1: of the keys from low_key to high_key), summed over the cluster
-    template <int LEVEL>
+    // MASSES false: counts alone, which is all that ranking the first top_k needs.
+    template <int LEVEL, bool MASSES>
     __device__ __forceinline__ void tally() {
         zero_raw();
         __syncthreads();
@@ -518,6 +519,7 @@ struct Row {
             }
             uint32_t *r = raw + 4 * range;
             atomicAdd(r, 1u);
+            if (!MASSES) return;
             if ((uint32_t)w & 0xffffu) atomicAdd(r + 1, (uint32_t)w & 0xffffu);
             if ((uint32_t)w >> 16) atomicAdd(r + 2, (uint32_t)w >> 16);
             if (w >> 32) atomicAdd(r + 3, (uint32_t)(w >> 32));
@@ -534,13 +536,13 @@ struct Row {
 #pragma unroll
             for (int e = 0; e < 4; ++e) k[e] = K::of(b[e], nan);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) w[e] = whole(k[e]);
+            for (int e = 0; e < 4; ++e) w[e] = MASSES ? whole(k[e]) : 0ull;
 #pragma unroll
             for (int e = 0; e < 4; ++e) add(k[e], w[e]);
         }, [&](uint32_t b, int) {
             bool nan = false;
             const uint32_t k = K::of(b, nan);
-            add(k, whole(k));
+            add(k, MASSES ? whole(k) : 0ull);
         });
         if (LEVEL == 0) {
             beyond = __reduce_add_sync(~0u, beyond);
@@ -566,14 +568,16 @@ struct Row {
     }
 
     // Every block gathers the at most kGather keys from low_key to high_key and ranks them, `base` and `mass_base` ahead of
-    // them: afterwards own[i] is the i-th of them, upto[i] their mass up to it.
+    // them: afterwards order[i] is the i-th of them, upto[i] their mass up to it.  (`own` is read by the other blocks until
+    // the next barrier of the cluster: a gathering always follows a find.)
     struct Ranked {
         uint32_t m, base;
         double mass_base;
     } ranked;
     __device__ __forceinline__ uint32_t *own() const { return reinterpret_cast<uint32_t *>(list); }
-    __device__ __forceinline__ uint32_t *above() const { return own() + 2 * kGather; }   // keys above one; high half: equal ones
-    __device__ __forceinline__ double *upto() const { return reinterpret_cast<double *>(own() + 3 * kGather); }
+    __device__ __forceinline__ uint32_t *order() const { return own() + 2 * kGather; }
+    __device__ __forceinline__ uint32_t *above() const { return own() + 3 * kGather; }   // keys above one; high half: equal ones
+    __device__ __forceinline__ double *upto() const { return reinterpret_cast<double *>(own() + 4 * kGather); }
     __device__ __forceinline__ void rank_keys(uint32_t base, double mass_base) {
         uint32_t *keys = own() + kGather;                              // all blocks'
         if (tid == 0) sh.listed = 0;
@@ -597,7 +601,7 @@ struct Row {
             for (uint32_t i = lane; i < k; i += 32)
                 if (first + i < kGather) keys[first + i] = ld_cluster_u(own() + i, r);
         }
-        cluster_sync();                                                // own is free again
+        __syncthreads();
         for (uint32_t i = tid; i < m; i += kThreads) {
             const uint32_t k = keys[i];
             uint32_t more = 0, equal = 0, ahead = 0;
@@ -608,14 +612,14 @@ struct Row {
                 equal += o == k;
                 ahead += o == k && j < i;
             }
-            own()[more + ahead] = k;
+            order()[more + ahead] = k;
             above()[more + ahead] = more | equal << 16;
         }
         __syncthreads();
         // masses up to each, in order: two neighbours a thread
         const uint32_t i0 = 2 * tid;
-        const double w0 = i0 < m ? units(K::value(own()[i0])) * kUnit : 0.0;
-        const double w1 = i0 + 1 < m ? units(K::value(own()[i0 + 1])) * kUnit : 0.0;
+        const double w0 = i0 < m ? units(K::value(order()[i0])) * kUnit : 0.0;
+        const double w1 = i0 + 1 < m ? units(K::value(order()[i0 + 1])) * kUnit : 0.0;
         double sum = w0 + w1;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
@@ -639,11 +643,11 @@ struct Row {
         __syncthreads();
         for (uint32_t i = tid; i < ranked.m; i += kThreads) {
             const double mass_to = ranked.mass_base + upto()[i];
-            const bool in = q.kind != BY_KEY || own()[i] >= q.key;
+            const bool in = q.kind != BY_KEY || order()[i] >= q.key;
             const bool reached = q.kind == BY_RANK ? ranked.base + i + 1 > q.rank
                                  : q.kind == BY_MASS ? mass_to >= q.mass : q.kind == PAST_MASS && mass_to > q.mass;
             if (in && reached) atomicMin(&sh.first, i);
-            if (in && (i + 1 == ranked.m || (q.kind == BY_KEY && own()[i + 1] < q.key))) sh.last = i + 1;
+            if (in && (i + 1 == ranked.m || (q.kind == BY_KEY && order()[i + 1] < q.key))) sh.last = i + 1;
         }
         __syncthreads();
         if (tid == 0) {
@@ -651,8 +655,8 @@ struct Row {
                 sh.place = Place{0, ranked.base, 0, ranked.mass_base, 0.0};
             } else {
                 const uint32_t i = sh.first != ~0u ? sh.first : sh.last - 1, more = above()[i] & 0xffffu;
-                sh.place = Place{own()[i], ranked.base + more, above()[i] >> 16, ranked.mass_base + (more ? upto()[more - 1] : 0.0),
-                                 units(K::value(own()[i])) * kUnit};
+                sh.place = Place{order()[i], ranked.base + more, above()[i] >> 16, ranked.mass_base + (more ? upto()[more - 1] : 0.0),
+                                 units(K::value(order()[i])) * kUnit};
             }
         }
         __syncthreads();
@@ -909,7 +913,12 @@ __global__ void __launch_bounds__(Plan<T>::kThreads, RES) sample_kernel(const __
         if constexpr (kHalf) {
             if (r.tally16() && p.flags) atomicOr(p.flags, STOM_FLAG_BAD_VALUE);
         } else {
-            r.template tally<0>();
+            const bool few = top_k > 0 && top_k <= (int)kGather;
+            if (few) {
+                r.template tally<0, false>();
+                if ((uint32_t)top_k < r.sums[0].total) r.rank_first((uint32_t)top_k - 1);
+            }
+            if (!r.all_ranked) r.template tally<0, true>();
         }
         // One warp decides after each answer; 32 would only wait for one another's binary64 operations.
         uint32_t count = r.sums[0].total;
@@ -920,8 +929,6 @@ __global__ void __launch_bounds__(Plan<T>::kThreads, RES) sample_kernel(const __
             mass = sh.mass;
         };
         if (top_k > 0 && (uint32_t)top_k < count) {
-            if constexpr (!kHalf)
-                if (top_k <= (int)kGather) r.rank_first((uint32_t)top_k - 1);
             const Place a = r.ask(Query{BY_RANK, (uint32_t)top_k - 1, 0, 0.0});
             count = top_k;
             mass = a.mass_before + (double)(top_k - a.before) * a.weight;
