@@ -19,6 +19,13 @@
 // whole weight.  The masses of ranges are whole multiples of 2^-44 (of the largest weight) in 64 bits: their sums are
 // exact and never fall, so that exactly one range holds a place and all blocks of a cluster see the same one.  Within the
 // last few keys weights and sums are binary64.
+//
+// What bounds it: not memory (128 rows of 151 001 bf16 logits are 6 us at the copy rate) but the chain of steps a row has
+// to go through, each a barrier, a look into another block's memory or a binary64 sum away from the next.  Measured: 128
+// such rows with mixed settings 78 us, three rounds of 49 clusters of 3 blocks; a block's 24 us are 6 for its 50 000
+// logits (4.3 cycles for a warp's shared-memory atomic, the rest the patterns' arithmetic), 5 for the ranges, 2 to 2.5 for
+// every place asked for, 3 for the index.  One row of 128 000 logits on 16 blocks: bf16 21 us, binary32 20 us with top-k,
+// 37 us with top-p alone (a ranking for each of two places).
 #include "stom_kv.cuh"
 #include "stom_sample.h"
 
