@@ -12,11 +12,12 @@
 //     shared-memory atomic per logit is all the work that grows with the row; order, infinities and NaN are sorted out
 //     when the counters are read, the exponential is taken per DISTINCT logit, and a mass is count times weight.
 //   binary32 logits: ranges of equal width in (x_max - x) / T, so that the logits spread over them; counts, and masses as
-//     sums of integers, weight * 2^44 in three 16-bit limbs, so that the order of the atomics leaves no trace.  The keys
+//     sums of integers, three limbs of 16 bits (18 for short rows), so that the order of the atomics leaves no trace.  The keys
 //     of a range are gathered and ranked; a range with more than kGather of them is cut into 2 048
 //     again.  With top-k everything else is decided among the keys ranked for it, if they are no more.
 // With 100 000 tokens left to draw from, binary32 sums would move a border between two tokens by more than some tokens'
-// whole weight.  The masses of ranges are whole multiples of 2^-44 (of the largest weight) in 64 bits: their sums are
+// whole weight.  The masses of ranges are whole numbers of UNITS in 64 bits, 2^-43 (the longest rows) to 2^-51 of the
+// largest weight, the smallest that a row's sum has room for: their sums are
 // exact and never fall, so that exactly one range holds a place and all blocks of a cluster see the same one.  Within the
 // last few keys weights and sums are binary64.
 //
@@ -39,12 +40,13 @@ constexpr int kMostRanges = 4096;
 constexpr int kMaxCluster = 16;
 constexpr uint32_t kGather = 1024;   // keys that are ranked at once (binary32)
 constexpr int kSummers = 256;        // threads that add up a block's ranges
-constexpr double kUnit = 0x1p-44;    // masses of ranges are whole multiples of this
 
 struct SampleParams {
     const char *logits;
     int64_t row_stride;
     int32_t n, slice;
+    int32_t unit_bits, limb;     // a unit is 2^-unit_bits; bits of a limb (binary32)
+    float per_nat;               // binary32: first ranges to a factor e of the weight
     const float *temperature, *top_p, *min_p, *u;
     const int32_t *top_k;
     int32_t *token, *kept;
@@ -178,7 +180,8 @@ struct Row {
     const T *x;                  // this block's slice
     int n;
     uint32_t rank, blocks, share, mine;   // ranges of a block, and of this one
-    double top, t, per_log2;     // per_log2: log2(e) / t
+    double top, t, per_log2, unit;   // per_log2: log2(e) / t
+    int unit_bits, limb;
     float top_f, per_range;      // binary32: ranges per unit of x
     int tid;
     uint32_t slot = 0;
@@ -208,8 +211,8 @@ struct Row {
         e = fma(e, r, 2.402265069591007e-1);
         e = fma(e, r, 6.931471805599453e-1);
         e = fma(e, r, 1.0) * sh.power[k & 63];
-        // times 2^(k >> 6) / kUnit, by the exponent
-        return __hiloint2double(__double2hiint(e) + ((k >> 6) + 44) * (1 << 20), __double2loint(e));
+        // times 2^(k >> 6) / unit, by the exponent
+        return __hiloint2double(__double2hiint(e) + ((k >> 6) + unit_bits) * (1 << 20), __double2loint(e));
     }
 
     // Block r of the cluster as the i-th to look at.  Every block begins with itself: if all began with block 0, they
@@ -384,7 +387,7 @@ struct Row {
             if (c == 0) return false;
             if (c == s.total) return true;
             if (q.kind == BY_RANK) return base + c > q.rank;
-            const double upto = (double)(mass_base + m) * kUnit;
+            const double upto = (double)(mass_base + m) * unit;
             return q.kind == BY_MASS ? upto >= q.mass : upto > q.mass;
         };
         bool holds = false;
@@ -422,7 +425,7 @@ struct Row {
         if constexpr (kHalf) return kRanges - 1 - (key >> 4);
         else return level ? (high_key - key) >> shift : range_at(K::single(key));
     }
-    // binary32, first level: equal widths in x, 65.5 of them to a factor e of the weight, down to weights of 2^-45.  Every
+    // binary32, first level: equal widths in x, about 64 of them to a factor e of the weight, down to half a unit.  Every
     // step of it is monotonous, so a range is a run of keys.
     __device__ __forceinline__ uint32_t range_at(float v) const {
         const float f = (top_f - v) * per_range;
@@ -442,7 +445,7 @@ struct Row {
                 const uint32_t key = (kRanges - 1 - cell.range) * 16 + 15 - (tid & 15);
                 bool nan = false;
                 uint32_t c = tid < 16 ? count_of(key, nan) : 0u;
-                const double w = c ? units(K::value(key)) * kUnit : 0.0;
+                const double w = c ? units(K::value(key)) * unit : 0.0;
                 uint32_t c1 = c;
                 double m1 = c * w;
 #pragma unroll
@@ -454,7 +457,7 @@ struct Row {
                         m1 += vm;
                     }
                 }
-                const double mb = (double)cell.mass_before * kUnit, ahead = __shfl_up_sync(~0u, m1, 1);
+                const double mb = (double)cell.mass_before * unit, ahead = __shfl_up_sync(~0u, m1, 1);
                 const bool in = c && (q.kind != BY_KEY || key >= q.key);
                 const bool reached = in && (q.kind == BY_RANK ? cell.before + c1 > q.rank
                                             : q.kind == BY_MASS ? mb + m1 >= q.mass : q.kind == PAST_MASS && mb + m1 > q.mass);
@@ -477,11 +480,11 @@ struct Row {
                 high_key -= cell.range << shift;
                 low_key = max(low_key, high_key - min(high_key, (1u << shift) - 1));
             }
-            const double mb = (double)cell.mass_before * kUnit;
+            const double mb = (double)cell.mass_before * unit;
             if (low_key == high_key) {
                 if (tid == 0) {
                     const bool in = cell.count && (q.kind != BY_KEY || high_key >= q.key);
-                    sh.place = in ? Place{high_key, cell.before, cell.count, mb, units(K::value(high_key)) * kUnit}
+                    sh.place = in ? Place{high_key, cell.before, cell.count, mb, units(K::value(high_key)) * unit}
                                   : Place{0, cell.before, 0, mb, 0.0};
                 }
                 __syncthreads();
@@ -520,16 +523,17 @@ struct Row {
         auto add = [&](uint32_t k, uint64_t w) {
             if (!k || (LEVEL && (k < low_key || k > high_key))) return;
             const uint32_t range = range_of(LEVEL, k);
-            if (LEVEL == 0 && range == kRanges - 1) {          // weights below 2^-45
+            if (LEVEL == 0 && range == kRanges - 1) {          // weights below half a unit
                 ++beyond;
                 return;
             }
             uint32_t *r = raw + 4 * range;
             atomicAdd(r, 1u);
             if (!MASSES) return;
-            if ((uint32_t)w & 0xffffu) atomicAdd(r + 1, (uint32_t)w & 0xffffu);
-            if ((uint32_t)w >> 16) atomicAdd(r + 2, (uint32_t)w >> 16);
-            if (w >> 32) atomicAdd(r + 3, (uint32_t)(w >> 32));
+            const uint32_t mask = (1u << limb) - 1, w0 = (uint32_t)w & mask, w1 = (uint32_t)(w >> limb) & mask, w2 = (uint32_t)(w >> 2 * limb);
+            if (w0) atomicAdd(r + 1, w0);
+            if (w1) atomicAdd(r + 2, w1);
+            if (w2) atomicAdd(r + 3, w2);
         };
         // to whole units: 2^52 added leaves them in the low bits
         auto whole = [&](uint32_t k) {
@@ -565,7 +569,7 @@ struct Row {
                 if (i < blocks) {
                     const uint4 v = ld_cluster_u4(r, turn(i));
                     c += v.x;
-                    w += (uint64_t)v.y + ((uint64_t)v.z << 16) + ((uint64_t)v.w << 32);
+                    w += (uint64_t)v.y + ((uint64_t)v.z << limb) + ((uint64_t)v.w << 2 * limb);
                 }
             cnt[LEVEL][j] = c;
             mass[LEVEL][j] = w;
@@ -625,8 +629,8 @@ struct Row {
         __syncthreads();
         // masses up to each, in order: two neighbours a thread
         const uint32_t i0 = 2 * tid;
-        const double w0 = i0 < m ? units(K::value(order()[i0])) * kUnit : 0.0;
-        const double w1 = i0 + 1 < m ? units(K::value(order()[i0 + 1])) * kUnit : 0.0;
+        const double w0 = i0 < m ? units(K::value(order()[i0])) * unit : 0.0;
+        const double w1 = i0 + 1 < m ? units(K::value(order()[i0 + 1])) * unit : 0.0;
         double sum = w0 + w1;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
@@ -663,7 +667,7 @@ struct Row {
             } else {
                 const uint32_t i = sh.first != ~0u ? sh.first : sh.last - 1, more = above()[i] & 0xffffu;
                 sh.place = Place{order()[i], ranked.base + more, above()[i] >> 16, ranked.mass_base + (more ? upto()[more - 1] : 0.0),
-                                 units(K::value(order()[i])) * kUnit};
+                                 units(K::value(order()[i])) * unit};
             }
         }
         __syncthreads();
@@ -888,10 +892,13 @@ __global__ void __launch_bounds__(Plan<T>::kThreads, RES) sample_kernel(const __
     r.top = K::value(best ? best : K::kLowest);
     r.t = cold ? 1.0 : (double)temp;
     r.per_log2 = 1.4426950408889634 / r.t;
+    r.unit_bits = p.unit_bits;
+    r.unit = __hiloint2double((1023 - p.unit_bits) << 20, 0);
+    r.limb = p.limb;
     if constexpr (!kHalf) {
         r.best = best;
         r.top_f = K::single(best ? best : K::kLowest);
-        r.per_range = fminf(65.5f / (cold ? 1.f : temp), 3.0e38f);
+        r.per_range = fminf(p.per_nat / (cold ? 1.f : temp), 3.0e38f);
     }
 
     // ---- the place drawn: key, and how many equal ones come before it
@@ -929,7 +936,7 @@ __global__ void __launch_bounds__(Plan<T>::kThreads, RES) sample_kernel(const __
         }
         // One warp decides after each answer; 32 would only wait for one another's binary64 operations.
         uint32_t count = r.sums[0].total;
-        double mass = (double)r.sums[0].all * kUnit;
+        double mass = (double)r.sums[0].all * r.unit;
         auto settled = [&]() {
             __syncthreads();
             count = sh.count;
@@ -1038,7 +1045,7 @@ __global__ void __launch_bounds__(Plan<T>::kThreads, RES) sample_kernel(const __
     auto answer = [&](int index) {
         p.token[row] = begin + index;
         if (p.kept) p.kept[row] = (int32_t)kept;
-        if (p.logprob) p.logprob[row] = (float)log(weight / total);
+        if (p.logprob) p.logprob[row] = (float)(log(weight) - log(total));
     };
     if (own <= kRoom) {
         if constexpr (kHalf) r.collect(key, found, kRoom);
@@ -1173,6 +1180,11 @@ extern "C" int32_t stom_sample_tokens(const void *logits, int32_t dtype, int32_t
                           reinterpret_cast<uintptr_t>(kept) | reinterpret_cast<uintptr_t>(logprob);
     if (all & 3u || reinterpret_cast<uintptr_t>(logits) % elem_bytes(dtype)) return STOM_ERR_ALIGNMENT;
     SampleParams p = {};
+    int bits = 0;
+    while ((1 << bits) < n) ++bits;
+    p.unit_bits = 62 - bits < 51 ? 62 - bits : 51;    // 2^bits weights of 1 are 2^62 units; binary64 holds 2^52 of them
+    p.limb = p.unit_bits > 47 ? 18 : 16;              // a slice's sum of limbs takes 32 bits: 2^14 (unit_bits >= 48) of 18
+    p.per_nat = (Plan<float>::kRanges - 1) / ((p.unit_bits + 1) * 0.69314718f);
     p.logits = static_cast<const char *>(logits);
     p.row_stride = row_stride;
     p.n = n;

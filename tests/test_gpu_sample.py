@@ -194,3 +194,21 @@ def test_draws_have_the_shares_of_the_distribution():
     got = torch.bincount(token.long(), minlength=n).double().cpu().numpy()
     p = torch.softmax(x[0].double(), 0).cpu().numpy()
     assert (np.abs(got - p * rows) <= 1.0 + 1e-6).all()
+
+
+@pytest.mark.parametrize("dtype", [BF, HF, FL])
+@pytest.mark.parametrize("n", [2, 9, 2000])
+def test_log_probability_of_a_token_that_is_nearly_certain(dtype, n):
+    """ln(w / mass) = -ln(1 + rest) where all the others weigh `rest` of the token drawn: relative to itself within the
+    mass's own step, 2^-51 of the largest weight for every one of n <= 2048 tokens, and 2^-22 for the rest of the way."""
+    oqm = _lib()
+    gaps = [2.0, 8.0, 16.0, 20.0, 24.0]
+    x = torch.zeros(len(gaps), n, dtype=dtype, device="cuda")
+    x[:, n // 2] = torch.tensor(gaps, device="cuda").to(dtype)
+    token, lp = torch.empty(len(gaps), dtype=torch.int32, device="cuda"), torch.empty(len(gaps), device="cuda")
+    oqm.stom_sample_tokens(x, torch.zeros(len(gaps), device="cuda"), token, logprob=lp)
+    for i, g in enumerate(gaps):
+        rest = (n - 1) * math.exp(-g)
+        want = -math.log1p(rest)
+        assert int(token[i]) == n // 2
+        assert abs(float(lp[i]) - want) <= abs(want) * 2.0 ** -22 + n * 2.0 ** -51
