@@ -61,6 +61,8 @@ typedef struct stom_kv_pool {
     int64_t stride_layer, stride_page, stride_token, stride_head;
 } stom_kv_pool;
 
+#define STOM_KV_MAX_SEQS 8192 /* rows that stom_kv_attend and stom_kv_reserve take */
+
 /* The sequences that live in a pool.  Row i of `table` names, in order, the
  * ceil(len[i]/page_tokens) pages of sequence i; what stands behind them is not
  * read.  refs[p] counts the rows that hold page p; 0 is a free page. */
@@ -136,7 +138,10 @@ int32_t stom_kv_append(const stom_kv_pool *pool, const stom_kv_seqs *seqs, int32
  * weights enter the second product as a high and a low 16-bit part.
  * q, out (pool->dtype): element (i, h, c) at i*stride_seq + h*stride_head + c.
  * lse: binary32 [n_seqs][n_q_heads], or NULL.
- * n_q_heads / n_kv_heads <= 64.  workspace: 16-byte aligned, of at least
+ * n_q_heads / n_kv_heads <= 64, n_seqs <= STOM_KV_MAX_SEQS, max_pages *
+ * page_tokens < 2^31 - 32, and n_seqs * n_kv_heads * max_pages * page_tokens
+ * below 2^34 (n_kv_heads counted twice where its query heads are more than 16,
+ * or 8 at head_dim 256, and so on).  workspace: 16-byte aligned, of at least
  * stom_kv_attend_workspace_bytes() bytes; its contents do not matter.
  * Errors: INVALID_ARG, SHAPE, UNSUPPORTED, ALIGNMENT, WORKSPACE, CUDA. */
 int64_t stom_kv_attend_workspace_bytes(const stom_kv_pool *pool, const stom_kv_seqs *seqs, int32_t n_q_heads);
@@ -159,7 +164,6 @@ int32_t stom_kv_attend(const stom_kv_pool *pool, const stom_kv_seqs *seqs, int32
  * max_pages*page_tokens is skipped and sets STOM_FLAG_BAD_INDEX.
  * n_seqs <= STOM_KV_MAX_SEQS.  workspace: 16-byte aligned, of at least
  * stom_kv_pages_workspace_bytes() bytes.  Errors as for stom_kv_attend. */
-#define STOM_KV_MAX_SEQS 8192
 int64_t stom_kv_pages_workspace_bytes(const stom_kv_pool *pool, const stom_kv_seqs *seqs);
 int32_t stom_kv_reserve(const stom_kv_pool *pool, const stom_kv_seqs *seqs, const int32_t *want, void *workspace,
                         int64_t workspace_bytes, uint32_t *dev_flags, void *stream);

@@ -46,6 +46,7 @@ struct KvAttendParams {
     int32_t n_kv_heads, group;    // query heads per kv head
     int32_t blocks_per_head;      // blocks of 8 * NT query heads a kv head's group is cut into
     FastDiv by_blocks, by_units;  // division by that, and by n_kv_heads * blocks_per_head
+    FastDiv by_warps;             // and by the grid's warps
     const char *q;
     int64_t q_stride_seq, q_stride_head;
     float scale, cap;             // softmax scale; cap <= 0: none
@@ -135,61 +136,58 @@ __global__ void __launch_bounds__(Shape<D, NT>::kWarps * 32, 1) kv_attend_kernel
     grid_dependency_wait();
     grid_launch_dependents();   // the joining kernel may take its places now; it waits for this grid's end
 
-    // ---- the stretch of this warp
+    // ---- the stretch of this warp.  The block adds up the sequences' tiles, in the memory of the first pieces.
     const int units = p.n_kv_heads * p.blocks_per_head;   // per sequence
-    const int seg = (p.n_seqs + 31) / 32;                 // sequences a lane adds up
-    long long mine = 0;
-#pragma unroll 4
-    for (int b = lane * seg; b < min(p.n_seqs, (lane + 1) * seg); ++b) mine += tiles_of(p, b);
-    mine *= units;
-    long long upto = mine;
+    uint32_t *tiles_before = reinterpret_cast<uint32_t *>(smem + kWarps * S::kRing);
+    uint32_t *warp_tiles = reinterpret_cast<uint32_t *>(piece_ml);
+    static_assert(kWarps * S::kPiece >= STOM_KV_MAX_SEQS * 4, "a number for each sequence");
+    uint32_t all_tiles;
+    {
+        const int seg = (p.n_seqs + kWarps * 32 - 1) / (kWarps * 32);   // sequences a thread adds up
+        const int b0 = threadIdx.x * seg, b1 = min(p.n_seqs, b0 + seg);
+        uint32_t mine = 0;
+        for (int b = b0; b < b1; ++b) {
+            tiles_before[b] = mine;
+            mine += tiles_of(p, b);
+        }
+        uint32_t upto = mine;
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const long long v = __shfl_up_sync(~0u, upto, o);
-        if (lane >= o) upto += v;
+        for (int o = 1; o < 32; o <<= 1) {
+            const uint32_t v = __shfl_up_sync(~0u, upto, o);
+            if (lane >= o) upto += v;
+        }
+        if (lane == 31) warp_tiles[warp] = upto;
+        __syncthreads();
+        const uint32_t of = lane < kWarps ? warp_tiles[lane] : 0u;
+        all_tiles = __reduce_add_sync(~0u, of);
+        const uint32_t before = __reduce_add_sync(~0u, lane < warp ? of : 0u) + upto - mine;
+        for (int b = b0; b < b1; ++b) tiles_before[b] += before;
+        __syncthreads();
     }
-    const long long total = __shfl_sync(~0u, upto, 31);
-    const long long warps = (long long)gridDim.x * kWarps;
-    const long long per = total >> 31 ? (total + warps - 1) / warps : max(1u, ((uint32_t)total + (uint32_t)warps - 1) / (uint32_t)warps);
-    const long long f0 = min(total, ((long long)blockIdx.x * kWarps + warp) * per), f1 = min(total, f0 + per);
-    int left = (int)(f1 - f0);
+    const uint32_t total = all_tiles * units, per = max(1u, div_by(p.by_warps, total + p.by_warps.d - 1));
+    const uint32_t f0 = min(total, (blockIdx.x * kWarps + warp) * per);
+    int left = (int)(min(total, f0 + per) - f0);
+    // its first tile's sequence: the last that begins at f0 or before (of several, the others are empty)
+    Cursor cur = {};
+    if (left > 0) {
+        int low = 0, high = p.n_seqs;                     // low begins there or before, high does not
+        while (high - low > 1) {
+            const int step = (high - low + 31) / 32, at = low + step * lane;
+            const uint32_t yes = __ballot_sync(~0u, at < high && tiles_before[at] * units <= f0);
+            low += step * (31 - __clz(yes));              // lane 0 stands at low
+            high = min(high, low + step);
+        }
+        cur.b = low;
+        span_of(p, cur.b, cur.first, cur.end);
+        cur.tiles = (cur.end - cur.first + kTile - 1) / kTile;
+        const uint32_t in = f0 - tiles_before[low] * units;
+        cur.hu = (int)(in / (uint32_t)cur.tiles);
+        cur.tile = (int)in - cur.hu * cur.tiles;
+    }
+    __syncthreads();   // the numbers have been read: pieces may take their place
 
     int pieces = 0;   // partial results this warp leaves in shared memory
     if (left > 0) {
-        // the sequence, head block and tile of f0
-        Cursor cur;
-        {
-            const uint32_t past = __ballot_sync(~0u, upto > f0);
-            const int at = __ffs(past) - 1;                       // the lane whose sequences hold it
-            long long before = __shfl_sync(~0u, upto - mine, at);
-            int b = at * seg;
-            cur.b = b;
-            const int end = min(p.n_seqs, b + seg);
-            for (; seg > 1; b += 32) {                                    // 32 of them at a time
-                const int t = b + lane < end ? tiles_of(p, b + lane) : 0;
-                long long sum = (long long)t * units;
-                const long long own = sum;
-#pragma unroll
-                for (int o = 1; o < 32; o <<= 1) {
-                    const long long v = __shfl_up_sync(~0u, sum, o);
-                    if (lane >= o) sum += v;
-                }
-                const uint32_t hit = __ballot_sync(~0u, before + sum > f0);
-                if (hit || b + 32 >= end) {
-                    const int j = hit ? __ffs(hit) - 1 : 0;
-                    before += __shfl_sync(~0u, sum - own, j);
-                    cur.b = b + j;
-                    break;
-                }
-                before += __shfl_sync(~0u, sum, 31);
-            }
-            span_of(p, cur.b, cur.first, cur.end);
-            cur.tiles = (cur.end - cur.first + kTile - 1) / kTile;
-            const long long in = f0 - before;
-            cur.hu = in >> 31 ? (int)(in / cur.tiles) : (int)((uint32_t)in / (uint32_t)cur.tiles);
-            cur.tile = (int)(in - (long long)cur.hu * cur.tiles);
-        }
-
         // ---- loads.  Lane r (and r + 16) looks up the page of row r two tiles ahead of the copies.
         Cursor ld = cur;
         int to_look = left;          // tiles not looked up yet
@@ -658,8 +656,9 @@ int heads_per_unit(int group, int head_dim) { return group > 8 && head_dim <= 12
 int64_t round16(int64_t x) { return (x + 15) & ~(int64_t)15; }
 
 template <typename T, int D, int NT>
-int32_t launch(const KvAttendParams &p, int sms, cudaStream_t stream) {
+int32_t launch(KvAttendParams &p, int sms, cudaStream_t stream) {
     using S = Shape<D, NT>;
+    p.by_warps = fast_div((uint32_t)(sms * S::kWarps));
     static std::atomic<uint64_t> allowed{0};
     cudaError_t e = allow_shared(reinterpret_cast<const void *>(kv_attend_kernel<T, D, NT>), S::kSmem, allowed);
     if (e == cudaSuccess)
@@ -675,7 +674,7 @@ int32_t launch(const KvAttendParams &p, int sms, cudaStream_t stream) {
 }
 
 template <typename T>
-int32_t dispatch(const KvAttendParams &p, int head_dim, int sms, cudaStream_t stream) {
+int32_t dispatch(KvAttendParams &p, int head_dim, int sms, cudaStream_t stream) {
     const bool two = heads_per_unit(p.group, head_dim) == 16;
     if (head_dim == 64) return two ? launch<T, 64, 2>(p, sms, stream) : launch<T, 64, 1>(p, sms, stream);
     if (head_dim == 128) return two ? launch<T, 128, 2>(p, sms, stream) : launch<T, 128, 1>(p, sms, stream);
@@ -709,6 +708,7 @@ extern "C" int32_t stom_kv_attend(const stom_kv_pool *pool, const stom_kv_seqs *
     if (!(softcap >= 0.f) || !(softcap <= 3.0e38f) || !(softmax_scale >= -3.0e38f && softmax_scale <= 3.0e38f))
         return STOM_ERR_INVALID_ARG;
     if (n_q_heads % pool->n_kv_heads || n_q_heads / pool->n_kv_heads > 64) return STOM_ERR_SHAPE;
+    if (seqs->n_seqs > STOM_KV_MAX_SEQS) return STOM_ERR_SHAPE;
     if (seqs->n_seqs == 0) return STOM_OK;
     if (!q || !out) return STOM_ERR_INVALID_ARG;
     if (!aligned16(q) || !aligned16(out) || !stride_ok(q_stride_seq, pool->dtype) || !stride_ok(q_stride_head, pool->dtype) ||
@@ -721,7 +721,9 @@ extern "C" int32_t stom_kv_attend(const stom_kv_pool *pool, const stom_kv_seqs *
     if (!workspace || !aligned16(workspace) || workspace_bytes < need) return STOM_ERR_WORKSPACE;
     const int per = heads_per_unit(group, d);
     const int64_t units = (int64_t)pool->n_kv_heads * ((group + per - 1) / per);
-    if (units * seqs->n_seqs > INT32_MAX) return STOM_ERR_SHAPE;
+    // the line of tiles is counted in 32 bits (with the grid's warps and a tile of each row to spare)
+    const int64_t most = (int64_t)seqs->max_pages * pool->page_tokens;
+    if (most > INT32_MAX - 32 || (most / kTile + 1) * seqs->n_seqs * units > INT32_MAX - 16 * kMaxBlocks) return STOM_ERR_SHAPE;
     int sms = sm_count();
     if (!sms) return STOM_ERR_CUDA;
     if (sms > kMaxBlocks) sms = kMaxBlocks;
@@ -737,8 +739,7 @@ extern "C" int32_t stom_kv_attend(const stom_kv_pool *pool, const stom_kv_seqs *
     p.table_stride = seqs->table_stride;
     p.n_seqs = seqs->n_seqs;
     p.n_pages = pool->n_pages;
-    const int64_t most = (int64_t)seqs->max_pages * pool->page_tokens;
-    p.max_tokens = (int32_t)(most < 0x7fffffe0 ? most : 0x7fffffe0);
+    p.max_tokens = (int32_t)most;
     p.page = fast_div((uint32_t)pool->page_tokens);
     p.n_kv_heads = pool->n_kv_heads;
     p.group = group;

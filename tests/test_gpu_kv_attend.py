@@ -79,6 +79,8 @@ def _case(lens, hq, hk, d, page, dtype, cap=0.0, window=0, order="token", layers
     ([64], 64, 1, 64, 8, BF),                          # the largest group
     ([5, 9, 2, 0, 31] * 60, 4, 2, 64, 4, BF),          # 300 short rows
     ([1] * 700 + [40] * 35, 2, 1, 64, 16, HF),
+    ([0] * 40 + [3] + [0] * 2000 + [700] + [0] * 50, 2, 1, 64, 16, HF),   # long runs of empty rows
+    (([0] * 3 + [1]) * 2048, 1, 1, 64, 2, BF),         # as many rows as it takes
 ])
 def test_matches_plain_attention(lens, hq, hk, d, page, dtype):
     _case(lens, hq, hk, d, page, dtype)

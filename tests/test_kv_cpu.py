@@ -72,6 +72,12 @@ def test_attend_refuses(oqm, kw, code):
     assert attend(oqm, **kw) == code
 
 
+def test_attend_refuses_more_sequences_or_longer_rows_than_it_counts(oqm):
+    assert attend(oqm, seqs=seqs_of(oqm, n_seqs=8193)) == -2
+    assert attend(oqm, seqs=seqs_of(oqm, n_seqs=8192, max_pages=1 << 24, table_stride=1 << 24)) == -2
+    assert attend(oqm, seqs=seqs_of(oqm, n_seqs=1, max_pages=1 << 30, table_stride=1 << 30)) == -2
+
+
 def test_attend_of_no_sequence_is_nothing(oqm):
     assert attend(oqm, seqs=seqs_of(oqm, n_seqs=0)) == 0
     assert attend(oqm, seqs=seqs_of(oqm, refs=None, n_seqs=0)) == 0            # counts are not needed here
