@@ -123,11 +123,14 @@ __global__ void __launch_bounds__(128) kv_fork_kernel(const __grid_constant__ Pa
     if (threadIdx.x == 0) p.len[i] = max(n, 0);
 }
 
-// One block.  Shared memory: share[n_seqs] (the partly filled page a growing row holds, or -1) and need[n_seqs] (new
-// pages, with bit 31 for a copy), which later holds the row's first place in the list of free pages.
+// One block.  Shared memory, a word per row each: the partly filled page that a growing row holds together with others,
+// or -1; how many hold it; and the row's first place in the list of free pages, with two bits on top.
+constexpr uint32_t kStays = 0x80000000u, kCopies = 0x40000000u, kPlace = 0x3fffffffu;
+
 __global__ void __launch_bounds__(kPlanThreads) kv_reserve_plan_kernel(const __grid_constant__ PagesParams p) {
     extern __shared__ int32_t plan_smem[];
-    int32_t *share = plan_smem, *need = plan_smem + p.n_seqs;
+    int32_t *share = plan_smem, *holders = share + p.n_seqs;
+    uint32_t *need = reinterpret_cast<uint32_t *>(holders + p.n_seqs);   // first pages, then places
     __shared__ int n_moves;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int64_t room = (int64_t)p.max_pages * p.page_tokens;
@@ -141,28 +144,26 @@ __global__ void __launch_bounds__(kPlanThreads) kv_reserve_plan_kernel(const __g
             raise(p, STOM_FLAG_BAD_INDEX);
             want = 0;
         }
-        int page = -1, pages = 0;
+        int page = -1, with = 0;
+        uint32_t pages = kStays;
         if (want > n) {
             const int held = held_of(p, n);
             pages = held_of(p, want) - held;
             if (n - (int)(div_by(p.by_page, (uint32_t)n) * p.by_page.d)) {
                 page = p.table[i * p.table_stride + held - 1];
-                if (!is_page(p, page)) {
-                    raise(p, STOM_FLAG_BAD_INDEX);
-                    page = -1;
-                }
+                if (is_page(p, page)) with = p.refs[page];
+                else raise(p, STOM_FLAG_BAD_INDEX);
             }
         }
-        share[i] = page;
-        need[i] = want > n ? pages : -1;    // -1: stays
+        share[i] = with > 1 ? page : -1;
+        holders[i] = with;
+        need[i] = pages;
     }
     __syncthreads();
     // who copies: all but the last of the growing rows that share a page, and that one too if a row stays behind
     for (int i = warp; i < p.n_seqs; i += kPlanThreads / 32) {
         const int page = share[i];
         if (page < 0) continue;
-        const int holders = p.refs[page];
-        if (holders <= 1) continue;
         int same = 0, later = 0;
         for (int j = lane; j < p.n_seqs; j += 32)
             if (share[j] == page) {
@@ -171,19 +172,18 @@ __global__ void __launch_bounds__(kPlanThreads) kv_reserve_plan_kernel(const __g
             }
         same = __reduce_add_sync(~0u, same);
         later = __any_sync(~0u, later);
-        if ((later || holders > same) && lane == 0) need[i] |= 0x40000000;
+        if ((later || holders[i] > same) && lane == 0) need[i] |= kCopies;
     }
     __syncthreads();
     // places in the list of free pages, row after row
     long long wanted = 0;
     for (int base = 0; base < p.n_seqs; base += kPlanThreads) {
         const int i = base + tid;
-        const int raw = i < p.n_seqs ? need[i] : -1;
-        const long long mine = raw < 0 ? 0 : (raw & 0x3fffffff) + (raw >> 30);
+        const uint32_t raw = i < p.n_seqs ? need[i] : kStays;
+        const long long mine = raw & kStays ? 0 : (raw & kPlace) + (raw & kCopies ? 1 : 0);
         long long sum;
         const long long before = block_sum_before(mine, sum);
-        // the row's page count can be worked out again from len and want, so its place takes its slot
-        if (i < p.n_seqs && raw >= 0) need[i] = (int)((wanted + before) & 0x3fffffff) | (raw & 0x40000000);
+        if (i < p.n_seqs) need[i] = (uint32_t)((wanted + before) & kPlace) | (raw & (kStays | kCopies));
         wanted += sum;
     }
     const int total = (int)min(wanted, (long long)INT32_MAX);
@@ -223,28 +223,27 @@ __global__ void __launch_bounds__(kPlanThreads) kv_reserve_plan_kernel(const __g
         }
         return;
     }
-    for (int i = warp; i < p.n_seqs; i += kPlanThreads / 32) {
-        const int raw = need[i];
-        if (raw < 0) continue;
-        const int place = raw & 0x3fffffff, copy = raw >> 30;
-        const int n = max(p.len[i], 0), want = p.wish[i];
-        const int held = held_of(p, n), begin = held - copy, count = held_of(p, want) - begin;
-        int32_t *row = p.table + i * p.table_stride;
-        for (int j = lane; j < count; j += 32) {
-            const int id = p.ids[place + j];
-            row[begin + j] = id;
-            p.refs[id] = 1;
+    // a thread for each page of the list: its row is the last whose first place is not behind it
+    for (int at = tid; at < total; at += kPlanThreads) {
+        int i = 0, high = p.n_seqs;
+        while (high - i > 1) {
+            const int mid = (i + high) >> 1;
+            if ((need[mid] & kPlace) <= (uint32_t)at) i = mid;
+            else high = mid;
         }
-        if (lane == 0) {
-            if (copy) {
-                atomicSub(p.refs + share[i], 1);
-                p.moves[atomicAdd(&n_moves, 1)] =
-                    Move{share[i], p.ids[place], n - (int)(div_by(p.by_page, (uint32_t)n) * p.by_page.d), 0};
-            }
-            p.len[i] = want;
+        const int copy = need[i] & kCopies ? 1 : 0, k = at - (int)(need[i] & kPlace), id = p.ids[at];
+        const int n = max(p.len[i], 0);
+        p.table[i * p.table_stride + held_of(p, n) - copy + k] = id;
+        p.refs[id] = 1;
+        if (copy && k == 0) {
+            atomicSub(p.refs + share[i], 1);
+            p.moves[atomicAdd(&n_moves, 1)] =
+                Move{share[i], id, n - (int)(div_by(p.by_page, (uint32_t)n) * p.by_page.d), 0};
         }
     }
     __syncthreads();
+    for (int i = tid; i < p.n_seqs; i += kPlanThreads)
+        if (!(need[i] & kStays)) p.len[i] = p.wish[i];
     if (tid == 0) p.head[0] = n_moves;
 }
 
@@ -422,10 +421,10 @@ extern "C" int32_t stom_kv_reserve(const stom_kv_pool *pool, const stom_kv_seqs 
     const int sms = sm_count();
     if (!sms) return STOM_ERR_CUDA;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    const size_t smem = (size_t)seqs->n_seqs * 8;
+    const size_t smem = (size_t)seqs->n_seqs * 12;
     cudaError_t e = cudaSuccess;
     static std::atomic<uint64_t> allowed{0};
-    if (smem > 47 * 1024) e = allow_shared(reinterpret_cast<const void *>(kv_reserve_plan_kernel), STOM_KV_MAX_SEQS * 8, allowed);
+    if (smem > 47 * 1024) e = allow_shared(reinterpret_cast<const void *>(kv_reserve_plan_kernel), STOM_KV_MAX_SEQS * 12, allowed);
     if (e == cudaSuccess) e = launch_after_producer(kv_reserve_plan_kernel, dim3(1), dim3(kPlanThreads), smem, s, p);
     if (e == cudaSuccess) e = launch_after_producer(kv_move_kernel<false>, dim3(sms * 8), dim3(256), 0, s, p);
     return e == cudaSuccess ? finish_launch() : failed(e);
