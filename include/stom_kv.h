@@ -14,7 +14,8 @@
  * Conventions are those of stom_oqm.h: device pointers unless marked "host",
  * structs read on the host, strides in elements with the channel axis
  * contiguous, caller-owned memory, work enqueued on `stream` without
- * synchronising, argument errors found before a launch, and bits set in the
+ * synchronising, argument errors found before a launch (a call of no token or
+ * no sequence does nothing, and its arrays may be NULL), and bits set in the
  * optional `dev_flags` word for what only the device can see.  Every buffer
  * lies on the device that is current at the call.  A workspace may be used by
  * one call at a time (calls on one stream, graphs replayed one after another);

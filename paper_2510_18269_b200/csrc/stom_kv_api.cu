@@ -25,7 +25,7 @@ int32_t check_pool(const stom_kv_pool *p) {
 
 int32_t check_seqs(const stom_kv_pool *, const stom_kv_seqs *s, bool need_refs) {
     if (!s || s->n_seqs < 0 || s->max_pages < 1 || s->table_stride < s->max_pages) return STOM_ERR_INVALID_ARG;
-    if (!s->table || !s->len || (need_refs && !s->refs)) return STOM_ERR_INVALID_ARG;
+    if ((s->n_seqs > 0 && (!s->table || !s->len)) || (need_refs && !s->refs)) return STOM_ERR_INVALID_ARG;
     if ((reinterpret_cast<uintptr_t>(s->table) | reinterpret_cast<uintptr_t>(s->len) | reinterpret_cast<uintptr_t>(s->refs)) & 3u)
         return STOM_ERR_ALIGNMENT;
     return STOM_OK;

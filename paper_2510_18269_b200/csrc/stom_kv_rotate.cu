@@ -396,9 +396,9 @@ int32_t prepare(RotateParams &p, const stom_kv_rope *rope, int32_t dtype, int32_
     if (d != 64 && d != 128 && d != 256) return STOM_ERR_SHAPE;
     if (rope->rot_dim < 0 || rope->rot_dim > d || rope->rot_dim % 16) return STOM_ERR_SHAPE;
     if (!(eps >= 0.f) || !(eps < 3e38f) || !(rope->magnitude >= -3e38f && rope->magnitude <= 3e38f)) return STOM_ERR_INVALID_ARG;
-    if (!q && !k) return STOM_ERR_INVALID_ARG;
-    if ((q && (n_q < 1 || !q_out)) || (k && n_k < 1)) return STOM_ERR_INVALID_ARG;
-    if (rope->rot_dim && (!rope->freq || !pos)) return STOM_ERR_INVALID_ARG;
+    if (n > 0 && !q && !k) return STOM_ERR_INVALID_ARG;   // without a token no array needs to be there
+    if ((q && (n_q < 1 || (n > 0 && !q_out))) || (k && n_k < 1)) return STOM_ERR_INVALID_ARG;
+    if (rope->rot_dim && (!rope->freq || (n > 0 && !pos))) return STOM_ERR_INVALID_ARG;
     if ((reinterpret_cast<uintptr_t>(rope->freq) & 7u) || (reinterpret_cast<uintptr_t>(pos) & 3u)) return STOM_ERR_ALIGNMENT;
     if (!aligned16(q) || !aligned16(q_out) || !aligned16(k) || !aligned16(q_weight) || !aligned16(k_weight))
         return STOM_ERR_ALIGNMENT;
@@ -453,7 +453,7 @@ extern "C" int32_t stom_kv_rotate(const stom_kv_rope *rope, int32_t dtype, int32
                          k_weight, eps);
     if (rc) return rc;
     if (k) {
-        if (!k_out) return STOM_ERR_INVALID_ARG;
+        if (!k_out && n_tokens > 0) return STOM_ERR_INVALID_ARG;
         if (!aligned16(k_out) || !stride_ok(k_out_stride_token, dtype) || !stride_ok(k_out_stride_head, dtype)) return STOM_ERR_ALIGNMENT;
         if ((n_tokens > 1 && k_out_stride_token < head_dim) || (n_k_heads > 1 && k_out_stride_head < head_dim) ||
             k_out_stride_token < 0 || k_out_stride_head < 0)
@@ -477,7 +477,7 @@ extern "C" int32_t stom_kv_append(const stom_kv_pool *pool, const stom_kv_seqs *
     int32_t rc = check_pool(pool);
     if (!rc) rc = check_seqs(pool, seqs, false);
     if (rc) return rc;
-    if (layer < 0 || layer >= pool->n_layers || !k || !v) return STOM_ERR_INVALID_ARG;
+    if (layer < 0 || layer >= pool->n_layers || (n_tokens != 0 && (!k || !v))) return STOM_ERR_INVALID_ARG;
     RotateParams p;
     rc = prepare(p, rope, pool->dtype, pool->head_dim, n_tokens, pos, q, n_q_heads, q_stride_token, q_stride_head, q_out,
                  q_out_stride_token, q_out_stride_head, q_weight, k, pool->n_kv_heads, k_stride_token, k_stride_head,
@@ -488,7 +488,7 @@ extern "C" int32_t stom_kv_append(const stom_kv_pool *pool, const stom_kv_seqs *
         return STOM_ERR_ALIGNMENT;
     if (v_stride_token < 0 || v_stride_head < 0) return STOM_ERR_INVALID_ARG;
     if (n_tokens == 0) return STOM_OK;
-    if (!slot || (!seq && n_tokens > seqs->n_seqs)) return STOM_ERR_INVALID_ARG;
+    if (!slot || !seqs->table || (!seq && n_tokens > seqs->n_seqs)) return STOM_ERR_INVALID_ARG;
     char *at_k = static_cast<char *>(pool->k) + 2 * layer * pool->stride_layer;
     char *at_v = static_cast<char *>(pool->v) + 2 * layer * pool->stride_layer;
     p.set[1].dst = at_k;

@@ -165,3 +165,38 @@ def test_captured_decode_step(orc):
         if seed < 4 or seed > G:
             s.check()
     assert s.len.tolist()[:2] == [TOPK * G + G + 3] * 2
+
+
+def test_an_empty_batch_changes_nothing():
+    """No token, no sequence, no row: every call returns, and only the pool's counts are looked at."""
+    from paper_2510_18269_b200 import oqm
+    oqm.lib()
+
+    def i32(*shape):
+        return torch.zeros(*shape, dtype=torch.int32, device="cuda")
+
+    k = torch.randn(1, 6, 16, 2, 64, device="cuda").to(torch.bfloat16)
+    pool = oqm.KvPool(k, k.clone())
+    before = pool.k.clone(), pool.v.clone()
+    refs = i32(6)
+    seqs = oqm.KvSeqs(i32(0, 4), i32(0), refs)
+    flags = i32(1)
+    rope = oqm.Rope(oqm.stom_kv_frequencies(64).cuda())
+    q, kv = torch.empty(0, 8, 64, dtype=k.dtype, device="cuda"), torch.empty(0, 2, 64, dtype=k.dtype, device="cuda")
+    ws = torch.empty(max(oqm.stom_kv_attend_workspace_bytes(pool, seqs, 8), oqm.stom_kv_pages_workspace_bytes(pool, seqs)),
+                     dtype=torch.uint8, device="cuda")
+    oqm.stom_kv_reserve(pool, seqs, i32(0), ws, dev_flags=flags)
+    oqm.stom_kv_fork(pool, seqs, i32(0), dev_flags=flags)
+    oqm.stom_kv_rotate(rope, i32(0), q, q, kv, kv)
+    oqm.stom_kv_append(pool, seqs, 0, rope, i32(0), i32(0), kv, kv, q=q, q_out=q, dev_flags=flags)
+    oqm.stom_kv_attend(pool, seqs, 0, q, torch.empty_like(q), 0.125, ws, dev_flags=flags)
+    oqm.stom_sample_tokens(torch.empty(0, 99, device="cuda"), torch.empty(0, device="cuda"), i32(0), dev_flags=flags)
+    oqm.stom_kv_free(pool, seqs, i32(0), dev_flags=flags)
+    live = i32(1) + 7
+    refs[4] = 1                                                  # a page that no row of these holds
+    pool.k[:, 4] = pool.v[:, 4] = before[0][:, 0] = before[1][:, 0] = 1.0
+    oqm.stom_kv_compact(pool, seqs, i32(0, 4), refs, live, ws, dev_flags=flags)
+    assert live.item() == 1 and refs.tolist() == [1, 0, 0, 0, 0, 0] and flags.item() == 0
+    for got, want in ((pool.k, before[0]), (pool.v, before[1])):
+        want[:, 4] = 1.0                                         # what stood there stays
+        assert torch.equal(got, want)

@@ -160,6 +160,21 @@ def test_append_and_pages_refuse_bad_pools_and_sequences(oqm):
     assert append(oqm, n=0) == 0
 
 
+def test_calls_of_nothing_need_no_arrays(oqm):
+    """Tensors without an element have no address."""
+    none = seqs_of(oqm, table=None, len=None, n_seqs=0)
+    assert attend(oqm, seqs=none, q=None, out=None) == 0
+    assert oqm.lib().stom_kv_attend_workspace_bytes(C.byref(pool_of(oqm)), C.byref(none), 28) > 0
+    assert rotate(oqm, n=0, pos=None, q=None, qo=None, k=None, ko=None) == 0
+    assert rotate(oqm, n=0, pos=None, qo=None, ko=None) == 0
+    assert append(oqm, n=0, pos=None, slot=None, q=None, qo=None, k=None, v=None) == 0
+    assert append(oqm, seqs=none, n=0, pos=None, slot=None, k=None, v=None) == 0
+    assert reserve(oqm, seqs=none, want=None) == 0 and fork(oqm, seqs=none, wish=None) == 0 and free(oqm, seqs=none, wish=None) == 0
+    # tokens without a sequence to go to, and pages without their counts
+    assert append(oqm, seqs=none) == -1 and append(oqm, seqs=none, seq=P) == -1
+    assert compact(oqm, seqs=none, r=None) == -1 and compact(oqm, t=None) == -1
+
+
 def _pages(oqm, name, pool, seqs, *args):
     return getattr(oqm.lib(), name)(C.byref(pool or pool_of(oqm)), C.byref(seqs or seqs_of(oqm)), *args)
 
