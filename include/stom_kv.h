@@ -136,7 +136,9 @@ int32_t stom_kv_append(const stom_kv_pool *pool, const stom_kv_seqs *seqs, int32
  * [0, n_pages) counts as absent and sets STOM_FLAG_BAD_INDEX; so does what
  * len[i] has beyond max_pages*page_tokens.  What a page holds behind len[i] is
  * not read.  Products of 16-bit operands are summed in binary32; the softmax
- * weights enter the second product as a high and a low 16-bit part.
+ * weights enter the second product as a high and a low 16-bit part: off by
+ * 2^-16 of themselves (bf16), or by 2^-22 of themselves or 2^-40 of the largest
+ * weight of their 16 tokens, whichever is more (fp16).
  * q, out (pool->dtype): element (i, h, c) at i*stride_seq + h*stride_head + c.
  * lse: binary32 [n_seqs][n_q_heads], or NULL.
  * n_q_heads / n_kv_heads <= 64, n_seqs <= STOM_KV_MAX_SEQS, max_pages *

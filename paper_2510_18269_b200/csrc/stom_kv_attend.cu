@@ -19,8 +19,12 @@
 // the 16 tokens, respectively 16 channels, its rows: S^T = K q^T with K as stored, O^T = V^T P^T with V transposed on
 // the way out of shared memory (ldmatrix.trans).  Scores and accumulators then have their head in the same thread, so
 // that rescaling needs no exchange.  The softmax weights go into the second product as a high and a low 16-bit part
-// (2^-17 relative at bf16): one part alone would add an error of the size of the output's own rounding, and the
-// second costs nothing in a kernel that waits for memory.
+// (2^-16 relative at bf16): one part alone would add an error of the size of the output's own rounding, and the
+// second costs nothing in a kernel that waits for memory.  fp16 has no numbers below 2^-24, so that weights relative to
+// the running maximum would vanish where thousands of tokens count only in sum, beside one that stands 15 nats above
+// them; there a tile's weights are relative to its own largest score, which gets 2^15, and its product has accumulators
+// of its own that are scaled into the running ones: a weight is off by 2^-22 of itself or 2^-40 of its tile's largest,
+// whichever is more.  bf16 has the exponents of binary32 and needs none of it.
 //
 // Measured (B200, copy rate 6 458 GB/s): 64 sequences of 17 to 16 411 tokens, 64 + 8 heads of 128, pages of 16: 230 us for
 // 1.47 GB, 6.4 TB/s.  One sequence of 12 583 tokens, 28 + 4 heads, pages of 50: 12.0 us, of which 4 are its 26 MB at the
@@ -28,11 +32,14 @@
 // join, 3 the second kernel.  233 sequences of 0 to 300 tokens, 16 + 2 heads of 64: 14.0 us, all of it such latencies.
 #include "stom_kv.cuh"
 
+#include <type_traits>
+
 namespace stom {
 
 namespace {
 
 constexpr int kTile = 16;         // tokens per tile
+constexpr float kLift = 15.f;     // fp16: the largest weight of a tile is 2^kLift
 constexpr int kMaxBlocks = 256;   // blocks of the grid the workspace has room for
 
 struct KvAttendParams {
@@ -122,6 +129,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::kWarps * 32, 1) kv_attend_kernel
     using S = Shape<D, NT>;
     constexpr int kWarps = S::kWarps, kHeads = S::kHeads, kStages = S::kStages;
     constexpr int kKs = D / 16;                      // steps of the first product, row blocks of the second
+    constexpr bool kOwnScale = std::is_same<T, __half>::value;   // weights relative to the tile's largest score
     constexpr int kChunks = D / 8;                   // 16-byte chunks of a row
     constexpr int kRowsPerCopy = 32 / kChunks;       // rows one warp-wide copy covers
     extern __shared__ __align__(16) uint8_t smem[];
@@ -305,7 +313,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::kWarps * 32, 1) kv_attend_kernel
                 }
             }
             const bool in0 = (rows >> (lane >> 2)) & 1u, in1 = (rows >> ((lane >> 2) + 8)) & 1u;
-            float alpha[NT][2];
+            float alpha[NT][2], beta[NT][2];   // factors of what has been added up, and (fp16) of this tile
             uint32_t ph[NT][2], pl[NT][2];
             bool moved = false;
 #pragma unroll
@@ -331,9 +339,18 @@ __global__ void __launch_bounds__(Shape<D, NT>::kWarps * 32, 1) kv_attend_kernel
                     moved |= m > m_run[n][c];
                     alpha[n][c] = exp2f(m_run[n][c] - base);
                     m_run[n][c] = m;
-                    w[c] = exp2f(x[c] - base);
-                    w[c + 2] = exp2f(x[c + 2] - base);
-                    l_run[n][c] = l_run[n][c] * alpha[n][c] + w[c] + w[c + 2];
+                    if constexpr (kOwnScale) {
+                        const bool none = top[c] == -INFINITY;
+                        const float one = none ? 0.f : top[c] - kLift;   // score of the weight 1
+                        beta[n][c] = none ? 0.f : exp2f(one - base);
+                        w[c] = exp2f(x[c] - one);
+                        w[c + 2] = exp2f(x[c + 2] - one);
+                        l_run[n][c] = l_run[n][c] * alpha[n][c] + (w[c] + w[c + 2]) * beta[n][c];
+                    } else {
+                        w[c] = exp2f(x[c] - base);
+                        w[c + 2] = exp2f(x[c + 2] - base);
+                        l_run[n][c] = l_run[n][c] * alpha[n][c] + w[c] + w[c + 2];
+                    }
                 }
 #pragma unroll
                 for (int r = 0; r < 2; ++r) {
@@ -361,8 +378,16 @@ __global__ void __launch_bounds__(Shape<D, NT>::kWarps * 32, 1) kv_attend_kernel
                     ldsm4_trans(a, vt + row * S::kRow + (((2 * ks + ((lane >> 3) & 1)) ^ (row & 7)) << 4));
 #pragma unroll
                     for (int n = 0; n < NT; ++n) {
-                        mma16x8x16<T>(o_acc[ks][n], a, ph[n][0], ph[n][1]);
-                        mma16x8x16<T>(o_acc[ks][n], a, pl[n][0], pl[n][1]);
+                        if constexpr (kOwnScale) {
+                            float t[4] = {0.f, 0.f, 0.f, 0.f};
+                            mma16x8x16<T>(t, a, ph[n][0], ph[n][1]);
+                            mma16x8x16<T>(t, a, pl[n][0], pl[n][1]);
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) o_acc[ks][n][e] = fmaf(t[e], beta[n][e & 1], o_acc[ks][n][e]);
+                        } else {
+                            mma16x8x16<T>(o_acc[ks][n], a, ph[n][0], ph[n][1]);
+                            mma16x8x16<T>(o_acc[ks][n], a, pl[n][0], pl[n][1]);
+                        }
                     }
                 }
             }

@@ -234,3 +234,51 @@ def test_on_another_stream():
     want, _, mag = K.attend_rows(s["k"], s["v"], s["table_host"], [400, 90], q, 0.125)
     for o, _ in outs:
         _close(o, want, mag, BF)
+
+
+def _sink_row(lens, gap, hq, hk, d, page, dtype, at=0, seed=0):
+    """One token of every row stands `gap` nats above all others, whose scores are zero, and has a value of zero; all other
+    values are positive.  The result is the tail's alone, however little a token of it weighs."""
+    oqm = _lib()
+    s = K.paged(np.random.default_rng(seed), lens, page, 1, hk, d, dtype, seed=seed)
+    s["k"].zero_()
+    s["v"].copy_(s["v"].abs() + 0.25)
+    for i, n in enumerate(lens):
+        if n:
+            t = min(at, n - 1)
+            s["k"][0, s["table_host"][i, t // page], t % page, :, 0] = gap
+            s["v"][0, s["table_host"][i, t // page], t % page] = 0
+    q = torch.zeros(len(lens), hq, d, dtype=dtype, device="cuda")
+    q[:, :, 0] = 4.0                                     # 4 * gap * 0.25: the score is exact
+    pool, seqs = oqm.KvPool(s["k"], s["v"]), oqm.KvSeqs(s["table"], s["len"])
+    ws = torch.full((oqm.stom_kv_attend_workspace_bytes(pool, seqs, hq),), 255, dtype=torch.uint8, device="cuda")
+    out, lse = torch.full_like(q, 7.0), torch.full((len(lens), hq), 7.0, device="cuda")
+    oqm.stom_kv_attend(pool, seqs, 0, q, out, 0.25, ws, lse=lse)
+    want, wlse, mag = K.attend_rows(s["k"], s["v"], s["table_host"], lens, q, 0.25)
+    _close(out, want, mag, dtype)
+    some = np.isfinite(wlse)
+    assert (np.abs(lse.double().cpu().numpy() - wlse)[some] <= 2.0 ** -15 + 2.0 ** -22 * np.abs(wlse[some])).all()
+
+
+@pytest.mark.parametrize("gap", [10.0, 13.0, 15.0, 15.5, 17.0, 17.5])
+@pytest.mark.parametrize("lens,hq,hk,d,page", [
+    ([48, 33, 0, 90] * 700, 1, 1, 64, 16),               # units that a warp holds whole
+    ([600] * 300, 2, 1, 64, 50),                         # units of several warps of a block
+    ([12583], 2, 1, 128, 50),                            # one unit over all blocks
+    ([5000, 40], 12, 1, 128, 7),                         # 16 heads a product
+    ([3000, 17], 1, 1, 256, 16),
+])
+def test_a_tail_that_counts_only_in_sum(lens, hq, hk, d, page, gap):
+    """fp16: a tail's weights are far below the type's smallest steps relative to the row's largest.  _close's limit has
+    room: a weight's two parts are off by 2^-22 of themselves or by 2^-40 of the largest weight of their 16 tokens,
+    whichever is more, and in the sum over the 15 tokens beside the sink that is below 2^-36, against the limit's 2^-24."""
+    _sink_row(lens, gap, hq, hk, d, page, HF, at=3)
+
+
+@pytest.mark.parametrize("n,gap", [(131072, 20.0), (131072, 24.0), (400009, 22.5)])
+def test_a_long_tail_that_counts_only_in_sum(n, gap):
+    _sink_row([n], gap, 1, 1, 64, 64, HF, at=n // 2)
+
+
+def test_a_tail_in_bf16():
+    _sink_row([12583, 600, 40], 17.0, 2, 1, 128, 50, BF, at=3)
