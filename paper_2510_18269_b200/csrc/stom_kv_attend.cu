@@ -85,9 +85,11 @@ struct Shape {
     static_assert(kSmem <= 227 * 1024, "shared memory");
 };
 
+// The tokens of a sequence that are looked at: the window ends at its length, also where that lies beyond its pages.
 __device__ __forceinline__ void span_of(const KvAttendParams &p, int b, int &first, int &end) {
-    end = min(max(p.len[b], 0), p.max_tokens);
-    first = p.window > 0 ? max(0, end - p.window) : 0;
+    const int len = max(p.len[b], 0);
+    end = min(len, p.max_tokens);
+    first = p.window > 0 ? min(end, max(0, len - p.window)) : 0;
 }
 __device__ __forceinline__ int tiles_of(const KvAttendParams &p, int b) {
     int first, end;
@@ -565,8 +567,9 @@ __global__ void __launch_bounds__(Shape<D, NT>::kWarps * 32, 1) kv_attend_kernel
         p.goes_on[blockIdx.x] = goes_on;
     }
 
-    // the empty sequences: zeros
+    // lengths beyond a row's pages are told; the empty sequences: zeros
     for (int b = blockIdx.x * kWarps + warp; b < p.n_seqs; b += gridDim.x * kWarps) {
+        if (p.flags && lane == 0 && p.len[b] > p.max_tokens) atomicOr(p.flags, STOM_FLAG_BAD_INDEX);
         if (tiles_of(p, b)) continue;
         const int heads = p.n_kv_heads * p.group;
         for (int h = 0; h < heads; ++h) {

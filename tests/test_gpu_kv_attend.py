@@ -282,3 +282,34 @@ def test_a_long_tail_that_counts_only_in_sum(n, gap):
 
 def test_a_tail_in_bf16():
     _sink_row([12583, 600, 40], 17.0, 2, 1, 128, 50, BF, at=3)
+
+
+@pytest.mark.parametrize("window", [0, 1, 20, 40, 64, 100, 5000])
+def test_lengths_beyond_the_pages_of_a_row(window):
+    """All pages are good: what a length has beyond them is absent, and flagged.  A window ends at the length, so it may
+    reach behind the pages in part or as a whole."""
+    oqm = _lib()
+    room, hq, hk, d = 64, 4, 2, 64
+    s = K.paged(np.random.default_rng(11), [room] * 5, 16, 1, hk, d, BF, seed=11)
+    lens = [100, 64, 70, 2 ** 31 - 1, 9]
+    q = torch.randn(5, hq, d, device="cuda").to(BF)
+    pool = oqm.KvPool(s["k"], s["v"])
+    for rows, flag in ((slice(0, 5), oqm.FLAG_BAD_INDEX), (slice(1, 2), 0), (slice(4, 5), 0), (slice(2, 3), oqm.FLAG_BAD_INDEX)):
+        n = torch.tensor(lens[rows], dtype=torch.int32, device="cuda")
+        seqs = oqm.KvSeqs(s["table"][rows], n)
+        ws = torch.empty(oqm.stom_kv_attend_workspace_bytes(pool, seqs, hq), dtype=torch.uint8, device="cuda")
+        flags = torch.zeros(1, dtype=torch.int32, device="cuda")
+        out, lse = torch.full_like(q[rows], 7.0), torch.full((len(n), hq), 7.0, device="cuda")
+        oqm.stom_kv_attend(pool, seqs, 0, q[rows], out, 0.125, ws, lse=lse, window=window, dev_flags=flags)
+        torch.cuda.synchronize()
+        assert flags.item() == flag
+        for j, length in enumerate(lens[rows]):
+            i = rows.start + j
+            end = min(length, room)
+            seen = end - (max(0, length - window) if window else 0)           # tokens of the window that are there
+            if seen <= 0:
+                assert (out[j] == 0).all() and (lse[j] == -math.inf).all()
+                continue
+            want, wlse, mag = K.attend_rows(s["k"], s["v"], s["table_host"][i:i + 1], [end], q[i:i + 1], 0.125, window=seen)
+            _close(out[j:j + 1], want, mag, BF)
+            assert (np.abs(lse[j].double().cpu().numpy() - wlse[0]) <= 2.0 ** -15 + 2.0 ** -22 * np.abs(wlse[0])).all()
