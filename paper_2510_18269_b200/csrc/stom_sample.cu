@@ -238,7 +238,7 @@ struct Row {
         if (key == K::kZero)
             for (uint32_t i = 0; i < blocks; ++i) c += count16(0x8000u, turn(i));
         bool is_nan = false;
-        if (K::of(b, is_nan) != key) {       // NaN, -inf, or -0
+        if (K::of(b, is_nan) != key || key == 0) {   // NaN (all bits set is the one whose place is key 0), -inf, or -0
             nan |= is_nan && c;
             c = 0;
         }

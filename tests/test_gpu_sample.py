@@ -212,3 +212,26 @@ def test_log_probability_of_a_token_that_is_nearly_certain(dtype, n):
         want = -math.log1p(rest)
         assert int(token[i]) == n // 2
         assert abs(float(lp[i]) - want) <= abs(want) * 2.0 ** -22 + n * 2.0 ** -51
+
+
+@pytest.mark.parametrize("dtype", [BF, HF, FL])
+def test_every_nan_pattern_is_seen_and_never_drawn(dtype):
+    """All bits set, as in a buffer that was filled with 0xff, among them; also at temperatures so high that the lowest
+    finite logit keeps its weight."""
+    oqm = _lib()
+    word, patterns = ((torch.int32, [-1, -15, 0x7fffffff, 0x7fc00000]) if dtype is FL else
+                      (torch.int16, [-1, -15, 0x7fff, 0x7fc0 if dtype is BF else 0x7e00]))
+    n, temps = 3000, [1.0, 0.3, 90.0, 1e4, 1e38, 2e38]
+    u = [0.2, 0.9, 0.5, 0.999, 0.7, 0.9999]
+    for p in patterns:
+        x = _logits(len(temps), n, dtype, seed=31)
+        x[:, 100] = torch.finfo(dtype).min
+        for where in (slice(7, 8), slice(0, 1500), slice(2000, 3000, 2)):
+            y = x.clone()
+            y.view(word)[:, where] = p
+            _check(y, u, temperature=temps, flags=oqm.FLAG_BAD_VALUE, ambiguous=0.4)
+            _check(y, u, temperature=temps, top_k=[0, 5, 2999, 2000, 0, 2999], top_p=[0.9, 1.0, 1.0, 0.999, 0.9, 1.0],
+                   flags=oqm.FLAG_BAD_VALUE, ambiguous=0.4)
+        y.view(word)[:] = p                              # nothing else
+        t, kept = _check(y, u, temperature=temps, flags=oqm.FLAG_BAD_VALUE)
+        assert (t == -1).all() and (kept == 0).all()
