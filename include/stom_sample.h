@@ -30,10 +30,10 @@ extern "C" {
  * never kept.  If the largest logit is +inf, the tokens at +inf share the mass.  A NaN logit
  * counts as -inf, a NaN setting as NULL; both set STOM_FLAG_BAD_VALUE.  A row
  * that has nothing to draw from gives token -1, kept 0 and logprob -inf.
- * Masses are sums of weights rounded to whole multiples of 2^-43 or less (by n;
- * 16-bit logits: of count times weight of each distinct value), exact and
- * without an order, and binary64 sums over the last few tokens: a token is off only where
- * u falls within 1e-10 of a border between two.
+ * Masses are exact sums, in no order, of the masses of up to 4 096 ranges of
+ * logits, each rounded once to a whole multiple of 2^-43 or less (by n), and
+ * binary64 sums over the last few tokens: a token is off only where u falls
+ * within 2^-34 (n <= 131 072; else 2^-32) of a border between two.
  * logits (dtype): element (r, j) at r*row_stride + j; any alignment of a
  *   whole element.  1 <= n <= STOM_SAMPLE_MAX_N.
  * token [rows] int32; kept [rows] int32, the number of tokens kept, or NULL;

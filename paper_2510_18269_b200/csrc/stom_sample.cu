@@ -18,8 +18,11 @@
 // With 100 000 tokens left to draw from, binary32 sums would move a border between two tokens by more than some tokens'
 // whole weight.  The masses of ranges are whole numbers of UNITS in 64 bits, 2^-43 (the longest rows) to 2^-51 of the
 // largest weight, the smallest that a row's sum has room for: their sums are
-// exact and never fall, so that exactly one range holds a place and all blocks of a cluster see the same one.  Within the
-// last few keys weights and sums are binary64.
+// exact and never fall, so that exactly one range holds a place and all blocks of a cluster see the same one.  A range is
+// rounded to a unit once, after it has been added up (16 bits: in binary64; binary32: in units that are smaller by the
+// range's own weight), so that the masses of a row are off by half a unit for each of 4 096 (2 048) ranges at most: 2^-34
+// of the largest weight up to 131 072 logits, 2^-32 for the longest rows.  Within the last few keys weights and sums are
+// binary64.
 //
 // What bounds it: not memory (128 rows of 151 001 bf16 logits are 6 us at the copy rate) but the chain of steps a row has
 // to go through, each a barrier, a look into another block's memory or a binary64 sum away from the next.  Measured: 128
@@ -47,6 +50,7 @@ struct SampleParams {
     int32_t n, slice;
     int32_t unit_bits, limb;     // a unit is 2^-unit_bits; bits of a limb (binary32)
     float per_nat;               // binary32: first ranges to a factor e of the weight
+    uint32_t log2_per_range;     // and the powers of two from one to the next, in 2^-16
     const float *temperature, *top_p, *min_p, *u;
     const int32_t *top_k;
     int32_t *token, *kept;
@@ -141,7 +145,7 @@ struct Place {           // the key of a place and what stands before that key
 };
 struct Cell {            // a range, and what stands before it
     uint32_t range, before, count;
-    uint64_t mass_before;
+    double mass_before;
 };
 
 struct Shared {
@@ -155,7 +159,7 @@ struct Shared {
     // 16 bits: ranges with logits of this block's slice; of this block's share, which of them every block has
     uint32_t occupied[kMostRanges / 32], held[kMostRanges / 32 + kMaxCluster];
     uint32_t ans_range[8], ans_before[8], ans_count[8];   // answers to queries, a slot each in turn
-    uint64_t ans_mass[8];
+    double ans_mass[8];
     uint32_t first, last;
     double power[64];                              // 2^(j/64)
     Place place;
@@ -183,6 +187,7 @@ struct Row {
     double top, t, per_log2, unit;   // per_log2: log2(e) / t
     int unit_bits, limb;
     float top_f, per_range;      // binary32: ranges per unit of x
+    uint32_t log2_per_range;     // powers of two from one range to the next, in 2^-16
     int tid;
     uint32_t slot = 0;
     // running sums of one level: before this thread's ranges, and with them
@@ -192,15 +197,16 @@ struct Row {
         uint32_t lowest;
     } sums[2];
     uint32_t low_key, high_key, shift;   // binary32: the keys that the second level covers, 2^shift to a range
+    int inner;                           // and its units: 2^-inner of the first level's
 
     // Zero below e^-700: close to where binary64 ends, the last steps of an exponential would decide what is kept.
     __device__ __forceinline__ double weight(double v) const {
         const double y = v == top ? 0.0 : (v - top) / t;
         return y < -700.0 ? 0.0 : exp(y);
     }
-    // The same in units (down to 2^-100), by 2^y = 2^(k/64) 2^r, |r| <= 1/128, the second factor by its Taylor polynomial
+    // The same in 2^-lift units (down to 2^-100), by 2^y = 2^(k/64) 2^r, |r| <= 1/128, the second factor by its Taylor polynomial
     // (the term left out is below 4e-17): without a branch, 11 binary64 operations in the place of a division and exp.
-    __device__ __forceinline__ double units(double v) const {
+    __device__ __forceinline__ double units(double v, int lift = 0) const {
         const double y = v == top ? 0.0 : fmax((v - top) * per_log2, -100.0);
         const double shifted = fma(y, 64.0, 6755399441055744.0);          // 1.5 * 2^52: rounds to a whole number
         const int k = __double2loint(shifted);
@@ -212,7 +218,7 @@ struct Row {
         e = fma(e, r, 6.931471805599453e-1);
         e = fma(e, r, 1.0) * sh.power[k & 63];
         // times 2^(k >> 6) / unit, by the exponent
-        return __hiloint2double(__double2hiint(e) + ((k >> 6) + unit_bits) * (1 << 20), __double2loint(e));
+        return __hiloint2double(__double2hiint(e) + ((k >> 6) + unit_bits + lift) * (1 << 20), __double2loint(e));
     }
 
     // Block r of the cluster as the i-th to look at.  Every block begins with itself: if all began with block 0, they
@@ -379,15 +385,16 @@ struct Row {
     }
 
     // The range that holds the place asked for, with what stands before it; agreed on by all blocks
-    __device__ __forceinline__ Cell find(int level, const Query &q, uint32_t base, uint64_t mass_base) {
+    __device__ __forceinline__ Cell find(int level, const Query &q, uint32_t base, double mass_base) {
         const Sums &s = sums[level];
+        const double step = level ? __hiloint2double((1023 - unit_bits - inner) << 20, 0) : unit;
         const int per = (share + kSummers - 1) / kSummers, first = tid * per, last = tid < kSummers ? min((int)mine, first + per) : 0;
         const uint32_t at = slot++ & 7u;
         auto reached = [&](uint32_t c, uint64_t m) {   // never true and then false along the order
             if (c == 0) return false;
             if (c == s.total) return true;
             if (q.kind == BY_RANK) return base + c > q.rank;
-            const double upto = (double)(mass_base + m) * unit;
+            const double upto = mass_base + (double)m * step;
             return q.kind == BY_MASS ? upto >= q.mass : upto > q.mass;
         };
         bool holds = false;
@@ -415,7 +422,7 @@ struct Row {
                 st_cluster_u(&sh.ans_range[at], r, rank * share + hit);
                 st_cluster_u(&sh.ans_before[at], r, base + hit_c);
                 st_cluster_u(&sh.ans_count[at], r, cnt[level][hit]);
-                st_cluster_u64(&sh.ans_mass[at], r, mass_base + hit_m);
+                st_cluster_u64(reinterpret_cast<uint64_t *>(&sh.ans_mass[at]), r, (uint64_t)__double_as_longlong(mass_base + (double)hit_m * step));
             }
         }
         cluster_sync();
@@ -432,13 +439,18 @@ struct Row {
         return v == top_f ? 0u : min((uint32_t)kRanges - 1, (uint32_t)f);
     }
 
+    // The weights of a range are at most 2^-(this), to 2^-15 by binary32's rounding of their place, and, but for the last
+    // range, little less: they are added up in units that much smaller, so that many light tokens are not each rounded
+    // to a unit of the sums.
+    __device__ __forceinline__ int lift_of(uint32_t range) const { return (int)(range * log2_per_range >> 16); }
+
     __device__ __forceinline__ Place ask(const Query &q) {
         if constexpr (!kHalf)
             if (all_ranked) {
                 pick(q);
                 return sh.place;
             }
-        Cell cell = find(0, q, 0, 0);
+        Cell cell = find(0, q, 0, 0.0);
         if constexpr (kHalf) {
             // 16 keys, a thread each; the first that reaches what is asked for, or (by key: always) the last
             if (tid < 32) {
@@ -457,7 +469,7 @@ struct Row {
                         m1 += vm;
                     }
                 }
-                const double mb = (double)cell.mass_before * unit, ahead = __shfl_up_sync(~0u, m1, 1);
+                const double mb = cell.mass_before, ahead = __shfl_up_sync(~0u, m1, 1);
                 const bool in = c && (q.kind != BY_KEY || key >= q.key);
                 const bool reached = in && (q.kind == BY_RANK ? cell.before + c1 > q.rank
                                             : q.kind == BY_MASS ? mb + m1 >= q.mass : q.kind == PAST_MASS && mb + m1 > q.mass);
@@ -472,6 +484,7 @@ struct Row {
             // the keys of the range: from the lowest whose range is not beyond it to below the lowest of the one ahead
             low_key = lowest_within(cell.range);
             high_key = cell.range ? lowest_within(cell.range - 1) - 1 : best;
+            inner = lift_of(cell.range);
             while (cell.count > kGather && low_key != high_key) {
                 const uint32_t span = high_key - low_key;
                 shift = max(0, 21 - __clz(span));                      // span >> shift < kRanges = 2^11
@@ -480,7 +493,7 @@ struct Row {
                 high_key -= cell.range << shift;
                 low_key = max(low_key, high_key - min(high_key, (1u << shift) - 1));
             }
-            const double mb = (double)cell.mass_before * unit;
+            const double mb = cell.mass_before;
             if (low_key == high_key) {
                 if (tid == 0) {
                     const bool in = cell.count && (q.kind != BY_KEY || high_key >= q.key);
@@ -520,11 +533,12 @@ struct Row {
         zero_raw();
         __syncthreads();
         uint32_t beyond = 0;                                   // of the last range, where everything far down is
-        auto add = [&](uint32_t k, uint64_t w) {
+        uint64_t beyond_mass = 0;
+        auto add = [&](uint32_t k, uint32_t range, uint64_t w) {
             if (!k || (LEVEL && (k < low_key || k > high_key))) return;
-            const uint32_t range = range_of(LEVEL, k);
-            if (LEVEL == 0 && range == kRanges - 1) {          // weights below half a unit
+            if (LEVEL == 0 && range == kRanges - 1) {          // weights below half a unit of the sums
                 ++beyond;
+                beyond_mass += w;
                 return;
             }
             uint32_t *r = raw + 4 * range;
@@ -535,29 +549,46 @@ struct Row {
             if (w1) atomicAdd(r + 2, w1);
             if (w2) atomicAdd(r + 3, w2);
         };
-        // to whole units: 2^52 added leaves them in the low bits
-        auto whole = [&](uint32_t k) {
-            return (uint64_t)__double_as_longlong(units(K::value(k ? k : best)) + 4503599627370496.0) & 0xfffffffffffffull;
+        // to whole units of its range: 2^52 added leaves them in the low bits
+        auto whole = [&](uint32_t k, uint32_t range) {
+            const double w = units(K::value(k), LEVEL ? inner : lift_of(range));
+            return (uint64_t)__double_as_longlong(w + 4503599627370496.0) & 0xfffffffffffffull;
         };
         each([&](const uint4 &q, int) {                        // four at a time: a weight is a chain of 12 operations
             const uint32_t b[4] = {q.x, q.y, q.z, q.w};
-            uint32_t k[4];
+            uint32_t k[4], range[4];
             uint64_t w[4];
             bool nan = false;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) k[e] = K::of(b[e], nan);
+            for (int e = 0; e < 4; ++e) {
+                k[e] = K::of(b[e], nan);
+                range[e] = range_of(LEVEL, k[e] ? k[e] : best);
+            }
 #pragma unroll
-            for (int e = 0; e < 4; ++e) w[e] = MASSES ? whole(k[e]) : 0ull;
+            for (int e = 0; e < 4; ++e) w[e] = MASSES ? whole(k[e] ? k[e] : best, range[e]) : 0ull;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) add(k[e], w[e]);
+            for (int e = 0; e < 4; ++e) add(k[e], range[e], w[e]);
         }, [&](uint32_t b, int) {
             bool nan = false;
-            const uint32_t k = K::of(b, nan);
-            add(k, MASSES ? whole(k) : 0ull);
+            const uint32_t k = K::of(b, nan), range = range_of(LEVEL, k ? k : best);
+            add(k, range, MASSES ? whole(k ? k : best, range) : 0ull);
         });
         if (LEVEL == 0) {
             beyond = __reduce_add_sync(~0u, beyond);
-            if (beyond && (tid & 31) == 0) atomicAdd(raw + 4 * (kRanges - 1), beyond);
+            if (MASSES) {
+#pragma unroll
+                for (int o = 16; o; o >>= 1) beyond_mass += __shfl_xor_sync(~0u, beyond_mass, o);
+            }
+            if (beyond && (tid & 31) == 0) {
+                uint32_t *r = raw + 4 * (kRanges - 1);
+                const uint32_t mask = (1u << limb) - 1;
+                atomicAdd(r, beyond);
+                if (beyond_mass) {
+                    atomicAdd(r + 1, (uint32_t)beyond_mass & mask);
+                    atomicAdd(r + 2, (uint32_t)(beyond_mass >> limb) & mask);
+                    atomicAdd(r + 3, (uint32_t)(beyond_mass >> 2 * limb));
+                }
+            }
         }
         cluster_sync();
         for (uint32_t j = tid; j < mine; j += kThreads) {
@@ -571,6 +602,10 @@ struct Row {
                     c += v.x;
                     w += (uint64_t)v.y + ((uint64_t)v.z << limb) + ((uint64_t)v.w << 2 * limb);
                 }
+            if (LEVEL == 0 && MASSES) {                        // to units of the sums, rounded
+                const int lift = lift_of(rank * share + j);
+                w = lift ? (w + (1ull << (lift - 1))) >> lift : w;
+            }
             cnt[LEVEL][j] = c;
             mass[LEVEL][j] = w;
         }
@@ -675,7 +710,7 @@ struct Row {
     // The keys of the first `rank` tokens and what shares their last range are ranked for good, if they are few enough
     bool all_ranked = false;
     __device__ __forceinline__ void rank_first(uint32_t rank_asked) {
-        const Cell cell = find(0, Query{BY_RANK, rank_asked, 0, 0.0}, 0, 0);
+        const Cell cell = find(0, Query{BY_RANK, rank_asked, 0, 0.0}, 0, 0.0);
         if (cell.before + cell.count > kGather) return;
         low_key = lowest_within(cell.range);
         high_key = best;
@@ -771,7 +806,7 @@ struct Row {
         constexpr int kAtOnce = 2;
         for (uint32_t base = 0; base < n_list; base += kAtOnce * (kThreads / 16)) {
             uint32_t c[kAtOnce];
-            uint64_t m[kAtOnce];
+            double m[kAtOnce];
 #pragma unroll
             for (int k = 0; k < kAtOnce; ++k) {
                 const uint32_t i = base + k * (kThreads / 16) + (tid >> 4);
@@ -782,7 +817,7 @@ struct Row {
             for (int k = 0; k < kAtOnce; ++k) {
                 const uint32_t i = base + k * (kThreads / 16) + (tid >> 4);
                 const uint32_t key = c[k] ? (kRanges - 1 - (rank * share + ranges[i])) * 16 + (tid & 15) : K::kZero;
-                m[k] = __double2ull_rn(c[k] * units(K::value(key)));
+                m[k] = c[k] * units(K::value(key));
             }
 #pragma unroll
             for (int k = 0; k < kAtOnce; ++k) {
@@ -794,7 +829,7 @@ struct Row {
                 }
                 if ((tid & 15) == 0 && i < n_list) {
                     cnt[0][ranges[i]] = c[k];
-                    mass[0][ranges[i]] = m[k];
+                    mass[0][ranges[i]] = __double2ull_rn(m[k]);   // one rounding for the 16 keys
                 }
             }
         }
@@ -899,6 +934,7 @@ __global__ void __launch_bounds__(Plan<T>::kThreads, RES) sample_kernel(const __
         r.best = best;
         r.top_f = K::single(best ? best : K::kLowest);
         r.per_range = fminf(p.per_nat / (cold ? 1.f : temp), 3.0e38f);
+        r.log2_per_range = p.log2_per_range;
     }
 
     // ---- the place drawn: key, and how many equal ones come before it
@@ -1185,6 +1221,7 @@ extern "C" int32_t stom_sample_tokens(const void *logits, int32_t dtype, int32_t
     p.unit_bits = 62 - bits < 51 ? 62 - bits : 51;    // 2^bits weights of 1 are 2^62 units; binary64 holds 2^52 of them
     p.limb = p.unit_bits > 47 ? 18 : 16;              // a slice's sum of limbs takes 32 bits: 2^14 (unit_bits >= 48) of 18
     p.per_nat = (Plan<float>::kRanges - 1) / ((p.unit_bits + 1) * 0.69314718f);
+    p.log2_per_range = (uint32_t)(((p.unit_bits + 1) << 16) / (Plan<float>::kRanges - 1));
     p.logits = static_cast<const char *>(logits);
     p.row_stride = row_stride;
     p.n = n;

@@ -235,3 +235,47 @@ def test_every_nan_pattern_is_seen_and_never_drawn(dtype):
         y.view(word)[:] = p                              # nothing else
         t, kept = _check(y, u, temperature=temps, flags=oqm.FLAG_BAD_VALUE)
         assert (t == -1).all() and (kept == 0).all()
+
+
+def _borders(n, part, near, far, seed):
+    """A peak, one other token and n - 2 equal ones that weigh `part` of 2^-(62 - ceil(log2 n)) each, and random numbers
+    u: rows whose border between the first two tokens lies between `near` and `far` of u, on either side."""
+    bits = (n - 1).bit_length()
+    low = np.float32(math.log(part) - (62 - bits) * math.log(2.0))
+    tail = (n - 2) * math.exp(float(low))
+    rows = []
+    for second in np.random.default_rng(seed).uniform(-1.5, -0.1, 20000).astype(np.float32):
+        border = 1.0 / (1.0 + math.exp(float(second)) + tail)
+        u = np.float32(border)
+        if near <= abs(float(u) / border - 1.0) <= far:
+            rows.append((second, u, 0 if float(u) < border else 1))
+        if len(rows) == 12:
+            break
+    assert len(rows) == 12 and len({r[2] for r in rows}) == 2
+    return low, rows
+
+
+@pytest.mark.parametrize("part", [0.49, 0.51, 1.49])
+@pytest.mark.parametrize("n,near,far", [(131072, 1e-10, 6e-10), (500000, 2.4e-10, 4e-9)])
+def test_masses_of_many_equal_light_tokens(n, near, far, part):
+    """binary32: many tokens of half a unit each (the unit of the sums of ranges, 2^-45 and 2^-43 of the largest weight
+    here) count for what they weigh together, in the draw and under top-p."""
+    oqm = _lib()
+    low, rows = _borders(n, part, near, far, n)
+    x = torch.full((len(rows), n), float(low), device="cuda")
+    x[:, 17] = 0.0
+    x[:, n - 5] = torch.tensor([float(r[0]) for r in rows], device="cuda")
+    v = torch.tensor([float(r[1]) for r in rows], device="cuda")
+    second = torch.tensor([r[2] for r in rows], device="cuda")
+    token, kept = (torch.empty(len(rows), dtype=torch.int32, device="cuda") for _ in range(2))
+    oqm.stom_sample_tokens(x, v, token, kept=kept)
+    assert token.tolist() == torch.where(second == 1, n - 5, 17).tolist() and (kept == n).all()
+    oqm.stom_sample_tokens(x, torch.zeros_like(v), token, top_p=v, kept=kept)
+    assert kept.tolist() == (second + 1).tolist() and (token == 17).all()
+    # all but the peak equal, and the draw among them: a token's place to within what a row of weights is off by
+    x[:, n - 5] = float(low)
+    total = 1.0 + (n - 1) * math.exp(float(low))
+    logp = torch.empty(len(rows), device="cuda")
+    oqm.stom_sample_tokens(x, torch.zeros_like(v), token, logprob=logp)
+    assert (token == 17).all()
+    assert (logp.double() + math.log(total)).abs().max() <= 2.4e-10 + 2.0 ** -22 * math.log(total)
