@@ -1,5 +1,6 @@
 """Builds libstom_oqm.so (sm_100a only) next to this file with nvcc, and _stom_bind.so, the Python binding of the
-calls that are made once per token, with g++ against torch's headers.
+calls that are made once per token, with g++ against the headers of the torch that is installed.  Without the binding the
+library is complete but for those calls; it is built first.
 
     python -m paper_2510_18269_b200.build [--force] [--verbose]
 
@@ -21,6 +22,7 @@ INCLUDE = PKG.parent / "include"
 OBJ = PKG / "_build"
 LIB = PKG / "libstom_oqm.so"
 BIND = PKG / "_stom_bind.so"
+BUILT_FOR = OBJ / "stom_bind.txt"   # the Python and the torch that the binding was built for
 
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
@@ -39,9 +41,20 @@ def sources():
     return sorted(CSRC.glob("*.cu"))
 
 
-def _deps_mtime() -> float:
-    files = list(CSRC.glob("*.cu")) + list(CSRC.glob("*.cuh")) + list(CSRC.glob("*.cpp")) + list(INCLUDE.glob("*.h")) + [Path(__file__)]
-    return max(f.stat().st_mtime for f in files)
+def _newer(target: Path, *patterns: str) -> bool:
+    """Whether a target is there and no older than its sources of these kinds, the headers and this file."""
+    files = [f for p in patterns for f in CSRC.glob(p)] + list(INCLUDE.glob("*.h")) + [Path(__file__)]
+    return target.exists() and target.stat().st_mtime >= max(f.stat().st_mtime for f in files)
+
+
+def _installed() -> str:
+    import torch
+
+    return f"{sys.implementation.cache_tag} torch {torch.__version__} {torch.__file__}"
+
+
+def _binding_fits() -> bool:
+    return _newer(BIND, "*.cpp") and BUILT_FOR.exists() and BUILT_FOR.read_text() == _installed()
 
 
 def _build_binding() -> None:
@@ -57,12 +70,10 @@ def _build_binding() -> None:
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode:
         raise RuntimeError(f"g++ failed for stom_bind.cpp:\n{r.stdout}\n{r.stderr}")
+    BUILT_FOR.write_text(_installed())
 
 
-def build(force: bool = False, verbose: bool = False) -> Path:
-    if not force and all(f.exists() and f.stat().st_mtime >= _deps_mtime() for f in (LIB, BIND)):
-        return LIB
-    OBJ.mkdir(exist_ok=True)
+def _build_library(verbose: bool) -> None:
     nvcc = _nvcc()
     extra = ["-Xptxas", "-v"] if verbose else []
 
@@ -77,13 +88,20 @@ def build(force: bool = False, verbose: bool = False) -> Path:
         return obj
 
     with ThreadPoolExecutor(max_workers=min(8, os.cpu_count() or 1)) as ex:
-        binding = ex.submit(_build_binding)
         objs = list(ex.map(compile_one, sources()))
-        binding.result()
     link = [nvcc, "-shared", "-gencode", "arch=compute_100a,code=sm_100a", "-o", str(LIB), *map(str, objs)]
     r = subprocess.run(link, capture_output=True, text=True)
     if r.returncode:
         raise RuntimeError(f"link failed:\n{r.stdout}\n{r.stderr}")
+
+
+def build(force: bool = False, verbose: bool = False) -> Path:
+    OBJ.mkdir(exist_ok=True)
+    with ThreadPoolExecutor(max_workers=1) as ex:
+        binding = ex.submit(lambda: None if not force and _binding_fits() else _build_binding())
+        if force or not _newer(LIB, "*.cu", "*.cuh"):
+            _build_library(verbose)
+        binding.result()   # what went wrong with the binding is raised when the library is there
     return LIB
 
 

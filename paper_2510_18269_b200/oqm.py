@@ -1,4 +1,5 @@
-"""Thin Python binding of libstom_oqm.so (argument marshalling only).
+"""Thin Python binding of libstom_oqm.so (argument marshalling only): ctypes, and for the calls of the paged cache and the
+next token, which are made once per token, _stom_bind.so (written against torch's C++ tensors; only those calls need it).
 
 Every step of the path runs in the library's CUDA kernels; PyTorch is used for
 device memory and streams.  There is no CPU fallback: if the library is not
@@ -100,14 +101,14 @@ _SIGNATURES = {
 }
 
 _lib = None
-_bind = None   # the binding of the calls that are made once per token, set with the library
+_bind = None   # the binding of the calls that are made once per token, loaded by the first of them
 _BOUND = ("stom_kv_attend", "stom_kv_rotate", "stom_kv_append", "stom_kv_reserve", "stom_kv_fork", "stom_kv_free",
           "stom_kv_compact", "stom_sample_tokens")
 
 
 def lib():
     """The loaded C-ABI library.  Fails loudly when it has not been built."""
-    global _lib, _bind
+    global _lib
     if _lib is None:
         if not LIB_PATH.exists():
             raise ImportError(
@@ -126,13 +127,6 @@ def lib():
         for name, (res, args) in _SIGNATURES.items():
             fn = getattr(L, name)
             fn.restype, fn.argtypes = res, [_CTYPE[a] for a in args]
-        try:
-            from . import _stom_bind
-        except ImportError as e:
-            raise ImportError(f"{_PKG / '_stom_bind.so'} is missing or does not fit: build it with "
-                              "`python -m paper_2510_18269_b200.build`") from e
-        _stom_bind.use(*(C.cast(getattr(L, n), C.c_void_p).value for n in _BOUND))
-        _bind = _stom_bind
         for name in EXPORTS:
             fn = getattr(L, name)
             if fn.restype is C.c_int:
@@ -407,8 +401,17 @@ def _dense(t, dtype, shape, name, dev):
 
 
 def _binding():
+    """The loaded binding of the calls made once per token.  Fails loudly when it has not been built for this torch."""
+    global _bind
     if _bind is None:
-        lib()
+        L = lib()
+        try:
+            from . import _stom_bind
+        except ImportError as e:
+            raise ImportError(f"{_PKG / '_stom_bind.so'} is missing or does not fit: build it with "
+                              "`python -m paper_2510_18269_b200.build`") from e
+        _stom_bind.use(*(C.cast(getattr(L, n), C.c_void_p).value for n in _BOUND))
+        _bind = _stom_bind
     return _bind
 
 

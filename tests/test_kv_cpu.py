@@ -300,3 +300,57 @@ def test_bindings_refuse_tensors_that_do_not_fit(oqm):
             oqm.stom_kv_attend(pool, seqs, 0, a["q"], a["out"], 0.1, ws, lse=a["lse"])
     with pytest.raises(ValueError):
         oqm.Rope(torch.zeros(8))
+
+
+def test_the_library_needs_no_binding_but_for_the_calls_that_use_it():
+    """A Python whose torch the binding does not fit, or without it, has all that is called through ctypes."""
+    import subprocess
+    import sys
+    from pathlib import Path
+
+    code = """
+import sys
+sys.modules["paper_2510_18269_b200._stom_bind"] = None        # importing it fails
+import torch
+from paper_2510_18269_b200 import oqm
+assert oqm.lib().stom_oqm_budget_to_k(12000, 50, 8) == 8
+assert oqm.stom_kv_frequencies(64).numel() == 32
+x = torch.zeros(1, 2, 64)
+for call in (lambda: oqm.stom_kv_rotate(oqm.Rope(), torch.zeros(1, dtype=torch.int32), q=x, q_out=x),
+             lambda: oqm.stom_sample_tokens(x[0], None, None)):
+    try:
+        call()
+    except ImportError as e:
+        assert "paper_2510_18269_b200.build" in str(e)
+    else:
+        raise SystemExit("no ImportError")
+"""
+    r = subprocess.run([sys.executable, "-c", code], cwd=Path(__file__).resolve().parent.parent, capture_output=True, text=True)
+    assert r.returncode == 0, r.stdout + r.stderr
+
+
+def test_the_binding_is_built_again_for_another_torch(oqm, monkeypatch, tmp_path):
+    from paper_2510_18269_b200 import build
+
+    built = []
+    monkeypatch.setattr(build, "_build_library", lambda verbose: built.append("library"))
+    monkeypatch.setattr(build, "_build_binding", lambda: built.append("binding"))
+    build.build()
+    assert built == []                                                       # both are there
+    monkeypatch.setattr(build, "BUILT_FOR", tmp_path / "other.txt")
+    build.build()
+    assert built == ["binding"]                                              # not known what for
+    (tmp_path / "other.txt").write_text(build._installed())
+    build.build()
+    (tmp_path / "other.txt").write_text(build._installed().replace("torch ", "torch 0."))
+    build.build()
+    assert built == ["binding"] * 2
+
+    def broken():
+        raise RuntimeError("no compiler")
+
+    monkeypatch.setattr(build, "_build_binding", broken)
+    monkeypatch.setattr(build, "LIB", tmp_path / "lib.so")
+    with pytest.raises(RuntimeError, match="no compiler"):
+        build.build()
+    assert built[-1] == "library"                                            # it was built all the same
