@@ -186,7 +186,7 @@ struct Row {
     uint32_t rank, blocks, share, mine;   // ranges of a block, and of this one
     double top, t, per_log2, unit;   // per_log2: log2(e) / t
     int unit_bits, limb;
-    float top_f, per_range;      // binary32: ranges per unit of x
+    float half_top, per_range;   // binary32: half of top; ranges per two units of x
     uint32_t log2_per_range;     // powers of two from one range to the next, in 2^-16
     int tid;
     uint32_t slot = 0;
@@ -433,10 +433,11 @@ struct Row {
         else return level ? (high_key - key) >> shift : range_at(K::single(key));
     }
     // binary32, first level: equal widths in x, about 64 of them to a factor e of the weight, down to half a unit.  Every
-    // step of it is monotonous, so a range is a run of keys.
+    // step of it is monotonous, so a range is a run of keys.  Halves, because the whole difference of two finite logits may
+    // not be finite.
     __device__ __forceinline__ uint32_t range_at(float v) const {
-        const float f = (top_f - v) * per_range;
-        return v == top_f ? 0u : min((uint32_t)kRanges - 1, (uint32_t)f);
+        const float f = fmaf(v, -0.5f, half_top) * per_range;
+        return 2.f * half_top == v ? 0u : (uint32_t)fminf(f, (float)(kRanges - 1));
     }
 
     // The weights of a range are at most 2^-(this), to 2^-15 by binary32's rounding of their place, and, but for the last
@@ -887,7 +888,6 @@ __global__ void __launch_bounds__(Plan<T>::kThreads, RES) sample_kernel(const __
     if (isnan(min_p)) bad = true, min_p = 0.f;
     if (isnan(u)) bad = true, u = 0.f;
     u = fminf(fmaxf(u, 0.f), 0x1.fffffep-1f);
-    temp = fminf(temp, 3.0e38f);
     const bool cold = temp <= 0.f;
 
     // ---- the largest key, and for 16-bit logits the count of every pattern
@@ -932,8 +932,9 @@ __global__ void __launch_bounds__(Plan<T>::kThreads, RES) sample_kernel(const __
     r.limb = p.limb;
     if constexpr (!kHalf) {
         r.best = best;
-        r.top_f = K::single(best ? best : K::kLowest);
-        r.per_range = fminf(p.per_nat / (cold ? 1.f : temp), 3.0e38f);
+        r.half_top = 0.5f * K::single(best ? best : K::kLowest);
+        // not 0 at an infinite temperature, so that +inf stays ahead of all else
+        r.per_range = fmaxf(fminf(2.f * p.per_nat / (cold ? 1.f : temp), 3.0e38f), 1e-38f);
         r.log2_per_range = p.log2_per_range;
     }
 

@@ -279,3 +279,19 @@ def test_masses_of_many_equal_light_tokens(n, near, far, part):
     oqm.stom_sample_tokens(x, torch.zeros_like(v), token, logprob=logp)
     assert (token == 17).all()
     assert (logp.double() + math.log(total)).abs().max() <= 2.4e-10 + 2.0 ** -22 * math.log(total)
+
+
+@pytest.mark.parametrize("dtype", [BF, HF, FL])
+def test_the_highest_temperatures(dtype):
+    """At T = inf every finite logit weighs the same, the type's lowest value too; just below it the formula holds."""
+    x = _logits(6, 3000, dtype, seed=33)
+    x[:, 5:2000:3] = torch.finfo(dtype).min
+    x[3:, 9] = torch.finfo(dtype).max
+    u, temps = [0.3, 0.61, 0.97, 0.2, 0.7, 0.99], [math.inf, 3.3e38, 3.4e38, math.inf, 3.3e38, 3.4e38]
+    t, kept = _check(x, u, temperature=temps, ambiguous=0.4)
+    assert (kept == 3000).all()
+    _check(x, u, temperature=temps, top_p=0.7, min_p=0.05, ambiguous=0.4)
+    _check(x, u, temperature=temps, top_k=500, ambiguous=0.4)
+    x[:, 20:23] = math.inf                               # these share the mass at any temperature
+    t, kept = _check(x, u, temperature=temps, ambiguous=0.4)
+    assert (kept == 3).all() and (t >= 20).all() and (t < 23).all()
