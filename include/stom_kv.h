@@ -141,6 +141,8 @@ int32_t stom_kv_append(const stom_kv_pool *pool, const stom_kv_seqs *seqs, int32
  * weight of their 16 tokens, whichever is more (fp16).
  * q, out (pool->dtype): element (i, h, c) at i*stride_seq + h*stride_head + c.
  * lse: binary32 [n_seqs][n_q_heads], or NULL.
+ * softmax_scale below 2e38 in magnitude; softcap 0, or below 2e38 with
+ * softmax_scale / softcap a normal number of binary32 (or 0).
  * n_q_heads / n_kv_heads <= 64, n_seqs <= STOM_KV_MAX_SEQS, max_pages *
  * page_tokens < 2^31 - 32, and n_seqs * n_kv_heads * max_pages * page_tokens
  * below 2^34 (n_kv_heads counted twice where its query heads are more than 16,

@@ -32,6 +32,8 @@
 // join, 3 the second kernel.  233 sequences of 0 to 300 tokens, 16 + 2 heads of 64: 14.0 us, all of it such latencies.
 #include "stom_kv.cuh"
 
+#include <math.h>
+
 #include <type_traits>
 
 namespace stom {
@@ -733,7 +735,9 @@ extern "C" int32_t stom_kv_attend(const stom_kv_pool *pool, const stom_kv_seqs *
     if (!rc) rc = check_seqs(pool, seqs, false);
     if (rc) return rc;
     if (layer < 0 || layer >= pool->n_layers || n_q_heads < 1 || window < 0) return STOM_ERR_INVALID_ARG;
-    if (!(softcap >= 0.f) || !(softcap <= 3.0e38f) || !(softmax_scale >= -3.0e38f && softmax_scale <= 3.0e38f))
+    // the factors that the kernel multiplies scores by have to be numbers, and one below binary32's normal ones lacks bits
+    const float s1 = fabsf(softcap > 0.f ? softmax_scale / softcap : softmax_scale * 1.4426950408889634f);
+    if (!(softcap >= 0.f) || !(softcap <= 2.0e38f) || !(s1 <= 3.0e38f) || (softcap > 0.f && s1 != 0.f && s1 < 1.2e-38f))
         return STOM_ERR_INVALID_ARG;
     if (n_q_heads % pool->n_kv_heads || n_q_heads / pool->n_kv_heads > 64) return STOM_ERR_SHAPE;
     if (seqs->n_seqs > STOM_KV_MAX_SEQS) return STOM_ERR_SHAPE;

@@ -354,3 +354,15 @@ def test_the_binding_is_built_again_for_another_torch(oqm, monkeypatch, tmp_path
     with pytest.raises(RuntimeError, match="no compiler"):
         build.build()
     assert built[-1] == "library"                                            # it was built all the same
+
+
+@pytest.mark.parametrize("scale,cap", [(0.1, 2.5e38), (0.0, 2.5e38), (2.5e38, 0.0), (-2.5e38, 0.0), (0.1, 1e-40), (-0.1, 1e-40),
+                                       (0.05, 1.9e38), (3e38, 0.5)])
+def test_attend_refuses_factors_that_are_no_numbers_of_32_bits(oqm, scale, cap):
+    """softcap * log2(e), softmax_scale / softcap or softmax_scale * log2(e) would overflow, or be a subnormal number."""
+    assert attend(oqm, scale=scale, cap=cap) == -1
+
+
+@pytest.mark.parametrize("scale,cap", [(0.0, 30.0), (2e38, 0.0), (0.1, 1e30), (0.1, 1e-30), (-0.5, 50.0), (0.0, 0.0)])
+def test_attend_takes_all_other_factors(oqm, scale, cap):
+    assert attend(oqm, scale=scale, cap=cap, seqs=seqs_of(oqm, n_seqs=0)) == 0
