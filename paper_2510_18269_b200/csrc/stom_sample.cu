@@ -12,16 +12,16 @@
 //     shared-memory atomic per logit is all the work that grows with the row; order, infinities and NaN are sorted out
 //     when the counters are read, the exponential is taken per DISTINCT logit, and a mass is count times weight.
 //   binary32 logits: ranges of equal width in (x_max - x) / T, so that the logits spread over them; counts, and masses as
-//     sums of integers, three limbs of 16 bits (18 for short rows), so that the order of the atomics leaves no trace.  The keys
+//     sums of integers, three limbs of 16 bits or more (by the slice), so that the order of the atomics leaves no trace.  The keys
 //     of a range are gathered and ranked; a range with more than kGather of them is cut into 2 048
 //     again.  With top-k everything else is decided among the keys ranked for it, if they are no more.
 // With 100 000 tokens left to draw from, binary32 sums would move a border between two tokens by more than some tokens'
 // whole weight.  The masses of ranges are whole numbers of UNITS in 64 bits, 2^-43 (the longest rows) to 2^-51 of the
 // largest weight, the smallest that a row's sum has room for: their sums are
 // exact and never fall, so that exactly one range holds a place and all blocks of a cluster see the same one.  A range is
-// rounded to a unit once, after it has been added up (16 bits: in binary64; binary32: in units that are smaller by the
-// range's own weight), so that the masses of a row are off by half a unit for each of 4 096 (2 048) ranges at most: 2^-34
-// of the largest weight up to 131 072 logits, 2^-32 for the longest rows.  Within the last few keys weights and sums are
+// rounded to a unit once, after it has been added up (16 bits: in binary64; binary32: in units smaller by up to n / 512), so
+// that the masses of a row are off by half a unit for each of 4 096 ranges (2 048, and 256 units) at most: 2^-34 of the
+// largest weight up to 131 072 logits, 2^-32 for the longest rows.  Within the last few keys weights and sums are
 // binary64.
 //
 // What bounds it: not memory (128 rows of 151 001 bf16 logits are 6 us at the copy rate) but the chain of steps a row has
@@ -51,6 +51,7 @@ struct SampleParams {
     int32_t unit_bits, limb;     // a unit is 2^-unit_bits; bits of a limb (binary32)
     float per_nat;               // binary32: first ranges to a factor e of the weight
     uint32_t log2_per_range;     // and the powers of two from one to the next, in 2^-16
+    int32_t most_lift;           // units that weights are rounded to are down to 2^-most_lift of those of the sums
     const float *temperature, *top_p, *min_p, *u;
     const int32_t *top_k;
     int32_t *token, *kept;
@@ -188,6 +189,7 @@ struct Row {
     int unit_bits, limb;
     float half_top, per_range;   // binary32: half of top; ranges per two units of x
     uint32_t log2_per_range;     // powers of two from one range to the next, in 2^-16
+    int most_lift;
     int tid;
     uint32_t slot = 0;
     // running sums of one level: before this thread's ranges, and with them
@@ -440,10 +442,10 @@ struct Row {
         return 2.f * half_top == v ? 0u : (uint32_t)fminf(f, (float)(kRanges - 1));
     }
 
-    // The weights of a range are at most 2^-(this), to 2^-15 by binary32's rounding of their place, and, but for the last
-    // range, little less: they are added up in units that much smaller, so that many light tokens are not each rounded
-    // to a unit of the sums.
-    __device__ __forceinline__ int lift_of(uint32_t range) const { return (int)(range * log2_per_range >> 16); }
+    // The weights of a range are at most 2^-(its place times log2_per_range), to 2^-15 by binary32's rounding of the place,
+    // so that they can be added up in units that much smaller; as many as `most_lift` are enough for n of them.  (More
+    // would cost: a weight is added limb by limb, those that are not zero.)
+    __device__ __forceinline__ int lift_of(uint32_t range) const { return min((int)(range * log2_per_range >> 16), most_lift); }
 
     __device__ __forceinline__ Place ask(const Query &q) {
         if constexpr (!kHalf)
@@ -936,6 +938,7 @@ __global__ void __launch_bounds__(Plan<T>::kThreads, RES) sample_kernel(const __
         // not 0 at an infinite temperature, so that +inf stays ahead of all else
         r.per_range = fmaxf(fminf(2.f * p.per_nat / (cold ? 1.f : temp), 3.0e38f), 1e-38f);
         r.log2_per_range = p.log2_per_range;
+        r.most_lift = p.most_lift;
     }
 
     // ---- the place drawn: key, and how many equal ones come before it
@@ -1180,6 +1183,9 @@ int32_t launch(SampleParams &p, int rows, cudaStream_t stream) {
         for (int c = cluster + 1; c <= kMaxCluster && p.n / (c - 1) > 8192 && rows <= most[c]; ++c) cluster = c;
     if ((int64_t)rows * cluster > INT32_MAX) return STOM_ERR_SHAPE;
     p.slice = ((p.n + cluster - 1) / cluster + 7) & ~7;
+    // a slice's sum of limbs takes 32 bits; three limbs hold a weight: 48 bits of 2^47 units at most (n > 2^14), 54 of 2^51
+    p.limb = 32;
+    while ((1ll << (32 - p.limb)) < p.slice) --p.limb;
     cudaLaunchAttribute at[2];
     const cudaLaunchConfig_t lc = config<T>(rows, cluster, stream, at);
     if (e == cudaSuccess) {
@@ -1220,7 +1226,7 @@ extern "C" int32_t stom_sample_tokens(const void *logits, int32_t dtype, int32_t
     int bits = 0;
     while ((1 << bits) < n) ++bits;
     p.unit_bits = 62 - bits < 51 ? 62 - bits : 51;    // 2^bits weights of 1 are 2^62 units; binary64 holds 2^52 of them
-    p.limb = p.unit_bits > 47 ? 18 : 16;              // a slice's sum of limbs takes 32 bits: 2^14 (unit_bits >= 48) of 18
+    p.most_lift = bits > 9 ? bits - 9 : 0;            // n halves of 2^-most_lift units are 2^8 units (ranges: 2^10 at most)
     p.per_nat = (Plan<float>::kRanges - 1) / ((p.unit_bits + 1) * 0.69314718f);
     p.log2_per_range = (uint32_t)(((p.unit_bits + 1) << 16) / (Plan<float>::kRanges - 1));
     p.logits = static_cast<const char *>(logits);
