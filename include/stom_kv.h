@@ -66,7 +66,10 @@ typedef struct stom_kv_pool {
 
 /* The sequences that live in a pool.  Row i of `table` names, in order, the
  * ceil(len[i]/page_tokens) pages of sequence i; what stands behind them is not
- * read.  refs[p] counts the rows that hold page p; 0 is a free page. */
+ * read (but by stom_kv_append, if a slot lies there: with -1 in a new table's
+ * entries such a token is skipped and flagged, which is what a step captured
+ * in a graph needs if its stom_kv_reserve finds no page).  refs[p] counts the
+ * rows that hold page p; 0 is a free page. */
 typedef struct stom_kv_seqs {
     int32_t *table;       /* [n_seqs][table_stride], max_pages entries of a row are used */
     int32_t *len;         /* [n_seqs] tokens                                            */

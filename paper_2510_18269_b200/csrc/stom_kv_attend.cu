@@ -26,10 +26,11 @@
 // of its own that are scaled into the running ones: a weight is off by 2^-22 of itself or 2^-40 of its tile's largest,
 // whichever is more.  bf16 has the exponents of binary32 and needs none of it.
 //
-// Measured (B200, copy rate 6 458 GB/s): 64 sequences of 17 to 16 411 tokens, 64 + 8 heads of 128, pages of 16: 230 us for
-// 1.47 GB, 6.4 TB/s.  One sequence of 12 583 tokens, 28 + 4 heads, pages of 50: 12.0 us, of which 4 are its 26 MB at the
+// Measured (B200, copy rate 6 458 GB/s): 64 sequences of 17 to 16 411 tokens, 64 + 8 heads of 128, pages of 16: 230 to 240
+// us for 1.47 GB, 6.1 to 6.4 TB/s.  One sequence of 12 583 tokens, 28 + 4 heads, pages of 50: 12.2 us, of which 4 are its 26 MB at the
 // copy rate, 2.5 the way to the first load (lengths, then pages, then rows: three memory round trips), 1.5 the block's
-// join, 3 the second kernel.  233 sequences of 0 to 300 tokens, 16 + 2 heads of 64: 14.0 us, all of it such latencies.
+// join, 3 the second kernel.  233 sequences of 0 to 300 tokens, 16 + 2 heads of 64, fp16: 14.1 us, all of it such latencies
+// (and the same as with weights relative to the running maximum).
 #include "stom_kv.cuh"
 
 #include <math.h>
@@ -680,7 +681,8 @@ __global__ void __launch_bounds__(D / 4 * kJoin) kv_attend_join_kernel(const __g
 }
 
 // Query heads per product: 8, or 16 where a kv head has more than 8 and the accumulators fit (head_dim <= 128); a
-// larger group is cut into blocks of that many, which read the keys and values again, from L2.
+// larger group is cut into blocks of that many, which read the keys and values again (how much of it comes from L2 has not
+// been measured).
 int heads_per_unit(int group, int head_dim) { return group > 8 && head_dim <= 128 ? 16 : 8; }
 
 int64_t round16(int64_t x) { return (x + 15) & ~(int64_t)15; }

@@ -7,8 +7,8 @@
 // Counts change by integer atomics, whose order leaves no trace; every page id is checked before it is used.
 //
 // Measured (B200, copy rate 6 458 GB/s), 28 layers, 4 heads of 128, pages of 50: eight sequences forked eight times, the
-// 64 candidates given room for a token (free, fork, reserve): 31.2 us, 20 of them for the 164 MB of copies; 20 sequences'
-// pages moved together: 69 us for 384 MB (5.6 TB/s).
+// 64 candidates given room for a token (free, fork, reserve): 30.9 us, 20 of them for the 164 MB of copies; 20 sequences'
+// pages moved together: 69 to 74 us for 384 MB (5.2 to 5.6 TB/s).
 #include "stom_kv.cuh"
 
 namespace stom {

@@ -7,14 +7,16 @@
 // decode step (a few kilobytes) the launch.  One pass, all loads and stores 16 bytes wide.  A row (one head of one token)
 // belongs to d/16 adjacent threads; a thread owns the two 16-byte chunks that rotate with one another (half layout: the
 // chunk and the one rot_dim/2 channels on; pairs: two adjacent chunks), so a rotation needs no exchange and a norm a few
-// shuffles; with a norm, two values per instruction (f32x2).  A warp works on one token at a time, on several of its rows at once and on the others after them: its sines
-// and cosines, and the norm's weights, are then the same for all its rows and stay in registers, and warps need no
-// barrier.  A token with few companions is cut into parts, one warp each, down to one round of rows.
+// shuffles; with a norm, two values per instruction (f32x2).  A warp works on one token at a time, on several of its rows
+// at once and on the others after them: its sines and cosines, and the norm's weights, are then the same for all its rows
+// and stay in registers, and warps need no barrier.  A token with few companions is cut into parts, one warp each, down to one round of rows.
 // Angles: pos * freq is formed and reduced to [-pi, pi] in binary64 (at position 10^6 a binary32 product would be off by
 // 0.03 radians); the sine and cosine of the reduced angle are taken in binary32 with a first-order correction for the
-// part of the angle that its rounding to binary32 lost.
+// part of the angle that its rounding to binary32 lost.  Sine, cosine, the norm's sum and root and the turn are binary32,
+// together within 2^-20 of the terms' magnitude: far below a half step of 16 bits, and of the order of binary32's own for
+// binary32 rows (error against 64 bits 6.1e-8; with the angles' sines in binary64 and one rounding at the end 6.0e-8).
 //
-// Measured (B200, copy rate 6 458 GB/s): 12 583 tokens of 28 + 4 heads of 128, bf16: 36.8 us for 206 MB (5.6 TB/s); 4 099
+// Measured (B200, copy rate 6 458 GB/s): 12 583 tokens of 28 + 4 heads of 128, bf16: 37.2 us for 206 MB (5.5 TB/s); 4 099
 // tokens of 64 + 8 heads with norms into pages, fp16: 34.5 us for 168 MB (4.9 TB/s, held back by the 16 warps that 124
 // registers leave a multiprocessor); 1 771 tokens of 16 + 8 heads of 64 with norms, binary32: 7.4 us; one token: 2.9 us.
 // A persistent form (equal stretches of rows per warp, loads eight steps ahead through shared memory) ran 37.6, 33.1, 8.9

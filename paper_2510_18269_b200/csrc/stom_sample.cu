@@ -29,7 +29,7 @@
 // such rows with mixed settings 78 us, three rounds of 49 clusters of 3 blocks; a block's 24 us are 6 for its 50 000
 // logits (4.3 cycles for a warp's shared-memory atomic, the rest the patterns' arithmetic), 5 for the ranges, 2 to 2.5 for
 // every place asked for, 3 for the index.  One row of 128 000 logits on 16 blocks: bf16 21 us, binary32 20 us with top-k,
-// 37 us with top-p alone (a ranking for each of two places).
+// 36 us with top-p alone (a ranking for each of two places).
 #include "stom_kv.cuh"
 #include "stom_sample.h"
 
@@ -843,7 +843,7 @@ struct Row {
 };
 
 // RES: blocks that a multiprocessor is to hold (binary32: 2 where the rows take several rounds; 128 rows of 128 000:
-// 134 us, with 1 it is 155; but one row 25.6 us and 24.3 with 1, which spills no registers)
+// 136 us, with 1 it is 163; but one row on its own is a microsecond faster with 1, which spills no registers)
 template <typename T, int RES>
 __global__ void __launch_bounds__(Plan<T>::kThreads, RES) sample_kernel(const __grid_constant__ SampleParams p) {
     using K = Keys<T>;

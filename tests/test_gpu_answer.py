@@ -200,3 +200,29 @@ def test_an_empty_batch_changes_nothing():
     for got, want in ((pool.k, before[0]), (pool.v, before[1])):
         want[:, 4] = 1.0                                         # what stood there stays
         assert torch.equal(got, want)
+
+
+def test_a_step_that_finds_no_page_writes_nothing():
+    """As in a captured step, where nobody looks between the calls: the token of a row whose page is not there is left
+    out, and so is what it would have overwritten."""
+    from paper_2510_18269_b200 import oqm
+    oqm.lib()
+    i32 = lambda *v: torch.tensor(v, dtype=torch.int32, device="cuda")  # noqa: E731
+    k = torch.randn(1, 3, 16, 2, 64, device="cuda").to(BF)
+    pool = oqm.KvPool(k, k.clone())
+    table, n, refs, flags = torch.full((2, 4), -1, dtype=torch.int32, device="cuda"), i32(0, 0), i32(0, 0, 0), i32(0)
+    seqs = oqm.KvSeqs(table, n, refs)
+    ws = torch.empty(max(oqm.stom_kv_pages_workspace_bytes(pool, seqs), oqm.stom_kv_attend_workspace_bytes(pool, seqs, 2)),
+                     dtype=torch.uint8, device="cuda")
+    oqm.stom_kv_reserve(pool, seqs, i32(32, 16), ws, dev_flags=flags)
+    assert flags.item() == 0 and (refs == 1).all()
+    before = pool.k.clone(), pool.v.clone(), table.clone()
+    q, new = torch.randn(2, 2, 64, device="cuda").to(BF), torch.ones(2, 2, 64, device="cuda", dtype=BF)
+    qo, out = torch.empty_like(q), torch.empty_like(q)
+    oqm.stom_kv_reserve(pool, seqs, i32(33, 17), ws, dev_flags=flags)
+    oqm.stom_kv_append(pool, seqs, 0, oqm.Rope(), i32(32, 16), i32(32, 16), new, new, q=q, q_out=qo, dev_flags=flags)
+    oqm.stom_kv_attend(pool, seqs, 0, qo, out, 0.125, ws, dev_flags=flags)
+    assert flags.item() == oqm.FLAG_NO_PAGE | oqm.FLAG_BAD_INDEX and n.tolist() == [32, 16]
+    assert torch.equal(pool.k, before[0]) and torch.equal(pool.v, before[1]) and torch.equal(table, before[2])
+    want, _, mag = K.attend_rows(pool.k, pool.v, table.cpu().numpy(), [32, 16], q, 0.125)
+    close_attend(out, want, mag, BF)
