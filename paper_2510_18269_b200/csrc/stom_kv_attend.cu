@@ -27,9 +27,9 @@
 // whichever is more.  bf16 has the exponents of binary32 and needs none of it.
 //
 // Measured (B200, copy rate 6 458 GB/s): 64 sequences of 17 to 16 411 tokens, 64 + 8 heads of 128, pages of 16: 230 to 240
-// us for 1.47 GB, 6.1 to 6.4 TB/s.  One sequence of 12 583 tokens, 28 + 4 heads, pages of 50: 12.2 us, of which 4 are its 26 MB at the
-// copy rate, 2.5 the way to the first load (lengths, then pages, then rows: three memory round trips), 1.5 the block's
-// join, 3 the second kernel.  233 sequences of 0 to 300 tokens, 16 + 2 heads of 64, fp16: 14.1 us, all of it such latencies
+// us for 1.47 GB, 6.1 to 6.4 TB/s.  One sequence of 12 583 tokens, 28 + 4 heads, pages of 50: 12.2 us, of which 4 are its
+// 26 MB at the copy rate, 2.5 the way to the first load (lengths, then pages, then rows: three memory round trips), 1.5 the
+// block's join, 3 the second kernel.  233 sequences of 0 to 300 tokens, 16 + 2 heads of 64, fp16: 14.1 us, all of it such latencies
 // (and the same as with weights relative to the running maximum).
 #include "stom_kv.cuh"
 

@@ -9,7 +9,8 @@
 // chunk and the one rot_dim/2 channels on; pairs: two adjacent chunks), so a rotation needs no exchange and a norm a few
 // shuffles; with a norm, two values per instruction (f32x2).  A warp works on one token at a time, on several of its rows
 // at once and on the others after them: its sines and cosines, and the norm's weights, are then the same for all its rows
-// and stay in registers, and warps need no barrier.  A token with few companions is cut into parts, one warp each, down to one round of rows.
+// and stay in registers, and warps need no barrier.  A token with few companions is cut into parts, one warp each, down to
+// one round of rows.
 // Angles: pos * freq is formed and reduced to [-pi, pi] in binary64 (at position 10^6 a binary32 product would be off by
 // 0.03 radians); the sine and cosine of the reduced angle are taken in binary32 with a first-order correction for the
 // part of the angle that its rounding to binary32 lost.  Sine, cosine, the norm's sum and root and the turn are binary32,

@@ -12,8 +12,8 @@
 //     shared-memory atomic per logit is all the work that grows with the row; order, infinities and NaN are sorted out
 //     when the counters are read, the exponential is taken per DISTINCT logit, and a mass is count times weight.
 //   binary32 logits: ranges of equal width in (x_max - x) / T, so that the logits spread over them; counts, and masses as
-//     sums of integers, three limbs of 16 bits or more (by the slice), so that the order of the atomics leaves no trace.  The keys
-//     of a range are gathered and ranked; a range with more than kGather of them is cut into 2 048
+//     sums of integers, three limbs of 16 bits or more (by the slice), so that the order of the atomics leaves no trace.
+//     The keys of a range are gathered and ranked; a range with more than kGather of them is cut into 2 048
 //     again.  With top-k everything else is decided among the keys ranked for it, if they are no more.
 // With 100 000 tokens left to draw from, binary32 sums would move a border between two tokens by more than some tokens'
 // whole weight.  The masses of ranges are whole numbers of UNITS in 64 bits, 2^-43 (the longest rows) to 2^-51 of the
