@@ -233,7 +233,6 @@ def prepare(case, seed):
         s["oqm"] = oqm
         if case["op"] == "w4":
             s["w"] = oqm.W4Matrix(s["codes"], s["w_scale"], s["w_zero"])
-            s["ws"] = torch.empty(oqm.stom_w4_workspace_bytes(s["w"], case["rows"]), dtype=torch.uint8, device=DEV)
             return s
         s["pool"] = oqm.KvPool(s["pool_k"], s["pool_v"])
         s["seqs"] = oqm.KvSeqs(s["table"], s["len"], s.get("refs"))
@@ -374,7 +373,7 @@ def run(state):
         s["oqm"].stom_kv_accept(s["pool"], s["seqs"], s["first"], s["draft"], s["chosen"], s["path"], s["accepted"], s["next"],
                                 parent=s["parent"])
     else:
-        s["oqm"].stom_w4_linear(s["w"], s["x"], s["y"], s["ws"], bias=s["bias"], add=s["add"])
+        s["oqm"].stom_w4_linear(s["w"], s["x"], s["y"], bias=s["bias"], add=s["add"])
     return _outputs(s)
 
 
