@@ -30,7 +30,7 @@
 extern "C" {
 #endif
 
-/* further bits of dev_flags */
+/* further bits of dev_flags (STOM_FLAG_TIMEOUT: stom_kv_attend_tree gave up; its outputs are not to be used) */
 #define STOM_FLAG_NO_PAGE 8u    /* stom_kv_reserve: too few free pages; the call changed nothing */
 #define STOM_FLAG_BAD_VALUE 16u /* stom_sample_tokens: a NaN among a row's logits or settings */
 
@@ -157,6 +157,66 @@ int32_t stom_kv_attend(const stom_kv_pool *pool, const stom_kv_seqs *seqs, int32
                        const void *q, int64_t q_stride_seq, int64_t q_stride_head, float softmax_scale, float softcap,
                        int32_t window, void *out, int64_t out_stride_seq, int64_t out_stride_head, float *lse,
                        void *workspace, int64_t workspace_bytes, uint32_t *dev_flags, void *stream);
+
+/* ---- attention of several new tokens per sequence -------------------------
+ * The last n_i = first[i+1] - first[i] of the len[i] tokens of sequence i are
+ * new: its NODES, rows first[i] .. first[i+1] - 1 of q, out, lse and parent.
+ * parent[first[i] + j], below j, is the node that node j follows, or -1: it
+ * follows the context, as a tree of drafted tokens may branch there too.  parent
+ * NULL: node j follows node j - 1 (a question, or one draft).  Node j stands at
+ * position (len[i] - n_i) + depth_j, where depth_j counts the nodes before it on
+ * its path, and sees, for every query head as in stom_kv_attend, the tokens
+ * before the nodes and the nodes of its path, itself among them; with a window,
+ * those of them whose position is above its own minus `window`.
+ * The nodes' keys and values are expected in the cache already, node j's at
+ * slot (len[i] - n_i) + j (stom_kv_append with that slot and the position
+ * above).
+ * first: int32 [n_seqs + 1]; rows of no sequence are left as they were.  A
+ * sequence whose first[i] .. first[i+1] do not lie in order within
+ * 0 .. n_tokens, that has more nodes than tokens or, with parents, more than
+ * STOM_KV_MAX_TREE, is skipped (its rows stay as they were) and sets
+ * STOM_FLAG_BAD_INDEX; so does a parent outside -1 .. j - 1, which counts as -1,
+ * and what stom_kv_attend flags.  A node that sees nothing (all of its pages
+ * are none) gives zeros and -inf.
+ * Keys and values of a token that a node does not see have no effect on it,
+ * also where they are no finite numbers.  Products of 16-bit operands are
+ * summed in binary32; a softmax weight enters the second product rounded to the
+ * pool's type: off by 2^-8 of itself (bf16), or by 2^-11 of itself or 2^-32 of
+ * the row's largest weight, whichever is more (fp16).
+ * q, out (pool->dtype): element (row, h, c) at row*stride_token +
+ * h*stride_head + c.  lse: binary32 [n_tokens][n_q_heads], or NULL.  Other
+ * limits are those of stom_kv_attend, and n_tokens * n_q_heads < 2^31.
+ * Errors as for stom_kv_attend. */
+#define STOM_KV_MAX_TREE 256
+int64_t stom_kv_attend_tree_workspace_bytes(const stom_kv_pool *pool, const stom_kv_seqs *seqs, int32_t n_tokens,
+                                            int32_t n_q_heads);
+int32_t stom_kv_attend_tree(const stom_kv_pool *pool, const stom_kv_seqs *seqs, int32_t layer, int32_t n_tokens,
+                            const int32_t *first, const int32_t *parent, int32_t n_q_heads, const void *q,
+                            int64_t q_stride_token, int64_t q_stride_head, float softmax_scale, float softcap,
+                            int32_t window, void *out, int64_t out_stride_token, int64_t out_stride_head, float *lse,
+                            void *workspace, int64_t workspace_bytes, uint32_t *dev_flags, void *stream);
+
+/* ---- a drafted path is kept ------------------------------------------------
+ * first, parent: as above.  draft[row] is the token that a node holds,
+ * chosen[row] the one that was chosen to follow it (stom_sample_tokens of the
+ * node's logits).  The path kept begins with node 0, whose token had been
+ * chosen in the step before; node j is followed by the lowest node c > j with
+ * parent j and draft[c] == chosen[j], until there is none (chosen[j] < 0: there
+ * is none).  For every sequence with nodes:
+ *     path[first[i] + k] = the path's k-th node, -1 behind its end;
+ *     n_accepted[i] = its length;  next[i] = chosen of its last node;
+ *     keys and values of its nodes, in all layers, move together to the slots
+ *     behind the context; len[i] = (len[i] - n_i) + n_accepted[i]; pages that
+ *     hold nothing any more are given back (as by stom_kv_free).
+ * A sequence without nodes keeps what it has: n_accepted 0, next -1; so does one
+ * that stom_kv_attend_tree would skip, or (without parents too) with more than
+ * STOM_KV_MAX_TREE nodes or tokens than its row has, and sets
+ * STOM_FLAG_BAD_INDEX.  Page ids outside [0, n_pages) are skipped and set it too.
+ * Pages that nodes lie in must not be shared.  path, n_accepted and next may be
+ * NULL.  Errors: INVALID_ARG, SHAPE, UNSUPPORTED, ALIGNMENT, CUDA. */
+int32_t stom_kv_accept(const stom_kv_pool *pool, const stom_kv_seqs *seqs, int32_t n_tokens, const int32_t *first,
+                       const int32_t *parent, const int32_t *draft, const int32_t *chosen, int32_t *path,
+                       int32_t *n_accepted, int32_t *next, uint32_t *dev_flags, void *stream);
 
 /* ---- pages: reserve, fork, free, compact -----------------------------------
  * All need seqs->refs and act on all layers.  Page ids outside [0, n_pages)

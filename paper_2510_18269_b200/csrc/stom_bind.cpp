@@ -1,4 +1,4 @@
-// Python binding of the calls that are made once per token (stom_kv.h, stom_sample.h): checks the tensors of a call
+// Python binding of the calls that are made once per token (stom_kv.h, stom_sample.h, stom_w4.h): checks the tensors of a call
 // against one another and passes their addresses on.  Written against torch's C++ tensors because the same checks in
 // Python, with ctypes for the call, take 10 us, several times what the smaller kernels run.
 //
@@ -17,6 +17,7 @@
 
 #include "stom_kv.h"
 #include "stom_sample.h"
+#include "stom_w4.h"
 
 namespace {
 
@@ -30,6 +31,9 @@ struct Library {
     decltype(&stom_kv_free) free_pages = nullptr;
     decltype(&stom_kv_compact) compact = nullptr;
     decltype(&stom_sample_tokens) sample = nullptr;
+    decltype(&stom_kv_attend_tree) attend_tree = nullptr;
+    decltype(&stom_kv_accept) accept = nullptr;
+    decltype(&stom_w4_linear) w4_linear = nullptr;
 } lib;
 
 [[noreturn]] void refuse(const char *name, const std::string &needed, const at::Tensor *t) {
@@ -174,6 +178,88 @@ PyObject *attend(PyObject *, PyObject *const *a, Py_ssize_t n) {
     });
 }
 
+// pool, seqs, device, layer, first, parent, q, out, scale, softcap, window, lse, workspace, dev_flags, stream
+PyObject *attend_tree(PyObject *, PyObject *const *a, Py_ssize_t count) {
+    return guarded(count, 15, [&] {
+        const auto *pool = at_address<stom_kv_pool>(a[0]);
+        const auto *seqs = at_address<stom_kv_seqs>(a[1]);
+        const int64_t dev = integer(a[2]);
+        const at::ScalarType type = type_of(pool->dtype);
+        const at::Tensor &x = must(a[6], "q");
+        if (x.dim() != 3 || x.size(0) > INT32_MAX) refuse("q", "a tensor of three axes", &x);
+        const int64_t n = x.size(0);
+        const Rows q = rows(a[6], type, n, -1, pool->head_dim, dev, "q");
+        const Rows out = rows(a[7], type, n, q.heads, pool->head_dim, dev, "out");
+        must(a[4], "first");
+        const int32_t *first = dense<int32_t>(a[4], at::kInt, (int64_t)seqs->n_seqs + 1, -1, dev, "first");
+        const int32_t *parent = dense<int32_t>(a[5], at::kInt, n, -1, dev, "parent");
+        float *lse = dense<float>(a[11], at::kFloat, n, q.heads, dev, "lse");
+        int64_t bytes;
+        void *ws = workspace(a[12], dev, bytes);
+        uint32_t *fl = flags(a[13], dev);
+        const On on(dev, a[14]);
+        return lib.attend_tree(pool, seqs, int32(a[3]), (int32_t)n, first, parent, q.heads, q.at, q.row, q.head, number(a[8]),
+                               number(a[9]), int32(a[10]), out.at, out.row, out.head, lse, ws, bytes, fl, on.stream);
+    });
+}
+
+// pool, seqs, device, first, parent, draft, chosen, path, n_accepted, next, dev_flags, stream
+PyObject *accept(PyObject *, PyObject *const *a, Py_ssize_t count) {
+    return guarded(count, 12, [&] {
+        const auto *seqs = at_address<stom_kv_seqs>(a[1]);
+        const int64_t dev = integer(a[2]);
+        const at::Tensor &x = must(a[5], "draft");
+        if (x.dim() != 1 || x.size(0) > INT32_MAX) refuse("draft", "a tensor of one axis", &x);
+        const int64_t n = x.size(0);
+        must(a[3], "first"), must(a[6], "chosen");
+        const int32_t *first = dense<int32_t>(a[3], at::kInt, (int64_t)seqs->n_seqs + 1, -1, dev, "first");
+        const int32_t *parent = dense<int32_t>(a[4], at::kInt, n, -1, dev, "parent");
+        const int32_t *draft = dense<int32_t>(a[5], at::kInt, n, -1, dev, "draft");
+        const int32_t *chosen = dense<int32_t>(a[6], at::kInt, n, -1, dev, "chosen");
+        int32_t *path = dense<int32_t>(a[7], at::kInt, n, -1, dev, "path");
+        int32_t *accepted = dense<int32_t>(a[8], at::kInt, seqs->n_seqs, -1, dev, "n_accepted");
+        int32_t *next = dense<int32_t>(a[9], at::kInt, seqs->n_seqs, -1, dev, "next");
+        uint32_t *fl = flags(a[10], dev);
+        const On on(dev, a[11]);
+        return lib.accept(at_address<stom_kv_pool>(a[0]), seqs, (int32_t)n, first, parent, draft, chosen, path, accepted, next, fl,
+                          on.stream);
+    });
+}
+
+// matrix, device, x, y, bias, add, stream
+PyObject *w4_linear(PyObject *, PyObject *const *a, Py_ssize_t count) {
+    return guarded(count, 7, [&] {
+        const auto *w = at_address<stom_w4_matrix>(a[0]);
+        const int64_t dev = integer(a[1]);
+        const at::Tensor &x = must(a[2], "x");
+        if (x.dim() != 2 || x.size(0) > INT32_MAX) refuse("x", "a tensor of two axes", &x);
+        const int32_t dtype = dtype_of(x, "x");
+        const int64_t n = x.size(0);
+        auto flat = [&](PyObject *o, int64_t cols, const char *name) {
+            const at::Tensor &t = must(o, name);
+            if (t.scalar_type() != x.scalar_type() || t.dim() != 2 || t.size(0) != n || t.size(1) != cols ||
+                (cols > 1 && t.stride(1) != 1) || !on(t, dev)) {
+                std::ostringstream s;
+                s << "a " << x.scalar_type() << " tensor of shape [" << n << ", " << cols << "] with adjacent entries on cuda:" << dev;
+                refuse(name, s.str(), &t);
+            }
+            return Rows{t.data_ptr(), t.stride(0), 0, 0};
+        };
+        const Rows in = flat(a[2], w->k, "x"), out = flat(a[3], w->n, "y");
+        const void *bias = nullptr;
+        if (a[4] != Py_None) {
+            const at::Tensor &t = must(a[4], "bias");
+            if (t.scalar_type() != x.scalar_type() || t.dim() != 1 || t.size(0) != w->n || !t.is_contiguous() || !on(t, dev))
+                refuse("bias", "a contiguous tensor of x's type, an entry for each row of the matrix", &t);
+            bias = t.data_ptr();
+        }
+        Rows add;
+        if (a[5] != Py_None) add = flat(a[5], w->n, "add");
+        const On on(dev, a[6]);
+        return lib.w4_linear(w, dtype, (int32_t)n, in.at, in.row, bias, add.at, add.row, out.at, out.row, on.stream);
+    });
+}
+
 // rope, pos, q, q_out, k, k_out, q_weight, k_weight, eps, stream, device of the frequencies
 PyObject *rotate(PyObject *, PyObject *const *a, Py_ssize_t count) {
     return guarded(count, 11, [&] {
@@ -314,7 +400,7 @@ PyObject *sample(PyObject *, PyObject *const *a, Py_ssize_t count) {
 
 // the addresses of the library's entry points, in the order of Library
 PyObject *use(PyObject *, PyObject *const *a, Py_ssize_t n) {
-    return guarded(n, 8, [&] {
+    return guarded(n, 11, [&] {
         lib.attend = reinterpret_cast<decltype(lib.attend)>(integer(a[0]));
         lib.rotate = reinterpret_cast<decltype(lib.rotate)>(integer(a[1]));
         lib.append = reinterpret_cast<decltype(lib.append)>(integer(a[2]));
@@ -323,6 +409,9 @@ PyObject *use(PyObject *, PyObject *const *a, Py_ssize_t n) {
         lib.free_pages = reinterpret_cast<decltype(lib.free_pages)>(integer(a[5]));
         lib.compact = reinterpret_cast<decltype(lib.compact)>(integer(a[6]));
         lib.sample = reinterpret_cast<decltype(lib.sample)>(integer(a[7]));
+        lib.attend_tree = reinterpret_cast<decltype(lib.attend_tree)>(integer(a[8]));
+        lib.accept = reinterpret_cast<decltype(lib.accept)>(integer(a[9]));
+        lib.w4_linear = reinterpret_cast<decltype(lib.w4_linear)>(integer(a[10]));
         return 0;
     });
 }
@@ -331,7 +420,8 @@ PyObject *use(PyObject *, PyObject *const *a, Py_ssize_t n) {
 PyMethodDef methods[] = {
     STOM_METHOD("use", use), STOM_METHOD("attend", attend), STOM_METHOD("rotate", rotate), STOM_METHOD("append", append),
     STOM_METHOD("reserve", reserve), STOM_METHOD("fork", fork_rows), STOM_METHOD("free", free_rows),
-    STOM_METHOD("compact", compact), STOM_METHOD("sample", sample), {nullptr, nullptr, 0, nullptr},
+    STOM_METHOD("compact", compact), STOM_METHOD("sample", sample), STOM_METHOD("attend_tree", attend_tree),
+    STOM_METHOD("accept", accept), STOM_METHOD("w4_linear", w4_linear), {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_stom_bind", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

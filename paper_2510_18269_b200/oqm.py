@@ -1,5 +1,5 @@
-"""Thin Python binding of libstom_oqm.so (argument marshalling only): ctypes, and for the calls of the paged cache and the
-next token, which are made once per token, _stom_bind.so (written against torch's C++ tensors; only those calls need it).
+"""Thin Python binding of libstom_oqm.so (argument marshalling only): ctypes, and for the calls of the paged cache, the
+next token and the 4-bit products, which are made once per token, _stom_bind.so (written against torch's C++ tensors; only those calls need it).
 
 Every step of the path runs in the library's CUDA kernels; PyTorch is used for
 device memory and streams.  There is no CPU fallback: if the library is not
@@ -41,6 +41,7 @@ EXPORTS = (
     "stom_kv_frequencies", "stom_kv_attend_workspace_bytes", "stom_kv_attend",
     "stom_kv_rotate", "stom_kv_append", "stom_kv_pages_workspace_bytes", "stom_kv_reserve", "stom_kv_fork",
     "stom_kv_free", "stom_kv_compact", "stom_sample_tokens",
+    "stom_kv_attend_tree_workspace_bytes", "stom_kv_attend_tree", "stom_kv_accept", "stom_w4_linear",
 )
 
 
@@ -76,6 +77,11 @@ class RopeDesc(C.Structure):
     _fields_ = [("freq", C.c_void_p), ("rot_dim", C.c_int32), ("layout", C.c_int32), ("magnitude", C.c_float)]
 
 
+class W4Desc(C.Structure):
+    _fields_ = [("codes", C.c_void_p), ("scale", C.c_void_p), ("zero", C.c_void_p)] + [(n, C.c_int32) for n in (
+        "n", "k", "group", "meta_dtype")] + [("code_stride", C.c_int64), ("meta_stride", C.c_int64)]
+
+
 class StomError(RuntimeError):
     def __init__(self, code: int, where: str):
         self.code = code
@@ -98,12 +104,16 @@ _SIGNATURES = {
     "stom_kv_free": (C.c_int32, "ppppp"),
     "stom_kv_compact": (C.c_int32, "ppppppl" + "pp"),
     "stom_sample_tokens": (C.c_int32, "piiil" + "ppppp" + "ppp" + "pp"),
+    "stom_kv_attend_tree_workspace_bytes": (C.c_int64, "ppii"),
+    "stom_kv_attend_tree": (C.c_int32, "ppii" + "pp" + "ipllffi" + "pllp" + "plpp"),
+    "stom_kv_accept": (C.c_int32, "ppi" + "pppp" + "ppp" + "pp"),
+    "stom_w4_linear": (C.c_int32, "piipl" + "ppl" + "pl" + "p"),
 }
 
 _lib = None
 _bind = None   # the binding of the calls that are made once per token, loaded by the first of them
 _BOUND = ("stom_kv_attend", "stom_kv_rotate", "stom_kv_append", "stom_kv_reserve", "stom_kv_fork", "stom_kv_free",
-          "stom_kv_compact", "stom_sample_tokens")
+          "stom_kv_compact", "stom_sample_tokens", "stom_kv_attend_tree", "stom_kv_accept", "stom_w4_linear")
 
 
 def lib():
@@ -495,6 +505,25 @@ def stom_kv_attend(pool: KvPool, seqs: KvSeqs, layer, q, out, softmax_scale, wor
         _check(rc, "stom_kv_attend")
 
 
+def stom_kv_attend_tree_workspace_bytes(pool: KvPool, seqs: KvSeqs, n_tokens: int, n_q_heads: int) -> int:
+    n = lib().stom_kv_attend_tree_workspace_bytes(pool.ref, seqs.ref, n_tokens, n_q_heads)
+    if n < 0:
+        _check(int(n), "stom_kv_attend_tree_workspace_bytes")
+    return int(n)
+
+
+def stom_kv_attend_tree(pool: KvPool, seqs: KvSeqs, layer, first, q, out, softmax_scale, workspace, parent=None, lse=None,
+                        softcap=0.0, window=0, dev_flags=None, stream=None):
+    """The last first[i + 1] - first[i] tokens of every sequence, rows first[i] ... of q and out ([n][query heads][d] of the
+    pool's type) and of lse ([n][query heads] float32 or None); first: int32 [n_seqs + 1]; parent: int32 [n], the node of
+    its sequence that each follows (-1: the context), or None: each follows the one before it."""
+    _same_device(pool, seqs)
+    rc = _binding().attend_tree(pool.ref, seqs.ref, pool.dev, layer, first, parent, q, out, softmax_scale, softcap, window, lse,
+                                workspace, dev_flags, _handle(stream))
+    if rc:
+        _check(rc, "stom_kv_attend_tree")
+
+
 def stom_kv_rotate(rope: Rope, pos, q=None, q_out=None, k=None, k_out=None, q_weight=None, k_weight=None, eps=1e-6,
                    stream=None):
     """q, k and their outputs: [n][heads][d], each with its own strides (an output may be its input); pos: int32 [n];
@@ -552,6 +581,15 @@ def stom_kv_compact(pool: KvPool, seqs: KvSeqs, table_out, refs_out, n_live, wor
                               _handle(stream)), "stom_kv_compact")
 
 
+def stom_kv_accept(pool: KvPool, seqs: KvSeqs, first, draft, chosen, path=None, n_accepted=None, next=None, parent=None,
+                   dev_flags=None, stream=None):
+    """Keeps each sequence's longest drafted path that was chosen.  first, parent as in stom_kv_attend_tree; draft, chosen,
+    path: int32 [n]; n_accepted, next: int32 [n_seqs]."""
+    _counts_of(pool, seqs)
+    _check(_binding().accept(pool.ref, seqs.ref, pool.dev, first, parent, draft, chosen, path, n_accepted, next, dev_flags,
+                             _handle(stream)), "stom_kv_accept")
+
+
 # ---------------------------------------------------------------- choice of the next token (include/stom_sample.h)
 
 def stom_sample_tokens(logits, u, token, temperature=None, top_k=None, top_p=None, min_p=None, logprob=None, kept=None,
@@ -560,3 +598,33 @@ def stom_sample_tokens(logits, u, token, temperature=None, top_k=None, top_p=Non
     rc = _binding().sample(logits, u, token, temperature, top_k, top_p, min_p, logprob, kept, dev_flags, _handle(stream))
     if rc:
         _check(rc, "stom_sample_tokens")
+
+
+# ---------------------------------------------------------------- products with 4-bit weights (include/stom_w4.h)
+
+class W4Matrix:
+    """[n][k] weights of 4 bits: codes uint8 [n][k / 2] (even columns in the low halves), scale and zero [n][k / group] of one
+    type and the same strides; zero None: a code stands for (code - 8) * scale."""
+
+    def __init__(self, codes, scale, zero=None):
+        if codes.dtype is not torch.uint8 or codes.dim() != 2 or (codes.shape[1] > 1 and codes.stride(1) != 1):
+            raise ValueError("codes: uint8 [n][k / 2] with adjacent entries")
+        n, k = codes.shape[0], 2 * codes.shape[1]
+        if (scale.dim() != 2 or scale.shape[0] != n or scale.shape[1] < 1 or k % scale.shape[1] or scale.dtype not in _DTYPE_CODE
+                or (scale.shape[1] > 1 and scale.stride(1) != 1) or scale.device != codes.device):
+            raise ValueError("scale: [n][k / group] with adjacent entries on the device of the codes")
+        if zero is not None and (zero.shape != scale.shape or zero.stride() != scale.stride() or zero.dtype != scale.dtype
+                                 or zero.device != scale.device):
+            raise ValueError("zero: like scale")
+        self.codes, self.scale, self.zero, self.dev = codes, scale, zero, codes.get_device()
+        self.n, self.k, self.group = n, k, k // scale.shape[1]
+        strides = [t.stride(0) if n > 1 else t.shape[1] for t in (codes, scale)]
+        self.desc = W4Desc(_addr(codes), _addr(scale), _addr(zero), n, k, self.group, dtype_code(scale.dtype), *strides)
+        self.ref = C.addressof(self.desc)
+
+
+def stom_w4_linear(w: W4Matrix, x, y, bias=None, add=None, stream=None):
+    """y = x W^T + bias + add; x: [rows][k], y and add: [rows][n], bias: [n], all bfloat16 or all float16; add may be y."""
+    rc = _binding().w4_linear(w.ref, w.dev, x, y, bias, add, _handle(stream))
+    if rc:
+        _check(rc, "stom_w4_linear")
