@@ -28,6 +28,7 @@
 
 #include "stom_async.cuh"
 #include "stom_internal.cuh"
+#include "stom_tensor.cuh"
 
 #include "stom_ctr.h"
 
@@ -58,58 +59,6 @@ __device__ __forceinline__ void cp_async16(uint32_t dst, const void *src) {
 __device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
 __device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
-
-// ---- tcgen05: tensor memory and the matrix product that reads both operands from shared memory
-__device__ __forceinline__ void tmem_alloc(uint32_t smem_dst, uint32_t cols) {  // one whole warp; writes the base address
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_dst), "r"(cols) : "memory");
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
-}
-__device__ __forceinline__ void tmem_dealloc(uint32_t taddr, uint32_t cols) {  // the same warp
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(taddr), "r"(cols) : "memory");
-}
-__device__ __forceinline__ void tc_fence_before_sync() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void tc_fence_after_sync() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-// writes of the generic proxy (cp.async, plain stores) become visible to the asynchronous proxy (the tensor cores)
-__device__ __forceinline__ void fence_proxy_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
-// Shared-memory matrix descriptor of a K-major operand in the 128-byte-swizzle layout: rows of 128 bytes, groups of 8
-// rows 1024 bytes apart; `addr` is where the tile starts (a multiple of 1024) plus 32 bytes per step of 16 channels.
-__device__ __forceinline__ uint64_t umma_desc_k128(uint32_t addr) {
-    return (uint64_t)((addr & 0x3FFFFu) >> 4) | (1ull << 16) | ((uint64_t)(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
-}
-// Instruction descriptor of kind::f16: binary32 accumulator, both operands of type `fmt` (0 fp16, 1 bf16) and K-major,
-// a tile of 128 rows by n columns
-__device__ __forceinline__ uint32_t umma_idesc(uint32_t fmt, uint32_t n) {
-    return (1u << 4) | (fmt << 7) | (fmt << 10) | ((n >> 3) << 17) | ((128u >> 4) << 24);
-}
-// D[tmem] (+)= A[smem] . B[smem]^T, issued by one thread
-__device__ __forceinline__ void umma_ss(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "setp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
-        ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
-        : "memory");
-}
-// all products issued so far by this thread arrive (once) on the mbarrier when they have completed
-__device__ __forceinline__ void umma_commit(uint32_t bar) {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
-}
-// 32 consecutive accumulator columns of this thread's lane (row) of tensor memory
-__device__ __forceinline__ void tmem_ld32(uint32_t taddr, float (&v)[32]) {
-    uint32_t r[32];
-    asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, "
-        "%18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
-        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
-          "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]),
-          "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]),
-          "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
-        : "r"(taddr)
-        : "memory");
-    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-#pragma unroll
-    for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
-}
 
 // position of d2(a, b) in the packed lower triangle
 __device__ __forceinline__ int tri(int a, int b) { return a >= b ? a * (a + 1) / 2 + b : b * (b + 1) / 2 + a; }
@@ -282,14 +231,14 @@ __global__ void __launch_bounds__(kMgThreads, 2) ctr_merge_kernel(const MergePar
         if (!dead) {
             // squared norms from the diagonal: row r of tile 0 for r < 128, of tile 1 above
             if (jw == 0 && 32 * q < L.rows) {
-                tmem_ld32(lane_base + 32 * q, v);
+                tmem_load(lane_base + 32 * q, v);
                 float dg = 0.0f;
 #pragma unroll
                 for (int i = 0; i < 32; ++i) dg = i == lane ? v[i] : dg;
                 if (r0 < N) nrm[r0] = dg;
             }
             if (jw == 1 && two_tiles) {
-                tmem_ld32(lane_base + 128 + R1 + 32 * q, v);
+                tmem_load(lane_base + 128 + R1 + 32 * q, v);
                 float dg = 0.0f;
 #pragma unroll
                 for (int i = 0; i < 32; ++i) dg = i == lane ? v[i] : dg;
@@ -301,7 +250,7 @@ __global__ void __launch_bounds__(kMgThreads, 2) ctr_merge_kernel(const MergePar
             const float inv_d = 1.0f / (float)D;
             // tile 0: rows 32 q .. 32 q + 31 need column blocks 0 .. q
             for (int cb = jw; cb <= q && 32 * q < L.rows; cb += 4) {
-                tmem_ld32(lane_base + 32 * cb, v);
+                tmem_load(lane_base + 32 * cb, v);
                 if (r0 < N) {
                     const float nr = nrm[r0];
 #pragma unroll
@@ -314,7 +263,7 @@ __global__ void __launch_bounds__(kMgThreads, 2) ctr_merge_kernel(const MergePar
             // tile 1: rows R1 + 32 q .. need column blocks 0 .. (R1 + 32 q + 31) / 32; only rows from 128 on are new
             if (two_tiles && R1 + 32 * q + 31 >= 128) {
                 for (int cb = jw; cb <= (R1 + 32 * q + 31) >> 5; cb += 4) {
-                    tmem_ld32(lane_base + 128 + 32 * cb, v);
+                    tmem_load(lane_base + 128 + 32 * cb, v);
                     if (r1 >= 128 && r1 < N) {
                         const float nr = nrm[r1];
 #pragma unroll

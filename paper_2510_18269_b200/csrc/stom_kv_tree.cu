@@ -1,21 +1,66 @@
 // Attention of several new tokens per sequence over a paged cache (stom_kv_attend_tree).
+//
+//   out_j = sum_t exp(x_jt) V_t / sum_t exp(x_jt),  x_jt = scale <q_j, K_t>, capped if asked for, t over what node j sees.
+//
+// The query heads of a kv head and the nodes of a sequence together are the ROWS of two products with the same keys and
+// values: row r is node r / group, head r % group.  Rows are cut into tiles of 128, the height of a tcgen05 product, and a
+// UNIT is one (sequence, row tile, kv head).  What bounds it: a tile of 128 rows does 4 * 128 flops for every pair of a
+// key's and a value's elements that it reads, 256 flops a byte, about as many as the device has; up to one tile it is the
+// cache's bytes, beyond (many heads times nodes, a question's prefill) the products, and the exponentials beside them.
+//
+// Split.  As for one new token, the work is one line of TILES of tokens (128, or 64 where head_dim is 256): sequence by
+// sequence, row tile by row tile, head by head.  Each block, one a multiprocessor, takes an equal, contiguous stretch of it;
+// units that a stretch's end cuts are joined by a second kernel over two partial results per block.
+//
+// A block.  Four warps load: 16-byte asynchronous copies, any page size, any strides, into a ring of tiles of keys and of
+// values, each of them in the 128-byte-swizzled layout in which keys are a K-major operand (rows: tokens) and values an
+// MN-major one (rows: the summed axis).  One thread issues the products: S = Q K^T of tile t + 2 when the values' product
+// of tile t is done, O += P V from tensor memory.  Eight warps do the softmax: a thread has half of the columns of one row;
+// the two halves exchange their maximum through shared memory.  P takes the place of S in tensor memory, in 16 bits.
+//
+// The running maximum moves only when a row's scores rise by more than 2^8 above it: the weights then are at most 2^8 (no
+// loss: they are floating-point numbers, and bf16 has binary32's exponents; in fp16 the reference weight is 2^7, so that
+// they end at 2^15 and begin at 2^-24, 2^-31 of it), and the accumulators in tensor memory are rescaled once or twice a unit
+// instead of once a tile.  Weights are rounded once to the pool's type for the second product; their sum is taken before.
+//
+// Masks.  Only tiles that reach the nodes, or a window's edge, are masked: 32 bits a row and 32 columns, from the range of
+// the context that the row sees and the bits of its path, which a row walks once per unit.  A product multiplies what a row
+// does not see by zero, which is not enough where it is no number: in such tiles the values are looked through, what is no
+// number is taken out, and put back afterwards in the rows that see it.
 #include "stom_kv.cuh"
+#include "stom_tensor.cuh"
 
 #include <math.h>
+
+#include <type_traits>
 
 namespace stom {
 
 namespace {
 
+constexpr int kRows = 128;            // rows of a tile
+constexpr int kMaxBlocks = 256;       // blocks of the grid the workspace has room for
+constexpr int kSoftWarps = 8, kLoadWarps = 4, kWarps = kSoftWarps + kLoadWarps + 1;
+constexpr int kSoftThreads = kSoftWarps * 32, kLoadThreads = kLoadWarps * 32, kThreads = kWarps * 32;
+constexpr int kPathWords = STOM_KV_MAX_TREE / 32;
+constexpr float kSlack = 8.f;         // log2 of what weights may exceed 1 by
+constexpr unsigned long long kWaitLimitNs = 1000000000ull;   // a wait that has taken 1 s ends the block
+
+// Of a unit that crosses a block's end, for the joining kernel
+struct Open {
+    int32_t row0, rows, node0, head;  // first row of the tile, rows it has, row of q of the sequence's first node, kv head
+};
+
 struct KvTreeParams {
-    const char *k, *v;            // at the layer
+    const char *k, *v;                // at the layer
     int64_t stride_page, stride_token, stride_head;
     const int32_t *table;
     const int32_t *len;
     int64_t table_stride;
     int32_t n_seqs, n_pages, max_tokens;
     FastDiv page;
-    int32_t n_kv_heads, group;    // query heads per kv head
+    int32_t n_kv_heads, group;        // query heads per kv head
+    FastDiv by_group;
     int32_t n_tokens;
     const int32_t *first, *parent;
     const char *q;
@@ -25,116 +70,760 @@ struct KvTreeParams {
     char *out;
     int64_t out_stride_token, out_stride_head;
     float *lse;
+    int32_t part_rows;                // rows a partial result has room for
+    float *part_o;                    // [blocks][2][part_rows][d]
+    float2 *part_ml;                  // [blocks][2][part_rows]: maximum and sum
+    Open *open;                       // [blocks]: unit that begins in the block and goes on behind it (rows 0: none)
+    int32_t *goes_on;                 // [blocks]: the unit that came in from the block before goes on behind this one too
     uint32_t *flags;
 };
 
-// Node range of a sequence; false: skipped
-__device__ __forceinline__ bool nodes_of(const KvTreeParams &p, int i, int &a, int &n, int &base) {
-    a = p.first[i];
-    const int b = p.first[i + 1], len = max(p.len[i], 0);
-    n = b - a;
-    base = len - n;
-    return a >= 0 && a <= b && b <= p.n_tokens && n <= len && (!p.parent || n <= STOM_KV_MAX_TREE);
+template <int D>
+struct Shape {
+    static constexpr int kTok = D == 256 ? 64 : 128;      // tokens of a tile
+    static constexpr int kHalf = kTok * D * 2;            // bytes of a tile's keys or values
+    static constexpr int kBlock = kTok * 128;             // bytes of 64 channels of them
+    static constexpr int kSlots = D == 64 ? 8 : 4;        // tiles of keys or values in the ring
+    static constexpr int kQ = kRows * D * 2;
+    static constexpr int kQBufs = D == 256 ? 1 : 2;
+    static constexpr int kCols = kTok / 2;                // columns of S that a softmax thread has
+    static constexpr int kSmem = 1024 + kSlots * kHalf + kQBufs * kQ;
+    static_assert(kSmem <= 220 * 1024, "shared memory");
+};
+
+// What a unit is, and the part of it that a block has
+struct Unit {
+    int32_t node0, n, base;           // row of q of the sequence's first node, its nodes, tokens before them
+    int32_t seq, head, row0, rows;    // rows: of this tile
+    int32_t first, end;               // tokens that some row looks at
+    int32_t tile0, tiles;             // the block's part
+    int32_t ends;                     // bit 0: it has the unit's first tile, bit 1: its last
+};
+
+struct Shared {                       // beside the operands
+    uint64_t full[8], empty[8], q_full[2], q_empty[2], unit_full[4], s_full[2], p_full[2], pv_done, drained;
+    uint32_t tmem, abort, never;      // never: stays 0
+    int32_t start_seq, start_tile_row, start_head, start_tile;
+    uint64_t warp_sum[kWarps];
+    Unit unit[4];
+    uint32_t tokens[8][4];            // per tile: which rows are tokens
+    uint32_t dirty[4];                // tokens of the tile with values that are no numbers
+    uint32_t seen[4][kRows];          // tokens of the tile that a row sees
+    float top[2][2][kRows];           // [tile's parity][half][row]
+    float sum[2][kRows];
+    uint32_t path[kRows][kPathWords];
+    int16_t parent[4][STOM_KV_MAX_TREE];
+};
+
+struct Seq {
+    int node0, n, base;
+};
+// A sequence's nodes; n = 0 if there are none or it does not fit
+__device__ __forceinline__ Seq seq_of(const KvTreeParams &p, int i, bool tell = false) {
+    const int a = p.first[i], b = p.first[i + 1], raw = p.len[i], len = max(raw, 0), n = b - a;
+    const bool good = a >= 0 && a <= b && b <= p.n_tokens && n <= len && (!p.parent || n <= STOM_KV_MAX_TREE);
+    if (tell && p.flags && (!good || (n > 0 && raw > p.max_tokens))) atomicOr(p.flags, STOM_FLAG_BAD_INDEX);
+    return Seq{a, good ? n : 0, len - n};
+}
+__device__ __forceinline__ int row_tiles(const KvTreeParams &p, int n) {
+    return (int)(((int64_t)n * p.group + kRows - 1) / kRows);
+}
+// Tokens that the rows of a tile look at, and tiles of them (at least one: a unit without any still has an output)
+template <int TOK>
+__device__ __forceinline__ int span_of(const KvTreeParams &p, const Seq &s, int tile_row, int &first, int &end) {
+    const int jf = (int)div_by(p.by_group, (uint32_t)tile_row * kRows);
+    const int jl = min(s.n - 1, (int)div_by(p.by_group, (uint32_t)tile_row * kRows + kRows - 1));
+    end = min(s.base + jl + 1, p.max_tokens);
+    first = p.window > 0 ? min(end, max(0, s.base + (p.parent ? 0 : jf) + 1 - p.window)) : 0;
+    return max(1, (end - first + TOK - 1) / TOK);
 }
 
-// One warp a (node, query head): a lane has a token at a time, then channels.
-template <typename T, int D>
-__global__ void __launch_bounds__(128) kv_tree_kernel(const __grid_constant__ KvTreeParams p) {
-    __shared__ float qs[4][D];
-    __shared__ uint32_t path[4][STOM_KV_MAX_TREE / 32];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, i = blockIdx.x, h = blockIdx.y * 4 + warp;
-    const int heads = p.n_kv_heads * p.group;
-    grid_dependency_wait();
-    int a, n, base;
-    if (!nodes_of(p, i, a, n, base)) {
-        if (p.flags && threadIdx.x == 0) atomicOr(p.flags, STOM_FLAG_BAD_INDEX);
-        return;
-    }
-    if (h >= heads) return;
-    if (p.flags && lane == 0 && n > 0 && p.len[i] > p.max_tokens) atomicOr(p.flags, STOM_FLAG_BAD_INDEX);
-    const int hk = h / p.group;
-    for (int j = 0; j < n; ++j) {
-        const T *q = reinterpret_cast<const T *>(p.q) + (a + j) * p.q_stride_token + h * p.q_stride_head;
-        for (int c = lane; c < D; c += 32) qs[warp][c] = static_cast<float>(q[c]);
-        for (int w = lane; w < STOM_KV_MAX_TREE / 32; w += 32) path[warp][w] = 0;
-        __syncwarp();
-        int depth = j;
-        if (p.parent) {
-            depth = 0;
-            if (lane == 0)
-                for (int c = j; c >= 0; ++depth) {
-                    if (!p.window || depth < p.window) path[warp][c >> 5] |= 1u << (c & 31);
-                    int up = p.parent[a + c];
-                    if (up < -1 || up >= c) {
-                        if (p.flags) atomicOr(p.flags, STOM_FLAG_BAD_INDEX);
-                        up = -1;
-                    }
-                    c = up;
-                }
-            depth = __shfl_sync(~0u, depth, 0) - 1;
-            __syncwarp();
-        }
-        const int end = min(base + j + 1, p.max_tokens);
-        const int begin = p.window ? (int)max(0ll, (long long)base + depth + 1 - p.window) : 0;
-        float m = -INFINITY, l = 0.f, o[D / 32];
-        for (int c = 0; c < D / 32; ++c) o[c] = 0.f;
-        for (int t0 = min(begin, base); t0 < end; t0 += 32) {
-            const int t = t0 + lane;
-            bool ok = t < end && (t >= base && p.parent ? path[warp][(t - base) >> 5] >> ((t - base) & 31) & 1u : t >= begin);
-            int64_t off = 0;
-            if (ok) {
-                const int pg = (int)div_by(p.page, (uint32_t)t), id = p.table[i * p.table_stride + pg];
-                if ((uint32_t)id >= (uint32_t)p.n_pages) {
-                    ok = false;
-                    if (p.flags) atomicOr(p.flags, STOM_FLAG_BAD_INDEX);
-                } else {
-                    off = 2 * (id * p.stride_page + (t - pg * (int)p.page.d) * p.stride_token + hk * p.stride_head);
-                }
-            }
-            float x = -INFINITY;
-            if (ok) {
-                const T *k = reinterpret_cast<const T *>(p.k + off);
-                float s = 0.f;
-                for (int c = 0; c < D; ++c) s += qs[warp][c] * static_cast<float>(k[c]);
-                x = s * p.scale;
-                if (p.cap > 0.f) x = p.cap * tanhf(x / p.cap);
-            }
-            float top = x;
-            for (int s = 16; s; s >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, s));
-            const float mn = fmaxf(m, top), ref = mn == -INFINITY ? 0.f : mn, alpha = expf(m - ref);
-            const float w = ok ? expf(x - ref) : 0.f;
-            m = mn;
-            l = l * alpha + w;
-            for (int c = 0; c < D / 32; ++c) o[c] *= alpha;
-            for (int s = 0; s < 32; ++s) {
-                const float ws = __shfl_sync(~0u, w, s);
-                const bool is = __shfl_sync(~0u, ok, s);
-                const int64_t at = __shfl_sync(~0u, off, s);
-                if (!is) continue;
-                const T *v = reinterpret_cast<const T *>(p.v + at);
-                for (int c = 0; c < D / 32; ++c) o[c] += ws * static_cast<float>(v[c * 32 + lane]);
-            }
-        }
-        for (int s = 16; s; s >>= 1) l += __shfl_xor_sync(~0u, l, s);
-        const float inv = l == 0.f ? 0.f : 1.f / l;
-        T *dst = reinterpret_cast<T *>(p.out) + (a + j) * p.out_stride_token + h * p.out_stride_head;
-        for (int c = 0; c < D / 32; ++c) dst[c * 32 + lane] = from_float<T>(o[c] * inv);
-        if (p.lse && lane == 0) p.lse[(int64_t)(a + j) * heads + h] = l == 0.f ? -INFINITY : m + logf(l);
-        __syncwarp();
-    }
+__device__ __forceinline__ void arrive_when_copied(uint32_t bar) {
+    asm volatile("cp.async.mbarrier.arrive.noinc.shared.b64 [%0];" ::"r"(bar) : "memory");
 }
-
+__device__ __forceinline__ void sync_some(int id, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
+__device__ __forceinline__ bool any_of_some(int id, int threads, bool mine) {
+    uint32_t r;
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\t"
+        "setp.ne.b32 p, %1, 0;\n\t"
+        "bar.red.or.pred q, %2, %3, p;\n\t"
+        "selp.u32 %0, 1, 0, q;\n\t}"
+        : "=r"(r)
+        : "r"((uint32_t)mine), "r"(id), "r"(threads)
+        : "memory");
+    return r != 0;
+}
+__device__ __forceinline__ float exp2_of(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+// Which of two 16-bit numbers are no finite ones: bits 15 and 31
 template <typename T>
-int32_t dispatch(const KvTreeParams &p, int d, cudaStream_t s) {
-    const dim3 grid(p.n_seqs, (p.n_kv_heads * p.group + 3) / 4), block(128);
-    cudaError_t e = d == 64    ? launch_after_producer(kv_tree_kernel<T, 64>, grid, block, 0, s, p)
-                    : d == 128 ? launch_after_producer(kv_tree_kernel<T, 128>, grid, block, 0, s, p)
-                               : launch_after_producer(kv_tree_kernel<T, 256>, grid, block, 0, s, p);
+__device__ __forceinline__ uint32_t not_finite(uint32_t w) {
+    return ((w & 0x7fff7fffu) + (std::is_same<T, __nv_bfloat16>::value ? 0x00800080u : 0x04000400u)) & 0x80008000u;
+}
+
+template <typename T, int D>
+__global__ void __launch_bounds__(kThreads, 1) kv_tree_kernel(const __grid_constant__ KvTreeParams p) {
+    using S = Shape<D>;
+    constexpr int kTok = S::kTok, kHalf = S::kHalf, kBlock = S::kBlock, kSlots = S::kSlots, kQBufs = S::kQBufs, kCols = S::kCols;
+    constexpr bool kHalfType = std::is_same<T, __half>::value;
+    constexpr float kLift = kHalfType ? 7.f : 0.f;   // log2 of the weight of a score at the reference
+    constexpr uint32_t kFmt = kHalfType ? 0u : 1u;
+    extern __shared__ uint8_t raw_smem[];
+    __shared__ Shared sh;
+    uint8_t *smem = raw_smem + ((1024u - (smem_u32(raw_smem) & 1023u)) & 1023u);   // the swizzle goes by addresses
+    const uint32_t ring_u = smem_u32(smem), q_u = ring_u + kSlots * kHalf;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    volatile uint32_t *abort_flag = &sh.abort;
+    auto bar = [&](const uint64_t &b) { return smem_u32(&b); };
+
+    if (tid == 0) {
+        for (int i = 0; i < 8; ++i) mbar_init(bar(sh.full[i]), kLoadThreads + kLoadWarps), mbar_init(bar(sh.empty[i]), 1);
+        for (int i = 0; i < 2; ++i) mbar_init(bar(sh.q_full[i]), kLoadThreads), mbar_init(bar(sh.q_empty[i]), 1);
+        for (int i = 0; i < 4; ++i) mbar_init(bar(sh.unit_full[i]), kLoadThreads);
+        for (int i = 0; i < 2; ++i) mbar_init(bar(sh.s_full[i]), 1), mbar_init(bar(sh.p_full[i]), kSoftThreads);
+        mbar_init(bar(sh.pv_done), 1), mbar_init(bar(sh.drained), 1);
+        sh.abort = sh.never = 0;
+        mbar_init_fence();
+    }
+    if (warp == kWarps - 1) tmem_alloc(smem_u32(&sh.tmem), 512);
+    grid_dependency_wait();
+    grid_launch_dependents();   // the joining kernel may take its places now; it waits for this grid's end
+
+    // ---- the stretch of this block: where it begins on the line, and how many tiles it has
+    int64_t left;
+    {
+        uint64_t *before = reinterpret_cast<uint64_t *>(smem);   // tiles before each sequence
+        static_assert(kSlots * kHalf >= STOM_KV_MAX_SEQS * 8, "a number for each sequence");
+        const int seg = (p.n_seqs + kThreads - 1) / kThreads, b0 = tid * seg;   // sequences a thread adds up
+        auto tiles_of = [&](const Seq &s, int tr) {
+            int f, e;
+            return (uint64_t)span_of<kTok>(p, s, tr, f, e);
+        };
+        uint64_t mine = 0;
+        for (int j = 0; j < seg; ++j) {
+            const int b = b0 + j;
+            Seq s = {0, 0, 0};
+            if (b < p.n_seqs) s = seq_of(p, b, blockIdx.x == 0);
+            const int trs = row_tiles(p, s.n);
+            uint64_t sum = 0;
+            if (trs <= 8)
+                for (int tr = 0; tr < trs; ++tr) sum += tiles_of(s, tr);
+            // long ones: the warp together
+            for (uint32_t many = __ballot_sync(~0u, trs > 8); many; many &= many - 1) {
+                const int of = __ffs(many) - 1;
+                const Seq o = {0, __shfl_sync(~0u, s.n, of), __shfl_sync(~0u, s.base, of)};
+                const int n = __shfl_sync(~0u, trs, of);
+                uint64_t part = 0;
+                for (int tr = lane; tr < n; tr += 32) part += tiles_of(o, tr);
+#pragma unroll
+                for (int x = 16; x; x >>= 1) part += __shfl_xor_sync(~0u, part, x);
+                if (lane == of) sum = part;
+            }
+            if (b < p.n_seqs) before[b] = mine;
+            mine += sum * p.n_kv_heads;
+        }
+        uint64_t upto = mine;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const uint64_t v = __shfl_up_sync(~0u, upto, o);
+            if (lane >= o) upto += v;
+        }
+        if (lane == 31) sh.warp_sum[warp] = upto;
+        __syncthreads();
+        uint64_t total = 0, ahead = upto - mine;
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) {
+            if (w < warp) ahead += sh.warp_sum[w];
+            total += sh.warp_sum[w];
+        }
+        for (int j = 0; j < seg && b0 + j < p.n_seqs; ++j) before[b0 + j] += ahead;
+        __syncthreads();
+        const uint64_t per = max((uint64_t)1, (total + gridDim.x - 1) / gridDim.x);
+        const uint64_t f0 = min(total, (uint64_t)blockIdx.x * per);
+        left = (int64_t)(min(total, f0 + per) - f0);
+        if (warp == 0 && left > 0) {
+            // its first tile's sequence: the last that begins at f0 or before (of several, the others are empty)
+            int low = 0, high = p.n_seqs;
+            while (high - low > 1) {
+                const int step = (high - low + 31) / 32, at = low + step * lane;
+                const uint32_t yes = __ballot_sync(~0u, at < high && before[at] <= f0);
+                low += step * (31 - __clz(yes));
+                high = min(high, low + step);
+            }
+            const Seq s = seq_of(p, low);
+            uint64_t in = f0 - before[low];
+            const int trs = row_tiles(p, s.n);
+            for (int t0 = 0;; t0 += 32) {
+                const uint64_t n = t0 + lane < trs ? tiles_of(s, t0 + lane) * p.n_kv_heads : 0;
+                uint64_t sum = n;
+#pragma unroll
+                for (int o = 1; o < 32; o <<= 1) {
+                    const uint64_t v = __shfl_up_sync(~0u, sum, o);
+                    if (lane >= o) sum += v;
+                }
+                const uint32_t here = __ballot_sync(~0u, in < sum);
+                if (here || t0 + 32 >= trs) {
+                    if (here && lane == __ffs(here) - 1) {
+                        const uint64_t rest = in - (sum - n), each = n / p.n_kv_heads;
+                        sh.start_seq = low;
+                        sh.start_tile_row = t0 + lane;
+                        sh.start_head = (int)(rest / each);
+                        sh.start_tile = (int)(rest - rest / each * each);
+                    }
+                    break;
+                }
+                in -= __shfl_sync(~0u, sum, 31);
+            }
+        }
+    }
+    tc_fence_before_sync();
+    __syncthreads();   // the numbers have been read: operands may take their place
+    tc_fence_after_sync();
+    const uint32_t tmem = sh.tmem;
+    const uint32_t n_tiles = (uint32_t)left;
+    auto wait = [&](const uint64_t &b, uint32_t parity) {
+        if (mbar_wait_bounded(bar(b), parity & 1u, abort_flag, kWaitLimitNs)) return true;
+        *abort_flag = 1;
+        return false;
+    };
+    // place of a tile's values in the order of loads: K0 K1 V0 K2 V1 ... V(n-1)
+    auto half_of_v = [&](uint32_t c) { return c + 1 < n_tiles ? 2 * c + 2 : 2 * c + 1; };
+    int open_rows = 0, goes_on = 0;
+
+    if (warp >= kSoftWarps && warp < kSoftWarps + kLoadWarps && left > 0) {
+        // ================================================================ loads
+        const int lt = tid - kSoftThreads, lw = warp - kSoftWarps;
+        constexpr int kChunks = D / 8;                    // 16-byte chunks of a row
+        constexpr int kOwn = kTok / kLoadWarps;           // rows of a tile that a warp copies
+        constexpr int kPerCopy = 32 / kChunks;            // rows that one warp-wide copy covers
+        // where the page look-ups are: a tile ahead of the copies
+        int seq = sh.start_seq, tr = sh.start_tile_row, head = sh.start_head, tile = sh.start_tile;
+        Seq s = seq_of(p, seq);
+        int trs = row_tiles(p, s.n), first, end, tiles = span_of<kTok>(p, s, tr, first, end);
+        int64_t to_look = left;
+        constexpr int kNone = INT32_MIN;
+        int page = kNone;
+        int64_t rest = 0;
+        auto look_up = [&]() {
+            page = kNone;
+            const int t = first + tile * kTok + lw * kOwn + lane % kOwn;
+            if (t < end) {
+                const uint32_t pg = div_by(p.page, (uint32_t)t);
+                rest = (int64_t)(t - (int)(pg * p.page.d)) * p.stride_token + (int64_t)head * p.stride_head;
+                page = p.table[seq * p.table_stride + pg];
+                if (page == kNone) page = -1;
+            }
+        };
+        auto advance = [&]() {   // to the next tile of the line
+            if (++tile < tiles) return;
+            tile = 0;
+            if (++head < p.n_kv_heads) return;
+            head = 0;
+            if (++tr >= trs) {
+                tr = 0;
+                do {                                      // there is one: tiles are left
+                    s = seq_of(p, min(++seq, p.n_seqs - 1));
+                    trs = row_tiles(p, s.n);
+                } while (trs == 0 && seq < p.n_seqs);
+            }
+            tiles = span_of<kTok>(p, s, tr, first, end);
+        };
+        uint32_t half = 0, unit = 0;
+        bool live = true;
+        auto wait_all = [&](const uint64_t &b, uint32_t parity) { return __all_sync(~0u, wait(b, parity)) != 0; };
+        auto copy_half = [&](const char *from, int64_t off) {
+            const uint32_t slot = half % kSlots, round = half / kSlots;
+            ++half;
+            if (round > 0 && !wait_all(sh.empty[slot], round - 1)) return false;
+            const uint32_t dst = ring_u + slot * kHalf;
+            const int sub = lane / kChunks, chunk = lane % kChunks;
+#pragma unroll 8
+            for (int i = 0; i < kOwn / kPerCopy; ++i) {
+                const int64_t o = __shfl_sync(~0u, off, i * kPerCopy + sub);
+                const int row = lw * kOwn + i * kPerCopy + sub;
+                copy16_async(dst + (chunk >> 3) * kBlock + row * 128 + (((chunk & 7) ^ (row & 7)) << 4),
+                             from + (o < 0 ? 0 : o) + chunk * 16, o < 0 ? 0u : 16u);
+            }
+            arrive_when_copied(bar(sh.full[slot]));
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(sh.full[slot]));
+            return true;
+        };
+        look_up();
+        int64_t off = -1, off_before = -1;
+        for (uint32_t c = 0; c < n_tiles && live; ++c) {
+            if (c == 0 || tile == 0) {
+                // a unit begins: its description, its parents, its rows of q
+                const uint32_t buf = unit % kQBufs, round = unit / kQBufs;
+                if (round > 0 && !wait_all(sh.q_empty[buf], round - 1)) {
+                    live = false;
+                    break;
+                }
+                const int rows = min(kRows, s.n * p.group - tr * kRows);
+                if (lt == 0) {
+                    const int part = (int)min((int64_t)(tiles - tile), to_look);
+                    sh.unit[unit & 3] = Unit{s.node0, s.n, s.base, seq, head, tr * kRows, rows, first, end, tile, part,
+                                             (tile == 0 ? 1 : 0) | (tile + part == tiles ? 2 : 0)};
+                }
+                if (p.parent)
+                    for (int j = lt; j < s.n; j += kLoadThreads) {
+                        int up = p.parent[s.node0 + j];
+                        if (up < -1 || up >= j) {
+                            if (p.flags) atomicOr(p.flags, STOM_FLAG_BAD_INDEX);
+                            up = -1;
+                        }
+                        sh.parent[unit & 3][j] = (int16_t)up;
+                    }
+                mbar_arrive(bar(sh.unit_full[unit & 3]));
+                const int sub = lt / kChunks, chunk = lt % kChunks;
+#pragma unroll 4
+                for (int i = 0; i < kRows * kChunks / kLoadThreads; ++i) {
+                    const int r = i * (kLoadThreads / kChunks) + sub, row = tr * kRows + r;
+                    const int node = (int)div_by(p.by_group, (uint32_t)row), g = row - node * p.group;
+                    const char *src = p.q;
+                    if (r < rows)
+                        src += 2 * ((s.node0 + node) * p.q_stride_token + (head * p.group + g) * p.q_stride_head) + chunk * 16;
+                    copy16_async(q_u + buf * S::kQ + (chunk >> 3) * (kRows * 128) + r * 128 + (((chunk & 7) ^ (r & 7)) << 4), src,
+                                 r < rows ? 16u : 0u);
+                }
+                arrive_when_copied(bar(sh.q_full[buf]));
+                ++unit;
+            }
+            const bool ok = (uint32_t)page < (uint32_t)p.n_pages;
+            if (page != kNone && !ok && p.flags) atomicOr(p.flags, STOM_FLAG_BAD_INDEX);
+            off = ok ? 2 * (page * p.stride_page + rest) : -1;
+            const uint32_t is = __ballot_sync(~0u, ok);
+            if (lane == 0) {
+                if (kOwn == 32) sh.tokens[c & 7][lw] = is;
+                else reinterpret_cast<uint16_t *>(sh.tokens[c & 7])[lw] = (uint16_t)is;
+            }
+            if (--to_look > 0) {
+                advance();
+                look_up();
+            }
+            live = copy_half(p.k, off) && (c == 0 || copy_half(p.v, off_before));
+            off_before = off;
+        }
+        if (live) copy_half(p.v, off_before);
+        asm volatile("cp.async.wait_all;" ::: "memory");
+    } else if (warp == kWarps - 1 && left > 0) {
+        // ================================================================ products
+        if (lane == 0) {
+            const uint32_t idesc_s = umma_idesc(kFmt, kTok), idesc_o = umma_idesc(kFmt, D) | kUmmaRightMn;
+            uint32_t unit = 0, in_unit = 0, unit_tiles = 0, fresh = 0;   // of the first products; fresh: bit c & 31, a unit begins
+            bool live = true;
+            auto scores = [&](uint32_t c) {
+                const uint32_t k = c == 0 ? 0 : 2 * c - 1, slot = k % kSlots;
+                const bool begins = in_unit == unit_tiles;
+                if (begins) {
+                    if (!wait(sh.unit_full[unit & 3], unit >> 2)) return false;
+                    unit_tiles = sh.unit[unit & 3].tiles;
+                    in_unit = 0;
+                    if (!wait(sh.q_full[unit % kQBufs], unit / kQBufs)) return false;
+                    ++unit;
+                }
+                fresh = (fresh & ~(1u << (c & 31))) | ((begins ? 1u : 0u) << (c & 31));
+                ++in_unit;
+                if (!wait(sh.full[slot], k / kSlots)) return false;
+                fence_proxy_async();
+                tc_fence_after_sync();
+                const uint32_t qb = q_u + ((unit - 1) % kQBufs) * S::kQ, kb = ring_u + slot * kHalf;
+#pragma unroll
+                for (int ks = 0; ks < D / 16; ++ks)
+                    umma_ss(tmem + (c & 1) * 128, umma_desc_k128(qb + (ks >> 2) * (kRows * 128) + (ks & 3) * 32),
+                            umma_desc_k128(kb + (ks >> 2) * kBlock + (ks & 3) * 32), idesc_s, ks != 0);
+                umma_commit(bar(sh.empty[slot]));
+                umma_commit(bar(sh.s_full[c & 1]));
+                if (in_unit == unit_tiles) umma_commit(bar(sh.q_empty[(unit - 1) % kQBufs]));
+                return true;
+            };
+            live = scores(0) && (n_tiles < 2 || scores(1));
+            for (uint32_t c = 0; c < n_tiles && live; ++c) {
+                const uint32_t v = half_of_v(c), slot = v % kSlots;
+                live = wait(sh.full[slot], v / kSlots) && wait(sh.p_full[c & 1], c >> 1);
+                if (!live) break;
+                fence_proxy_async();
+                tc_fence_after_sync();
+                const uint32_t vb = ring_u + slot * kHalf;
+                const uint32_t more = !(fresh >> (c & 31) & 1u);
+#pragma unroll
+                for (int ks = 0; ks < kTok / 16; ++ks)
+                    umma_ts(tmem + 256, tmem + (c & 1) * 128 + ks * 8, umma_desc_mn128(vb + ks * 2048, kBlock), idesc_o,
+                            more | (ks != 0));
+                umma_commit(bar(sh.empty[slot]));
+                umma_commit(bar(sh.pv_done));
+                if (c + 2 < n_tiles) live = wait(sh.pv_done, c) && scores(c + 2);   // S of tile c + 2 takes P's place
+            }
+            umma_commit(bar(sh.drained));   // before tensor memory is given back
+            if (!mbar_wait_bounded(bar(sh.drained), 0, &sh.never, kWaitLimitNs)) *abort_flag = 1;
+        }
+    } else if (warp < kSoftWarps && left > 0) {
+        // ================================================================ softmax
+        const int quarter = warp & 3, side = warp >> 2, row = quarter * 32 + lane;
+        const uint32_t lane_base = tmem + ((uint32_t)(32 * quarter) << 16);
+        const float log2e = 1.4426950408889634f;
+        const float s1 = p.cap > 0.f ? p.scale / p.cap : p.scale * log2e, s2 = p.cap * log2e;
+        // A wait that fails (the block has given up) is not a reason to leave the others alone at a barrier: the unit goes on
+        // with what is there, and all leave together where the next one begins.
+        auto wait_on = [&](const uint64_t &b, uint32_t parity) {
+            const bool ok = wait(b, parity);
+            __syncwarp();
+            return ok;
+        };
+        uint32_t c = 0;
+        for (uint32_t unit = 0; c < n_tiles; ++unit) {
+            if (any_of_some(5, kSoftThreads, !wait_on(sh.unit_full[unit & 3], unit >> 2))) break;
+            const Unit u = sh.unit[unit & 3];
+            const int at = u.row0 + row, node = (int)div_by(p.by_group, (uint32_t)at);
+            const bool is = row < u.rows, some = quarter * 32 < u.rows;
+            // the context that the row sees: [begin, until), and with a tree the bits of its path from u.base on
+            int depth = node;
+            if (p.parent) {
+                if (side == 0) {
+#pragma unroll
+                    for (int w = 0; w < kPathWords; ++w) sh.path[row][w] = 0;
+                    depth = 0;
+                    if (is)
+                        for (int j = node; j >= 0; j = sh.parent[unit & 3][j], ++depth)
+                            if (!p.window || depth < p.window) sh.path[row][j >> 5] |= 1u << (j & 31);
+                    sh.sum[0][row] = __int_as_float(depth - 1);
+                }
+                sync_some(1 + quarter, 64);
+                depth = __float_as_int(sh.sum[0][row]);
+            }
+            const int begin = !is ? INT32_MAX : p.window > 0 ? max(0, u.base + depth + 1 - p.window) : 0;
+            const int until = p.parent ? u.base : u.base + node + 1;
+            // tiles before this token (and, with a window, from that one on) are not masked
+            const int clean_end = u.n == 1 ? u.end : p.parent ? u.base : u.base + (int)div_by(p.by_group, (uint32_t)u.row0) + 1;
+            const int clean_begin = p.window > 0 ? u.base + u.n - p.window : 0;
+            float m_ref = -INFINITY, l = 0.f;
+            for (int t = 0; t < u.tiles; ++t, ++c) {
+                const int t_all = u.first + (u.tile0 + t) * kTok, t0 = t_all + side * kCols;
+                wait_on(sh.s_full[c & 1], c >> 1);
+                tc_fence_after_sync();
+                const uint32_t s_at = lane_base + (c & 1) * 128;
+                float x[kCols];
+                float top = -INFINITY;
+                uint32_t there[kCols / 32];
+                bool every = true;
+#pragma unroll
+                for (int w = 0; w < kTok / 32; ++w) every &= sh.tokens[c & 7][w] == ~0u;
+                const bool inside = t_all >= clean_begin && t_all + kTok <= clean_end;
+                if (some) {
+                    tmem_load(s_at + side * kCols, x);
+#pragma unroll
+                    for (int i = 0; i < kCols; ++i) x[i] *= s1;
+                    if (p.cap > 0.f)
+#pragma unroll
+                        for (int i = 0; i < kCols; ++i) x[i] = s2 * tanhf(x[i]);
+                    if (!every || !inside) {
+#pragma unroll
+                        for (int w = 0; w < kCols / 32; ++w) {
+                            const int from = t0 + 32 * w;
+                            // bits of tokens from + 0 .. 31 in [begin, until)
+                            const int lo = begin - from, hi = until - from;
+                            uint32_t mask = hi <= 0 ? 0u : hi >= 32 ? ~0u : (1u << hi) - 1u;
+                            mask &= lo <= 0 ? ~0u : lo >= 32 ? 0u : ~0u << lo;
+                            if (p.parent && from + 31 >= u.base) {
+                                const int bit = from - u.base;                   // of the path, -31 .. 255 (or beyond: none)
+                                const int wd = bit >> 5;                         // floor
+                                const uint32_t a = wd >= 0 && wd < kPathWords ? sh.path[row][wd] : 0u;
+                                const uint32_t b = wd + 1 >= 0 && wd + 1 < kPathWords ? sh.path[row][wd + 1] : 0u;
+                                mask |= __funnelshift_r(a, b, bit & 31);
+                            }
+                            there[w] = mask & sh.tokens[c & 7][side * (kCols / 32) + w];
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) x[32 * w + i] = there[w] >> i & 1u ? x[32 * w + i] : -INFINITY;
+                        }
+                    }
+#pragma unroll
+                    for (int i = 0; i < kCols; ++i) top = fmaxf(top, x[i]);
+                }
+                sh.top[c & 1][side][row] = top;
+                // values that are no numbers, in tiles where rows differ in what they see
+                bool dirty = false;
+                if (!inside && u.n > 1) {
+                    const uint32_t vh = half_of_v(c), slot = vh % kSlots;
+                    wait_on(sh.full[slot], vh / kSlots);
+                    uint4 *words = reinterpret_cast<uint4 *>(smem + slot * kHalf);
+                    uint32_t found = 0;
+                    for (int i = tid; i < kHalf / 16; i += kSoftThreads) {
+                        const uint4 v = words[i];
+                        found |= not_finite<T>(v.x) | not_finite<T>(v.y) | not_finite<T>(v.z) | not_finite<T>(v.w);
+                    }
+                    dirty = any_of_some(5, kSoftThreads, found != 0);
+                    if (dirty) {
+                        if (tid < 4) sh.dirty[tid] = 0;
+                        sync_some(5, kSoftThreads);
+                        for (int i = tid; i < kHalf / 16; i += kSoftThreads) {
+                            uint4 v = words[i];
+                            uint32_t *w = reinterpret_cast<uint32_t *>(&v);
+                            bool any = false;
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) {
+                                const uint32_t f = not_finite<T>(w[j]);
+                                any |= f != 0;
+                                w[j] &= ~((f >> 15 & 0x10001u) * 0xffffu);
+                            }
+                            if (any) {
+                                words[i] = v;
+                                const int tok = (i % (kBlock / 16)) / 8;
+                                atomicOr(&sh.dirty[tok >> 5], 1u << (tok & 31));
+                            }
+                        }
+                        fence_proxy_async();
+                        sync_some(5, kSoftThreads);
+                    }
+                }
+                tc_fence_before_sync();
+                sync_some(1 + quarter, 64);      // both halves have their scores: P may take their place
+                tc_fence_after_sync();
+                if (some) {
+                    top = fmaxf(top, sh.top[c & 1][side ^ 1][row]);
+                    const bool moves = top > m_ref + kSlack || (m_ref == -INFINITY && top > -INFINITY);
+                    const float m_new = moves ? top : m_ref;
+                    const float alpha = moves ? exp2_of(m_ref - m_new) : 1.f;
+                    m_ref = m_new;
+                    l *= alpha;
+                    if (t > 0 && __any_sync(~0u, moves)) {
+                        wait_on(sh.pv_done, c - 1);
+                        tc_fence_after_sync();
+#pragma unroll 1
+                        for (int o = 0; o < D / 2; o += 32) {
+                            float v[32];
+                            uint32_t w[32];
+                            tmem_load(lane_base + 256 + side * (D / 2) + o, v);
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) w[i] = __float_as_uint(v[i] * alpha);
+                            tmem_store(lane_base + 256 + side * (D / 2) + o, w);
+                        }
+                        tmem_wait_store();
+                    }
+                    const float one = (m_ref == -INFINITY ? 0.f : m_ref) - kLift;   // score of the weight 1
+                    float l0 = 0.f, l1 = 0.f;
+                    uint32_t w[kCols / 2];
+#pragma unroll
+                    for (int i = 0; i < kCols / 2; ++i) {
+                        const float a = exp2_of(x[2 * i] - one), b = exp2_of(x[2 * i + 1] - one);
+                        l0 += a;
+                        l1 += b;
+                        w[i] = pack2<T>(a, b);
+                    }
+                    l += l0 + l1;
+                    tmem_store(s_at + side * (kCols / 2), w);
+                    tmem_wait_store();
+                }
+                tc_fence_before_sync();
+                mbar_arrive(bar(sh.p_full[c & 1]));
+                if (dirty) {
+                    // put back what was taken out, in the rows that see it (its weight is positive)
+                    wait_on(sh.pv_done, c);
+                    tc_fence_after_sync();
+                    if (some)
+#pragma unroll
+                        for (int w = 0; w < kCols / 32; ++w) sh.seen[side * (kCols / 32) + w][row] = there[w];
+                    sync_some(5, kSoftThreads);
+                    if (some)
+#pragma unroll 1
+                        for (int o = 0; o < D / 2; o += 32) {
+                            float v[32];
+                            uint32_t w[32];
+                            const int ch = side * (D / 2) + o;
+                            tmem_load(lane_base + 256 + ch, v);
+#pragma unroll 1
+                            for (int k = 0; k < kTok; ++k) {
+                                if (!(sh.dirty[k >> 5] >> (k & 31) & 1u)) continue;
+                                const int tok = t_all + k;
+                                const uint32_t pg = div_by(p.page, (uint32_t)tok);
+                                const int id = p.table[u.seq * p.table_stride + pg];
+                                const T *src = reinterpret_cast<const T *>(p.v) + id * p.stride_page +
+                                               (int64_t)(tok - (int)(pg * p.page.d)) * p.stride_token + u.head * p.stride_head + ch;
+                                const bool mine = sh.seen[k >> 5][row] >> (k & 31) & 1u;
+#pragma unroll
+                                for (int i = 0; i < 32; ++i) {
+                                    const float y = static_cast<float>(src[i]);
+                                    if (mine && !isfinite(y)) v[i] += y;
+                                }
+                            }
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) w[i] = __float_as_uint(v[i]);
+                            tmem_store(lane_base + 256 + ch, w);
+                        }
+                    tmem_wait_store();
+                    tc_fence_before_sync();
+                }
+            }
+            // ---- the unit's end, or the stretch's
+            wait_on(sh.pv_done, c - 1);
+            tc_fence_after_sync();
+            sh.sum[side][row] = l;
+            sync_some(1 + quarter, 64);
+            l = sh.sum[0][row] + sh.sum[1][row];
+            const bool whole = u.ends == 3;
+            if (some) {
+                const int g = at - node * p.group, h = u.head * p.group + g;
+                const float inv = l == 0.f ? 0.f : 1.f / l;
+                const int64_t slot = (int64_t)blockIdx.x * 2 + (u.ends & 1);
+                char *dst = p.out + 2 * ((int64_t)(u.node0 + node) * p.out_stride_token + h * p.out_stride_head);
+                float *part = p.part_o + (slot * p.part_rows + row) * D;
+#pragma unroll 1
+                for (int o = 0; o < D / 2; o += 32) {
+                    float v[32];
+                    const int ch = side * (D / 2) + o;
+                    tmem_load(lane_base + 256 + ch, v);
+                    if (is && whole) {
+#pragma unroll
+                        for (int i = 0; i < 32; i += 8)
+                            *reinterpret_cast<uint4 *>(dst + 2 * (ch + i)) =
+                                make_uint4(pack2<T>(v[i] * inv, v[i + 1] * inv), pack2<T>(v[i + 2] * inv, v[i + 3] * inv),
+                                           pack2<T>(v[i + 4] * inv, v[i + 5] * inv), pack2<T>(v[i + 6] * inv, v[i + 7] * inv));
+                    } else if (is) {
+#pragma unroll
+                        for (int i = 0; i < 32; i += 4)
+                            *reinterpret_cast<float4 *>(part + ch + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+                    }
+                }
+                if (is && side == 0) {
+                    if (!whole) p.part_ml[slot * p.part_rows + row] = make_float2(m_ref, l);
+                    else if (p.lse)
+                        p.lse[(int64_t)(u.node0 + node) * (p.n_kv_heads * p.group) + h] =
+                            l == 0.f ? -INFINITY : 0.6931471805599453f * (m_ref - kLift) + logf(l);
+                }
+            }
+            tc_fence_before_sync();
+            if (!whole && !(u.ends & 2)) {
+                if (u.ends & 1) {
+                    open_rows = u.rows;
+                    if (tid == 0) p.open[blockIdx.x] = Open{u.row0, u.rows, u.node0, u.head};
+                } else {
+                    goes_on = 1;
+                }
+            }
+            sync_some(1 + quarter, 64);          // sums and paths have been read
+        }
+    }
+    __syncthreads();
+    if (tid == 0) {
+        if (!open_rows) p.open[blockIdx.x].rows = 0;
+        p.goes_on[blockIdx.x] = goes_on;
+        if (*abort_flag && p.flags) atomicOr(p.flags, STOM_FLAG_TIMEOUT);
+    }
+    if (warp == kWarps - 1) tmem_dealloc(tmem, 512);
+}
+
+// Joins the partial results of the units that cross a block's end: block (x, y) of this grid takes rows 2 y and 2 y + 1 of the
+// unit that begins in block x of the kernel above and goes on behind it, if there is one.  Four warps a row, each with every
+// fourth partial result.
+template <typename T, int D>
+__global__ void __launch_bounds__(256) kv_tree_join_kernel(const __grid_constant__ KvTreeParams p) {
+    constexpr int kVec = D / 32 < 4 ? D / 32 : 4, kVecs = D / 32 / kVec;   // channels of a lane: kVecs times kVec adjacent ones
+    constexpr float kLift = std::is_same<T, __half>::value ? 7.f : 0.f;
+    __shared__ float sums[2][4][D];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, share = warp & 3, x = blockIdx.x, blocks = gridDim.x;
+    const int row = blockIdx.y * 2 + (warp >> 2);
+    grid_dependency_wait();
+    const Open u = p.open[x];
+    if ((int)blockIdx.y * 2 >= u.rows) return;
+    // the blocks it goes through: x, x + 1, ..., x + n - 1
+    int n = 1;
+    for (;;) {
+        const int j = x + n + lane;
+        const uint32_t ends = __ballot_sync(~0u, j >= blocks || !p.goes_on[j]);
+        if (ends) {
+            n = min(n + __ffs(ends), blocks - x);
+            break;
+        }
+        n += 32;
+    }
+    const bool is = row < u.rows;
+    auto at = [&](int j) { return ((int64_t)(x + j) * 2 + (j == 0 ? 1 : 0)) * p.part_rows + row; };
+    float m = -INFINITY, l = 0.f;
+    if (is)
+        for (int j = lane; j < n; j += 32) m = fmaxf(m, p.part_ml[at(j)].x);
+#pragma unroll
+    for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(~0u, m, o));
+    const float base = m == -INFINITY ? 0.f : m;
+    if (is)
+        for (int j = lane; j < n; j += 32) {
+            const float2 ml = p.part_ml[at(j)];
+            l += exp2_of(ml.x - base) * ml.y;
+        }
+#pragma unroll
+    for (int o = 16; o; o >>= 1) l += __shfl_xor_sync(~0u, l, o);
+    float o[kVecs][kVec];
+#pragma unroll
+    for (int v = 0; v < kVecs; ++v)
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) o[v][i] = 0.f;
+    if (is) {
+#pragma unroll 4
+        for (int j = share; j < n; j += 4) {
+            const float f = exp2_of(p.part_ml[at(j)].x - base);
+            const float *src = p.part_o + at(j) * D + lane * kVec;
+#pragma unroll
+            for (int v = 0; v < kVecs; ++v) {
+                float y[kVec];
+                if constexpr (kVec == 4) *reinterpret_cast<float4 *>(y) = *reinterpret_cast<const float4 *>(src + v * 128);
+                else *reinterpret_cast<float2 *>(y) = *reinterpret_cast<const float2 *>(src);
+#pragma unroll
+                for (int i = 0; i < kVec; ++i) o[v][i] = fmaf(f, y[i], o[v][i]);
+            }
+        }
+    }
+#pragma unroll
+    for (int v = 0; v < kVecs; ++v)
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) sums[warp >> 2][share][v * 128 + lane * kVec + i] = o[v][i];
+    __syncthreads();
+    if (!is || share) return;
+    const int at_row = u.row0 + row, node = (int)div_by(p.by_group, (uint32_t)at_row);
+    const int h = u.head * p.group + at_row - node * p.group;
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    T *dst = reinterpret_cast<T *>(p.out) + (int64_t)(u.node0 + node) * p.out_stride_token + h * p.out_stride_head;
+    for (int c = 2 * lane; c < D; c += 64) {
+        float y[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const float(*s)[D] = sums[warp >> 2];
+            y[i] = ((s[0][c + i] + s[1][c + i]) + (s[2][c + i] + s[3][c + i])) * inv;
+        }
+        *reinterpret_cast<uint32_t *>(dst + c) = pack2<T>(y[0], y[1]);
+    }
+    if (p.lse && lane == 0)
+        p.lse[(int64_t)(u.node0 + node) * (p.n_kv_heads * p.group) + h] =
+            l == 0.f ? -INFINITY : 0.6931471805599453f * (m - kLift) + logf(l);
+}
+
+int64_t round256(int64_t x) { return (x + 255) & ~(int64_t)255; }
+
+// Rows of a partial result: those of a tile, or as many as there are
+int64_t part_rows(int32_t n_tokens, int32_t group) {
+    const int64_t rows = (int64_t)n_tokens * group;
+    return rows < kRows ? rows : kRows;
+}
+
+template <typename T, int D>
+int32_t launch(const KvTreeParams &p, int sms, cudaStream_t stream) {
+    static std::atomic<uint64_t> allowed{0};
+    cudaError_t e = allow_shared(reinterpret_cast<const void *>(kv_tree_kernel<T, D>), Shape<D>::kSmem, allowed);
+    if (e == cudaSuccess)
+        e = launch_after_producer(kv_tree_kernel<T, D>, dim3(sms), dim3(kThreads), Shape<D>::kSmem, stream, p);
+    if (e == cudaSuccess)
+        e = launch_after_producer(kv_tree_join_kernel<T, D>, dim3(sms, (p.part_rows + 1) / 2), dim3(256), 0, stream, p);
     if (e != cudaSuccess) {
         set_last_cuda_error(e);
         return STOM_ERR_CUDA;
     }
     return finish_launch();
+}
+
+template <typename T>
+int32_t dispatch(const KvTreeParams &p, int d, int sms, cudaStream_t s) {
+    return d == 64 ? launch<T, 64>(p, sms, s) : d == 128 ? launch<T, 128>(p, sms, s) : launch<T, 256>(p, sms, s);
 }
 
 }  // namespace
@@ -150,7 +839,8 @@ extern "C" int64_t stom_kv_attend_tree_workspace_bytes(const stom_kv_pool *pool,
     if (rc) return rc;
     if (n_tokens < 0) return STOM_ERR_INVALID_ARG;
     if (n_q_heads < 1 || n_q_heads % pool->n_kv_heads) return STOM_ERR_SHAPE;
-    return 256;
+    const int64_t rows = (int64_t)kMaxBlocks * 2 * part_rows(n_tokens, n_q_heads / pool->n_kv_heads);
+    return round256(rows * pool->head_dim * 4) + round256(rows * 8) + kMaxBlocks * (int64_t)(sizeof(Open) + 4);
 }
 
 extern "C" int32_t stom_kv_attend_tree(const stom_kv_pool *pool, const stom_kv_seqs *seqs, int32_t layer, int32_t n_tokens,
@@ -168,7 +858,7 @@ extern "C" int32_t stom_kv_attend_tree(const stom_kv_pool *pool, const stom_kv_s
     if (!(softcap >= 0.f) || !(softcap <= 2.0e38f) || !(s1 <= 3.0e38f) || (softcap > 0.f && s1 != 0.f && s1 < 1.2e-38f))
         return STOM_ERR_INVALID_ARG;
     if (n_q_heads % pool->n_kv_heads || n_q_heads / pool->n_kv_heads > 64) return STOM_ERR_SHAPE;
-    if (seqs->n_seqs > STOM_KV_MAX_SEQS || (int64_t)n_tokens * n_q_heads > INT32_MAX) return STOM_ERR_SHAPE;
+    if (seqs->n_seqs > STOM_KV_MAX_SEQS || (int64_t)n_tokens * n_q_heads > INT32_MAX - kRows) return STOM_ERR_SHAPE;
     const int64_t most = (int64_t)seqs->max_pages * pool->page_tokens;
     if (most > INT32_MAX - 32) return STOM_ERR_SHAPE;
     if (seqs->n_seqs == 0 || n_tokens == 0) return STOM_OK;
@@ -183,6 +873,9 @@ extern "C" int32_t stom_kv_attend_tree(const stom_kv_pool *pool, const stom_kv_s
     if (n_tokens > 1 && (out_stride_token < d || q_stride_token < 0)) return STOM_ERR_INVALID_ARG;
     const int64_t need = stom_kv_attend_tree_workspace_bytes(pool, seqs, n_tokens, n_q_heads);
     if (!workspace || !aligned16(workspace) || workspace_bytes < need) return STOM_ERR_WORKSPACE;
+    int sms = sm_count();
+    if (!sms) return STOM_ERR_CUDA;
+    if (sms > kMaxBlocks) sms = kMaxBlocks;
 
     KvTreeParams p = {};
     p.k = static_cast<const char *>(pool->k) + 2 * layer * pool->stride_layer;
@@ -199,6 +892,7 @@ extern "C" int32_t stom_kv_attend_tree(const stom_kv_pool *pool, const stom_kv_s
     p.page = fast_div((uint32_t)pool->page_tokens);
     p.n_kv_heads = pool->n_kv_heads;
     p.group = n_q_heads / pool->n_kv_heads;
+    p.by_group = fast_div((uint32_t)p.group);
     p.n_tokens = n_tokens;
     p.first = first;
     p.parent = parent;
@@ -212,7 +906,14 @@ extern "C" int32_t stom_kv_attend_tree(const stom_kv_pool *pool, const stom_kv_s
     p.out_stride_token = out_stride_token;
     p.out_stride_head = out_stride_head;
     p.lse = lse;
+    p.part_rows = (int32_t)part_rows(n_tokens, p.group);
+    const int64_t rows = (int64_t)kMaxBlocks * 2 * p.part_rows;
+    char *ws = static_cast<char *>(workspace);
+    p.part_o = reinterpret_cast<float *>(ws);
+    p.part_ml = reinterpret_cast<float2 *>(ws + round256(rows * d * 4));
+    p.open = reinterpret_cast<Open *>(ws + round256(rows * d * 4) + round256(rows * 8));
+    p.goes_on = reinterpret_cast<int32_t *>(p.open + kMaxBlocks);
     p.flags = dev_flags;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    return pool->dtype == STOM_BF16 ? dispatch<__nv_bfloat16>(p, d, s) : dispatch<__half>(p, d, s);
+    return pool->dtype == STOM_BF16 ? dispatch<__nv_bfloat16>(p, d, sms, s) : dispatch<__half>(p, d, sms, s);
 }
