@@ -581,6 +581,9 @@ __global__ void __launch_bounds__(kThreads, 1) kv_tree_kernel(const __grid_const
                 }
                 tc_fence_before_sync();
                 sync_some(1 + quarter, 64);      // both halves have their scores: P may take their place
+                // The product of the tile before is done: the accumulators may be rescaled.  Every thread waits for every tile's,
+                // since a barrier's parity tells only neighbouring phases apart; the next product could not begin before.
+                if (c > 0) wait_on(sh.pv_done, c - 1);
                 tc_fence_after_sync();
                 if (some) {
                     top = fmaxf(top, sh.top[c & 1][side ^ 1][row]);
@@ -590,8 +593,6 @@ __global__ void __launch_bounds__(kThreads, 1) kv_tree_kernel(const __grid_const
                     m_ref = m_new;
                     l *= alpha;
                     if (t > 0 && __any_sync(~0u, moves)) {
-                        wait_on(sh.pv_done, c - 1);
-                        tc_fence_after_sync();
 #pragma unroll 1
                         for (int o = 0; o < D / 2; o += 32) {
                             float v[32];

@@ -143,6 +143,26 @@ def test_the_same_call_gives_the_same_bits():
     assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
 
 
+@pytest.mark.parametrize("d,hq,hk,page,dtype", [(128, 64, 8, 16, HF), (64, 16, 2, 50, BF), (256, 8, 4, 64, BF)])
+def test_many_units_a_block_again_and_again(d, hq, hk, page, dtype):
+    """Blocks go through many short units, warps at their own pace: every call gives the bits of the first, which are right."""
+    rng = np.random.default_rng(d)
+    had, new = rng.integers(0, 2000, 40).tolist(), rng.integers(1, 34, 40).tolist()
+    s = _make(had, new, hq, hk, d, page, dtype)
+    out, lse = _call(s)
+    for _ in range(15):
+        again = _call(s)
+        assert torch.equal(again[0], out) and torch.equal(again[1], lse)
+    keep = {0: s["first"][0], 20: s["first"][20], 39: s["first"][39]}
+    want, wlse, mag = T.attend_nodes(s["k"], s["v"], s["table_host"][list(keep)], [s["lens"][i] for i in keep],
+                                     [0] + np.cumsum([new[i] for i in keep]).tolist(),
+                                     [p for i in keep for p in s["parent"][s["first"][i]:s["first"][i + 1]]],
+                                     torch.cat([s["q"][s["first"][i]:s["first"][i + 1]] for i in keep]), d ** -0.5)
+    rows = [r for i in keep for r in range(s["first"][i], s["first"][i + 1])]
+    _close(out[rows], want, mag, dtype)
+    _close_lse(lse[rows], wlse)
+
+
 @pytest.mark.parametrize("order", ["token", "head"])
 def test_layers_strides_and_rows_behind_the_last_sequence(order):
     s = _make([150, 64], [10, 3], 8, 4, 128, 16, BF, order=order, layers=3, extra=5)
