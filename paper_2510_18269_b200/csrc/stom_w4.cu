@@ -31,6 +31,9 @@ namespace {
 
 constexpr int kRows = 32;     // of the matrix, per block
 constexpr int kWarps = 8;
+constexpr int kStages = 4;
+constexpr int kPitch = 80;    // bytes from row to row of a stage in shared memory: 8 rows' words of 4 lanes lie in 32 banks
+constexpr int kStageBytes = kRows * kPitch;
 
 struct W4Params {
     const uint8_t *codes;
@@ -63,46 +66,70 @@ __device__ __forceinline__ float meta_at(const void *base, int64_t i, int dtype)
     return __half2float(__ldg(static_cast<const __half *>(base) + i));
 }
 
-// W words of 8 codes
-template <int W>
-__device__ __forceinline__ void load_codes(uint32_t (&w)[W], const uint8_t *at) {
-    if constexpr (W == 4) {
-        const uint4 v = __ldg(reinterpret_cast<const uint4 *>(at));
-        w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
-    } else if constexpr (W == 2) {
-        const uint2 v = __ldg(reinterpret_cast<const uint2 *>(at));
-        w[0] = v.x, w[1] = v.y;
-    } else {
-        w[0] = __ldg(reinterpret_cast<const uint32_t *>(at));
-    }
-}
-
-// GROUP columns a group; NT blocks of 8 tokens
+// GROUP columns a group; NT blocks of 8 tokens.
+// A warp goes through stages of 128 columns (the block's warps take them in turn): 64 bytes of each of its 32 rows, copied
+// to its own ring in shared memory kStages - 1 stages ahead; the tokens' values and the rows' scales a stage ahead in
+// registers.  No barrier but the one before the warps' sums are joined.
 template <typename T, int GROUP, int NT>
-__global__ void __launch_bounds__(kWarps * 32) w4_kernel(const __grid_constant__ W4Params p) {
-    constexpr int W = GROUP / 32;
+__global__ void __launch_bounds__(kWarps * 32, 2) w4_few_kernel(const __grid_constant__ W4Params p) {
+    constexpr int kGroups = 128 / GROUP;             // of a stage
     constexpr uint32_t ones = std::is_same<T, __nv_bfloat16>::value ? 0x3f803f80u : 0x3c003c00u;
-    __shared__ float sums[kWarps][kRows][8 * NT + 1];
+    extern __shared__ __align__(16) uint8_t smem[];
+    __shared__ float2 meta_s[kWarps][2][kGroups][kRows];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
     const int row0 = blockIdx.x * kRows, tok0 = blockIdx.y * 8 * NT;
+    const int stages = (p.k + 127) / 128;
+    const int mine = warp < stages ? (stages - warp + kWarps - 1) / kWarps : 0;   // stages warp, warp + kWarps, ...
+    uint8_t *ring = smem + warp * kStages * kStageBytes;
+    const uint32_t ring_u = smem_u32(ring);
     grid_dependency_wait();
 
+    // copies: lane (g, t) the t-th 16 bytes of rows g, g + 8, g + 16, g + 24 (rows behind the last: the last, never written)
     const uint8_t *codes[4];
-    int64_t meta[4];
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-        const int row = min(row0 + r * 8 + g, p.n - 1);   // rows behind the last: its numbers, never written
-        codes[r] = p.codes + row * p.code_stride + t * (GROUP / 8);
-        meta[r] = row * p.meta_stride;
-    }
+    for (int r = 0; r < 4; ++r) codes[r] = p.codes + min(row0 + r * 8 + g, p.n - 1) * p.code_stride + t * 16;
+    auto copy_stage = [&](int i) {
+        if (i < mine) {
+            const int at = (warp + i * kWarps) * 64;
+            const uint32_t bytes = 2 * at + t * 32 < p.k ? 16u : 0u;   // columns behind the last: zeros
+            const uint32_t dst = ring_u + (i % kStages) * kStageBytes + g * kPitch + t * 16;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) copy16_async(dst + r * 8 * kPitch, codes[r] + (bytes ? at : 0), bytes);
+        }
+        copy_commit();
+    };
+    // scales: a lane has a row
+    const int64_t meta0 = min(row0 + lane, p.n - 1) * p.meta_stride;
+    float sc[kGroups], ze[kGroups];
+    auto load_meta = [&](int i) {
+        if (i >= mine) return;
+#pragma unroll
+        for (int q = 0; q < kGroups; ++q) {
+            const int gr = min((warp + i * kWarps) * kGroups + q, p.groups - 1);
+            sc[q] = meta_at(p.scale, meta0 + gr, p.meta_dtype);
+            ze[q] = p.zero ? meta_at(p.zero, meta0 + gr, p.meta_dtype) : -8.f * sc[q];
+        }
+    };
+    // tokens: lane (g, t) the 8 values of columns 32 j + 8 t of token g, in pairs 4 columns apart as the codes of a word
     const T *x[NT];
     bool is[NT];
 #pragma unroll
     for (int j = 0; j < NT; ++j) {
         const int tok = tok0 + j * 8 + g;
         is[j] = tok < p.tokens;
-        x[j] = static_cast<const T *>(p.x) + (is[j] ? tok : 0) * p.x_stride + t * (GROUP / 4);
+        x[j] = static_cast<const T *>(p.x) + (is[j] ? tok : 0) * p.x_stride + t * 8;
     }
+    uint4 xv[4][NT];
+    auto load_x = [&](int i) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int b = 0; b < NT; ++b) {
+                const int col = (warp + i * kWarps) * 128 + j * 32;
+                xv[j][b] = make_uint4(0, 0, 0, 0);
+                if (is[b] && i < mine && col < p.k) xv[j][b] = __ldg(reinterpret_cast<const uint4 *>(x[b] + col));
+            }
+    };
     float acc[2][NT][4];
 #pragma unroll
     for (int m = 0; m < 2; ++m)
@@ -111,28 +138,44 @@ __global__ void __launch_bounds__(kWarps * 32) w4_kernel(const __grid_constant__
 #pragma unroll
             for (int e = 0; e < 4; ++e) acc[m][j][e] = 0.f;
 
-    for (int gr = warp; gr < p.groups; gr += kWarps) {
-        uint32_t w[4][W];
-        float s[4], z[4];
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            load_codes<W>(w[r], codes[r] + gr * (int64_t)(GROUP / 2));
-            s[r] = meta_at(p.scale, meta[r] + gr, p.meta_dtype);
-            z[r] = p.zero ? meta_at(p.zero, meta[r] + gr, p.meta_dtype) : -8.f * s[r];
-        }
+    for (int i = 0; i < kStages - 1; ++i) copy_stage(i);
+    load_meta(0);
+    load_x(0);
+#pragma unroll 1
+    for (int i = 0; i < mine; ++i) {
+        float2(*meta)[kRows] = meta_s[warp][i & 1];
+#pragma unroll
+        for (int q = 0; q < kGroups; ++q) meta[q][lane] = make_float2(16.f * sc[q], ze[q] - 16.f * sc[q]);
+        load_meta(i + 1);
+        uint32_t b[4][NT][4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int c = 0; c < NT; ++c) {
+                const uint4 v = xv[j][c];
+                b[j][c][0] = __byte_perm(v.x, v.z, 0x5410), b[j][c][1] = __byte_perm(v.x, v.z, 0x7632);
+                b[j][c][2] = __byte_perm(v.y, v.w, 0x5410), b[j][c][3] = __byte_perm(v.y, v.w, 0x7632);
+            }
+        load_x(i + 1);
+        copy_wait<kStages - 2>();
+        __syncwarp();
+        copy_stage(i + kStages - 1);   // into the slot that the stage before this one has left
+        const uint8_t *at = ring + (i % kStages) * kStageBytes + g * kPitch + t * 4;
         float d[2][NT][4], sx[NT][4];
 #pragma unroll
-        for (int j = 0; j < NT; ++j)
+        for (int j = 0; j < 4; ++j) {
+            if (j * 32 % GROUP == 0)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) d[0][j][e] = d[1][j][e] = sx[j][e] = 0.f;
+                for (int c = 0; c < NT; ++c)
 #pragma unroll
-        for (int i = 0; i < W; ++i) {
+                    for (int e = 0; e < 4; ++e) d[0][c][e] = d[1][c][e] = sx[c][e] = 0.f;
             uint32_t a[2][2][4];   // [16 rows][product][register]
 #pragma unroll
             for (int m = 0; m < 2; ++m)
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    const uint32_t v = w[2 * m + h][i];
+                    const uint32_t v = *reinterpret_cast<const uint32_t *>(at + (2 * m + h) * 8 * kPitch + j * 16);
                     a[m][0][h] = code_pair<T, 0>(v);
                     a[m][0][2 + h] = code_pair<T, 1>(v);
                     a[m][1][h] = code_pair<T, 2>(v);
@@ -140,33 +183,36 @@ __global__ void __launch_bounds__(kWarps * 32) w4_kernel(const __grid_constant__
                 }
             const uint32_t one[4] = {ones, ones, ones, ones};
 #pragma unroll
-            for (int j = 0; j < NT; ++j) {
-                uint4 v = make_uint4(0, 0, 0, 0);
-                if (is[j]) v = __ldg(reinterpret_cast<const uint4 *>(x[j] + gr * (int64_t)GROUP + 8 * i));
-                const uint32_t b0 = __byte_perm(v.x, v.z, 0x5410), b1 = __byte_perm(v.x, v.z, 0x7632);
-                const uint32_t b2 = __byte_perm(v.y, v.w, 0x5410), b3 = __byte_perm(v.y, v.w, 0x7632);
+            for (int c = 0; c < NT; ++c) {
 #pragma unroll
                 for (int m = 0; m < 2; ++m) {
-                    mma16x8x16<T>(d[m][j], a[m][0], b0, b1);
-                    mma16x8x16<T>(d[m][j], a[m][1], b2, b3);
+                    mma16x8x16<T>(d[m][c], a[m][0], b[j][c][0], b[j][c][1]);
+                    mma16x8x16<T>(d[m][c], a[m][1], b[j][c][2], b[j][c][3]);
                 }
-                mma16x8x16<T>(sx[j], one, b0, b1);
-                mma16x8x16<T>(sx[j], one, b2, b3);
+                mma16x8x16<T>(sx[c], one, b[j][c][0], b[j][c][1]);
+                mma16x8x16<T>(sx[c], one, b[j][c][2], b[j][c][3]);
+            }
+            if ((j + 1) * 32 % GROUP == 0) {
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const float2 f = meta[j * 32 / GROUP][r * 8 + g];
+#pragma unroll
+                    for (int c = 0; c < NT; ++c)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            float &y = acc[r >> 1][c][(r & 1) * 2 + e];
+                            y = fmaf(f.x, d[r >> 1][c][(r & 1) * 2 + e], y);
+                            y = fmaf(f.y, sx[c][e], y);
+                        }
+                }
             }
         }
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const float s16 = 16.f * s[r], o = z[r] - s16;
-#pragma unroll
-            for (int j = 0; j < NT; ++j)
-#pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    float &y = acc[r >> 1][j][(r & 1) * 2 + c];
-                    y = fmaf(s16, d[r >> 1][j][(r & 1) * 2 + c], y);
-                    y = fmaf(o, sx[j][c], y);
-                }
-        }
     }
+    copy_wait<0>();
+    __syncthreads();
+    // the warps' sums, in the rings' place
+    float(*sums)[kRows][8 * NT + 1] = reinterpret_cast<float(*)[kRows][8 * NT + 1]>(smem);
+    static_assert(sizeof(float) * kWarps * kRows * (8 * NT + 1) <= kWarps * kStages * kStageBytes, "room for the sums");
 #pragma unroll
     for (int m = 0; m < 2; ++m)
 #pragma unroll
@@ -189,12 +235,15 @@ __global__ void __launch_bounds__(kWarps * 32) w4_kernel(const __grid_constant__
 template <typename T, int GROUP, int NT>
 cudaError_t launch(const W4Params &p, cudaStream_t s) {
     const dim3 grid((p.n + kRows - 1) / kRows, (p.tokens + 8 * NT - 1) / (8 * NT));
-    return launch_after_producer(w4_kernel<T, GROUP, NT>, grid, dim3(kWarps * 32), 0, s, p);
+    constexpr int smem = kWarps * kStages * kStageBytes;
+    static std::atomic<uint64_t> allowed{0};
+    const cudaError_t e = allow_shared(reinterpret_cast<const void *>(w4_few_kernel<T, GROUP, NT>), smem, allowed);
+    return e != cudaSuccess ? e : launch_after_producer(w4_few_kernel<T, GROUP, NT>, grid, dim3(kWarps * 32), smem, s, p);
 }
 
 template <typename T, int GROUP>
 cudaError_t by_tokens(const W4Params &p, cudaStream_t s) {
-    return p.tokens <= 8 ? launch<T, GROUP, 1>(p, s) : p.tokens <= 16 ? launch<T, GROUP, 2>(p, s) : launch<T, GROUP, 4>(p, s);
+    return p.tokens <= 8 ? launch<T, GROUP, 1>(p, s) : launch<T, GROUP, 2>(p, s);
 }
 
 template <typename T>
