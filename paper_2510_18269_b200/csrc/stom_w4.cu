@@ -60,17 +60,28 @@ __device__ __forceinline__ uint32_t code_pair(uint32_t w) {
     return (at & mask) | one;
 }
 
-__device__ __forceinline__ float meta_at(const void *base, int64_t i, int dtype) {
-    if (dtype == STOM_FP32) return __ldg(static_cast<const float *>(base) + i);
-    if (dtype == STOM_BF16) return __bfloat162float(__ldg(static_cast<const __nv_bfloat16 *>(base) + i));
-    return __half2float(__ldg(static_cast<const __half *>(base) + i));
+__device__ __forceinline__ float to_float(float x) { return x; }
+__device__ __forceinline__ float to_float(__nv_bfloat16 x) { return __bfloat162float(x); }
+__device__ __forceinline__ float to_float(__half x) { return __half2float(x); }
+
+// c (16x8) = a (16x16) b (16x8): the first product of a sum
+template <typename T>
+__device__ __forceinline__ void mma16x8x16_first(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    if constexpr (std::is_same<T, __nv_bfloat16>::value)
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+            : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
+            : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
+    else
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+            : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
+            : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
 }
 
 // GROUP columns a group; NT blocks of 8 tokens.
 // A warp goes through stages of 128 columns (the block's warps take them in turn): 64 bytes of each of its 32 rows, copied
 // to its own ring in shared memory kStages - 1 stages ahead; the tokens' values and the rows' scales a stage ahead in
 // registers.  No barrier but the one before the warps' sums are joined.
-template <typename T, int GROUP, int NT>
+template <typename T, typename M, int GROUP, int NT>
 __global__ void __launch_bounds__(kWarps * 32, 2) w4_few_kernel(const __grid_constant__ W4Params p) {
     constexpr int kGroups = 128 / GROUP;             // of a stage
     constexpr uint32_t ones = std::is_same<T, __nv_bfloat16>::value ? 0x3f803f80u : 0x3c003c00u;
@@ -87,27 +98,33 @@ __global__ void __launch_bounds__(kWarps * 32, 2) w4_few_kernel(const __grid_con
     // copies: lane (g, t) the t-th 16 bytes of rows g, g + 8, g + 16, g + 24 (rows behind the last: the last, never written)
     const uint8_t *codes[4];
 #pragma unroll
-    for (int r = 0; r < 4; ++r) codes[r] = p.codes + min(row0 + r * 8 + g, p.n - 1) * p.code_stride + t * 16;
-    auto copy_stage = [&](int i) {
-        if (i < mine) {
-            const int at = (warp + i * kWarps) * 64;
-            const uint32_t bytes = 2 * at + t * 32 < p.k ? 16u : 0u;   // columns behind the last: zeros
-            const uint32_t dst = ring_u + (i % kStages) * kStageBytes + g * kPitch + t * 16;
+    for (int r = 0; r < 4; ++r) codes[r] = p.codes + min(row0 + r * 8 + g, p.n - 1) * p.code_stride + t * 16 + warp * 64;
+    int copied = 0;
+    auto copy_stage = [&]() {
+        if (copied < mine) {
+            const uint32_t dst = ring_u + (copied % kStages) * kStageBytes + g * kPitch + t * 16;
+            if (GROUP == 128 || (warp + copied * kWarps) * 128 + t * 32 < p.k) {
 #pragma unroll
-            for (int r = 0; r < 4; ++r) copy16_async(dst + r * 8 * kPitch, codes[r] + (bytes ? at : 0), bytes);
+                for (int r = 0; r < 4; ++r) copy16_async(dst + r * 8 * kPitch, codes[r], 16);
+            }   // (of columns behind the last any codes will do: their tokens' values are zeros)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) codes[r] += kWarps * 64;
         }
+        ++copied;
         copy_commit();
     };
     // scales: a lane has a row
-    const int64_t meta0 = min(row0 + lane, p.n - 1) * p.meta_stride;
-    float sc[kGroups], ze[kGroups];
+    const M *scale = static_cast<const M *>(p.scale) + min(row0 + lane, p.n - 1) * p.meta_stride;
+    const M *zero = p.zero ? static_cast<const M *>(p.zero) + min(row0 + lane, p.n - 1) * p.meta_stride : nullptr;
+    M sc[kGroups], ze[kGroups];
     auto load_meta = [&](int i) {
         if (i >= mine) return;
 #pragma unroll
         for (int q = 0; q < kGroups; ++q) {
-            const int gr = min((warp + i * kWarps) * kGroups + q, p.groups - 1);
-            sc[q] = meta_at(p.scale, meta0 + gr, p.meta_dtype);
-            ze[q] = p.zero ? meta_at(p.zero, meta0 + gr, p.meta_dtype) : -8.f * sc[q];
+            int gr = (warp + i * kWarps) * kGroups + q;
+            if (GROUP < 128) gr = min(gr, p.groups - 1);
+            sc[q] = __ldg(scale + gr);
+            if (zero) ze[q] = __ldg(zero + gr);
         }
     };
     // tokens: lane (g, t) the 8 values of columns 32 j + 8 t of token g, in pairs 4 columns apart as the codes of a word
@@ -117,18 +134,20 @@ __global__ void __launch_bounds__(kWarps * 32, 2) w4_few_kernel(const __grid_con
     for (int j = 0; j < NT; ++j) {
         const int tok = tok0 + j * 8 + g;
         is[j] = tok < p.tokens;
-        x[j] = static_cast<const T *>(p.x) + (is[j] ? tok : 0) * p.x_stride + t * 8;
+        x[j] = static_cast<const T *>(p.x) + (is[j] ? tok : 0) * p.x_stride + t * 8 + warp * 128;
     }
     uint4 xv[4][NT];
     auto load_x = [&](int i) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
+        for (int b = 0; b < NT; ++b) {
+            const bool on = is[b] && i < mine;
 #pragma unroll
-            for (int b = 0; b < NT; ++b) {
-                const int col = (warp + i * kWarps) * 128 + j * 32;
+            for (int j = 0; j < 4; ++j) {
                 xv[j][b] = make_uint4(0, 0, 0, 0);
-                if (is[b] && i < mine && col < p.k) xv[j][b] = __ldg(reinterpret_cast<const uint4 *>(x[b] + col));
+                if (on && (GROUP == 128 || (warp + i * kWarps) * 128 + j * 32 < p.k))
+                    xv[j][b] = __ldg(reinterpret_cast<const uint4 *>(x[b] + i * (kWarps * 128) + j * 32));
             }
+        }
     };
     float acc[2][NT][4];
 #pragma unroll
@@ -139,14 +158,17 @@ __global__ void __launch_bounds__(kWarps * 32, 2) w4_few_kernel(const __grid_con
             for (int e = 0; e < 4; ++e) acc[m][j][e] = 0.f;
 
 #pragma unroll
-    for (int i = 0; i < kStages - 1; ++i) copy_stage(i);
+    for (int i = 0; i < kStages - 1; ++i) copy_stage();
     load_meta(0);
     load_x(0);
 #pragma unroll 1
     for (int i = 0; i < mine; ++i) {
         float2(*meta)[kRows] = meta_s[warp][i & 1];
 #pragma unroll
-        for (int q = 0; q < kGroups; ++q) meta[q][lane] = make_float2(16.f * sc[q], ze[q] - 16.f * sc[q]);
+        for (int q = 0; q < kGroups; ++q) {
+            const float s = 16.f * to_float(sc[q]);
+            meta[q][lane] = make_float2(s, zero ? to_float(ze[q]) - s : -1.5f * s);
+        }
         load_meta(i + 1);
         uint32_t b[4][NT][4];
 #pragma unroll
@@ -160,16 +182,11 @@ __global__ void __launch_bounds__(kWarps * 32, 2) w4_few_kernel(const __grid_con
         load_x(i + 1);
         copy_wait<kStages - 2>();
         __syncwarp();
-        copy_stage(i + kStages - 1);   // into the slot that the stage before this one has left
+        copy_stage();   // into the slot that the stage before this one has left
         const uint8_t *at = ring + (i % kStages) * kStageBytes + g * kPitch + t * 4;
         float d[2][NT][4], sx[NT][4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            if (j * 32 % GROUP == 0)
-#pragma unroll
-                for (int c = 0; c < NT; ++c)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) d[0][c][e] = d[1][c][e] = sx[c][e] = 0.f;
             uint32_t a[2][2][4];   // [16 rows][product][register]
 #pragma unroll
             for (int m = 0; m < 2; ++m)
@@ -182,14 +199,17 @@ __global__ void __launch_bounds__(kWarps * 32, 2) w4_few_kernel(const __grid_con
                     a[m][1][2 + h] = code_pair<T, 3>(v);
                 }
             const uint32_t one[4] = {ones, ones, ones, ones};
+            const bool first = j * 32 % GROUP == 0;
 #pragma unroll
             for (int c = 0; c < NT; ++c) {
 #pragma unroll
                 for (int m = 0; m < 2; ++m) {
-                    mma16x8x16<T>(d[m][c], a[m][0], b[j][c][0], b[j][c][1]);
+                    if (first) mma16x8x16_first<T>(d[m][c], a[m][0], b[j][c][0], b[j][c][1]);
+                    else mma16x8x16<T>(d[m][c], a[m][0], b[j][c][0], b[j][c][1]);
                     mma16x8x16<T>(d[m][c], a[m][1], b[j][c][2], b[j][c][3]);
                 }
-                mma16x8x16<T>(sx[c], one, b[j][c][0], b[j][c][1]);
+                if (first) mma16x8x16_first<T>(sx[c], one, b[j][c][0], b[j][c][1]);
+                else mma16x8x16<T>(sx[c], one, b[j][c][0], b[j][c][1]);
                 mma16x8x16<T>(sx[c], one, b[j][c][2], b[j][c][3]);
             }
             if ((j + 1) * 32 % GROUP == 0) {
@@ -232,23 +252,30 @@ __global__ void __launch_bounds__(kWarps * 32, 2) w4_few_kernel(const __grid_con
     }
 }
 
-template <typename T, int GROUP, int NT>
+template <typename T, typename M, int GROUP, int NT>
 cudaError_t launch(const W4Params &p, cudaStream_t s) {
     const dim3 grid((p.n + kRows - 1) / kRows, (p.tokens + 8 * NT - 1) / (8 * NT));
     constexpr int smem = kWarps * kStages * kStageBytes;
     static std::atomic<uint64_t> allowed{0};
-    const cudaError_t e = allow_shared(reinterpret_cast<const void *>(w4_few_kernel<T, GROUP, NT>), smem, allowed);
-    return e != cudaSuccess ? e : launch_after_producer(w4_few_kernel<T, GROUP, NT>, grid, dim3(kWarps * 32), smem, s, p);
+    const cudaError_t e = allow_shared(reinterpret_cast<const void *>(w4_few_kernel<T, M, GROUP, NT>), smem, allowed);
+    return e != cudaSuccess ? e : launch_after_producer(w4_few_kernel<T, M, GROUP, NT>, grid, dim3(kWarps * 32), smem, s, p);
+}
+
+template <typename T, typename M, int GROUP>
+cudaError_t by_tokens(const W4Params &p, cudaStream_t s) {
+    return p.tokens <= 8 ? launch<T, M, GROUP, 1>(p, s) : launch<T, M, GROUP, 2>(p, s);
 }
 
 template <typename T, int GROUP>
-cudaError_t by_tokens(const W4Params &p, cudaStream_t s) {
-    return p.tokens <= 8 ? launch<T, GROUP, 1>(p, s) : launch<T, GROUP, 2>(p, s);
+cudaError_t by_meta(const W4Params &p, cudaStream_t s) {
+    return p.meta_dtype == STOM_FP32   ? by_tokens<T, float, GROUP>(p, s)
+           : p.meta_dtype == STOM_BF16 ? by_tokens<T, __nv_bfloat16, GROUP>(p, s)
+                                       : by_tokens<T, __half, GROUP>(p, s);
 }
 
 template <typename T>
 cudaError_t by_group(const W4Params &p, int group, cudaStream_t s) {
-    return group == 32 ? by_tokens<T, 32>(p, s) : group == 64 ? by_tokens<T, 64>(p, s) : by_tokens<T, 128>(p, s);
+    return group == 32 ? by_meta<T, 32>(p, s) : group == 64 ? by_meta<T, 64>(p, s) : by_meta<T, 128>(p, s);
 }
 
 }  // namespace
