@@ -36,10 +36,13 @@ typedef struct stom_w4_matrix {
  * rounded once to dtype.
  * x, add, y (dtype: STOM_BF16 | STOM_FP16): element (t, i) at t*stride + i; x
  * and its stride 16-byte aligned, the others any alignment of an element.
- * bias [n] (dtype) and add may be NULL; add may be y.
+ * bias [n] (dtype) and add may be NULL; add may be y; x and y do not overlap.
+ * STOM_FLAG_TIMEOUT in the optional dev_flags: a bounded wait inside a kernel
+ * ran out, y is not to be used.
  * Errors: INVALID_ARG, SHAPE, UNSUPPORTED, ALIGNMENT, CUDA. */
 int32_t stom_w4_linear(const stom_w4_matrix *w, int32_t dtype, int32_t rows, const void *x, int64_t x_stride,
-                       const void *bias, const void *add, int64_t add_stride, void *y, int64_t y_stride, void *stream);
+                       const void *bias, const void *add, int64_t add_stride, void *y, int64_t y_stride,
+                       uint32_t *dev_flags, void *stream);
 
 #ifdef __cplusplus
 }

@@ -226,9 +226,9 @@ PyObject *accept(PyObject *, PyObject *const *a, Py_ssize_t count) {
     });
 }
 
-// matrix, device, x, y, bias, add, stream
+// matrix, device, x, y, bias, add, dev_flags, stream
 PyObject *w4_linear(PyObject *, PyObject *const *a, Py_ssize_t count) {
-    return guarded(count, 7, [&] {
+    return guarded(count, 8, [&] {
         const auto *w = at_address<stom_w4_matrix>(a[0]);
         const int64_t dev = integer(a[1]);
         const at::Tensor &x = must(a[2], "x");
@@ -255,8 +255,9 @@ PyObject *w4_linear(PyObject *, PyObject *const *a, Py_ssize_t count) {
         }
         Rows add;
         if (a[5] != Py_None) add = flat(a[5], w->n, "add");
-        const On on(dev, a[6]);
-        return lib.w4_linear(w, dtype, (int32_t)n, in.at, in.row, bias, add.at, add.row, out.at, out.row, on.stream);
+        uint32_t *fl = flags(a[6], dev);
+        const On on(dev, a[7]);
+        return lib.w4_linear(w, dtype, (int32_t)n, in.at, in.row, bias, add.at, add.row, out.at, out.row, fl, on.stream);
     });
 }
 

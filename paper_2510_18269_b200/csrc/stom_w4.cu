@@ -4,278 +4,271 @@
 //
 // What bounds it: the codes, half a byte a weight, are read once; at one token each takes part in one multiply-add, so
 // that memory gives 46 weights a clock to a multiprocessor.  The scalar units would need as many multiply-adds and an
-// unpacking for each; on the tensor cores (m16n8k16, the weights the 16 rows, the tokens the 8 columns) a warp-wide
-// product takes 256 of them, and the unpacking is what is left to make short.
-//
-// Codes as numbers.  A code c put under the exponent of 1, at the top of the mantissa, is the 16-bit number 1 + c/16: one
-// shift and one three-input logic operation turn two codes of a word into an operand register.  With D = sum (1 + c/16) x
-// and X = sum x, both exact products summed in binary32, sum c x = 16 (D - X), so that a group adds 16 s D + (z - 16 s) X.
-// X comes from a product of the same tokens with ones, in the very registers where D's tokens stand.  The difference
-// costs at most a factor (16 + 15) / 7.5 of binary32's 2^-24, where the output has 2^-8 or 2^-11.
+// unpacking for each; on the tensor cores (m16n8k16: the weights the 16 rows, the tokens the 8 columns) a warp-wide product
+// takes 256 of them behind five instructions that unpack (see stom_w4.cuh).
 //
 // Layout.  Codes are used as they lie in memory.  The order of columns within a product is free as long as weights and
-// tokens agree, so lane (g, t) of a fragment takes group / 32 adjacent words of 8 codes of rows g and g + 8, and the
-// tokens' eight values of the same columns; halves of a register hold columns 4 apart, as the nibbles of a word do.  All of
+// tokens agree: lane (g, t) of a fragment takes the t-th word (8 codes) of a row's 32 columns, two products' worth.  All of
 // a product's columns lie in one group.
-//
-// Split.  A block has 32 rows, its warps take groups in turn, and their sums are joined in shared memory.
-#include "stom_internal.cuh"
-#include "stom_kv.cuh"
-#include "stom_w4.h"
-
-#include <type_traits>
+#include "stom_w4.cuh"
 
 namespace stom {
 
 namespace {
 
-constexpr int kRows = 32;     // of the matrix, per block
-constexpr int kWarps = 8;
-constexpr int kStages = 4;
-constexpr int kPitch = 80;    // bytes from row to row of a stage in shared memory: 8 rows' words of 4 lanes lie in 32 banks
-constexpr int kStageBytes = kRows * kPitch;
+constexpr int kRows = 16;     // of the matrix, per slab
+constexpr int kTeams = 2, kTeamWarps = 8, kWarps = kTeams * kTeamWarps, kThreads = kWarps * 32;   // of a block
+constexpr int kUnitCols = 256;                // columns of a unit
+constexpr int kPitch = kUnitCols / 2 + 16;    // bytes from row to row in shared memory: 8 rows' words of 4 lanes lie in 32 banks
+constexpr int kUnitBytes = kRows * kPitch;
+constexpr int kMostShared = 194 * 1024;       // dynamic shared memory of a block
 
-struct W4Params {
-    const uint8_t *codes;
-    const void *scale, *zero;
-    int32_t n, k, groups, meta_dtype;
-    int64_t code_stride, meta_stride;
-    const void *x;
-    int64_t x_stride;
-    const void *bias, *add;
-    int64_t add_stride;
-    void *y;
-    int64_t y_stride;
-    int32_t tokens;
+__device__ __forceinline__ void named_sync(int id, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
+
+// c = a b, 16x16 by 16x8: the first product of a sum
+__device__ __forceinline__ void mma16x8x16_first(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+        : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
+}
+
+// Bytes of shared memory: the tokens' operands, a factor and a sum for each token and group, the warps' results, the rings
+template <int NT>
+struct FewLayout {
+    int64_t factor, sums, rings, total;
+    __host__ __device__ FewLayout(int k, int groups, int tokens, int depth) {
+        const int64_t units = (k + kUnitCols - 1) / kUnitCols, group = k / groups;   // (columns behind the last: zeros)
+        factor = units * (kUnitCols / 32) * tokens * 64;
+        sums = factor + units * (kUnitCols / group) * (8 * NT) * 8;
+        rings = sums + kTeams * 2 * kTeamWarps * kRows * (8 * NT + 1) * 4;
+        total = rings + kWarps * depth * kUnitBytes;
+    }
 };
 
-// Two codes of a word (nibbles SH / 4 and SH / 4 + 4) as the numbers 1 + c/16
-template <typename T, int NIB>
-__device__ __forceinline__ uint32_t code_pair(uint32_t w) {
-    constexpr bool bf = std::is_same<T, __nv_bfloat16>::value;
-    constexpr int top = bf ? 3 : 6;          // where the four highest bits of the mantissa begin
-    constexpr uint32_t one = bf ? 0x3f803f80u : 0x3c003c00u, mask = 0x000f000fu << top;
-    constexpr int shift = top - 4 * NIB;
-    const uint32_t at = shift >= 0 ? w << (shift >= 0 ? shift : 0) : w >> (shift >= 0 ? 0 : -shift);
-    return (at & mask) | one;
-}
-
-__device__ __forceinline__ float to_float(float x) { return x; }
-__device__ __forceinline__ float to_float(__nv_bfloat16 x) { return __bfloat162float(x); }
-__device__ __forceinline__ float to_float(__half x) { return __half2float(x); }
-
-// c (16x8) = a (16x16) b (16x8): the first product of a sum
-template <typename T>
-__device__ __forceinline__ void mma16x8x16_first(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-    if constexpr (std::is_same<T, __nv_bfloat16>::value)
-        asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
-            : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
-            : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
-    else
-        asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
-            : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
-            : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
-}
-
-// GROUP columns a group; NT blocks of 8 tokens.
-// A warp goes through stages of 128 columns (the block's warps take them in turn): 64 bytes of each of its 32 rows, copied
-// to its own ring in shared memory kStages - 1 stages ahead; the tokens' values and the rows' scales a stage ahead in
-// registers.  No barrier but the one before the warps' sums are joined.
-template <typename T, typename M, int GROUP, int NT>
-__global__ void __launch_bounds__(kWarps * 32, 2) w4_few_kernel(const __grid_constant__ W4Params p) {
-    constexpr int kGroups = 128 / GROUP;             // of a stage
-    constexpr uint32_t ones = std::is_same<T, __nv_bfloat16>::value ? 0x3f803f80u : 0x3c003c00u;
+// Up to 8 NT tokens; GROUP columns a group; a ring of DEPTH units.
+// A block, one a multiprocessor, has two teams of eight warps.  A team goes through slabs of 16 rows, whose UNITS of 256
+// columns its warps take in turn (and go on in turn with the next slab's, so that none has more of them).  A warp is alone
+// with its units: its own ring in shared memory, filled by 16-byte asynchronous copies DEPTH - 1 units ahead, the rows' scales
+// a unit ahead in registers.  At a slab's end the warps' sums are joined in shared memory, with one barrier of the team.
+// Tokens stay in shared memory, in the order of the fragments.
+template <typename T, int GROUP, int NT, int DEPTH>
+__global__ void __launch_bounds__(kThreads, 1) w4_few_kernel(const __grid_constant__ W4Params p) {
+    constexpr int kGroups = kUnitCols / GROUP;   // of a unit
+    constexpr int kTok = 8 * NT;
     extern __shared__ __align__(16) uint8_t smem[];
     __shared__ float2 meta_s[kWarps][2][kGroups][kRows];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
-    const int row0 = blockIdx.x * kRows, tok0 = blockIdx.y * 8 * NT;
-    const int stages = (p.k + 127) / 128;
-    const int mine = warp < stages ? (stages - warp + kWarps - 1) / kWarps : 0;   // stages warp, warp + kWarps, ...
-    uint8_t *ring = smem + warp * kStages * kStageBytes;
-    const uint32_t ring_u = smem_u32(ring);
+    const FewLayout<NT> at(p.k, p.groups, p.tokens, DEPTH);
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, team = warp / kTeamWarps, tw = warp % kTeamWarps;
+    const int g = lane >> 2, t = lane & 3;
+    const int units = (p.k + kUnitCols - 1) / kUnitCols, slabs = (p.n + kRows - 1) / kRows;
+    // the team's slabs: slab0, slab0 + slab_step, ...; as long as there are no more than blocks, each has a block of its own
+    const int slab0 = blockIdx.x + team * gridDim.x, slab_step = kTeams * gridDim.x;
+    const int mine = slab0 < slabs ? (slabs - slab0 + slab_step - 1) / slab_step : 0;
+    auto first_unit = [&](int sl) { return (tw - sl * units) & (kTeamWarps - 1); };
+    uint8_t *ring = smem + at.rings + warp * DEPTH * kUnitBytes;
+    const uint32_t ring_u = smem_u32(ring) + (lane >> 3) * kPitch + (lane & 7) * 16;
     grid_dependency_wait();
 
-    // copies: lane (g, t) the t-th 16 bytes of rows g, g + 8, g + 16, g + 24 (rows behind the last: the last, never written)
-    const uint8_t *codes[4];
+    // ---- copies: lane l the (l % 8)-th 16 bytes of rows l / 8, + 4, + 8, + 12 (rows behind the last: the last, never written)
+    int csl = -1, cu = units, cslot = 0;         // the unit to copy next
+    const uint8_t *cp[4];
+    auto copy_unit = [&]() {
+        if (cu >= units) {
+            while (cu >= units && ++csl < mine) cu = first_unit(csl);
+            if (cu < units)
 #pragma unroll
-    for (int r = 0; r < 4; ++r) codes[r] = p.codes + min(row0 + r * 8 + g, p.n - 1) * p.code_stride + t * 16 + warp * 64;
-    int copied = 0;
-    auto copy_stage = [&]() {
-        if (copied < mine) {
-            const uint32_t dst = ring_u + (copied % kStages) * kStageBytes + g * kPitch + t * 16;
-            if (GROUP == 128 || (warp + copied * kWarps) * 128 + t * 32 < p.k) {
-#pragma unroll
-                for (int r = 0; r < 4; ++r) copy16_async(dst + r * 8 * kPitch, codes[r], 16);
-            }   // (of columns behind the last any codes will do: their tokens' values are zeros)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) codes[r] += kWarps * 64;
+                for (int r = 0; r < 4; ++r)
+                    cp[r] = p.codes + min((slab0 + csl * slab_step) * kRows + (lane >> 3) + 4 * r, p.n - 1) * p.code_stride +
+                            cu * (kUnitCols / 2) + (lane & 7) * 16;
         }
-        ++copied;
+        if (cu < units) {
+            // (of columns behind the last any codes will do: the tokens are zeros there)
+            if ((cu + 1) * kUnitCols <= p.k || cu * kUnitCols + (lane & 7) * 32 < p.k) {
+                const uint32_t dst = ring_u + cslot * kUnitBytes;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) copy16_async(dst + 4 * r * kPitch, cp[r], 16);
+            }
+#pragma unroll
+            for (int r = 0; r < 4; ++r) cp[r] += kTeamWarps * (kUnitCols / 2);
+            cu += kTeamWarps;
+        }
         copy_commit();
+        cslot = cslot + 1 == DEPTH ? 0 : cslot + 1;
     };
-    // scales: a lane has a row
-    const M *scale = static_cast<const M *>(p.scale) + min(row0 + lane, p.n - 1) * p.meta_stride;
-    const M *zero = p.zero ? static_cast<const M *>(p.zero) + min(row0 + lane, p.n - 1) * p.meta_stride : nullptr;
-    M sc[kGroups], ze[kGroups];
-    auto load_meta = [&](int i) {
-        if (i >= mine) return;
-#pragma unroll
-        for (int q = 0; q < kGroups; ++q) {
-            int gr = (warp + i * kWarps) * kGroups + q;
-            if (GROUP < 128) gr = min(gr, p.groups - 1);
-            sc[q] = __ldg(scale + gr);
-            if (zero) ze[q] = __ldg(zero + gr);
+    // ---- scales: lane l < 16 that of row l, lane 16 + l its offset (or the scale again, where there is none)
+    const bool wide = p.meta_dtype == STOM_FP32, narrow_bf = p.meta_dtype == STOM_BF16;
+    const int es = wide ? 4 : 2;
+    const char *meta_of = static_cast<const char *>(lane >= kRows && p.zero ? p.zero : p.scale), *mp = meta_of;
+    const float meta_times = lane < kRows ? kCodeUnit : p.zero ? 1.f : -8.f;
+    int msl = -1, mu = units;                    // the unit whose scales come next
+    uint32_t raw[kGroups];
+    auto load_meta = [&]() {
+        if (mu >= units) {
+            while (mu >= units && ++msl < mine) mu = first_unit(msl);
+            if (mu >= units) return;
+            mp = meta_of + (min((slab0 + msl * slab_step) * kRows + (lane & 15), p.n - 1) * p.meta_stride + mu * kGroups) * es;
         }
-    };
-    // tokens: lane (g, t) the 8 values of columns 32 j + 8 t of token g, in pairs 4 columns apart as the codes of a word
-    const T *x[NT];
-    bool is[NT];
+        const int last = p.groups - 1 - mu * kGroups;   // (groups behind the last: the last, times zeros)
+        if (wide) {
 #pragma unroll
-    for (int j = 0; j < NT; ++j) {
-        const int tok = tok0 + j * 8 + g;
-        is[j] = tok < p.tokens;
-        x[j] = static_cast<const T *>(p.x) + (is[j] ? tok : 0) * p.x_stride + t * 8 + warp * 128;
-    }
-    uint4 xv[4][NT];
-    auto load_x = [&](int i) {
+            for (int q = 0; q < kGroups; ++q) raw[q] = __ldg(reinterpret_cast<const uint32_t *>(mp) + min(q, last));
+        } else {
 #pragma unroll
-        for (int b = 0; b < NT; ++b) {
-            const bool on = is[b] && i < mine;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                xv[j][b] = make_uint4(0, 0, 0, 0);
-                if (on && (GROUP == 128 || (warp + i * kWarps) * 128 + j * 32 < p.k))
-                    xv[j][b] = __ldg(reinterpret_cast<const uint4 *>(x[b] + i * (kWarps * 128) + j * 32));
-            }
+            for (int q = 0; q < kGroups; ++q) raw[q] = __ldg(reinterpret_cast<const uint16_t *>(mp) + min(q, last));
         }
+        mp += kTeamWarps * kGroups * es;
+        mu += kTeamWarps;
     };
-    float acc[2][NT][4];
 #pragma unroll
-    for (int m = 0; m < 2; ++m)
-#pragma unroll
-        for (int j = 0; j < NT; ++j)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) acc[m][j][e] = 0.f;
+    for (int i = 0; i < DEPTH - 1; ++i) copy_unit();
+    load_meta();
 
+    // ---- tokens: a warp takes 256 columns of one at a time, a lane 8 of them; the lanes of a group find its largest value and
+    // its sum
+    float2 *factor = reinterpret_cast<float2 *>(smem + at.factor);   // [group][kTok / 2][factors, sums]
+    for (int i = warp; i < units * p.tokens; i += kWarps) {
+        const int tok = i / units, col = (i - tok * units) * kUnitCols + lane * 8;
+        uint4 v = make_uint4(0, 0, 0, 0);
+        if (col < p.k) v = __ldg(reinterpret_cast<const uint4 *>(static_cast<const T *>(p.x) + tok * p.x_stride + col));
+        float a[8];
+        unpack2<T>(v.x, a[0], a[1]);
+        unpack2<T>(v.y, a[2], a[3]);
+        unpack2<T>(v.z, a[4], a[5]);
+        unpack2<T>(v.w, a[6], a[7]);
+        float sum = ((a[0] + a[1]) + (a[2] + a[3])) + ((a[4] + a[5]) + (a[6] + a[7]));
+        uint32_t m = __vmaxu2(__vmaxu2(v.x & 0x7fff7fffu, v.y & 0x7fff7fffu), __vmaxu2(v.z & 0x7fff7fffu, v.w & 0x7fff7fffu));
+        m = max(m & 0xffffu, m >> 16);
 #pragma unroll
-    for (int i = 0; i < kStages - 1; ++i) copy_stage();
-    load_meta(0);
-    load_x(0);
-#pragma unroll 1
-    for (int i = 0; i < mine; ++i) {
-        float2(*meta)[kRows] = meta_s[warp][i & 1];
-#pragma unroll
-        for (int q = 0; q < kGroups; ++q) {
-            const float s = 16.f * to_float(sc[q]);
-            meta[q][lane] = make_float2(s, zero ? to_float(ze[q]) - s : -1.5f * s);
+        for (int o = 1; o < GROUP / 8; o <<= 1) {
+            sum += __shfl_xor_sync(~0u, sum, o);
+            m = max(m, __shfl_xor_sync(~0u, m, o));
         }
-        load_meta(i + 1);
-        uint32_t b[4][NT][4];
+        float before, after;
+        factors_of<T>(m, before, after);
+        *reinterpret_cast<uint4 *>(smem + ((int64_t)(col / 32 * p.tokens + tok) * 4 + (lane & 3)) * 16) = token_operand<T>(v, before);
+        if (lane % (GROUP / 8) == 0) {
+            float *to = reinterpret_cast<float *>(factor + (col / GROUP * (kTok / 2) + (tok >> 1)) * 2) + (tok & 1);
+            to[0] = after;
+            to[2] = sum;
+        }
+    }
+    __syncthreads();
+
+    // ---- products (a lane of a token that there is not reads the last one's: its columns of the product are not used)
+    const uint8_t *own_x[NT];
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
+    for (int c = 0; c < NT; ++c) own_x[c] = smem + (min(c * 8 + g, p.tokens - 1) * 4 + t) * 16;
+    int slot = 0, turn = 0;
+#pragma unroll 1
+    for (int sl = 0; sl < mine; ++sl) {
+        float acc[NT][4];
 #pragma unroll
-            for (int c = 0; c < NT; ++c) {
-                const uint4 v = xv[j][c];
-                b[j][c][0] = __byte_perm(v.x, v.z, 0x5410), b[j][c][1] = __byte_perm(v.x, v.z, 0x7632);
-                b[j][c][2] = __byte_perm(v.y, v.w, 0x5410), b[j][c][3] = __byte_perm(v.y, v.w, 0x7632);
+        for (int c = 0; c < NT; ++c)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[c][e] = 0.f;
+#pragma unroll 1
+        for (int u = first_unit(sl); u < units; u += kTeamWarps) {
+            float2(*meta)[kRows] = meta_s[warp][turn & 1];
+            ++turn;
+            float *to = reinterpret_cast<float *>(&meta[0][lane & 15]) + (lane >> 4);
+            if (wide || narrow_bf) {
+                const int up = wide ? 0 : 16;
+#pragma unroll
+                for (int q = 0; q < kGroups; ++q) to[q * (2 * kRows)] = __uint_as_float(raw[q] << up) * meta_times;
+            } else {
+#pragma unroll
+                for (int q = 0; q < kGroups; ++q)
+                    to[q * (2 * kRows)] = __half2float(__ushort_as_half((unsigned short)raw[q])) * meta_times;
             }
-        load_x(i + 1);
-        copy_wait<kStages - 2>();
-        __syncwarp();
-        copy_stage();   // into the slot that the stage before this one has left
-        const uint8_t *at = ring + (i % kStages) * kStageBytes + g * kPitch + t * 4;
-        float d[2][NT][4], sx[NT][4];
+            load_meta();
+            copy_wait<DEPTH - 2>();
+            __syncwarp();
+            copy_unit();   // into the slot that the unit before this one has left
+            const uint8_t *cs = ring + slot * kUnitBytes + g * kPitch + t * 4;
+            slot = slot + 1 == DEPTH ? 0 : slot + 1;
+            float d[NT][4];
+            const uint32_t x_at = u * (kUnitCols / 32) * (p.tokens * 64);
+            const float4 *fx = reinterpret_cast<const float4 *>(factor) + u * kGroups * (kTok / 2) + t;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            uint32_t a[2][2][4];   // [16 rows][product][register]
-#pragma unroll
-            for (int m = 0; m < 2; ++m)
+            for (int j = 0; j < kUnitCols / 32; ++j) {
+                uint32_t a[2][4];   // [product][register]
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    const uint32_t v = *reinterpret_cast<const uint32_t *>(at + (2 * m + h) * 8 * kPitch + j * 16);
-                    a[m][0][h] = code_pair<T, 0>(v);
-                    a[m][0][2 + h] = code_pair<T, 1>(v);
-                    a[m][1][h] = code_pair<T, 2>(v);
-                    a[m][1][2 + h] = code_pair<T, 3>(v);
+                    const uint32_t v = *reinterpret_cast<const uint32_t *>(cs + h * 8 * kPitch + j * 16), w = v >> 8;
+                    a[0][h] = v & 0x000f000fu;
+                    a[0][2 + h] = v & 0x00f000f0u;
+                    a[1][h] = w & 0x000f000fu;
+                    a[1][2 + h] = w & 0x00f000f0u;
                 }
-            const uint32_t one[4] = {ones, ones, ones, ones};
-            const bool first = j * 32 % GROUP == 0;
 #pragma unroll
-            for (int c = 0; c < NT; ++c) {
-#pragma unroll
-                for (int m = 0; m < 2; ++m) {
-                    if (first) mma16x8x16_first<T>(d[m][c], a[m][0], b[j][c][0], b[j][c][1]);
-                    else mma16x8x16<T>(d[m][c], a[m][0], b[j][c][0], b[j][c][1]);
-                    mma16x8x16<T>(d[m][c], a[m][1], b[j][c][2], b[j][c][3]);
+                for (int c = 0; c < NT; ++c) {
+                    const uint4 b = *reinterpret_cast<const uint4 *>(own_x[c] + x_at + j * (p.tokens * 64));
+                    if (j * 32 % GROUP == 0) mma16x8x16_first(d[c], a[0], b.x, b.y);
+                    else mma16x8x16<__half>(d[c], a[0], b.x, b.y);
+                    mma16x8x16<__half>(d[c], a[1], b.z, b.w);
                 }
-                if (first) mma16x8x16_first<T>(sx[c], one, b[j][c][0], b[j][c][1]);
-                else mma16x8x16<T>(sx[c], one, b[j][c][0], b[j][c][1]);
-                mma16x8x16<T>(sx[c], one, b[j][c][2], b[j][c][3]);
+                if ((j + 1) * 32 % GROUP == 0) {
+                    const int q = j * 32 / GROUP;
+                    const float2 f0 = meta[q][g], f1 = meta[q][g + 8];
+#pragma unroll
+                    for (int c = 0; c < NT; ++c) {
+                        const float4 x = fx[q * (kTok / 2) + c * 4];   // factors and sums of tokens 2 t, 2 t + 1
+                        acc[c][0] = fmaf(f0.y, x.z, fmaf(f0.x, d[c][0] * x.x, acc[c][0]));
+                        acc[c][1] = fmaf(f0.y, x.w, fmaf(f0.x, d[c][1] * x.y, acc[c][1]));
+                        acc[c][2] = fmaf(f1.y, x.z, fmaf(f1.x, d[c][2] * x.x, acc[c][2]));
+                        acc[c][3] = fmaf(f1.y, x.w, fmaf(f1.x, d[c][3] * x.y, acc[c][3]));
+                    }
+                }
             }
-            if ((j + 1) * 32 % GROUP == 0) {
+        }
+        float(*part)[kRows][kTok + 1] =
+            reinterpret_cast<float(*)[kRows][kTok + 1]>(smem + at.sums) + (team * 2 + (sl & 1)) * kTeamWarps;
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const float2 f = meta[j * 32 / GROUP][r * 8 + g];
+        for (int c = 0; c < NT; ++c)
 #pragma unroll
-                    for (int c = 0; c < NT; ++c)
+            for (int e = 0; e < 4; ++e) part[tw][(e >> 1) * 8 + g][c * 8 + t * 2 + (e & 1)] = acc[c][e];
+        named_sync(1 + team, kTeamWarps * 32);   // (the slab after the next waits here before it writes to this part again)
+        const int row = (slab0 + sl * slab_step) * kRows + (lane & 15);
 #pragma unroll
-                        for (int e = 0; e < 2; ++e) {
-                            float &y = acc[r >> 1][c][(r & 1) * 2 + e];
-                            y = fmaf(f.x, d[r >> 1][c][(r & 1) * 2 + e], y);
-                            y = fmaf(f.y, sx[c][e], y);
-                        }
-                }
+        for (int h = 0; h < (NT + 1) / 2; ++h) {
+            const int c = h * 16 + tw * 2 + (lane >> 4);
+            if (row < p.n && c < p.tokens) {
+                float y = 0.f;
+#pragma unroll
+                for (int w = 0; w < kTeamWarps; ++w) y += part[w][lane & 15][c];
+                if (p.bias) y += to_float(static_cast<const T *>(p.bias)[row]);
+                if (p.add) y += to_float(static_cast<const T *>(p.add)[c * p.add_stride + row]);
+                static_cast<T *>(p.y)[c * p.y_stride + row] = from_float<T>(y);
             }
         }
     }
     copy_wait<0>();
-    __syncthreads();
-    // the warps' sums, in the rings' place
-    float(*sums)[kRows][8 * NT + 1] = reinterpret_cast<float(*)[kRows][8 * NT + 1]>(smem);
-    static_assert(sizeof(float) * kWarps * kRows * (8 * NT + 1) <= kWarps * kStages * kStageBytes, "room for the sums");
-#pragma unroll
-    for (int m = 0; m < 2; ++m)
-#pragma unroll
-        for (int j = 0; j < NT; ++j)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) sums[warp][m * 16 + (e >> 1) * 8 + g][j * 8 + t * 2 + (e & 1)] = acc[m][j][e];
-    __syncthreads();
-    for (int i = threadIdx.x; i < kRows * 8 * NT; i += kWarps * 32) {
-        const int r = i % kRows, c = i / kRows;
-        if (row0 + r >= p.n || tok0 + c >= p.tokens) continue;
-        float y = 0.f;
-#pragma unroll
-        for (int w = 0; w < kWarps; ++w) y += sums[w][r][c];
-        if (p.bias) y += static_cast<float>(static_cast<const T *>(p.bias)[row0 + r]);
-        if (p.add) y += static_cast<float>(static_cast<const T *>(p.add)[(tok0 + c) * p.add_stride + row0 + r]);
-        static_cast<T *>(p.y)[(tok0 + c) * p.y_stride + row0 + r] = from_float<T>(y);
-    }
 }
 
-template <typename T, typename M, int GROUP, int NT>
-cudaError_t launch(const W4Params &p, cudaStream_t s) {
-    const dim3 grid((p.n + kRows - 1) / kRows, (p.tokens + 8 * NT - 1) / (8 * NT));
-    constexpr int smem = kWarps * kStages * kStageBytes;
+template <typename T, int GROUP, int NT, int DEPTH>
+bool launch_few(const W4Params &p, int sms, cudaStream_t s, cudaError_t &e) {
+    const FewLayout<NT> l(p.k, p.groups, p.tokens, DEPTH);
+    if (l.total > kMostShared) return false;
     static std::atomic<uint64_t> allowed{0};
-    const cudaError_t e = allow_shared(reinterpret_cast<const void *>(w4_few_kernel<T, M, GROUP, NT>), smem, allowed);
-    return e != cudaSuccess ? e : launch_after_producer(w4_few_kernel<T, M, GROUP, NT>, grid, dim3(kWarps * 32), smem, s, p);
+    e = allow_shared(reinterpret_cast<const void *>(w4_few_kernel<T, GROUP, NT, DEPTH>), kMostShared, allowed);
+    const int slabs = (p.n + kRows - 1) / kRows;
+    if (e == cudaSuccess)
+        e = launch_after_producer(w4_few_kernel<T, GROUP, NT, DEPTH>, dim3(slabs < sms ? slabs : sms), dim3(kThreads), (size_t)l.total, s, p);
+    return true;
 }
 
-template <typename T, typename M, int GROUP>
-cudaError_t by_tokens(const W4Params &p, cudaStream_t s) {
-    return p.tokens <= 8 ? launch<T, M, GROUP, 1>(p, s) : launch<T, M, GROUP, 2>(p, s);
-}
-
+// The few-tokens kernel where its tokens fit into shared memory, with the longest rings that fit beside them
 template <typename T, int GROUP>
-cudaError_t by_meta(const W4Params &p, cudaStream_t s) {
-    return p.meta_dtype == STOM_FP32   ? by_tokens<T, float, GROUP>(p, s)
-           : p.meta_dtype == STOM_BF16 ? by_tokens<T, __nv_bfloat16, GROUP>(p, s)
-                                       : by_tokens<T, __half, GROUP>(p, s);
+cudaError_t by_tokens(const W4Params &p, int sms, cudaStream_t s) {
+    cudaError_t e = cudaSuccess;
+    if (p.tokens <= 8 && (launch_few<T, GROUP, 1, 4>(p, sms, s, e) || launch_few<T, GROUP, 1, 3>(p, sms, s, e))) return e;
+    if (p.tokens > 8 && p.tokens <= 16 && launch_few<T, GROUP, 2, 3>(p, sms, s, e)) return e;
+    return w4_many<T>(p, GROUP, sms, s);
 }
 
 template <typename T>
-cudaError_t by_group(const W4Params &p, int group, cudaStream_t s) {
-    return group == 32 ? by_meta<T, 32>(p, s) : group == 64 ? by_meta<T, 64>(p, s) : by_meta<T, 128>(p, s);
+cudaError_t by_group(const W4Params &p, int group, int sms, cudaStream_t s) {
+    return group == 32 ? by_tokens<T, 32>(p, sms, s) : group == 64 ? by_tokens<T, 64>(p, sms, s) : by_tokens<T, 128>(p, sms, s);
 }
 
 }  // namespace
@@ -286,7 +279,7 @@ using namespace stom;
 
 extern "C" int32_t stom_w4_linear(const stom_w4_matrix *w, int32_t dtype, int32_t rows, const void *x, int64_t x_stride,
                                   const void *bias, const void *add, int64_t add_stride, void *y, int64_t y_stride,
-                                  void *stream) {
+                                  uint32_t *dev_flags, void *stream) {
     if (!w || !w->codes || !w->scale || w->n < 1 || w->k < 1 || rows < 0) return STOM_ERR_INVALID_ARG;
     if (w->group != 32 && w->group != 64 && w->group != 128) return STOM_ERR_SHAPE;
     if (w->k % w->group || rows > 65535 * 8) return STOM_ERR_SHAPE;
@@ -302,6 +295,8 @@ extern "C" int32_t stom_w4_linear(const stom_w4_matrix *w, int32_t dtype, int32_
     if ((reinterpret_cast<uintptr_t>(bias) | reinterpret_cast<uintptr_t>(add) | reinterpret_cast<uintptr_t>(y)) & 1u)
         return STOM_ERR_ALIGNMENT;
     if (rows > 1 && (x_stride < 0 || y_stride < w->n || (add && add_stride < 0))) return STOM_ERR_INVALID_ARG;
+    const int sms = sm_count();
+    if (!sms) return STOM_ERR_CUDA;
     W4Params p = {};
     p.codes = w->codes;
     p.scale = w->scale;
@@ -320,8 +315,9 @@ extern "C" int32_t stom_w4_linear(const stom_w4_matrix *w, int32_t dtype, int32_
     p.y = y;
     p.y_stride = y_stride;
     p.tokens = rows;
+    p.flags = dev_flags;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    const cudaError_t e = dtype == STOM_BF16 ? by_group<__nv_bfloat16>(p, w->group, s) : by_group<__half>(p, w->group, s);
+    const cudaError_t e = dtype == STOM_BF16 ? by_group<__nv_bfloat16>(p, w->group, sms, s) : by_group<__half>(p, w->group, sms, s);
     if (e != cudaSuccess) {
         set_last_cuda_error(e);
         return STOM_ERR_CUDA;

@@ -107,7 +107,7 @@ _SIGNATURES = {
     "stom_kv_attend_tree_workspace_bytes": (C.c_int64, "ppii"),
     "stom_kv_attend_tree": (C.c_int32, "ppii" + "pp" + "ipllffi" + "pllp" + "plpp"),
     "stom_kv_accept": (C.c_int32, "ppi" + "pppp" + "ppp" + "pp"),
-    "stom_w4_linear": (C.c_int32, "piipl" + "ppl" + "pl" + "p"),
+    "stom_w4_linear": (C.c_int32, "piipl" + "ppl" + "pl" + "pp"),
 }
 
 _lib = None
@@ -623,8 +623,8 @@ class W4Matrix:
         self.ref = C.addressof(self.desc)
 
 
-def stom_w4_linear(w: W4Matrix, x, y, bias=None, add=None, stream=None):
+def stom_w4_linear(w: W4Matrix, x, y, bias=None, add=None, dev_flags=None, stream=None):
     """y = x W^T + bias + add; x: [rows][k], y and add: [rows][n], bias: [n], all bfloat16 or all float16; add may be y."""
-    rc = _binding().w4_linear(w.ref, w.dev, x, y, bias, add, _handle(stream))
+    rc = _binding().w4_linear(w.ref, w.dev, x, y, bias, add, dev_flags, _handle(stream))
     if rc:
         _check(rc, "stom_w4_linear")

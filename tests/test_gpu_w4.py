@@ -63,9 +63,11 @@ def _call(s, bias=True, add=True):
     oqm = _lib()
     n = s["codes"].shape[0]
     y = torch.full((s["x"].shape[0], n), 7.0, dtype=s["x"].dtype, device="cuda")
+    flags = torch.zeros(1, dtype=torch.int32, device="cuda")
     oqm.stom_w4_linear(oqm.W4Matrix(s["codes"], s["scale"], s["zero"]), s["x"], y, bias=s["bias"] if bias else None,
-                       add=s["add"] if add else None)
+                       add=s["add"] if add else None, dev_flags=flags)
     torch.cuda.synchronize()
+    assert flags.item() == 0
     return y
 
 

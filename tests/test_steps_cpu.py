@@ -86,7 +86,7 @@ def linear(oqm, w=None, **kw):  # noqa: F811
     a.update(kw)
     desc = oqm.W4Desc(*[m[n] for n, _ in oqm.W4Desc._fields_])
     return oqm.lib().stom_w4_linear(C.byref(desc), a["dt"], a["rows"], a["x"], a["xs"], a["bias"], a["add"], a["adds"], a["y"],
-                                    a["ys"], None)
+                                    a["ys"], None, None)
 
 
 @pytest.mark.parametrize("w,code", [
