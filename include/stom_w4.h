@@ -36,13 +36,20 @@ typedef struct stom_w4_matrix {
  * rounded once to dtype.
  * x, add, y (dtype: STOM_BF16 | STOM_FP16): element (t, i) at t*stride + i; x
  * and its stride 16-byte aligned, the others any alignment of an element.
+ * x values below 2^-22 (fp16) or 2^-25 (bf16) of the largest of their token and
+ * group lose bits, 2^-36 of that at most; a token with a value that is no finite
+ * number gives no finite numbers.
  * bias [n] (dtype) and add may be NULL; add may be y; x and y do not overlap.
  * STOM_FLAG_TIMEOUT in the optional dev_flags: a bounded wait inside a kernel
  * ran out, y is not to be used.
- * Errors: INVALID_ARG, SHAPE, UNSUPPORTED, ALIGNMENT, CUDA. */
+ * workspace: 128-byte aligned, of at least stom_w4_workspace_bytes() bytes (none
+ * for few tokens); its contents do not matter, and it may be used by one call at
+ * a time.  k <= 2^24, n < 2^23 - 127, rows <= 524 280.
+ * Errors: INVALID_ARG, SHAPE, UNSUPPORTED, ALIGNMENT, WORKSPACE, CUDA. */
+int64_t stom_w4_workspace_bytes(const stom_w4_matrix *w, int32_t rows);
 int32_t stom_w4_linear(const stom_w4_matrix *w, int32_t dtype, int32_t rows, const void *x, int64_t x_stride,
                        const void *bias, const void *add, int64_t add_stride, void *y, int64_t y_stride,
-                       uint32_t *dev_flags, void *stream);
+                       void *workspace, int64_t workspace_bytes, uint32_t *dev_flags, void *stream);
 
 #ifdef __cplusplus
 }

@@ -7,6 +7,7 @@
 #include <Python.h>
 
 #include <ATen/core/Tensor.h>
+#include <ATen/ops/empty.h>
 #include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
@@ -34,6 +35,7 @@ struct Library {
     decltype(&stom_kv_attend_tree) attend_tree = nullptr;
     decltype(&stom_kv_accept) accept = nullptr;
     decltype(&stom_w4_linear) w4_linear = nullptr;
+    decltype(&stom_w4_workspace_bytes) w4_workspace = nullptr;
 } lib;
 
 [[noreturn]] void refuse(const char *name, const std::string &needed, const at::Tensor *t) {
@@ -226,9 +228,10 @@ PyObject *accept(PyObject *, PyObject *const *a, Py_ssize_t count) {
     });
 }
 
-// matrix, device, x, y, bias, add, dev_flags, stream
+// matrix, device, x, y, bias, add, workspace, dev_flags, stream; a workspace that is needed and not given is taken from torch's
+// allocator, for the stream of the call
 PyObject *w4_linear(PyObject *, PyObject *const *a, Py_ssize_t count) {
-    return guarded(count, 8, [&] {
+    return guarded(count, 9, [&] {
         const auto *w = at_address<stom_w4_matrix>(a[0]);
         const int64_t dev = integer(a[1]);
         const at::Tensor &x = must(a[2], "x");
@@ -255,9 +258,22 @@ PyObject *w4_linear(PyObject *, PyObject *const *a, Py_ssize_t count) {
         }
         Rows add;
         if (a[5] != Py_None) add = flat(a[5], w->n, "add");
-        uint32_t *fl = flags(a[6], dev);
-        const On on(dev, a[7]);
-        return lib.w4_linear(w, dtype, (int32_t)n, in.at, in.row, bias, add.at, add.row, out.at, out.row, fl, on.stream);
+        uint32_t *fl = flags(a[7], dev);
+        const On on(dev, a[8]);
+        int64_t bytes = 0;
+        void *ws = nullptr;
+        at::Tensor own;
+        if (a[6] != Py_None) {
+            ws = workspace(a[6], dev, bytes);
+        } else if (n > 0 && (bytes = lib.w4_workspace(w, (int32_t)n)) > 0) {
+            const c10::cuda::CUDAStream current = c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)dev);
+            c10::cuda::OptionalCUDAStreamGuard use;
+            if (on.stream != (void *)current.stream())
+                use.reset_stream(c10::cuda::getStreamFromExternal((cudaStream_t)on.stream, (c10::DeviceIndex)dev));
+            own = at::empty({bytes}, at::TensorOptions().dtype(at::kByte).device(at::kCUDA, (c10::DeviceIndex)dev));
+            ws = own.data_ptr();
+        }
+        return lib.w4_linear(w, dtype, (int32_t)n, in.at, in.row, bias, add.at, add.row, out.at, out.row, ws, bytes, fl, on.stream);
     });
 }
 
@@ -401,7 +417,7 @@ PyObject *sample(PyObject *, PyObject *const *a, Py_ssize_t count) {
 
 // the addresses of the library's entry points, in the order of Library
 PyObject *use(PyObject *, PyObject *const *a, Py_ssize_t n) {
-    return guarded(n, 11, [&] {
+    return guarded(n, 12, [&] {
         lib.attend = reinterpret_cast<decltype(lib.attend)>(integer(a[0]));
         lib.rotate = reinterpret_cast<decltype(lib.rotate)>(integer(a[1]));
         lib.append = reinterpret_cast<decltype(lib.append)>(integer(a[2]));
@@ -413,6 +429,7 @@ PyObject *use(PyObject *, PyObject *const *a, Py_ssize_t n) {
         lib.attend_tree = reinterpret_cast<decltype(lib.attend_tree)>(integer(a[8]));
         lib.accept = reinterpret_cast<decltype(lib.accept)>(integer(a[9]));
         lib.w4_linear = reinterpret_cast<decltype(lib.w4_linear)>(integer(a[10]));
+        lib.w4_workspace = reinterpret_cast<decltype(lib.w4_workspace)>(integer(a[11]));
         return 0;
     });
 }

@@ -129,7 +129,7 @@ __global__ void __launch_bounds__(kThreads, 1) w4_few_kernel(const __grid_consta
     for (int i = warp; i < units * p.tokens; i += kWarps) {
         const int tok = i / units, col = (i - tok * units) * kUnitCols + lane * 8;
         uint4 v = make_uint4(0, 0, 0, 0);
-        if (col < p.k) v = __ldg(reinterpret_cast<const uint4 *>(static_cast<const T *>(p.x) + tok * p.x_stride + col));
+        if (col < p.k) v = *reinterpret_cast<const uint4 *>(static_cast<const T *>(p.x) + tok * p.x_stride + col);
         float a[8];
         unpack2<T>(v.x, a[0], a[1]);
         unpack2<T>(v.y, a[2], a[3]);
@@ -245,30 +245,35 @@ __global__ void __launch_bounds__(kThreads, 1) w4_few_kernel(const __grid_consta
     copy_wait<0>();
 }
 
+// Units of a warp's ring with which the few-tokens kernel fits into shared memory, or 0
+template <int NT>
+int depth_of(int k, int groups, int tokens) {
+    for (int depth = 4; depth >= 3; --depth)
+        if (FewLayout<NT>(k, groups, tokens, depth).total <= kMostShared) return depth;
+    return 0;
+}
+// The few-tokens kernel where there are at most 8 and they fit into shared memory
+bool is_few(int k, int groups, int tokens) { return tokens <= 8 && depth_of<1>(k, groups, tokens) > 0; }
+
 template <typename T, int GROUP, int NT, int DEPTH>
-bool launch_few(const W4Params &p, int sms, cudaStream_t s, cudaError_t &e) {
+cudaError_t launch_few(const W4Params &p, int sms, cudaStream_t s) {
     const FewLayout<NT> l(p.k, p.groups, p.tokens, DEPTH);
-    if (l.total > kMostShared) return false;
     static std::atomic<uint64_t> allowed{0};
-    e = allow_shared(reinterpret_cast<const void *>(w4_few_kernel<T, GROUP, NT, DEPTH>), kMostShared, allowed);
+    const cudaError_t e = allow_shared(reinterpret_cast<const void *>(w4_few_kernel<T, GROUP, NT, DEPTH>), kMostShared, allowed);
+    if (e != cudaSuccess) return e;
     const int slabs = (p.n + kRows - 1) / kRows;
-    if (e == cudaSuccess)
-        e = launch_after_producer(w4_few_kernel<T, GROUP, NT, DEPTH>, dim3(slabs < sms ? slabs : sms), dim3(kThreads), (size_t)l.total, s, p);
-    return true;
+    return launch_after_producer(w4_few_kernel<T, GROUP, NT, DEPTH>, dim3(slabs < sms ? slabs : sms), dim3(kThreads), (size_t)l.total, s, p);
 }
 
-// The few-tokens kernel where its tokens fit into shared memory, with the longest rings that fit beside them
 template <typename T, int GROUP>
-cudaError_t by_tokens(const W4Params &p, int sms, cudaStream_t s) {
-    cudaError_t e = cudaSuccess;
-    if (p.tokens <= 8 && (launch_few<T, GROUP, 1, 4>(p, sms, s, e) || launch_few<T, GROUP, 1, 3>(p, sms, s, e))) return e;
-    if (p.tokens > 8 && p.tokens <= 16 && launch_few<T, GROUP, 2, 3>(p, sms, s, e)) return e;
-    return w4_many<T>(p, GROUP, sms, s);
+cudaError_t by_tokens(const W4Params &p, int sms, void *workspace, cudaStream_t s) {
+    if (!is_few(p.k, p.groups, p.tokens)) return w4_many<T>(p, GROUP, workspace, s);
+    return depth_of<1>(p.k, p.groups, p.tokens) == 4 ? launch_few<T, GROUP, 1, 4>(p, sms, s) : launch_few<T, GROUP, 1, 3>(p, sms, s);
 }
 
 template <typename T>
-cudaError_t by_group(const W4Params &p, int group, int sms, cudaStream_t s) {
-    return group == 32 ? by_tokens<T, 32>(p, sms, s) : group == 64 ? by_tokens<T, 64>(p, sms, s) : by_tokens<T, 128>(p, sms, s);
+cudaError_t by_group(const W4Params &p, int group, int sms, void *ws, cudaStream_t s) {
+    return group == 32 ? by_tokens<T, 32>(p, sms, ws, s) : group == 64 ? by_tokens<T, 64>(p, sms, ws, s) : by_tokens<T, 128>(p, sms, ws, s);
 }
 
 }  // namespace
@@ -277,24 +282,38 @@ cudaError_t by_group(const W4Params &p, int group, int sms, cudaStream_t s) {
 
 using namespace stom;
 
-extern "C" int32_t stom_w4_linear(const stom_w4_matrix *w, int32_t dtype, int32_t rows, const void *x, int64_t x_stride,
-                                  const void *bias, const void *add, int64_t add_stride, void *y, int64_t y_stride,
-                                  uint32_t *dev_flags, void *stream) {
+static int32_t check_matrix(const stom_w4_matrix *w, int32_t rows) {
     if (!w || !w->codes || !w->scale || w->n < 1 || w->k < 1 || rows < 0) return STOM_ERR_INVALID_ARG;
     if (w->group != 32 && w->group != 64 && w->group != 128) return STOM_ERR_SHAPE;
-    if (w->k % w->group || rows > 65535 * 8) return STOM_ERR_SHAPE;
+    if (w->k % w->group || w->k > (1 << 24) || w->n > (1 << 23) - 128 || rows > 65535 * 8) return STOM_ERR_SHAPE;
     if (w->meta_dtype != STOM_BF16 && w->meta_dtype != STOM_FP16 && w->meta_dtype != STOM_FP32) return STOM_ERR_UNSUPPORTED;
-    if (dtype != STOM_BF16 && dtype != STOM_FP16) return STOM_ERR_UNSUPPORTED;
     if (!aligned16(w->codes) || w->code_stride % 16) return STOM_ERR_ALIGNMENT;
     const uintptr_t meta = reinterpret_cast<uintptr_t>(w->scale) | reinterpret_cast<uintptr_t>(w->zero);
     if (meta & (elem_bytes(w->meta_dtype) - 1)) return STOM_ERR_ALIGNMENT;
     if (w->n > 1 && (w->code_stride < w->k / 2 || w->meta_stride < w->k / w->group)) return STOM_ERR_INVALID_ARG;
+    return STOM_OK;
+}
+
+extern "C" int64_t stom_w4_workspace_bytes(const stom_w4_matrix *w, int32_t rows) {
+    const int32_t rc = check_matrix(w, rows);
+    if (rc) return rc;
+    return rows == 0 || is_few(w->k, w->k / w->group, rows) ? 0 : w4_many_workspace(w->k, w->group, rows);
+}
+
+extern "C" int32_t stom_w4_linear(const stom_w4_matrix *w, int32_t dtype, int32_t rows, const void *x, int64_t x_stride,
+                                  const void *bias, const void *add, int64_t add_stride, void *y, int64_t y_stride,
+                                  void *workspace, int64_t workspace_bytes, uint32_t *dev_flags, void *stream) {
+    const int32_t rc = check_matrix(w, rows);
+    if (rc) return rc;
+    if (dtype != STOM_BF16 && dtype != STOM_FP16) return STOM_ERR_UNSUPPORTED;
     if (rows == 0) return STOM_OK;
     if (!x || !y) return STOM_ERR_INVALID_ARG;
     if (!aligned16(x) || !stride_ok(x_stride, dtype)) return STOM_ERR_ALIGNMENT;
     if ((reinterpret_cast<uintptr_t>(bias) | reinterpret_cast<uintptr_t>(add) | reinterpret_cast<uintptr_t>(y)) & 1u)
         return STOM_ERR_ALIGNMENT;
     if (rows > 1 && (x_stride < 0 || y_stride < w->n || (add && add_stride < 0))) return STOM_ERR_INVALID_ARG;
+    const int64_t need = stom_w4_workspace_bytes(w, rows);
+    if (need > 0 && (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 127u) || workspace_bytes < need)) return STOM_ERR_WORKSPACE;
     const int sms = sm_count();
     if (!sms) return STOM_ERR_CUDA;
     W4Params p = {};
@@ -317,7 +336,8 @@ extern "C" int32_t stom_w4_linear(const stom_w4_matrix *w, int32_t dtype, int32_
     p.tokens = rows;
     p.flags = dev_flags;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    const cudaError_t e = dtype == STOM_BF16 ? by_group<__nv_bfloat16>(p, w->group, sms, s) : by_group<__half>(p, w->group, sms, s);
+    const cudaError_t e = dtype == STOM_BF16 ? by_group<__nv_bfloat16>(p, w->group, sms, workspace, s)
+                                             : by_group<__half>(p, w->group, sms, workspace, s);
     if (e != cudaSuccess) {
         set_last_cuda_error(e);
         return STOM_ERR_CUDA;

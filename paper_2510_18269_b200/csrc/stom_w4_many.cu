@@ -1,240 +1,401 @@
-// Products of many tokens with 4-bit weights (stom_w4_linear).
+// Products of many tokens with 4-bit weights (stom_w4_linear): from about as many tokens on as a fragment has, the multiplying
+// is done by the fifth-generation tensor cores.
+//
+// What bounds it: at 16 tokens the codes' bytes, as for one; at 64 the instructions that make operands of them and that
+// scale the groups' sums.  A first small kernel makes operands of the tokens, once for all blocks (see stom_w4.cuh): the tiles
+// of the right operand as they lie in shared memory, 128-byte-swizzled, and a factor and a sum for each token and group.
+//
+// A block has 128 rows of the matrix, N tokens and a part of the columns, a STAGE of 128 of them at a time.  Codes arrive by
+// 16-byte asynchronous copies, 256 columns at a time, several ahead.  Eight warps unpack: a thread has one row and half of a stage's
+// columns, 8 words that become 8 chunks of 16 bytes in the left operand (K-major, 128-byte swizzle; two stages of it).  One
+// thread issues the products, each group into accumulators of their own in tensor memory, since scales differ from
+// group to group; the eight warps fold those of the stage before into their sums while the products of this one run: a
+// thread has a row again, and half of the tokens.
+// Blocks that share out the columns of the same rows form a cluster (up to 8, so many that all multiprocessors have a
+// block), whose sums are joined over distributed shared memory.
+#include "stom_tensor.cuh"
 #include "stom_w4.cuh"
 
 namespace stom {
 
 namespace {
 
-constexpr int kRows = 32, kWarps = 8, kSomeStages = 4;
-constexpr int kSomePitch = 80;    // bytes from row to row of a stage in shared memory: 8 rows' words of 4 lanes lie in 32 banks
-constexpr int kSomeStageBytes = kRows * kSomePitch;
+constexpr int kRows = 128, kStageCols = 128;
+constexpr int kWorkWarps = 8, kWorkThreads = kWorkWarps * 32, kThreads = kWorkThreads + 4 * 32;
+constexpr int kChunkCols = 256, kChunks = 4;              // columns of a copy, copies in the ring
+constexpr int kPitch = kChunkCols / 2 + 16, kChunkBytes = kRows * kPitch;   // an odd number of 16 bytes: a row a thread without conflicts
+constexpr int kAStage = kRows * kStageCols * 2, kBStages = 3;
+constexpr unsigned long long kWaitLimitNs = 1000000000ull;   // a wait that has taken 1 s ends the block
 
-// Two codes of a word (nibbles SH / 4 and SH / 4 + 4) as the numbers 1 + c/16
-template <typename T, int NIB>
-__device__ __forceinline__ uint32_t code_pair(uint32_t w) {
-    constexpr bool bf = std::is_same<T, __nv_bfloat16>::value;
-    constexpr int top = bf ? 3 : 6;          // where the four highest bits of the mantissa begin
-    constexpr uint32_t one = bf ? 0x3f803f80u : 0x3c003c00u, mask = 0x000f000fu << top;
-    constexpr int shift = top - 4 * NIB;
-    const uint32_t at = shift >= 0 ? w << (shift >= 0 ? shift : 0) : w >> (shift >= 0 ? 0 : -shift);
-    return (at & mask) | one;
-}
+// Bytes of a stage's operand of the tokens, factors and sums
+__host__ __device__ constexpr int stage_bytes(int group, int n) { return n * kStageCols * 2 + kStageCols / group * n * 8; }
 
+struct ManyParams {
+    W4Params w;
+    uint8_t *image;        // [token tile][stage]: operand [2][N][128 bytes], factors [group][N], sums [group][N]
+    int32_t stages, split; // of 128 columns; blocks of a cluster
+};
 
 __device__ __forceinline__ void named_sync(int id, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
 
-// c (16x8) = a (16x16) b (16x8): the first product of a sum
-template <typename T>
-__device__ __forceinline__ void mma16x8x16_first(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-    if constexpr (std::is_same<T, __nv_bfloat16>::value)
-        asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
-            : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
-            : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
-    else
-        asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
-            : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
-            : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
-}
-
-// GROUP columns a group; NT blocks of 8 tokens.
-// A warp goes through stages of 128 columns (the block's warps take them in turn): 64 bytes of each of its 32 rows, copied
-// to its own ring in shared memory kSomeStages - 1 stages ahead; the tokens' values and the rows' scales a stage ahead in
-// registers.  No barrier but the one before the warps' sums are joined.
-template <typename T, typename M, int GROUP, int NT>
-__global__ void __launch_bounds__(kWarps * 32, 2) w4_some_kernel(const __grid_constant__ W4Params p) {
-    constexpr int kGroups = 128 / GROUP;             // of a stage
-    constexpr uint32_t ones = std::is_same<T, __nv_bfloat16>::value ? 0x3f803f80u : 0x3c003c00u;
-    extern __shared__ __align__(16) uint8_t smem[];
-    __shared__ float2 meta_s[kWarps][2][kGroups][kRows];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
-    const int row0 = blockIdx.x * kRows, tok0 = blockIdx.y * 8 * NT;
-    const int stages = (p.k + 127) / 128;
-    const int mine = warp < stages ? (stages - warp + kWarps - 1) / kWarps : 0;   // stages warp, warp + kWarps, ...
-    uint8_t *ring = smem + warp * kSomeStages * kSomeStageBytes;
-    const uint32_t ring_u = smem_u32(ring);
+// Operands of the tokens: a warp has 256 columns of one, a lane 8; tokens and columns behind the last become zeros
+template <typename T, int GROUP, int N>
+__global__ void __launch_bounds__(256) w4_tokens_kernel(const __grid_constant__ ManyParams p) {
     grid_dependency_wait();
-
-    // copies: lane (g, t) the t-th 16 bytes of rows g, g + 8, g + 16, g + 24 (rows behind the last: the last, never written)
-    const uint8_t *codes[4];
+    grid_launch_dependents();   // (behind the wait: what the next kernel reads before its own wait, the weights, is there)
+    const int lane = threadIdx.x & 31, spans = (p.stages + 1) / 2;
+    const int i = blockIdx.x * 8 + (threadIdx.x >> 5), tok = i / spans, col = (i - tok * spans) * 256 + lane * 8;
+    if (tok >= (p.w.tokens + N - 1) / N * N) return;
+    uint4 v = make_uint4(0, 0, 0, 0);
+    if (tok < p.w.tokens && col < p.w.k)
+        v = *reinterpret_cast<const uint4 *>(static_cast<const T *>(p.w.x) + tok * p.w.x_stride + col);
+    float a[8];
+    unpack2<T>(v.x, a[0], a[1]);
+    unpack2<T>(v.y, a[2], a[3]);
+    unpack2<T>(v.z, a[4], a[5]);
+    unpack2<T>(v.w, a[6], a[7]);
+    float sum = ((a[0] + a[1]) + (a[2] + a[3])) + ((a[4] + a[5]) + (a[6] + a[7]));
+    uint32_t m = __vmaxu2(__vmaxu2(v.x & 0x7fff7fffu, v.y & 0x7fff7fffu), __vmaxu2(v.z & 0x7fff7fffu, v.w & 0x7fff7fffu));
+    m = max(m & 0xffffu, m >> 16);
 #pragma unroll
-    for (int r = 0; r < 4; ++r) codes[r] = p.codes + min(row0 + r * 8 + g, p.n - 1) * p.code_stride + t * 16 + warp * 64;
-    int copied = 0;
-    auto copy_stage = [&]() {
-        if (copied < mine) {
-            const uint32_t dst = ring_u + (copied % kSomeStages) * kSomeStageBytes + g * kSomePitch + t * 16;
-            if (GROUP == 128 || (warp + copied * kWarps) * 128 + t * 32 < p.k) {
-#pragma unroll
-                for (int r = 0; r < 4; ++r) copy16_async(dst + r * 8 * kSomePitch, codes[r], 16);
-            }   // (of columns behind the last any codes will do: their tokens' values are zeros)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) codes[r] += kWarps * 64;
-        }
-        ++copied;
-        copy_commit();
-    };
-    // scales: a lane has a row
-    const M *scale = static_cast<const M *>(p.scale) + min(row0 + lane, p.n - 1) * p.meta_stride;
-    const M *zero = p.zero ? static_cast<const M *>(p.zero) + min(row0 + lane, p.n - 1) * p.meta_stride : nullptr;
-    M sc[kGroups], ze[kGroups];
-    auto load_meta = [&](int i) {
-        if (i >= mine) return;
-#pragma unroll
-        for (int q = 0; q < kGroups; ++q) {
-            int gr = (warp + i * kWarps) * kGroups + q;
-            if (GROUP < 128) gr = min(gr, p.groups - 1);
-            sc[q] = __ldg(scale + gr);
-            if (zero) ze[q] = __ldg(zero + gr);
-        }
-    };
-    // tokens: lane (g, t) the 8 values of columns 32 j + 8 t of token g, in pairs 4 columns apart as the codes of a word
-    const T *x[NT];
-    bool is[NT];
-#pragma unroll
-    for (int j = 0; j < NT; ++j) {
-        const int tok = tok0 + j * 8 + g;
-        is[j] = tok < p.tokens;
-        x[j] = static_cast<const T *>(p.x) + (is[j] ? tok : 0) * p.x_stride + t * 8 + warp * 128;
+    for (int o = 1; o < GROUP / 8; o <<= 1) {
+        sum += __shfl_xor_sync(~0u, sum, o);
+        m = max(m, __shfl_xor_sync(~0u, m, o));
     }
-    uint4 xv[4][NT];
-    auto load_x = [&](int i) {
-#pragma unroll
-        for (int b = 0; b < NT; ++b) {
-            const bool on = is[b] && i < mine;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                xv[j][b] = make_uint4(0, 0, 0, 0);
-                if (on && (GROUP == 128 || (warp + i * kWarps) * 128 + j * 32 < p.k))
-                    xv[j][b] = __ldg(reinterpret_cast<const uint4 *>(x[b] + i * (kWarps * 128) + j * 32));
-            }
-        }
-    };
-    float acc[2][NT][4];
-#pragma unroll
-    for (int m = 0; m < 2; ++m)
-#pragma unroll
-        for (int j = 0; j < NT; ++j)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) acc[m][j][e] = 0.f;
+    const int stage = col / kStageCols;
+    if (stage >= p.stages) return;
+    float before, after;
+    factors_of<T>(m, before, after);
+    const int tile = tok / N, row = tok % N, block = col / 64 & 1, chunk = col / 8 & 7;
+    constexpr int kGroups = kStageCols / GROUP;
+    uint8_t *to = p.image + ((int64_t)tile * p.stages + stage) * stage_bytes(GROUP, N);
+    *reinterpret_cast<uint4 *>(to + (block * N + row) * 128 + ((chunk ^ (row & 7)) << 4)) = token_operand<T>(v, before);
+    if (lane % (GROUP / 8) == 0) {
+        float *f = reinterpret_cast<float *>(to + N * kStageCols * 2) + (col / GROUP % kGroups) * N + row;
+        f[0] = after;
+        f[kGroups * N] = sum;
+    }
+}
 
+template <int GROUP, int N>
+struct Many {
+    static constexpr int kGroups = kStageCols / GROUP;         // of a stage
+    static constexpr int kBStage = (stage_bytes(GROUP, N) + 1023) / 1024 * 1024;
+    static constexpr int kMeta = kChunkCols / GROUP * kRows * 8;
+    static constexpr int kCols = 2 * kGroups * N < 32 ? 32 : 2 * kGroups * N;   // of tensor memory, a power of two
+    static constexpr int kOffB = 2 * kAStage, kOffCodes = kOffB + kBStages * kBStage, kOffMeta = kOffCodes + kChunks * kChunkBytes;
+    static constexpr int kSmem = 1024 + kOffMeta + 3 * kMeta;
+    static constexpr int kPitchOut = kRows + 4;                // floats from token to token of the sums that a cluster joins
+    static_assert(kSmem <= 226 * 1024 && kCols <= 512, "room");
+    static_assert(N * kPitchOut * 4 <= 2 * kAStage, "the sums take the left operand's place");
+};
+
+template <typename T, int GROUP, int N>
+__global__ void __launch_bounds__(kThreads, 1) w4_many_kernel(const __grid_constant__ ManyParams p) {
+    using S = Many<GROUP, N>;
+    constexpr int kGroups = S::kGroups, kBStage = S::kBStage, kHalf = N / 2;
+    extern __shared__ uint8_t raw_smem[];
+    __shared__ uint64_t c_full[kChunks], c_empty[kChunks], b_full[kBStages], b_empty[kBStages], a_full[2], done[2], folded[2], drained;
+    __shared__ uint32_t tmem_word, abort_word, never_word;   // never_word stays 0
+    uint8_t *smem = raw_smem + ((1024u - (smem_u32(raw_smem) & 1023u)) & 1023u);   // the swizzle goes by addresses
+    const uint32_t smem_at = smem_u32(smem);
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int rank = blockIdx.x, row0 = blockIdx.y * kRows, tile = blockIdx.z;
+    // the block's stages, as equal shares as they can be
+    const int s0 = (int)((int64_t)p.stages * rank / p.split), n_stages = (int)((int64_t)p.stages * (rank + 1) / p.split) - s0;
+    const int col0 = s0 * kStageCols, n_chunks = (n_stages + 1) / 2;
+    volatile uint32_t *abort_flag = &abort_word;
+    if (tid == 0) {
+        for (int i = 0; i < kChunks; ++i) mbar_init(smem_u32(&c_full[i]), 64), mbar_init(smem_u32(&c_empty[i]), kWorkWarps);
+        for (int i = 0; i < kBStages; ++i) mbar_init(smem_u32(&b_full[i]), 1), mbar_init(smem_u32(&b_empty[i]), 1 + kWorkWarps);
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(smem_u32(&a_full[i]), kWorkThreads);
+            mbar_init(smem_u32(&done[i]), 1);
+            mbar_init(smem_u32(&folded[i]), kWorkThreads);
+        }
+        mbar_init(smem_u32(&drained), 1);
+        abort_word = never_word = 0;
+        mbar_init_fence();
+    }
+    if (warp == kWorkWarps + 1) tmem_alloc(smem_u32(&tmem_word), S::kCols);
+    tc_fence_before_sync();
+    __syncthreads();
+    tc_fence_after_sync();
+    const uint32_t tmem = tmem_word;
+    auto wait = [&](uint64_t &b, uint32_t parity) {
+        const bool ok = mbar_wait_bounded(smem_u32(&b), parity & 1u, abort_flag, kWaitLimitNs);
+        if (!ok) *abort_flag = 1;
+        return ok;
+    };
+    float acc[kHalf];
 #pragma unroll
-    for (int i = 0; i < kSomeStages - 1; ++i) copy_stage();
-    load_meta(0);
-    load_x(0);
+    for (int i = 0; i < kHalf; ++i) acc[i] = 0.f;
+    const int quarter = warp & 3, side = warp >> 2, row = quarter * 32 + lane;   // of a working thread
+
+    if (warp == kWorkWarps || warp == kWorkWarps + 3) {
+        // ---- codes: two warps with half of the rows each, 16 bytes a lane, 4 rows at a time (rows behind the last: the last,
+        // never written).  Weights are read before the tokens' kernel is waited for: it began when all before it had ended.
+        // (Bulk copies of a row's 128 bytes each would take as long as 60 clocks apiece.)
+        const int half = (warp - kWorkWarps) / 3 * 64, mine = row0 + half + (lane >> 3);
+        const uint8_t *from = p.w.codes + col0 / 2 + (lane & 7) * 16;
+        uint32_t to = smem_at + S::kOffCodes + (half + (lane >> 3)) * kPitch + (lane & 7) * 16;
+        for (int c = 0; c < n_chunks; ++c) {
+            const int slot = c % kChunks;
+            if (c >= kChunks && !__all_sync(~0u, wait(c_empty[slot], c / kChunks - 1))) break;
+            if (col0 + c * kChunkCols + (lane & 7) * 32 < p.w.k) {   // (of columns behind the last any codes will do)
+                const uint8_t *src = from + c * (kChunkCols / 2);
+                const uint32_t dst = to + slot * kChunkBytes;
+                if (row0 + kRows <= p.w.n) {
+                    src += mine * p.w.code_stride;
+#pragma unroll
+                    for (int r = 0; r < 16; ++r, src += 4 * p.w.code_stride) copy16_async(dst + r * 4 * kPitch, src, 16);
+                } else {
+#pragma unroll 4
+                    for (int r = 0; r < 16; ++r)
+                        copy16_async(dst + r * 4 * kPitch, src + min(mine + 4 * r, p.w.n - 1) * p.w.code_stride, 16);
+                }
+            }
+            asm volatile("cp.async.mbarrier.arrive.noinc.shared.b64 [%0];" ::"r"(smem_u32(&c_full[slot])) : "memory");
+        }
+        asm volatile("cp.async.wait_all;" ::: "memory");
+    } else if (warp == kWorkWarps + 2) {
+        // ---- operands of the tokens
+        grid_dependency_wait();
+        if (lane == 0)
+            for (int s = 0; s < n_stages; ++s) {
+                const int slot = s % kBStages;
+                if (s >= kBStages && !wait(b_empty[slot], s / kBStages - 1)) break;
+                constexpr int kBytes = stage_bytes(GROUP, N);
+                mbar_expect_tx(smem_u32(&b_full[slot]), kBytes);
+                bulk_load(smem_at + S::kOffB + slot * kBStage, p.image + ((int64_t)tile * p.stages + s0 + s) * kBytes, kBytes,
+                          smem_u32(&b_full[slot]));
+            }
+    } else if (warp == kWorkWarps + 1) {
+        // ---- products
+        if (lane == 0) {
+            const uint32_t idesc = umma_idesc(0, N);
+            for (int s = 0; s < n_stages; ++s) {
+                const int b = s & 1, slot = s % kBStages;
+                if (!(wait(b_full[slot], s / kBStages) && wait(a_full[b], s >> 1) && (s < 2 || wait(folded[b], (s >> 1) - 1)))) break;
+                tc_fence_after_sync();
+                const uint32_t as = smem_at + b * kAStage, bs = smem_at + S::kOffB + slot * kBStage;
+#pragma unroll
+                for (int ks = 0; ks < kStageCols / 16; ++ks)
+                    umma_ss(tmem + (b * kGroups + ks * 16 / GROUP) * N, umma_desc_k128(as + (ks >> 2) * (kRows * 128) + (ks & 3) * 32),
+                            umma_desc_k128(bs + (ks >> 2) * (N * 128) + (ks & 3) * 32), idesc, ks * 16 % GROUP != 0);
+                umma_commit(smem_u32(&b_empty[slot]));
+                umma_commit(smem_u32(&done[b]));
+            }
+            umma_commit(smem_u32(&drained));   // before tensor memory is given back
+            if (!mbar_wait_bounded(smem_u32(&drained), 0, &never_word, kWaitLimitNs)) *abort_flag = 1;
+        }
+    } else {
+        // ---- unpacking and folding.  Scales of a chunk's groups go to shared memory as pairs; a thread brings kPairs of them,
+        // a chunk ahead in registers, into one of three buffers (the one before the last may still be read).
+        constexpr int kChunkGroups = kChunkCols / GROUP, kPairs = kChunkGroups * kRows / kWorkThreads;
+        const bool wide = p.w.meta_dtype == STOM_FP32, narrow_bf = p.w.meta_dtype == STOM_BF16;
+        uint32_t rs[kPairs], rz[kPairs];
+        auto load_meta = [&](int c) {
+#pragma unroll
+            for (int i = 0; i < kPairs; ++i) {
+                const int e = i * kWorkThreads + tid, r = e / kChunkGroups, gr = (col0 + c * kChunkCols) / GROUP + e % kChunkGroups;
+                rs[i] = rz[i] = 0;
+                if (c >= n_chunks || gr >= p.w.groups) continue;
+                const int64_t at = min(row0 + r, p.w.n - 1) * p.w.meta_stride + gr;
+                if (wide) {
+                    rs[i] = __ldg(static_cast<const uint32_t *>(p.w.scale) + at);
+                    if (p.w.zero) rz[i] = __ldg(static_cast<const uint32_t *>(p.w.zero) + at);
+                } else {
+                    rs[i] = __ldg(static_cast<const uint16_t *>(p.w.scale) + at);
+                    if (p.w.zero) rz[i] = __ldg(static_cast<const uint16_t *>(p.w.zero) + at);
+                }
+            }
+        };
+        auto number = [&](uint32_t bits) {
+            return wide ? __uint_as_float(bits) : narrow_bf ? __uint_as_float(bits << 16) : __half2float(__ushort_as_half((unsigned short)bits));
+        };
+        auto fold = [&](int s) {
+            const int b = s & 1;
+            wait(b_full[s % kBStages], s / kBStages);
+            wait(done[b], s >> 1);   // (a wait that has failed: what is there is used, and the call flagged)
+            __syncwarp();
+            tc_fence_after_sync();
+            const float2 *meta = reinterpret_cast<const float2 *>(smem + S::kOffMeta + (s >> 1) % 3 * S::kMeta) +
+                                 (s & 1) * kGroups * kRows + row;
+#pragma unroll
+            for (int q = 0; q < kGroups; ++q) {
+                float d[kHalf];
+                tmem_load(tmem + ((uint32_t)(32 * quarter) << 16) + (b * kGroups + q) * N + side * kHalf, d);
+                if (q == kGroups - 1) {
+                    tc_fence_before_sync();
+                    mbar_arrive(smem_u32(&folded[b]));
+                }
+                const float2 f = meta[q * kRows];
+                const float4 *fx = reinterpret_cast<const float4 *>(smem + S::kOffB + s % kBStages * kBStage + N * kStageCols * 2) +
+                                   (q * N + side * kHalf) / 4;
+                const float4 *sx = fx + kGroups * N / 4;
+#pragma unroll
+                for (int i = 0; i < kHalf; i += 4) {
+                    const float4 x = fx[i / 4], y = sx[i / 4];
+                    acc[i] = fmaf(f.y, y.x, fmaf(f.x, d[i] * x.x, acc[i]));
+                    acc[i + 1] = fmaf(f.y, y.y, fmaf(f.x, d[i + 1] * x.y, acc[i + 1]));
+                    acc[i + 2] = fmaf(f.y, y.z, fmaf(f.x, d[i + 2] * x.z, acc[i + 2]));
+                    acc[i + 3] = fmaf(f.y, y.w, fmaf(f.x, d[i + 3] * x.w, acc[i + 3]));
+                }
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&b_empty[s % kBStages]));
+        };
+        load_meta(0);
+        for (int c = 0; c < n_chunks; ++c) {
+            float2 *meta = reinterpret_cast<float2 *>(smem + S::kOffMeta + c % 3 * S::kMeta);
+#pragma unroll
+            for (int i = 0; i < kPairs; ++i) {
+                const int e = i * kWorkThreads + tid, r = e / kChunkGroups, q = e % kChunkGroups;
+                const float s = number(rs[i]);
+                meta[q * kRows + r] = make_float2(kCodeUnit * s, p.w.zero ? number(rz[i]) : -8.f * s);
+            }
+            load_meta(c + 1);
+            named_sync(1, kWorkThreads);
+            wait(c_full[c % kChunks], c / kChunks);
+            __syncwarp();
 #pragma unroll 1
-    for (int i = 0; i < mine; ++i) {
-        float2(*meta)[kRows] = meta_s[warp][i & 1];
+            for (int h = 0; h < 2; ++h) {
+                const int s = 2 * c + h, b = s & 1;
+                if (s >= n_stages) break;
+                // (the products of stage s - 2 are done: this thread has folded them)
+                const uint4 *from = reinterpret_cast<const uint4 *>(smem + S::kOffCodes + c % kChunks * kChunkBytes + row * kPitch + h * 64 + side * 32);
+                uint8_t *to = smem + b * kAStage + side * (kRows * 128) + row * 128;
 #pragma unroll
-        for (int q = 0; q < kGroups; ++q) {
-            const float s = 16.f * to_float(sc[q]);
-            meta[q][lane] = make_float2(s, zero ? to_float(ze[q]) - s : -1.5f * s);
-        }
-        load_meta(i + 1);
-        uint32_t b[4][NT][4];
+                for (int i = 0; i < 2; ++i) {
+                    const uint4 v = from[i];
+                    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-#pragma unroll
-            for (int c = 0; c < NT; ++c) {
-                const uint4 v = xv[j][c];
-                b[j][c][0] = __byte_perm(v.x, v.z, 0x5410), b[j][c][1] = __byte_perm(v.x, v.z, 0x7632);
-                b[j][c][2] = __byte_perm(v.y, v.w, 0x5410), b[j][c][3] = __byte_perm(v.y, v.w, 0x7632);
-            }
-        load_x(i + 1);
-        copy_wait<kSomeStages - 2>();
-        __syncwarp();
-        copy_stage();   // into the slot that the stage before this one has left
-        const uint8_t *at = ring + (i % kSomeStages) * kSomeStageBytes + g * kSomePitch + t * 4;
-        float d[2][NT][4], sx[NT][4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            uint32_t a[2][2][4];   // [16 rows][product][register]
-#pragma unroll
-            for (int m = 0; m < 2; ++m)
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const uint32_t v = *reinterpret_cast<const uint32_t *>(at + (2 * m + h) * 8 * kSomePitch + j * 16);
-                    a[m][0][h] = code_pair<T, 0>(v);
-                    a[m][0][2 + h] = code_pair<T, 1>(v);
-                    a[m][1][h] = code_pair<T, 2>(v);
-                    a[m][1][2 + h] = code_pair<T, 3>(v);
+                    for (int j = 0; j < 4; ++j) {
+                        const uint32_t u = w[j] >> 8;
+                        *reinterpret_cast<uint4 *>(to + (((i * 4 + j) ^ (row & 7)) << 4)) =
+                            make_uint4(w[j] & 0x000f000fu, w[j] & 0x00f000f0u, u & 0x000f000fu, u & 0x00f000f0u);
+                    }
                 }
-            const uint32_t one[4] = {ones, ones, ones, ones};
-            const bool first = j * 32 % GROUP == 0;
-#pragma unroll
-            for (int c = 0; c < NT; ++c) {
-#pragma unroll
-                for (int m = 0; m < 2; ++m) {
-                    if (first) mma16x8x16_first<T>(d[m][c], a[m][0], b[j][c][0], b[j][c][1]);
-                    else mma16x8x16<T>(d[m][c], a[m][0], b[j][c][0], b[j][c][1]);
-                    mma16x8x16<T>(d[m][c], a[m][1], b[j][c][2], b[j][c][3]);
+                fence_proxy_async();
+                mbar_arrive(smem_u32(&a_full[b]));
+                if (h == 1 || s + 1 == n_stages) {
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(smem_u32(&c_empty[c % kChunks]));
                 }
-                if (first) mma16x8x16_first<T>(sx[c], one, b[j][c][0], b[j][c][1]);
-                else mma16x8x16<T>(sx[c], one, b[j][c][0], b[j][c][1]);
-                mma16x8x16<T>(sx[c], one, b[j][c][2], b[j][c][3]);
-            }
-            if ((j + 1) * 32 % GROUP == 0) {
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const float2 f = meta[j * 32 / GROUP][r * 8 + g];
-#pragma unroll
-                    for (int c = 0; c < NT; ++c)
-#pragma unroll
-                        for (int e = 0; e < 2; ++e) {
-                            float &y = acc[r >> 1][c][(r & 1) * 2 + e];
-                            y = fmaf(f.x, d[r >> 1][c][(r & 1) * 2 + e], y);
-                            y = fmaf(f.y, sx[c][e], y);
-                        }
-                }
+                if (s > 0) fold(s - 1);
             }
         }
+        fold(n_stages - 1);
+        // sums to where the left operand was: its products are done
+        float *out = reinterpret_cast<float *>(smem);
+#pragma unroll
+        for (int i = 0; i < kHalf; ++i) out[(side * kHalf + i) * S::kPitchOut + row] = acc[i];
     }
-    copy_wait<0>();
     __syncthreads();
-    // the warps' sums, in the rings' place
-    float(*sums)[kRows][8 * NT + 1] = reinterpret_cast<float(*)[kRows][8 * NT + 1]>(smem);
-    static_assert(sizeof(float) * kWarps * kRows * (8 * NT + 1) <= kWarps * kSomeStages * kSomeStageBytes, "room for the sums");
-#pragma unroll
-    for (int m = 0; m < 2; ++m)
-#pragma unroll
-        for (int j = 0; j < NT; ++j)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) sums[warp][m * 16 + (e >> 1) * 8 + g][j * 8 + t * 2 + (e & 1)] = acc[m][j][e];
-    __syncthreads();
-    for (int i = threadIdx.x; i < kRows * 8 * NT; i += kWarps * 32) {
-        const int r = i % kRows, c = i / kRows;
-        if (row0 + r >= p.n || tok0 + c >= p.tokens) continue;
-        float y = 0.f;
-#pragma unroll
-        for (int w = 0; w < kWarps; ++w) y += sums[w][r][c];
-        if (p.bias) y += static_cast<float>(static_cast<const T *>(p.bias)[row0 + r]);
-        if (p.add) y += static_cast<float>(static_cast<const T *>(p.add)[(tok0 + c) * p.add_stride + row0 + r]);
-        static_cast<T *>(p.y)[(tok0 + c) * p.y_stride + row0 + r] = from_float<T>(y);
+    if (tid == 0 && *abort_flag && p.w.flags) atomicOr(p.w.flags, STOM_FLAG_TIMEOUT);
+    if (warp == kWorkWarps + 1) tmem_dealloc(tmem, S::kCols);
+    grid_dependency_wait();
+    cluster_sync();   // every block's sums are there
+    // a block of the cluster joins every split-th token
+    const float *out = reinterpret_cast<const float *>(smem);
+    if (tid < kWorkThreads) {
+        const int r = tid & (kRows - 1), at_row = row0 + r;
+        for (int i = rank + (tid >> 7) * p.split; i < N; i += 2 * p.split) {
+            const int tok = tile * N + i;
+            if (tok >= p.w.tokens || at_row >= p.w.n) continue;
+            float y = 0.f;
+            for (int b = 0; b < p.split; ++b) y += ld_cluster_f(out + i * S::kPitchOut + r, b);
+            if (p.w.bias) y += to_float(static_cast<const T *>(p.w.bias)[at_row]);
+            if (p.w.add) y += to_float(static_cast<const T *>(p.w.add)[tok * p.w.add_stride + at_row]);
+            static_cast<T *>(p.w.y)[tok * p.w.y_stride + at_row] = from_float<T>(y);
+        }
     }
+    cluster_sync();   // nobody reads this block's sums any more
 }
 
-template <typename T, typename M, int GROUP, int NT>
-cudaError_t launch(const W4Params &p, cudaStream_t s) {
-    const dim3 grid((p.n + kRows - 1) / kRows, (p.tokens + 8 * NT - 1) / (8 * NT));
-    constexpr int smem = kWarps * kSomeStages * kSomeStageBytes;
+int tokens_of_tile(int tokens) { return tokens <= 16 ? 16 : tokens <= 32 ? 32 : 64; }
+
+// Blocks that share out the columns: the number for which the longest-working multiprocessor has the fewest stages to go
+// through (a block's beginning and end count for about six).  room[i]: clusters of i + 1 blocks that the device holds at once
+// (fewer than its multiprocessors would do: a cluster lies within one of its parts).
+int split_of(int stages, int64_t tiles, const int (&room)[8]) {
+    int best = 1;
+    int64_t least = INT64_MAX;
+    for (int split = 1; split <= 8 && split <= stages; ++split) {
+        if (room[split - 1] < 1) continue;
+        const int64_t rounds = (tiles + room[split - 1] - 1) / room[split - 1], cost = rounds * ((stages + split - 1) / split + 6);
+        if (cost < least) {
+            least = cost;
+            best = split;
+        }
+    }
+    return best;
+}
+
+template <typename T, int GROUP, int N>
+cudaError_t launch(ManyParams &p, cudaStream_t s) {
+    const int row_tiles = (p.w.n + kRows - 1) / kRows, tiles = (p.w.tokens + N - 1) / N;
     static std::atomic<uint64_t> allowed{0};
-    const cudaError_t e = allow_shared(reinterpret_cast<const void *>(w4_some_kernel<T, M, GROUP, NT>), smem, allowed);
-    return e != cudaSuccess ? e : launch_after_producer(w4_some_kernel<T, M, GROUP, NT>, grid, dim3(kWarps * 32), smem, s, p);
+    cudaError_t e = allow_shared(reinterpret_cast<const void *>(w4_many_kernel<T, GROUP, N>), Many<GROUP, N>::kSmem, allowed);
+    if (e != cudaSuccess) return e;
+    cudaLaunchConfig_t lc = {};
+    lc.blockDim = dim3(kThreads);
+    lc.dynamicSmemBytes = Many<GROUP, N>::kSmem;
+    lc.stream = s;
+    cudaLaunchAttribute at[2];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+    at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[1].val.programmaticStreamSerializationAllowed = 1;
+    lc.attrs = at;
+    // what a device holds does not change: asked for once
+    static std::atomic<int> known[64][8];
+    int dev = 0, room[8];
+    e = cudaGetDevice(&dev);
+    for (int i = 0; i < 8 && e == cudaSuccess; ++i) {
+        room[i] = dev < 64 ? known[dev][i].load(std::memory_order_relaxed) : 0;
+        if (room[i]) continue;
+        at[0].val.clusterDim.x = i + 1;
+        lc.gridDim = dim3(i + 1);
+        lc.numAttrs = 1;
+        e = cudaOccupancyMaxActiveClusters(&room[i], w4_many_kernel<T, GROUP, N>, &lc);
+        if (room[i] < 1) room[i] = -1;
+        if (dev < 64) known[dev][i].store(room[i], std::memory_order_relaxed);
+    }
+    if (e != cudaSuccess) return e;
+    p.split = split_of(p.stages, (int64_t)row_tiles * tiles, room);
+    const int warps = tiles * N * ((p.stages + 1) / 2);
+    e = launch_after_producer(w4_tokens_kernel<T, GROUP, N>, dim3((warps + 7) / 8), dim3(256), 0, s, p);
+    if (e != cudaSuccess) return e;
+    lc.gridDim = dim3(p.split, row_tiles, tiles);
+    at[0].val.clusterDim.x = p.split;
+    lc.numAttrs = 2;
+    return cudaLaunchKernelEx(&lc, w4_many_kernel<T, GROUP, N>, p);
 }
-
 
 template <typename T, int GROUP>
-cudaError_t by_meta(const W4Params &p, cudaStream_t s) {
-    return p.meta_dtype == STOM_FP32   ? launch<T, float, GROUP, 2>(p, s)
-           : p.meta_dtype == STOM_BF16 ? launch<T, __nv_bfloat16, GROUP, 2>(p, s)
-                                       : launch<T, __half, GROUP, 2>(p, s);
+cudaError_t by_tokens(ManyParams &p, cudaStream_t s) {
+    const int n = tokens_of_tile(p.w.tokens);
+    return n == 16 ? launch<T, GROUP, 16>(p, s) : n == 32 ? launch<T, GROUP, 32>(p, s) : launch<T, GROUP, 64>(p, s);
 }
 
 }  // namespace
 
-template <typename T>
-cudaError_t w4_many(const W4Params &p, int group, int sms, cudaStream_t s) {
-    return group == 32 ? by_meta<T, 32>(p, s) : group == 64 ? by_meta<T, 64>(p, s) : by_meta<T, 128>(p, s);
+int64_t w4_many_workspace(int32_t k, int32_t group, int32_t tokens) {
+    const int64_t n = tokens_of_tile(tokens);
+    return (tokens + n - 1) / n * ((k + kStageCols - 1) / kStageCols) * stage_bytes(group, (int)n);
 }
-template cudaError_t w4_many<__nv_bfloat16>(const W4Params &, int, int, cudaStream_t);
-template cudaError_t w4_many<__half>(const W4Params &, int, int, cudaStream_t);
+
+template <typename T>
+cudaError_t w4_many(const W4Params &w, int group, void *workspace, cudaStream_t s) {
+    ManyParams p = {};
+    p.w = w;
+    p.stages = (w.k + kStageCols - 1) / kStageCols;
+    p.image = static_cast<uint8_t *>(workspace);
+    return group == 32 ? by_tokens<T, 32>(p, s) : group == 64 ? by_tokens<T, 64>(p, s) : by_tokens<T, 128>(p, s);
+}
+template cudaError_t w4_many<__nv_bfloat16>(const W4Params &, int, void *, cudaStream_t);
+template cudaError_t w4_many<__half>(const W4Params &, int, void *, cudaStream_t);
 
 }  // namespace stom

@@ -41,7 +41,8 @@ EXPORTS = (
     "stom_kv_frequencies", "stom_kv_attend_workspace_bytes", "stom_kv_attend",
     "stom_kv_rotate", "stom_kv_append", "stom_kv_pages_workspace_bytes", "stom_kv_reserve", "stom_kv_fork",
     "stom_kv_free", "stom_kv_compact", "stom_sample_tokens",
-    "stom_kv_attend_tree_workspace_bytes", "stom_kv_attend_tree", "stom_kv_accept", "stom_w4_linear",
+    "stom_kv_attend_tree_workspace_bytes", "stom_kv_attend_tree", "stom_kv_accept", "stom_w4_workspace_bytes",
+    "stom_w4_linear",
 )
 
 
@@ -107,13 +108,15 @@ _SIGNATURES = {
     "stom_kv_attend_tree_workspace_bytes": (C.c_int64, "ppii"),
     "stom_kv_attend_tree": (C.c_int32, "ppii" + "pp" + "ipllffi" + "pllp" + "plpp"),
     "stom_kv_accept": (C.c_int32, "ppi" + "pppp" + "ppp" + "pp"),
-    "stom_w4_linear": (C.c_int32, "piipl" + "ppl" + "pl" + "pp"),
+    "stom_w4_workspace_bytes": (C.c_int64, "pi"),
+    "stom_w4_linear": (C.c_int32, "piipl" + "ppl" + "pl" + "plpp"),
 }
 
 _lib = None
 _bind = None   # the binding of the calls that are made once per token, loaded by the first of them
 _BOUND = ("stom_kv_attend", "stom_kv_rotate", "stom_kv_append", "stom_kv_reserve", "stom_kv_fork", "stom_kv_free",
-          "stom_kv_compact", "stom_sample_tokens", "stom_kv_attend_tree", "stom_kv_accept", "stom_w4_linear")
+          "stom_kv_compact", "stom_sample_tokens", "stom_kv_attend_tree", "stom_kv_accept", "stom_w4_linear",
+          "stom_w4_workspace_bytes")
 
 
 def lib():
@@ -623,8 +626,16 @@ class W4Matrix:
         self.ref = C.addressof(self.desc)
 
 
-def stom_w4_linear(w: W4Matrix, x, y, bias=None, add=None, dev_flags=None, stream=None):
-    """y = x W^T + bias + add; x: [rows][k], y and add: [rows][n], bias: [n], all bfloat16 or all float16; add may be y."""
-    rc = _binding().w4_linear(w.ref, w.dev, x, y, bias, add, dev_flags, _handle(stream))
+def stom_w4_workspace_bytes(w: W4Matrix, rows: int) -> int:
+    n = lib().stom_w4_workspace_bytes(w.ref, rows)
+    if n < 0:
+        _check(int(n), "stom_w4_workspace_bytes")
+    return int(n)
+
+
+def stom_w4_linear(w: W4Matrix, x, y, bias=None, add=None, workspace=None, dev_flags=None, stream=None):
+    """y = x W^T + bias + add; x: [rows][k], y and add: [rows][n], bias: [n], all bfloat16 or all float16; add may be y.
+    workspace None: what is needed is taken from torch's allocator for the call."""
+    rc = _binding().w4_linear(w.ref, w.dev, x, y, bias, add, workspace, dev_flags, _handle(stream))
     if rc:
         _check(rc, "stom_w4_linear")

@@ -199,6 +199,26 @@ def test_captured_replayed_and_repeated(rows):
     _check(s, y, False, False)
 
 
+def test_workspaces_given_and_not_given_on_any_stream():
+    oqm = _lib()
+    s = _make(40, 300, 1024, 128)
+    w = oqm.W4Matrix(s["codes"], s["scale"], s["zero"])
+    assert oqm.stom_w4_workspace_bytes(w, 3) == 0 and oqm.stom_w4_workspace_bytes(w, 0) == 0
+    need = oqm.stom_w4_workspace_bytes(w, 40)
+    want = _call(s, False, False)
+    ws = torch.full((need + 64,), 255, dtype=torch.uint8, device="cuda")
+    ys = [torch.zeros_like(want) for _ in range(3)]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    oqm.stom_w4_linear(w, s["x"], ys[0], workspace=ws[:need])
+    for i, st in enumerate(streams):                               # two calls at once, each with a workspace of torch's
+        oqm.stom_w4_linear(w, s["x"], ys[1 + i], stream=st)
+    torch.cuda.synchronize()
+    assert all(torch.equal(y, want) for y in ys) and (ws[need:] == 255).all()
+    with pytest.raises(oqm.StomError):
+        oqm.stom_w4_linear(w, s["x"], ys[0], workspace=ws[:need - 1])
+
+
 def test_no_token():
     s = _make(0, 70, 512, 64)
     assert _call(s).shape == (0, 70)

@@ -82,17 +82,18 @@ def test_accept_needs_counts(oqm):  # noqa: F811
 def linear(oqm, w=None, **kw):  # noqa: F811
     m = dict(codes=P, scale=P, zero=P, n=70, k=512, group=64, meta_dtype=0, code_stride=256, meta_stride=8)
     m.update(w or {})
-    a = dict(dt=0, rows=5, x=P, xs=512, bias=P, add=P, adds=70, y=P, ys=70)
+    a = dict(dt=0, rows=5, x=P, xs=512, bias=P, add=P, adds=70, y=P, ys=70, ws=P, nb=1 << 30)
     a.update(kw)
     desc = oqm.W4Desc(*[m[n] for n, _ in oqm.W4Desc._fields_])
     return oqm.lib().stom_w4_linear(C.byref(desc), a["dt"], a["rows"], a["x"], a["xs"], a["bias"], a["add"], a["adds"], a["y"],
-                                    a["ys"], None, None)
+                                    a["ys"], a["ws"], a["nb"], None, None)
 
 
 @pytest.mark.parametrize("w,code", [
     (dict(codes=None), -1), (dict(scale=None), -1), (dict(n=0), -1), (dict(k=0), -1), (dict(k=96, group=64), -2), (dict(group=16), -2),
     (dict(group=256), -2), (dict(group=0), -2), (dict(meta_dtype=3), -6), (dict(codes=P + 8), -3), (dict(code_stride=264), -3),
     (dict(code_stride=240), -1), (dict(meta_stride=7), -1), (dict(scale=P + 1), -3), (dict(zero=P + 2, meta_dtype=2), -3),
+    (dict(n=1 << 23), -2), (dict(k=(1 << 24) + 64, code_stride=1 << 24, meta_stride=1 << 20), -2),
 ])
 def test_linear_refuses_bad_matrices(oqm, w, code):  # noqa: F811
     assert linear(oqm, w) == code
@@ -101,7 +102,8 @@ def test_linear_refuses_bad_matrices(oqm, w, code):  # noqa: F811
 @pytest.mark.parametrize("kw,code", [
     (dict(dt=2), -6), (dict(dt=5), -6), (dict(rows=-1), -1), (dict(x=None), -1), (dict(y=None), -1), (dict(x=P + 8), -3),
     (dict(xs=516), -3), (dict(xs=-512), -1), (dict(ys=69), -1), (dict(adds=-70), -1), (dict(y=P + 1), -3), (dict(bias=P + 1), -3),
-    (dict(add=P + 1), -3), (dict(rows=65535 * 8 + 1), -2),
+    (dict(add=P + 1), -3), (dict(rows=65535 * 8 + 1), -2), (dict(rows=40, ws=None), -8), (dict(rows=40, ws=P + 64), -8),
+    (dict(rows=40, nb=1000), -8),
 ])
 def test_linear_refuses(oqm, kw, code):  # noqa: F811
     assert linear(oqm, **kw) == code
