@@ -6,11 +6,11 @@
 // of the right operand as they lie in shared memory, 128-byte-swizzled, and a factor and a sum for each token and group.
 //
 // A block has 128 rows of the matrix, N tokens and a part of the columns, a STAGE of 128 of them at a time.  Codes arrive by
-// 16-byte asynchronous copies, 256 columns at a time, several ahead.  Eight warps unpack: a thread has one row and half of a stage's
-// columns, 8 words that become 8 chunks of 16 bytes in the left operand (K-major, 128-byte swizzle; two stages of it).  One
+// 16-byte asynchronous copies, 256 columns at a time, several ahead.  Sixteen warps unpack: a thread has one row and a quarter of a
+// stage's columns, 4 words that become 4 chunks of 16 bytes in the left operand (K-major, 128-byte swizzle; two stages of it).  One
 // thread issues the products, each group into accumulators of their own in tensor memory, since scales differ from
-// group to group; the eight warps fold those of the stage before into their sums while the products of this one run: a
-// thread has a row again, and half of the tokens.
+// group to group; the sixteen warps fold those of the stage before into their sums while the products of this one run: a
+// thread has a row again, and a quarter of the tokens.
 // Blocks that share out the columns of the same rows form a cluster (up to 8, so many that all multiprocessors have a
 // block), whose sums are joined over distributed shared memory.
 #include "stom_tensor.cuh"
@@ -21,7 +21,7 @@ namespace stom {
 namespace {
 
 constexpr int kRows = 128, kStageCols = 128;
-constexpr int kWorkWarps = 8, kWorkThreads = kWorkWarps * 32, kThreads = kWorkThreads + 4 * 32;
+constexpr int kWorkWarps = 16, kSides = kWorkWarps / 4, kWorkThreads = kWorkWarps * 32, kThreads = kWorkThreads + 4 * 32;
 constexpr int kChunkCols = 256, kChunks = 4;              // columns of a copy, copies in the ring
 constexpr int kPitch = kChunkCols / 2 + 16, kChunkBytes = kRows * kPitch;   // an odd number of 16 bytes: a row a thread without conflicts
 constexpr int kAStage = kRows * kStageCols * 2, kBStages = 3;
@@ -93,7 +93,7 @@ struct Many {
 template <typename T, int GROUP, int N>
 __global__ void __launch_bounds__(kThreads, 1) w4_many_kernel(const __grid_constant__ ManyParams p) {
     using S = Many<GROUP, N>;
-    constexpr int kGroups = S::kGroups, kBStage = S::kBStage, kHalf = N / 2;
+    constexpr int kGroups = S::kGroups, kBStage = S::kBStage, kOwn = N / kSides;   // tokens of a thread
     extern __shared__ uint8_t raw_smem[];
     __shared__ uint64_t c_full[kChunks], c_empty[kChunks], b_full[kBStages], b_empty[kBStages], a_full[2], done[2], folded[2], drained;
     __shared__ uint32_t tmem_word, abort_word, never_word;   // never_word stays 0
@@ -127,9 +127,9 @@ __global__ void __launch_bounds__(kThreads, 1) w4_many_kernel(const __grid_const
         if (!ok) *abort_flag = 1;
         return ok;
     };
-    float acc[kHalf];
+    float acc[kOwn];
 #pragma unroll
-    for (int i = 0; i < kHalf; ++i) acc[i] = 0.f;
+    for (int i = 0; i < kOwn; ++i) acc[i] = 0.f;
     const int quarter = warp & 3, side = warp >> 2, row = quarter * 32 + lane;   // of a working thread
 
     if (warp == kWorkWarps || warp == kWorkWarps + 3) {
@@ -192,7 +192,7 @@ __global__ void __launch_bounds__(kThreads, 1) w4_many_kernel(const __grid_const
     } else {
         // ---- unpacking and folding.  Scales of a chunk's groups go to shared memory as pairs; a thread brings kPairs of them,
         // a chunk ahead in registers, into one of three buffers (the one before the last may still be read).
-        constexpr int kChunkGroups = kChunkCols / GROUP, kPairs = kChunkGroups * kRows / kWorkThreads;
+        constexpr int kChunkGroups = kChunkCols / GROUP, kAll = kChunkGroups * kRows, kPairs = (kAll + kWorkThreads - 1) / kWorkThreads;
         const bool wide = p.w.meta_dtype == STOM_FP32, narrow_bf = p.w.meta_dtype == STOM_BF16;
         uint32_t rs[kPairs], rz[kPairs];
         auto load_meta = [&](int c) {
@@ -200,7 +200,7 @@ __global__ void __launch_bounds__(kThreads, 1) w4_many_kernel(const __grid_const
             for (int i = 0; i < kPairs; ++i) {
                 const int e = i * kWorkThreads + tid, r = e / kChunkGroups, gr = (col0 + c * kChunkCols) / GROUP + e % kChunkGroups;
                 rs[i] = rz[i] = 0;
-                if (c >= n_chunks || gr >= p.w.groups) continue;
+                if ((kAll % kWorkThreads && e >= kAll) || c >= n_chunks || gr >= p.w.groups) continue;
                 const int64_t at = min(row0 + r, p.w.n - 1) * p.w.meta_stride + gr;
                 if (wide) {
                     rs[i] = __ldg(static_cast<const uint32_t *>(p.w.scale) + at);
@@ -224,18 +224,18 @@ __global__ void __launch_bounds__(kThreads, 1) w4_many_kernel(const __grid_const
                                  (s & 1) * kGroups * kRows + row;
 #pragma unroll
             for (int q = 0; q < kGroups; ++q) {
-                float d[kHalf];
-                tmem_load(tmem + ((uint32_t)(32 * quarter) << 16) + (b * kGroups + q) * N + side * kHalf, d);
+                float d[kOwn];
+                tmem_load(tmem + ((uint32_t)(32 * quarter) << 16) + (b * kGroups + q) * N + side * kOwn, d);
                 if (q == kGroups - 1) {
                     tc_fence_before_sync();
                     mbar_arrive(smem_u32(&folded[b]));
                 }
                 const float2 f = meta[q * kRows];
                 const float4 *fx = reinterpret_cast<const float4 *>(smem + S::kOffB + s % kBStages * kBStage + N * kStageCols * 2) +
-                                   (q * N + side * kHalf) / 4;
+                                   (q * N + side * kOwn) / 4;
                 const float4 *sx = fx + kGroups * N / 4;
 #pragma unroll
-                for (int i = 0; i < kHalf; i += 4) {
+                for (int i = 0; i < kOwn; i += 4) {
                     const float4 x = fx[i / 4], y = sx[i / 4];
                     acc[i] = fmaf(f.y, y.x, fmaf(f.x, d[i] * x.x, acc[i]));
                     acc[i + 1] = fmaf(f.y, y.y, fmaf(f.x, d[i + 1] * x.y, acc[i + 1]));
@@ -253,6 +253,7 @@ __global__ void __launch_bounds__(kThreads, 1) w4_many_kernel(const __grid_const
             for (int i = 0; i < kPairs; ++i) {
                 const int e = i * kWorkThreads + tid, r = e / kChunkGroups, q = e % kChunkGroups;
                 const float s = number(rs[i]);
+                if (kAll % kWorkThreads && e >= kAll) continue;
                 meta[q * kRows + r] = make_float2(kCodeUnit * s, p.w.zero ? number(rz[i]) : -8.f * s);
             }
             load_meta(c + 1);
@@ -264,18 +265,15 @@ __global__ void __launch_bounds__(kThreads, 1) w4_many_kernel(const __grid_const
                 const int s = 2 * c + h, b = s & 1;
                 if (s >= n_stages) break;
                 // (the products of stage s - 2 are done: this thread has folded them)
-                const uint4 *from = reinterpret_cast<const uint4 *>(smem + S::kOffCodes + c % kChunks * kChunkBytes + row * kPitch + h * 64 + side * 32);
-                uint8_t *to = smem + b * kAStage + side * (kRows * 128) + row * 128;
+                const uint4 *from = reinterpret_cast<const uint4 *>(smem + S::kOffCodes + c % kChunks * kChunkBytes + row * kPitch + h * 64 + side * 16);
+                uint8_t *to = smem + b * kAStage + (side >> 1) * (kRows * 128) + row * 128;
+                const uint4 v = *from;
+                const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const uint4 v = from[i];
-                    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const uint32_t u = w[j] >> 8;
-                        *reinterpret_cast<uint4 *>(to + (((i * 4 + j) ^ (row & 7)) << 4)) =
-                            make_uint4(w[j] & 0x000f000fu, w[j] & 0x00f000f0u, u & 0x000f000fu, u & 0x00f000f0u);
-                    }
+                for (int j = 0; j < 4; ++j) {
+                    const uint32_t u = w[j] >> 8;
+                    *reinterpret_cast<uint4 *>(to + ((((side & 1) * 4 + j) ^ (row & 7)) << 4)) =
+                        make_uint4(w[j] & 0x000f000fu, w[j] & 0x00f000f0u, u & 0x000f000fu, u & 0x00f000f0u);
                 }
                 fence_proxy_async();
                 mbar_arrive(smem_u32(&a_full[b]));
@@ -290,7 +288,7 @@ __global__ void __launch_bounds__(kThreads, 1) w4_many_kernel(const __grid_const
         // sums to where the left operand was: its products are done
         float *out = reinterpret_cast<float *>(smem);
 #pragma unroll
-        for (int i = 0; i < kHalf; ++i) out[(side * kHalf + i) * S::kPitchOut + row] = acc[i];
+        for (int i = 0; i < kOwn; ++i) out[(side * kOwn + i) * S::kPitchOut + row] = acc[i];
     }
     __syncthreads();
     if (tid == 0 && *abort_flag && p.w.flags) atomicOr(p.w.flags, STOM_FLAG_TIMEOUT);
@@ -301,7 +299,7 @@ __global__ void __launch_bounds__(kThreads, 1) w4_many_kernel(const __grid_const
     const float *out = reinterpret_cast<const float *>(smem);
     if (tid < kWorkThreads) {
         const int r = tid & (kRows - 1), at_row = row0 + r;
-        for (int i = rank + (tid >> 7) * p.split; i < N; i += 2 * p.split) {
+        for (int i = rank + (tid >> 7) * p.split; i < N; i += kSides * p.split) {
             const int tok = tile * N + i;
             if (tok >= p.w.tokens || at_row >= p.w.n) continue;
             float y = 0.f;
