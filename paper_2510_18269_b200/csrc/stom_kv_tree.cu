@@ -43,6 +43,7 @@ constexpr int kMaxBlocks = 256;       // blocks of the grid the workspace has ro
 constexpr int kSoftWarps = 8, kLoadWarps = 4, kWarps = kSoftWarps + kLoadWarps + 1;
 constexpr int kSoftThreads = kSoftWarps * 32, kLoadThreads = kLoadWarps * 32, kThreads = kWarps * 32;
 constexpr int kPathWords = STOM_KV_MAX_TREE / 32;
+constexpr int kUnitCost = 2;          // what a unit's beginning and end take, in tiles
 constexpr float kSlack = 8.f;         // log2 of what weights may exceed 1 by
 constexpr unsigned long long kWaitLimitNs = 1000000000ull;   // a wait that has taken 1 s ends the block
 
@@ -104,7 +105,8 @@ struct Shared {                       // beside the operands
     uint64_t full[8], empty[8], q_full[2], q_empty[2], unit_full[4], s_full[2], p_full[2], pv_done, drained;
     uint32_t tmem, abort, never;      // never: stays 0
     int32_t start_seq, start_tile_row, start_head, start_tile;
-    uint64_t warp_sum[kWarps];
+    uint64_t warp_sum[kWarps], tiles_before[2];
+    uint32_t warp_units[kWarps];
     Unit unit[4];
     uint32_t tokens[8][4];            // per tile: which rows are tokens
     uint32_t dirty[4];                // tokens of the tile with values that are no numbers
@@ -159,6 +161,23 @@ __device__ __forceinline__ float exp2_of(float x) {
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
+// Two binary32 numbers in a register pair, and arithmetic on both at once
+__device__ __forceinline__ uint64_t pair_of(float a, float b) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ void parts_of(uint64_t p, float &a, float &b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(p)); }
+__device__ __forceinline__ uint64_t fma_pair(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint64_t add_pair(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
 // Which of two 16-bit numbers are no finite ones: bits 15 and 31
 template <typename T>
 __device__ __forceinline__ uint32_t not_finite(uint32_t w) {
@@ -193,17 +212,19 @@ __global__ void __launch_bounds__(kThreads, 1) kv_tree_kernel(const __grid_const
     grid_dependency_wait();
     grid_launch_dependents();   // the joining kernel may take its places now; it waits for this grid's end
 
-    // ---- the stretch of this block: where it begins on the line, and how many tiles it has
-    int64_t left;
+    // ---- the stretch of this block: where it begins on the line, and how many tiles it has.  On the line, a unit's tiles come
+    // behind kUnitCost places for its beginning and end.
     {
-        uint64_t *before = reinterpret_cast<uint64_t *>(smem);   // tiles before each sequence
-        static_assert(kSlots * kHalf >= STOM_KV_MAX_SEQS * 8, "a number for each sequence");
+        uint64_t *before = reinterpret_cast<uint64_t *>(smem);                          // places before each sequence
+        uint32_t *units_before = reinterpret_cast<uint32_t *>(before + STOM_KV_MAX_SEQS);   // and units
+        static_assert(kSlots * kHalf >= STOM_KV_MAX_SEQS * 12, "two numbers for each sequence");
         const int seg = (p.n_seqs + kThreads - 1) / kThreads, b0 = tid * seg;   // sequences a thread adds up
-        auto tiles_of = [&](const Seq &s, int tr) {
+        auto places_of = [&](const Seq &s, int tr) {
             int f, e;
-            return (uint64_t)span_of<kTok>(p, s, tr, f, e);
+            return (uint64_t)span_of<kTok>(p, s, tr, f, e) + kUnitCost;
         };
         uint64_t mine = 0;
+        uint32_t mine_units = 0;
         for (int j = 0; j < seg; ++j) {
             const int b = b0 + j;
             Seq s = {0, 0, 0};
@@ -211,72 +232,101 @@ __global__ void __launch_bounds__(kThreads, 1) kv_tree_kernel(const __grid_const
             const int trs = row_tiles(p, s.n);
             uint64_t sum = 0;
             if (trs <= 8)
-                for (int tr = 0; tr < trs; ++tr) sum += tiles_of(s, tr);
+                for (int tr = 0; tr < trs; ++tr) sum += places_of(s, tr);
             // long ones: the warp together
             for (uint32_t many = __ballot_sync(~0u, trs > 8); many; many &= many - 1) {
                 const int of = __ffs(many) - 1;
                 const Seq o = {0, __shfl_sync(~0u, s.n, of), __shfl_sync(~0u, s.base, of)};
                 const int n = __shfl_sync(~0u, trs, of);
                 uint64_t part = 0;
-                for (int tr = lane; tr < n; tr += 32) part += tiles_of(o, tr);
+                for (int tr = lane; tr < n; tr += 32) part += places_of(o, tr);
 #pragma unroll
                 for (int x = 16; x; x >>= 1) part += __shfl_xor_sync(~0u, part, x);
                 if (lane == of) sum = part;
             }
-            if (b < p.n_seqs) before[b] = mine;
+            if (b < p.n_seqs) {
+                before[b] = mine;
+                units_before[b] = mine_units;
+            }
             mine += sum * p.n_kv_heads;
+            mine_units += (uint32_t)trs * p.n_kv_heads;
         }
         uint64_t upto = mine;
+        uint32_t upto_units = mine_units;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
             const uint64_t v = __shfl_up_sync(~0u, upto, o);
-            if (lane >= o) upto += v;
+            const uint32_t w = __shfl_up_sync(~0u, upto_units, o);
+            if (lane >= o) {
+                upto += v;
+                upto_units += w;
+            }
         }
-        if (lane == 31) sh.warp_sum[warp] = upto;
+        if (lane == 31) {
+            sh.warp_sum[warp] = upto;
+            sh.warp_units[warp] = upto_units;
+        }
         __syncthreads();
         uint64_t total = 0, ahead = upto - mine;
+        uint32_t all_units = 0, ahead_units = upto_units - mine_units;
 #pragma unroll
         for (int w = 0; w < kWarps; ++w) {
-            if (w < warp) ahead += sh.warp_sum[w];
+            if (w < warp) {
+                ahead += sh.warp_sum[w];
+                ahead_units += sh.warp_units[w];
+            }
             total += sh.warp_sum[w];
+            all_units += sh.warp_units[w];
         }
-        for (int j = 0; j < seg && b0 + j < p.n_seqs; ++j) before[b0 + j] += ahead;
+        for (int j = 0; j < seg && b0 + j < p.n_seqs; ++j) {
+            before[b0 + j] += ahead;
+            units_before[b0 + j] += ahead_units;
+        }
         __syncthreads();
         const uint64_t per = max((uint64_t)1, (total + gridDim.x - 1) / gridDim.x);
-        const uint64_t f0 = min(total, (uint64_t)blockIdx.x * per);
-        left = (int64_t)(min(total, f0 + per) - f0);
-        if (warp == 0 && left > 0) {
-            // its first tile's sequence: the last that begins at f0 or before (of several, the others are empty)
-            int low = 0, high = p.n_seqs;
-            while (high - low > 1) {
-                const int step = (high - low + 31) / 32, at = low + step * lane;
-                const uint32_t yes = __ballot_sync(~0u, at < high && before[at] <= f0);
-                low += step * (31 - __clz(yes));
-                high = min(high, low + step);
-            }
-            const Seq s = seq_of(p, low);
-            uint64_t in = f0 - before[low];
-            const int trs = row_tiles(p, s.n);
-            for (int t0 = 0;; t0 += 32) {
-                const uint64_t n = t0 + lane < trs ? tiles_of(s, t0 + lane) * p.n_kv_heads : 0;
-                uint64_t sum = n;
+        if (warp < 2) {
+            // warp 0 looks for the stretch's first place, warp 1 for the first behind it: tiles before it, and where it is
+            const uint64_t f = min(total, ((uint64_t)blockIdx.x + warp) * per);
+            if (f == total) {
+                if (lane == 0) sh.tiles_before[warp] = total - (uint64_t)all_units * kUnitCost;
+            } else {
+                // its sequence: the last that begins there or before (of several, the others are empty)
+                int low = 0, high = p.n_seqs;
+                while (high - low > 1) {
+                    const int step = (high - low + 31) / 32, at = low + step * lane;
+                    const uint32_t yes = __ballot_sync(~0u, at < high && before[at] <= f);
+                    low += step * (31 - __clz(yes));
+                    high = min(high, low + step);
+                }
+                const Seq s = seq_of(p, low);
+                uint64_t in = f - before[low];
+                const int trs = row_tiles(p, s.n);
+                for (int t0 = 0; t0 < trs; t0 += 32) {
+                    const uint64_t n = t0 + lane < trs ? places_of(s, t0 + lane) * p.n_kv_heads : 0;
+                    uint64_t sum = n;
 #pragma unroll
-                for (int o = 1; o < 32; o <<= 1) {
-                    const uint64_t v = __shfl_up_sync(~0u, sum, o);
-                    if (lane >= o) sum += v;
-                }
-                const uint32_t here = __ballot_sync(~0u, in < sum);
-                if (here || t0 + 32 >= trs) {
-                    if (here && lane == __ffs(here) - 1) {
-                        const uint64_t rest = in - (sum - n), each = n / p.n_kv_heads;
-                        sh.start_seq = low;
-                        sh.start_tile_row = t0 + lane;
-                        sh.start_head = (int)(rest / each);
-                        sh.start_tile = (int)(rest - rest / each * each);
+                    for (int o = 1; o < 32; o <<= 1) {
+                        const uint64_t v = __shfl_up_sync(~0u, sum, o);
+                        if (lane >= o) sum += v;
                     }
-                    break;
+                    const uint32_t here = __ballot_sync(~0u, in < sum);
+                    if (here) {
+                        if (lane == __ffs(here) - 1) {
+                            const uint64_t rest = in - (sum - n), each = n / p.n_kv_heads, head = rest / each;
+                            const int place = (int)(rest - head * each), tile = max(0, place - kUnitCost);
+                            if (warp == 0) {
+                                sh.start_seq = low;
+                                sh.start_tile_row = t0 + lane;
+                                sh.start_head = (int)head;
+                                sh.start_tile = tile;
+                            }
+                            const uint64_t units = units_before[low] + (uint64_t)(t0 + lane) * p.n_kv_heads + head;
+                            sh.tiles_before[warp] = f - place - units * kUnitCost + tile;
+                        }
+                        break;
+                    }
+                    in -= __shfl_sync(~0u, sum, 31);
                 }
-                in -= __shfl_sync(~0u, sum, 31);
             }
         }
     }
@@ -284,7 +334,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_tree_kernel(const __grid_const
     __syncthreads();   // the numbers have been read: operands may take their place
     tc_fence_after_sync();
     const uint32_t tmem = sh.tmem;
-    const uint32_t n_tiles = (uint32_t)left;
+    const uint32_t n_tiles = (uint32_t)(sh.tiles_before[1] - sh.tiles_before[0]);
     auto wait = [&](const uint64_t &b, uint32_t parity) {
         if (mbar_wait_bounded(bar(b), parity & 1u, abort_flag, kWaitLimitNs)) return true;
         *abort_flag = 1;
@@ -294,17 +344,16 @@ __global__ void __launch_bounds__(kThreads, 1) kv_tree_kernel(const __grid_const
     auto half_of_v = [&](uint32_t c) { return c + 1 < n_tiles ? 2 * c + 2 : 2 * c + 1; };
     int open_rows = 0, goes_on = 0;
 
-    if (warp >= kSoftWarps && warp < kSoftWarps + kLoadWarps && left > 0) {
+    if (warp >= kSoftWarps && warp < kSoftWarps + kLoadWarps && n_tiles > 0) {
         // ================================================================ loads
         const int lt = tid - kSoftThreads, lw = warp - kSoftWarps;
         constexpr int kChunks = D / 8;                    // 16-byte chunks of a row
         constexpr int kOwn = kTok / kLoadWarps;           // rows of a tile that a warp copies
-        constexpr int kPerCopy = 32 / kChunks;            // rows that one warp-wide copy covers
         // where the page look-ups are: a tile ahead of the copies
         int seq = sh.start_seq, tr = sh.start_tile_row, head = sh.start_head, tile = sh.start_tile;
         Seq s = seq_of(p, seq);
         int trs = row_tiles(p, s.n), first, end, tiles = span_of<kTok>(p, s, tr, first, end);
-        int64_t to_look = left;
+        uint32_t to_look = n_tiles;
         constexpr int kNone = INT32_MIN;
         int page = kNone;
         int64_t rest = 0;
@@ -335,18 +384,25 @@ __global__ void __launch_bounds__(kThreads, 1) kv_tree_kernel(const __grid_const
         uint32_t half = 0, unit = 0;
         bool live = true;
         auto wait_all = [&](const uint64_t &b, uint32_t parity) { return __all_sync(~0u, wait(b, parity)) != 0; };
-        auto copy_half = [&](const char *from, int64_t off) {
+        // Eight lanes copy 128 bytes of a row, four rows at a time; a lane keeps the offsets of its rows, of this tile for the
+        // keys and of the one before for the values.
+        constexpr int kGo = kOwn / 4;                     // rounds of four rows
+        int64_t offs[kGo], offs_before[kGo];
+        const int sub = lane >> 3, piece = lane & 7;
+        const uint32_t lane_dst = ring_u + (lw * kOwn + sub) * 128;
+        auto copy_half = [&](const char *from, const int64_t (&of)[kGo]) {
             const uint32_t slot = half % kSlots, round = half / kSlots;
             ++half;
             if (round > 0 && !wait_all(sh.empty[slot], round - 1)) return false;
-            const uint32_t dst = ring_u + slot * kHalf;
-            const int sub = lane / kChunks, chunk = lane % kChunks;
-#pragma unroll 8
-            for (int i = 0; i < kOwn / kPerCopy; ++i) {
-                const int64_t o = __shfl_sync(~0u, off, i * kPerCopy + sub);
-                const int row = lw * kOwn + i * kPerCopy + sub;
-                copy16_async(dst + (chunk >> 3) * kBlock + row * 128 + (((chunk & 7) ^ (row & 7)) << 4),
-                             from + (o < 0 ? 0 : o) + chunk * 16, o < 0 ? 0u : 16u);
+            const uint32_t dst = lane_dst + slot * kHalf;
+            const char *src = from + piece * 16;
+#pragma unroll
+            for (int i = 0; i < kGo; ++i) {
+                const uint32_t bytes = of[i] < 0 ? 0u : 16u;
+                const char *row = src + (of[i] < 0 ? 0 : of[i]);
+                const uint32_t to = dst + i * 512 + ((piece ^ ((i * 4 + sub) & 7)) << 4);   // (a warp's first row is a multiple of 8)
+#pragma unroll
+                for (int b = 0; b < D / 64; ++b) copy16_async(to + b * kBlock, row + b * 128, bytes);
             }
             arrive_when_copied(bar(sh.full[slot]));
             __syncwarp();
@@ -354,7 +410,6 @@ __global__ void __launch_bounds__(kThreads, 1) kv_tree_kernel(const __grid_const
             return true;
         };
         look_up();
-        int64_t off = -1, off_before = -1;
         for (uint32_t c = 0; c < n_tiles && live; ++c) {
             if (c == 0 || tile == 0) {
                 // a unit begins: its description, its parents, its rows of q
@@ -365,7 +420,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_tree_kernel(const __grid_const
                 }
                 const int rows = min(kRows, s.n * p.group - tr * kRows);
                 if (lt == 0) {
-                    const int part = (int)min((int64_t)(tiles - tile), to_look);
+                    const int part = (int)min((uint32_t)(tiles - tile), to_look);
                     sh.unit[unit & 3] = Unit{s.node0, s.n, s.base, seq, head, tr * kRows, rows, first, end, tile, part,
                                              (tile == 0 ? 1 : 0) | (tile + part == tiles ? 2 : 0)};
                 }
@@ -395,7 +450,12 @@ __global__ void __launch_bounds__(kThreads, 1) kv_tree_kernel(const __grid_const
             }
             const bool ok = (uint32_t)page < (uint32_t)p.n_pages;
             if (page != kNone && !ok && p.flags) atomicOr(p.flags, STOM_FLAG_BAD_INDEX);
-            off = ok ? 2 * (page * p.stride_page + rest) : -1;
+            const int64_t off = ok ? 2 * (page * p.stride_page + rest) : -1;
+#pragma unroll
+            for (int i = 0; i < kGo; ++i) {
+                offs_before[i] = offs[i];
+                offs[i] = __shfl_sync(~0u, off, i * 4 + sub);
+            }
             const uint32_t is = __ballot_sync(~0u, ok);
             if (lane == 0) {
                 if (kOwn == 32) sh.tokens[c & 7][lw] = is;
@@ -405,12 +465,11 @@ __global__ void __launch_bounds__(kThreads, 1) kv_tree_kernel(const __grid_const
                 advance();
                 look_up();
             }
-            live = copy_half(p.k, off) && (c == 0 || copy_half(p.v, off_before));
-            off_before = off;
+            live = copy_half(p.k, offs) && (c == 0 || copy_half(p.v, offs_before));
         }
-        if (live) copy_half(p.v, off_before);
+        if (live) copy_half(p.v, offs);
         asm volatile("cp.async.wait_all;" ::: "memory");
-    } else if (warp == kWarps - 1 && left > 0) {
+    } else if (warp == kWarps - 1 && n_tiles > 0) {
         // ================================================================ products
         if (lane == 0) {
             const uint32_t idesc_s = umma_idesc(kFmt, kTok), idesc_o = umma_idesc(kFmt, D) | kUmmaRightMn;
@@ -461,7 +520,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_tree_kernel(const __grid_const
             umma_commit(bar(sh.drained));   // before tensor memory is given back
             if (!mbar_wait_bounded(bar(sh.drained), 0, &sh.never, kWaitLimitNs)) *abort_flag = 1;
         }
-    } else if (warp < kSoftWarps && left > 0) {
+    } else if (warp < kSoftWarps && n_tiles > 0) {
         // ================================================================ softmax
         const int quarter = warp & 3, side = warp >> 2, row = quarter * 32 + lane;
         const uint32_t lane_base = tmem + ((uint32_t)(32 * quarter) << 16);
@@ -474,15 +533,22 @@ __global__ void __launch_bounds__(kThreads, 1) kv_tree_kernel(const __grid_const
             __syncwarp();
             return ok;
         };
+        // Without a cap and with a positive scale the scores stay unscaled until the exponent, where scaling and the step to
+        // the reference are one multiply-add.
+        const bool plain = !(p.cap > 0.f) && s1 > 0.f;
+        const float times = plain ? s1 : 1.f;
         uint32_t c = 0;
+        int paths_of_seq = -1, paths_of_row = -1, depth = 0;   // whose paths are in shared memory
         for (uint32_t unit = 0; c < n_tiles; ++unit) {
             if (any_of_some(5, kSoftThreads, !wait_on(sh.unit_full[unit & 3], unit >> 2))) break;
             const Unit u = sh.unit[unit & 3];
             const int at = u.row0 + row, node = (int)div_by(p.by_group, (uint32_t)at);
             const bool is = row < u.rows, some = quarter * 32 < u.rows;
             // the context that the row sees: [begin, until), and with a tree the bits of its path from u.base on
-            int depth = node;
-            if (p.parent) {
+            if (!p.parent) depth = node;
+            else if (u.seq != paths_of_seq || u.row0 != paths_of_row) {   // (heads of the same rows have the same)
+                paths_of_seq = u.seq;
+                paths_of_row = u.row0;
                 if (side == 0) {
 #pragma unroll
                     for (int w = 0; w < kPathWords; ++w) sh.path[row][w] = 0;
@@ -515,11 +581,13 @@ __global__ void __launch_bounds__(kThreads, 1) kv_tree_kernel(const __grid_const
                 const bool inside = t_all >= clean_begin && t_all + kTok <= clean_end;
                 if (some) {
                     tmem_load(s_at + side * kCols, x);
+                    if (!plain) {
 #pragma unroll
-                    for (int i = 0; i < kCols; ++i) x[i] *= s1;
-                    if (p.cap > 0.f)
+                        for (int i = 0; i < kCols; ++i) x[i] *= s1;
+                        if (p.cap > 0.f)
 #pragma unroll
-                        for (int i = 0; i < kCols; ++i) x[i] = s2 * tanhf(x[i]);
+                            for (int i = 0; i < kCols; ++i) x[i] = s2 * tanhf(x[i]);
+                    }
                     if (!every || !inside) {
 #pragma unroll
                         for (int w = 0; w < kCols / 32; ++w) {
@@ -540,8 +608,10 @@ __global__ void __launch_bounds__(kThreads, 1) kv_tree_kernel(const __grid_const
                             for (int i = 0; i < 32; ++i) x[32 * w + i] = there[w] >> i & 1u ? x[32 * w + i] : -INFINITY;
                         }
                     }
+                    float tops[4] = {x[0], x[1], x[2], x[3]};
 #pragma unroll
-                    for (int i = 0; i < kCols; ++i) top = fmaxf(top, x[i]);
+                    for (int i = 4; i < kCols; ++i) tops[i & 3] = fmaxf(tops[i & 3], x[i]);
+                    top = times * fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
                 }
                 sh.top[c & 1][side][row] = top;
                 // values that are no numbers, in tiles where rows differ in what they see
@@ -605,16 +675,30 @@ __global__ void __launch_bounds__(kThreads, 1) kv_tree_kernel(const __grid_const
                         tmem_wait_store();
                     }
                     const float one = (m_ref == -INFINITY ? 0.f : m_ref) - kLift;   // score of the weight 1
-                    float l0 = 0.f, l1 = 0.f;
+                    // (a product that has not been rounded may exceed the reference, which has: by little, unless that is huge)
+                    float by_one = times;
+                    const bool huge = plain && !(fabsf(m_ref) < 65536.f);   // (each row by itself: what others see changes no bit of it)
+                    if (__any_sync(~0u, huge)) {
+#pragma unroll
+                        for (int i = 0; i < kCols; ++i) x[i] = huge ? x[i] * s1 : x[i];
+                        by_one = huge ? 1.f : times;
+                    }
+                    uint64_t sum = 0, sum1 = 0;   // two numbers each
                     uint32_t w[kCols / 2];
+                    const uint64_t by = pair_of(by_one, by_one), less = pair_of(-one, -one);
 #pragma unroll
                     for (int i = 0; i < kCols / 2; ++i) {
-                        const float a = exp2_of(x[2 * i] - one), b = exp2_of(x[2 * i + 1] - one);
-                        l0 += a;
-                        l1 += b;
+                        float a, b;
+                        parts_of(fma_pair(pair_of(x[2 * i], x[2 * i + 1]), by, less), a, b);
+                        a = exp2_of(a);
+                        b = exp2_of(b);
+                        uint64_t &to = i & 1 ? sum1 : sum;
+                        to = add_pair(to, pair_of(a, b));
                         w[i] = pack2<T>(a, b);
                     }
-                    l += l0 + l1;
+                    float la, lb;
+                    parts_of(add_pair(sum, sum1), la, lb);
+                    l += la + lb;
                     tmem_store(s_at + side * (kCols / 2), w);
                     tmem_wait_store();
                 }
