@@ -14,9 +14,9 @@
 //
 // A block.  Four warps load: 16-byte asynchronous copies, any page size, any strides, into a ring of tiles of keys and of
 // values, each of them in the 128-byte-swizzled layout in which keys are a K-major operand (rows: tokens) and values an
-// MN-major one (rows: the summed axis).  One thread issues the products: S = Q K^T of tile t + 2 when the values' product
-// of tile t is done, O += P V from tensor memory.  Eight warps do the softmax: a thread has half of the columns of one row;
-// the two halves exchange their maximum through shared memory.  P takes the place of S in tensor memory, in 16 bits.
+// MN-major one (rows: the summed axis).  One thread issues the products: S = Q K^T of tile t + 3 when the values' product
+// of tile t is done, O += P V from tensor memory.  Eight warps do the softmax, two groups in turn with the tiles, a thread with
+// one row: while one group waits, the other's exponentials run.  P takes the place of S in tensor memory, in 16 bits.
 //
 // The running maximum moves only when a row's scores rise by more than 2^8 above it: the weights then are at most 2^8 (no
 // loss: they are floating-point numbers, and bf16 has binary32's exponents; in fp16 the reference weight is 2^7, so that
@@ -43,6 +43,8 @@ constexpr int kMaxBlocks = 256;       // blocks of the grid the workspace has ro
 constexpr int kSoftWarps = 8, kLoadWarps = 4, kWarps = kSoftWarps + kLoadWarps + 1;
 constexpr int kSoftThreads = kSoftWarps * 32, kLoadThreads = kLoadWarps * 32, kThreads = kWarps * 32;
 constexpr int kPathWords = STOM_KV_MAX_TREE / 32;
+constexpr int kSBufs = 3;            // buffers of scores: one is multiplied, one or two are in the softmax
+constexpr int kUnits = 8;            // descriptions of units that are kept
 constexpr int kUnitCost = 2;          // what a unit's beginning and end take, in tiles
 constexpr float kSlack = 8.f;         // log2 of what weights may exceed 1 by
 constexpr unsigned long long kWaitLimitNs = 1000000000ull;   // a wait that has taken 1 s ends the block
@@ -71,6 +73,7 @@ struct KvTreeParams {
     char *out;
     int64_t out_stride_token, out_stride_head;
     float *lse;
+    int32_t blocks;                   // of the grid
     int32_t part_rows;                // rows a partial result has room for
     float *part_o;                    // [blocks][2][part_rows][d]
     float2 *part_ml;                  // [blocks][2][part_rows]: maximum and sum
@@ -85,11 +88,12 @@ struct Shape {
     static constexpr int kHalf = kTok * D * 2;            // bytes of a tile's keys or values
     static constexpr int kBlock = kTok * 128;             // bytes of 64 channels of them
     static constexpr int kSlots = D == 64 ? 8 : 4;        // tiles of keys or values in the ring
+    static constexpr int kSAt = D;                        // column of tensor memory behind the accumulators, where the scores begin
     static constexpr int kQ = kRows * D * 2;
     static constexpr int kQBufs = D == 256 ? 1 : 2;
-    static constexpr int kCols = kTok / 2;                // columns of S that a softmax thread has
     static constexpr int kSmem = 1024 + kSlots * kHalf + kQBufs * kQ;
-    static_assert(kSmem <= 220 * 1024, "shared memory");
+    static_assert(kSmem <= 212 * 1024, "shared memory");
+    static_assert(kSAt + kSBufs * kTok <= 512, "tensor memory");
 };
 
 // What a unit is, and the part of it that a block has
@@ -102,19 +106,18 @@ struct Unit {
 };
 
 struct Shared {                       // beside the operands
-    uint64_t full[8], empty[8], q_full[2], q_empty[2], unit_full[4], s_full[2], p_full[2], pv_done, drained;
+    uint64_t full[8], empty[8], q_full[2], q_empty[2], unit_full[kUnits], s_full[kSBufs], p_full[kSBufs], pv_done[2], drained;   // pv_done: of even and odd tiles
     uint32_t tmem, abort, never;      // never: stays 0
     int32_t start_seq, start_tile_row, start_head, start_tile;
     uint64_t warp_sum[kWarps], tiles_before[2];
     uint32_t warp_units[kWarps];
-    Unit unit[4];
+    Unit unit[kUnits];
     uint32_t tokens[8][4];            // per tile: which rows are tokens
-    uint32_t dirty[4];                // tokens of the tile with values that are no numbers
-    uint32_t seen[4][kRows];          // tokens of the tile that a row sees
-    float top[2][2][kRows];           // [tile's parity][half][row]
+    uint32_t dirty[2][4];             // per group: tokens of the tile with values that are no numbers
+    float ref[2][kRows];              // per group: its last tile's reference
     float sum[2][kRows];
     uint32_t path[kRows][kPathWords];
-    int16_t parent[4][STOM_KV_MAX_TREE];
+    int16_t parent[kUnits][STOM_KV_MAX_TREE];
 };
 
 struct Seq {
@@ -144,6 +147,7 @@ __device__ __forceinline__ void arrive_when_copied(uint32_t bar) {
     asm volatile("cp.async.mbarrier.arrive.noinc.shared.b64 [%0];" ::"r"(bar) : "memory");
 }
 __device__ __forceinline__ void sync_some(int id, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
+__device__ __forceinline__ void arrive_some(int id, int threads) { asm volatile("bar.arrive %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
 __device__ __forceinline__ bool any_of_some(int id, int threads, bool mine) {
     uint32_t r;
     asm volatile(
@@ -187,7 +191,7 @@ __device__ __forceinline__ uint32_t not_finite(uint32_t w) {
 template <typename T, int D>
 __global__ void __launch_bounds__(kThreads, 1) kv_tree_kernel(const __grid_constant__ KvTreeParams p) {
     using S = Shape<D>;
-    constexpr int kTok = S::kTok, kHalf = S::kHalf, kBlock = S::kBlock, kSlots = S::kSlots, kQBufs = S::kQBufs, kCols = S::kCols;
+    constexpr int kTok = S::kTok, kHalf = S::kHalf, kBlock = S::kBlock, kSlots = S::kSlots, kQBufs = S::kQBufs;
     constexpr bool kHalfType = std::is_same<T, __half>::value;
     constexpr float kLift = kHalfType ? 7.f : 0.f;   // log2 of the weight of a score at the reference
     constexpr uint32_t kFmt = kHalfType ? 0u : 1u;
@@ -202,9 +206,10 @@ __global__ void __launch_bounds__(kThreads, 1) kv_tree_kernel(const __grid_const
     if (tid == 0) {
         for (int i = 0; i < 8; ++i) mbar_init(bar(sh.full[i]), kLoadThreads + kLoadWarps), mbar_init(bar(sh.empty[i]), 1);
         for (int i = 0; i < 2; ++i) mbar_init(bar(sh.q_full[i]), kLoadThreads), mbar_init(bar(sh.q_empty[i]), 1);
-        for (int i = 0; i < 4; ++i) mbar_init(bar(sh.unit_full[i]), kLoadThreads);
-        for (int i = 0; i < 2; ++i) mbar_init(bar(sh.s_full[i]), 1), mbar_init(bar(sh.p_full[i]), kSoftThreads);
-        mbar_init(bar(sh.pv_done), 1), mbar_init(bar(sh.drained), 1);
+        for (int i = 0; i < kUnits; ++i) mbar_init(bar(sh.unit_full[i]), kLoadThreads);
+        for (int i = 0; i < kSBufs; ++i) mbar_init(bar(sh.s_full[i]), 1), mbar_init(bar(sh.p_full[i]), kSoftThreads / 2);
+        for (int i = 0; i < 2; ++i) mbar_init(bar(sh.pv_done[i]), 1);
+        mbar_init(bar(sh.drained), 1);
         sh.abort = sh.never = 0;
         mbar_init_fence();
     }
@@ -340,8 +345,9 @@ __global__ void __launch_bounds__(kThreads, 1) kv_tree_kernel(const __grid_const
         *abort_flag = 1;
         return false;
     };
-    // place of a tile's values in the order of loads: K0 K1 V0 K2 V1 ... V(n-1)
-    auto half_of_v = [&](uint32_t c) { return c + 1 < n_tiles ? 2 * c + 2 : 2 * c + 1; };
+    // places of a tile's keys and values in the order of loads: K0 K1 K2 V0 K3 V1 ... V(n-1)
+    auto half_of_k = [&](uint32_t c) { return c < kSBufs ? c : 2 * c - (kSBufs - 1); };
+    auto half_of_v = [&](uint32_t c) { return c + min(c + kSBufs, n_tiles); };
     int open_rows = 0, goes_on = 0;
 
     if (warp >= kSoftWarps && warp < kSoftWarps + kLoadWarps && n_tiles > 0) {
@@ -385,9 +391,9 @@ __global__ void __launch_bounds__(kThreads, 1) kv_tree_kernel(const __grid_const
         bool live = true;
         auto wait_all = [&](const uint64_t &b, uint32_t parity) { return __all_sync(~0u, wait(b, parity)) != 0; };
         // Eight lanes copy 128 bytes of a row, four rows at a time; a lane keeps the offsets of its rows, of this tile for the
-        // keys and of the one before for the values.
+        // keys and of the one two before for the values.
         constexpr int kGo = kOwn / 4;                     // rounds of four rows
-        int64_t offs[kGo], offs_before[kGo];
+        int64_t offs[kGo], before1[kGo], before2[kGo];   // (kSBufs - 1 tiles behind)
         const int sub = lane >> 3, piece = lane & 7;
         const uint32_t lane_dst = ring_u + (lw * kOwn + sub) * 128;
         auto copy_half = [&](const char *from, const int64_t (&of)[kGo]) {
@@ -421,7 +427,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_tree_kernel(const __grid_const
                 const int rows = min(kRows, s.n * p.group - tr * kRows);
                 if (lt == 0) {
                     const int part = (int)min((uint32_t)(tiles - tile), to_look);
-                    sh.unit[unit & 3] = Unit{s.node0, s.n, s.base, seq, head, tr * kRows, rows, first, end, tile, part,
+                    sh.unit[unit % kUnits] = Unit{s.node0, s.n, s.base, seq, head, tr * kRows, rows, first, end, tile, part,
                                              (tile == 0 ? 1 : 0) | (tile + part == tiles ? 2 : 0)};
                 }
                 if (p.parent)
@@ -431,9 +437,9 @@ __global__ void __launch_bounds__(kThreads, 1) kv_tree_kernel(const __grid_const
                             if (p.flags) atomicOr(p.flags, STOM_FLAG_BAD_INDEX);
                             up = -1;
                         }
-                        sh.parent[unit & 3][j] = (int16_t)up;
+                        sh.parent[unit % kUnits][j] = (int16_t)up;
                     }
-                mbar_arrive(bar(sh.unit_full[unit & 3]));
+                mbar_arrive(bar(sh.unit_full[unit % kUnits]));
                 const int sub = lt / kChunks, chunk = lt % kChunks;
 #pragma unroll 4
                 for (int i = 0; i < kRows * kChunks / kLoadThreads; ++i) {
@@ -453,7 +459,8 @@ __global__ void __launch_bounds__(kThreads, 1) kv_tree_kernel(const __grid_const
             const int64_t off = ok ? 2 * (page * p.stride_page + rest) : -1;
 #pragma unroll
             for (int i = 0; i < kGo; ++i) {
-                offs_before[i] = offs[i];
+                before2[i] = before1[i];
+                before1[i] = offs[i];
                 offs[i] = __shfl_sync(~0u, off, i * 4 + sub);
             }
             const uint32_t is = __ballot_sync(~0u, ok);
@@ -465,8 +472,10 @@ __global__ void __launch_bounds__(kThreads, 1) kv_tree_kernel(const __grid_const
                 advance();
                 look_up();
             }
-            live = copy_half(p.k, offs) && (c == 0 || copy_half(p.v, offs_before));
+            live = copy_half(p.k, offs) && (c < kSBufs - 1 || copy_half(p.v, before2));
         }
+        static_assert(kSBufs == 3, "the values' offsets are kept for two tiles");
+        if (live && n_tiles > 1) live = copy_half(p.v, before1);
         if (live) copy_half(p.v, offs);
         asm volatile("cp.async.wait_all;" ::: "memory");
     } else if (warp == kWarps - 1 && n_tiles > 0) {
@@ -476,11 +485,11 @@ __global__ void __launch_bounds__(kThreads, 1) kv_tree_kernel(const __grid_const
             uint32_t unit = 0, in_unit = 0, unit_tiles = 0, fresh = 0;   // of the first products; fresh: bit c & 31, a unit begins
             bool live = true;
             auto scores = [&](uint32_t c) {
-                const uint32_t k = c == 0 ? 0 : 2 * c - 1, slot = k % kSlots;
+                const uint32_t k = half_of_k(c), slot = k % kSlots;
                 const bool begins = in_unit == unit_tiles;
                 if (begins) {
-                    if (!wait(sh.unit_full[unit & 3], unit >> 2)) return false;
-                    unit_tiles = sh.unit[unit & 3].tiles;
+                    if (!wait(sh.unit_full[unit % kUnits], unit / kUnits)) return false;
+                    unit_tiles = sh.unit[unit % kUnits].tiles;
                     in_unit = 0;
                     if (!wait(sh.q_full[unit % kQBufs], unit / kQBufs)) return false;
                     ++unit;
@@ -493,17 +502,17 @@ __global__ void __launch_bounds__(kThreads, 1) kv_tree_kernel(const __grid_const
                 const uint32_t qb = q_u + ((unit - 1) % kQBufs) * S::kQ, kb = ring_u + slot * kHalf;
 #pragma unroll
                 for (int ks = 0; ks < D / 16; ++ks)
-                    umma_ss(tmem + (c & 1) * 128, umma_desc_k128(qb + (ks >> 2) * (kRows * 128) + (ks & 3) * 32),
+                    umma_ss(tmem + S::kSAt + c % kSBufs * kTok, umma_desc_k128(qb + (ks >> 2) * (kRows * 128) + (ks & 3) * 32),
                             umma_desc_k128(kb + (ks >> 2) * kBlock + (ks & 3) * 32), idesc_s, ks != 0);
                 umma_commit(bar(sh.empty[slot]));
-                umma_commit(bar(sh.s_full[c & 1]));
+                umma_commit(bar(sh.s_full[c % kSBufs]));
                 if (in_unit == unit_tiles) umma_commit(bar(sh.q_empty[(unit - 1) % kQBufs]));
                 return true;
             };
-            live = scores(0) && (n_tiles < 2 || scores(1));
+            for (uint32_t c = 0; c < kSBufs && c < n_tiles && live; ++c) live = scores(c);
             for (uint32_t c = 0; c < n_tiles && live; ++c) {
                 const uint32_t v = half_of_v(c), slot = v % kSlots;
-                live = wait(sh.full[slot], v / kSlots) && wait(sh.p_full[c & 1], c >> 1);
+                live = wait(sh.full[slot], v / kSlots) && wait(sh.p_full[c % kSBufs], c / kSBufs);
                 if (!live) break;
                 fence_proxy_async();
                 tc_fence_after_sync();
@@ -511,19 +520,21 @@ __global__ void __launch_bounds__(kThreads, 1) kv_tree_kernel(const __grid_const
                 const uint32_t more = !(fresh >> (c & 31) & 1u);
 #pragma unroll
                 for (int ks = 0; ks < kTok / 16; ++ks)
-                    umma_ts(tmem + 256, tmem + (c & 1) * 128 + ks * 8, umma_desc_mn128(vb + ks * 2048, kBlock), idesc_o,
+                    umma_ts(tmem, tmem + S::kSAt + c % kSBufs * kTok + ks * 8, umma_desc_mn128(vb + ks * 2048, kBlock), idesc_o,
                             more | (ks != 0));
                 umma_commit(bar(sh.empty[slot]));
-                umma_commit(bar(sh.pv_done));
-                if (c + 2 < n_tiles) live = wait(sh.pv_done, c) && scores(c + 2);   // S of tile c + 2 takes P's place
+                umma_commit(bar(sh.pv_done[c & 1]));
+                if (c + kSBufs < n_tiles) live = wait(sh.pv_done[c & 1], c >> 1) && scores(c + kSBufs);   // its S takes P's place
             }
             umma_commit(bar(sh.drained));   // before tensor memory is given back
             if (!mbar_wait_bounded(bar(sh.drained), 0, &sh.never, kWaitLimitNs)) *abort_flag = 1;
         }
     } else if (warp < kSoftWarps && n_tiles > 0) {
         // ================================================================ softmax
-        const int quarter = warp & 3, side = warp >> 2, row = quarter * 32 + lane;
-        const uint32_t lane_base = tmem + ((uint32_t)(32 * quarter) << 16);
+        // Two groups of four warps take the tiles in turn, a thread a row.  A tile's reference comes from the group before,
+        // which passes it on as soon as it has its own tile's maximum.
+        const int quarter = warp & 3, group = warp >> 2, row = quarter * 32 + lane;
+        const uint32_t lane_base = tmem + ((uint32_t)(32 * quarter) << 16), o_at = lane_base;
         const float log2e = 1.4426950408889634f;
         const float s1 = p.cap > 0.f ? p.scale / p.cap : p.scale * log2e, s2 = p.cap * log2e;
         // A wait that fails (the block has given up) is not a reason to leave the others alone at a barrier: the unit goes on
@@ -535,13 +546,14 @@ __global__ void __launch_bounds__(kThreads, 1) kv_tree_kernel(const __grid_const
         };
         // Without a cap and with a positive scale the scores stay unscaled until the exponent, where scaling and the step to
         // the reference are one multiply-add.
-        const bool plain = !(p.cap > 0.f) && s1 > 0.f;
-        const float times = plain ? s1 : 1.f;
+        const bool plain = !(p.cap > 0.f) && s1 > 0.f, falls = s1 < 0.f;
+        auto scaled = [&](float x) { return p.cap > 0.f ? s2 * tanhf(x * s1) : x * s1; };
         uint32_t c = 0;
         int paths_of_seq = -1, paths_of_row = -1, depth = 0;   // whose paths are in shared memory
         for (uint32_t unit = 0; c < n_tiles; ++unit) {
-            if (any_of_some(5, kSoftThreads, !wait_on(sh.unit_full[unit & 3], unit >> 2))) break;
-            const Unit u = sh.unit[unit & 3];
+            // (this barrier also ends the unit before: its accumulators, sums and paths have been read)
+            if (any_of_some(5, kSoftThreads, !wait_on(sh.unit_full[unit % kUnits], unit / kUnits))) break;
+            const Unit u = sh.unit[unit % kUnits];
             const int at = u.row0 + row, node = (int)div_by(p.by_group, (uint32_t)at);
             const bool is = row < u.rows, some = quarter * 32 < u.rows;
             // the context that the row sees: [begin, until), and with a tree the bits of its path from u.base on
@@ -549,12 +561,12 @@ __global__ void __launch_bounds__(kThreads, 1) kv_tree_kernel(const __grid_const
             else if (u.seq != paths_of_seq || u.row0 != paths_of_row) {   // (heads of the same rows have the same)
                 paths_of_seq = u.seq;
                 paths_of_row = u.row0;
-                if (side == 0) {
+                if (group == 0) {
 #pragma unroll
                     for (int w = 0; w < kPathWords; ++w) sh.path[row][w] = 0;
                     depth = 0;
                     if (is)
-                        for (int j = node; j >= 0; j = sh.parent[unit & 3][j], ++depth)
+                        for (int j = node; j >= 0; j = sh.parent[unit % kUnits][j], ++depth)
                             if (!p.window || depth < p.window) sh.path[row][j >> 5] |= 1u << (j & 31);
                     sh.sum[0][row] = __int_as_float(depth - 1);
                 }
@@ -566,70 +578,79 @@ __global__ void __launch_bounds__(kThreads, 1) kv_tree_kernel(const __grid_const
             // tiles before this token (and, with a window, from that one on) are not masked
             const int clean_end = u.n == 1 ? u.end : p.parent ? u.base : u.base + (int)div_by(p.by_group, (uint32_t)u.row0) + 1;
             const int clean_begin = p.window > 0 ? u.base + u.n - p.window : 0;
-            float m_ref = -INFINITY, l = 0.f;
+            float m_own = -INFINITY, l = 0.f;    // the reference that this group's sum is relative to
             for (int t = 0; t < u.tiles; ++t, ++c) {
-                const int t_all = u.first + (u.tile0 + t) * kTok, t0 = t_all + side * kCols;
-                wait_on(sh.s_full[c & 1], c >> 1);
+                if ((int)(c & 1) != group) continue;
+                const int t0 = u.first + (u.tile0 + t) * kTok;
+                wait_on(sh.s_full[c % kSBufs], c / kSBufs);
                 tc_fence_after_sync();
-                const uint32_t s_at = lane_base + (c & 1) * 128;
-                float x[kCols];
-                float top = -INFINITY;
-                uint32_t there[kCols / 32];
-                bool every = true;
+                const uint32_t s_at = lane_base + S::kSAt + c % kSBufs * kTok;
+                bool masked = !(t0 >= clean_begin && t0 + kTok <= clean_end);
+                const bool inside = !masked;
 #pragma unroll
-                for (int w = 0; w < kTok / 32; ++w) every &= sh.tokens[c & 7][w] == ~0u;
-                const bool inside = t_all >= clean_begin && t_all + kTok <= clean_end;
-                if (some) {
-                    tmem_load(s_at + side * kCols, x);
-                    if (!plain) {
+                for (int w = 0; w < kTok / 32; ++w) masked |= sh.tokens[c & 7][w] != ~0u;
+                uint32_t there[kTok / 32];
 #pragma unroll
-                        for (int i = 0; i < kCols; ++i) x[i] *= s1;
-                        if (p.cap > 0.f)
+                for (int w = 0; w < kTok / 32; ++w) there[w] = ~0u;
+                if (masked && some) {
 #pragma unroll
-                            for (int i = 0; i < kCols; ++i) x[i] = s2 * tanhf(x[i]);
-                    }
-                    if (!every || !inside) {
-#pragma unroll
-                        for (int w = 0; w < kCols / 32; ++w) {
-                            const int from = t0 + 32 * w;
-                            // bits of tokens from + 0 .. 31 in [begin, until)
-                            const int lo = begin - from, hi = until - from;
-                            uint32_t mask = hi <= 0 ? 0u : hi >= 32 ? ~0u : (1u << hi) - 1u;
-                            mask &= lo <= 0 ? ~0u : lo >= 32 ? 0u : ~0u << lo;
-                            if (p.parent && from + 31 >= u.base) {
-                                const int bit = from - u.base;                   // of the path, -31 .. 255 (or beyond: none)
-                                const int wd = bit >> 5;                         // floor
-                                const uint32_t a = wd >= 0 && wd < kPathWords ? sh.path[row][wd] : 0u;
-                                const uint32_t b = wd + 1 >= 0 && wd + 1 < kPathWords ? sh.path[row][wd + 1] : 0u;
-                                mask |= __funnelshift_r(a, b, bit & 31);
-                            }
-                            there[w] = mask & sh.tokens[c & 7][side * (kCols / 32) + w];
-#pragma unroll
-                            for (int i = 0; i < 32; ++i) x[32 * w + i] = there[w] >> i & 1u ? x[32 * w + i] : -INFINITY;
+                    for (int w = 0; w < kTok / 32; ++w) {
+                        const int from = t0 + 32 * w;
+                        // bits of tokens from + 0 .. 31 in [begin, until)
+                        const int lo = begin - from, hi = until - from;
+                        uint32_t mask = hi <= 0 ? 0u : hi >= 32 ? ~0u : (1u << hi) - 1u;
+                        mask &= lo <= 0 ? ~0u : lo >= 32 ? 0u : ~0u << lo;
+                        if (p.parent && from + 31 >= u.base) {
+                            const int bit = from - u.base;                   // of the path, -31 .. 255 (or beyond: none)
+                            const int wd = bit >> 5;                         // floor
+                            const uint32_t a = wd >= 0 && wd < kPathWords ? sh.path[row][wd] : 0u;
+                            const uint32_t b = wd + 1 >= 0 && wd + 1 < kPathWords ? sh.path[row][wd + 1] : 0u;
+                            mask |= __funnelshift_r(a, b, bit & 31);
                         }
+                        there[w] = mask & sh.tokens[c & 7][w];
                     }
-                    float tops[4] = {x[0], x[1], x[2], x[3]};
-#pragma unroll
-                    for (int i = 4; i < kCols; ++i) tops[i & 3] = fmaxf(tops[i & 3], x[i]);
-                    top = times * fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
                 }
-                sh.top[c & 1][side][row] = top;
+                // 64 columns of S, what is not seen as what never is the largest
+                auto load_scores = [&](int ch, float (&x)[64]) {
+                    tmem_load(s_at + ch * 64, x);
+                    if (falls)
+#pragma unroll
+                        for (int i = 0; i < 64; ++i) x[i] = -x[i];
+                    if (masked)
+#pragma unroll
+                        for (int i = 0; i < 64; ++i) x[i] = there[ch * 2 + (i >> 5)] >> (i & 31) & 1u ? x[i] : -INFINITY;
+                };
+                float top = -INFINITY;
+                if (some) {
+#pragma unroll 1
+                    for (int ch = 0; ch < kTok / 64; ++ch) {
+                        float x[64];
+                        if (kTok > 64 && ch) load_scores(1, x);
+                        else load_scores(0, x);
+                        float tops[4] = {x[0], x[1], x[2], x[3]};
+#pragma unroll
+                        for (int i = 4; i < 64; ++i) tops[i & 3] = fmaxf(tops[i & 3], x[i]);
+                        top = fmaxf(top, fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])));
+                    }
+                    if (top > -INFINITY) top = scaled(falls ? -top : top);
+                }
                 // values that are no numbers, in tiles where rows differ in what they see
                 bool dirty = false;
                 if (!inside && u.n > 1) {
                     const uint32_t vh = half_of_v(c), slot = vh % kSlots;
+                    if (c > 1) wait_on(sh.pv_done[c & 1], (c - 2) >> 1);   // what was in that slot before is used, so loaded
                     wait_on(sh.full[slot], vh / kSlots);
                     uint4 *words = reinterpret_cast<uint4 *>(smem + slot * kHalf);
                     uint32_t found = 0;
-                    for (int i = tid; i < kHalf / 16; i += kSoftThreads) {
+                    for (int i = row; i < kHalf / 16; i += kRows) {
                         const uint4 v = words[i];
                         found |= not_finite<T>(v.x) | not_finite<T>(v.y) | not_finite<T>(v.z) | not_finite<T>(v.w);
                     }
-                    dirty = any_of_some(5, kSoftThreads, found != 0);
+                    dirty = any_of_some(6 + group, kRows, found != 0);
                     if (dirty) {
-                        if (tid < 4) sh.dirty[tid] = 0;
-                        sync_some(5, kSoftThreads);
-                        for (int i = tid; i < kHalf / 16; i += kSoftThreads) {
+                        if (row < 4) sh.dirty[group][row] = 0;
+                        sync_some(6 + group, kRows);
+                        for (int i = row; i < kHalf / 16; i += kRows) {
                             uint4 v = words[i];
                             uint32_t *w = reinterpret_cast<uint32_t *>(&v);
                             bool any = false;
@@ -642,110 +663,120 @@ __global__ void __launch_bounds__(kThreads, 1) kv_tree_kernel(const __grid_const
                             if (any) {
                                 words[i] = v;
                                 const int tok = (i % (kBlock / 16)) / 8;
-                                atomicOr(&sh.dirty[tok >> 5], 1u << (tok & 31));
+                                atomicOr(&sh.dirty[group][tok >> 5], 1u << (tok & 31));
                             }
                         }
                         fence_proxy_async();
-                        sync_some(5, kSoftThreads);
+                        sync_some(6 + group, kRows);
                     }
                 }
-                tc_fence_before_sync();
-                sync_some(1 + quarter, 64);      // both halves have their scores: P may take their place
-                // The product of the tile before is done: the accumulators may be rescaled.  Every thread waits for every tile's,
-                // since a barrier's parity tells only neighbouring phases apart; the next product could not begin before.
-                if (c > 0) wait_on(sh.pv_done, c - 1);
-                tc_fence_after_sync();
+                // the reference so far, from the group of the tile before; this tile's, to the group of the next
+                if (c > 0) sync_some(8 + group, kSoftThreads);
+                const float m_before = t > 0 ? sh.ref[group ^ 1][row] : -INFINITY;
+                const bool moves = top > m_before + kSlack || (m_before == -INFINITY && top > -INFINITY);
+                const float m_ref = moves ? top : m_before;
+                sh.ref[group][row] = m_ref;
+                if (!dirty && c + 1 < n_tiles) arrive_some(8 + (group ^ 1), kSoftThreads);
+                if (m_own != m_ref) l *= exp2_of(m_own - m_ref);
+                m_own = m_ref;
                 if (some) {
-                    top = fmaxf(top, sh.top[c & 1][side ^ 1][row]);
-                    const bool moves = top > m_ref + kSlack || (m_ref == -INFINITY && top > -INFINITY);
-                    const float m_new = moves ? top : m_ref;
-                    const float alpha = moves ? exp2_of(m_ref - m_new) : 1.f;
-                    m_ref = m_new;
-                    l *= alpha;
-                    if (t > 0 && __any_sync(~0u, moves)) {
-#pragma unroll 1
-                        for (int o = 0; o < D / 2; o += 32) {
-                            float v[32];
-                            uint32_t w[32];
-                            tmem_load(lane_base + 256 + side * (D / 2) + o, v);
-#pragma unroll
-                            for (int i = 0; i < 32; ++i) w[i] = __float_as_uint(v[i] * alpha);
-                            tmem_store(lane_base + 256 + side * (D / 2) + o, w);
-                        }
-                        tmem_wait_store();
-                    }
                     const float one = (m_ref == -INFINITY ? 0.f : m_ref) - kLift;   // score of the weight 1
-                    // (a product that has not been rounded may exceed the reference, which has: by little, unless that is huge)
-                    float by_one = times;
-                    const bool huge = plain && !(fabsf(m_ref) < 65536.f);   // (each row by itself: what others see changes no bit of it)
-                    if (__any_sync(~0u, huge)) {
-#pragma unroll
-                        for (int i = 0; i < kCols; ++i) x[i] = huge ? x[i] * s1 : x[i];
-                        by_one = huge ? 1.f : times;
-                    }
-                    uint64_t sum = 0, sum1 = 0;   // two numbers each
-                    uint32_t w[kCols / 2];
+                    // (a product that has not been rounded may exceed the reference, which has: by little, unless that is
+                    // huge; each row decides by itself, so that what others see changes no bit of it)
+                    const bool fused = plain && fabsf(m_ref) < 65536.f;
+                    const float by_one = fused ? s1 : 1.f;
+                    const bool all_fused = __all_sync(~0u, fused || m_ref == -INFINITY) && plain;
                     const uint64_t by = pair_of(by_one, by_one), less = pair_of(-one, -one);
+                    uint64_t sum = 0, sum1 = 0;   // two numbers each
+#pragma unroll 1
+                    for (int ch = 0; ch < kTok / 64; ++ch) {
+                        float x[64];
+                        if (kTok > 64 && ch) load_scores(1, x);
+                        else load_scores(0, x);
+                        if (!all_fused) {
 #pragma unroll
-                    for (int i = 0; i < kCols / 2; ++i) {
-                        float a, b;
-                        parts_of(fma_pair(pair_of(x[2 * i], x[2 * i + 1]), by, less), a, b);
-                        a = exp2_of(a);
-                        b = exp2_of(b);
-                        uint64_t &to = i & 1 ? sum1 : sum;
-                        to = add_pair(to, pair_of(a, b));
-                        w[i] = pack2<T>(a, b);
+                            for (int i = 0; i < 64; ++i)
+                                if (!fused && x[i] > -INFINITY) x[i] = scaled(falls ? -x[i] : x[i]);
+                        }
+                        uint32_t w[32];
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) {
+                            float a, b;
+                            parts_of(fma_pair(pair_of(x[2 * i], x[2 * i + 1]), by, less), a, b);
+                            a = exp2_of(a);
+                            b = exp2_of(b);
+                            uint64_t &to = i & 1 ? sum1 : sum;
+                            to = add_pair(to, pair_of(a, b));
+                            w[i] = pack2<T>(a, b);
+                        }
+                        tmem_store(s_at + ch * 32, w);   // (over columns that have been read: of this half, or of the first)
                     }
                     float la, lb;
                     parts_of(add_pair(sum, sum1), la, lb);
                     l += la + lb;
-                    tmem_store(s_at + side * (kCols / 2), w);
+                    tmem_wait_store();
+                }
+                // The product of the tile before is done: the accumulators may be rescaled.  (Every thread waits for it every time:
+                // a barrier's parity tells only neighbouring phases apart.)
+                if (c > 0) wait_on(sh.pv_done[(c - 1) & 1], (c - 1) >> 1);
+                if (some && t > 0 && __any_sync(~0u, moves)) {
+                    tc_fence_after_sync();
+                    const float alpha = moves ? exp2_of(m_before - m_ref) : 1.f;
+#pragma unroll 1
+                    for (int o = 0; o < D; o += 32) {
+                        float v[32];
+                        uint32_t w[32];
+                        tmem_load(o_at + o, v);
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) w[i] = __float_as_uint(v[i] * alpha);
+                        tmem_store(o_at + o, w);
+                    }
                     tmem_wait_store();
                 }
                 tc_fence_before_sync();
-                mbar_arrive(bar(sh.p_full[c & 1]));
+                mbar_arrive(bar(sh.p_full[c % kSBufs]));
                 if (dirty) {
-                    // put back what was taken out, in the rows that see it (its weight is positive)
-                    wait_on(sh.pv_done, c);
+                    // put back what was taken out, in the rows that see it (its weight is positive); the next tile's product
+                    // waits for it, because its group waits for the reference
+                    wait_on(sh.pv_done[c & 1], c >> 1);
                     tc_fence_after_sync();
                     if (some)
-#pragma unroll
-                        for (int w = 0; w < kCols / 32; ++w) sh.seen[side * (kCols / 32) + w][row] = there[w];
-                    sync_some(5, kSoftThreads);
-                    if (some)
 #pragma unroll 1
-                        for (int o = 0; o < D / 2; o += 32) {
+                        for (int o = 0; o < D; o += 32) {
                             float v[32];
                             uint32_t w[32];
-                            const int ch = side * (D / 2) + o;
-                            tmem_load(lane_base + 256 + ch, v);
-#pragma unroll 1
-                            for (int k = 0; k < kTok; ++k) {
-                                if (!(sh.dirty[k >> 5] >> (k & 31) & 1u)) continue;
-                                const int tok = t_all + k;
-                                const uint32_t pg = div_by(p.page, (uint32_t)tok);
-                                const int id = p.table[u.seq * p.table_stride + pg];
-                                const T *src = reinterpret_cast<const T *>(p.v) + id * p.stride_page +
-                                               (int64_t)(tok - (int)(pg * p.page.d)) * p.stride_token + u.head * p.stride_head + ch;
-                                const bool mine = sh.seen[k >> 5][row] >> (k & 31) & 1u;
+                            tmem_load(o_at + o, v);
 #pragma unroll
-                                for (int i = 0; i < 32; ++i) {
-                                    const float y = static_cast<float>(src[i]);
-                                    if (mine && !isfinite(y)) v[i] += y;
+                            for (int g = 0; g < kTok / 32; ++g) {
+                                for (uint32_t bits = sh.dirty[group][g] & sh.tokens[c & 7][g]; bits; bits &= bits - 1) {
+                                    const int b = __ffs(bits) - 1, tok = t0 + g * 32 + b;
+                                    const uint32_t pg = div_by(p.page, (uint32_t)tok);
+                                    const int id = p.table[u.seq * p.table_stride + pg];
+                                    const T *src = reinterpret_cast<const T *>(p.v) + id * p.stride_page +
+                                                   (int64_t)(tok - (int)(pg * p.page.d)) * p.stride_token + u.head * p.stride_head + o;
+#pragma unroll
+                                    for (int i = 0; i < 32; ++i) {
+                                        const float y = static_cast<float>(src[i]);
+                                        if ((there[g] >> b & 1u) && !isfinite(y)) v[i] += y;
+                                    }
                                 }
                             }
 #pragma unroll
                             for (int i = 0; i < 32; ++i) w[i] = __float_as_uint(v[i]);
-                            tmem_store(lane_base + 256 + ch, w);
+                            tmem_store(o_at + o, w);
                         }
                     tmem_wait_store();
                     tc_fence_before_sync();
+                    if (c + 1 < n_tiles) arrive_some(8 + (group ^ 1), kSoftThreads);
                 }
             }
             // ---- the unit's end, or the stretch's
-            wait_on(sh.pv_done, c - 1);
+            const uint32_t last = c - 1;
+            if ((int)(last & 1) == group) wait_on(sh.pv_done[last & 1], last >> 1);
+            sync_some(5, kSoftThreads);          // the last reference is there, and the accumulators
             tc_fence_after_sync();
-            sh.sum[side][row] = l;
+            const float m_ref = sh.ref[last & 1][row];
+            sh.sum[group][row] = m_own == m_ref ? l : l * exp2_of(m_own - m_ref);
             sync_some(1 + quarter, 64);
             l = sh.sum[0][row] + sh.sum[1][row];
             const bool whole = u.ends == 3;
@@ -758,8 +789,8 @@ __global__ void __launch_bounds__(kThreads, 1) kv_tree_kernel(const __grid_const
 #pragma unroll 1
                 for (int o = 0; o < D / 2; o += 32) {
                     float v[32];
-                    const int ch = side * (D / 2) + o;
-                    tmem_load(lane_base + 256 + ch, v);
+                    const int ch = group * (D / 2) + o;
+                    tmem_load(o_at + ch, v);
                     if (is && whole) {
 #pragma unroll
                         for (int i = 0; i < 32; i += 8)
@@ -772,7 +803,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_tree_kernel(const __grid_const
                             *reinterpret_cast<float4 *>(part + ch + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
                     }
                 }
-                if (is && side == 0) {
+                if (is && group == 0) {
                     if (!whole) p.part_ml[slot * p.part_rows + row] = make_float2(m_ref, l);
                     else if (p.lse)
                         p.lse[(int64_t)(u.node0 + node) * (p.n_kv_heads * p.group) + h] =
@@ -788,7 +819,6 @@ __global__ void __launch_bounds__(kThreads, 1) kv_tree_kernel(const __grid_const
                     goes_on = 1;
                 }
             }
-            sync_some(1 + quarter, 64);          // sums and paths have been read
         }
     }
     __syncthreads();
@@ -800,53 +830,76 @@ __global__ void __launch_bounds__(kThreads, 1) kv_tree_kernel(const __grid_const
     if (warp == kWarps - 1) tmem_dealloc(tmem, 512);
 }
 
-// Joins the partial results of the units that cross a block's end: block (x, y) of this grid takes rows 2 y and 2 y + 1 of the
-// unit that begins in block x of the kernel above and goes on behind it, if there is one.  Four warps a row, each with every
-// fourth partial result.
+// Joins the partial results of the units that cross a block's end.  Every block reads what units those are (they begin in one
+// block of the kernel above each and go on behind it).  Their rows are taken by a warp each, or, where there are so few that
+// every one can have a block, by its eight warps, with every eighth partial result each.
 template <typename T, int D>
 __global__ void __launch_bounds__(256) kv_tree_join_kernel(const __grid_constant__ KvTreeParams p) {
     constexpr int kVec = D / 32 < 4 ? D / 32 : 4, kVecs = D / 32 / kVec;   // channels of a lane: kVecs times kVec adjacent ones
     constexpr float kLift = std::is_same<T, __half>::value ? 7.f : 0.f;
-    __shared__ float sums[2][4][D];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, share = warp & 3, x = blockIdx.x, blocks = gridDim.x;
-    const int row = blockIdx.y * 2 + (warp >> 2);
+    static_assert(kMaxBlocks == 256, "a thread for each block of the kernel above");
+    __shared__ float sums[8][D];
+    __shared__ int before[kMaxBlocks + 1], warp_rows[8];   // rows before each block's unit
+    __shared__ uint32_t on[kMaxBlocks / 32];               // blocks behind which the unit that came in goes on
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     grid_dependency_wait();
-    const Open u = p.open[x];
-    if ((int)blockIdx.y * 2 >= u.rows) return;
-    // the blocks it goes through: x, x + 1, ..., x + n - 1
-    int n = 1;
-    for (;;) {
-        const int j = x + n + lane;
-        const uint32_t ends = __ballot_sync(~0u, j >= blocks || !p.goes_on[j]);
-        if (ends) {
-            n = min(n + __ffs(ends), blocks - x);
-            break;
-        }
-        n += 32;
-    }
-    const bool is = row < u.rows;
-    auto at = [&](int j) { return ((int64_t)(x + j) * 2 + (j == 0 ? 1 : 0)) * p.part_rows + row; };
-    float m = -INFINITY, l = 0.f;
-    if (is)
-        for (int j = lane; j < n; j += 32) m = fmaxf(m, p.part_ml[at(j)].x);
+    {
+        const int rows = tid < p.blocks ? p.open[tid].rows : 0;
+        const uint32_t goes = __ballot_sync(~0u, tid < p.blocks && p.goes_on[tid]);
+        int upto = rows;
 #pragma unroll
-    for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(~0u, m, o));
-    const float base = m == -INFINITY ? 0.f : m;
-    if (is)
+        for (int o = 1; o < 32; o <<= 1) {
+            const int v = __shfl_up_sync(~0u, upto, o);
+            if (lane >= o) upto += v;
+        }
+        if (lane == 31) warp_rows[warp] = upto;
+        if (lane == 0) on[warp] = goes;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < 8; ++w) upto += w < warp ? warp_rows[w] : 0;
+        before[tid + 1] = upto;
+        if (tid == 0) before[0] = 0;
+        __syncthreads();
+    }
+    const int total = before[kMaxBlocks];
+    const bool together = total <= (int)gridDim.x;
+    const int step = together ? 8 : 1;
+    const int items = gridDim.x * (together ? 1 : 8);
+    for (int item = together ? blockIdx.x : blockIdx.x * 8 + warp; item < total; item += items) {
+        // its unit: the last block whose rows begin there or before
+        int x = 0;
+#pragma unroll
+        for (int s = kMaxBlocks / 2; s; s >>= 1)
+            if (before[x + s] <= item) x += s;
+        const int row = item - before[x];
+        // the blocks it goes through: x, x + 1, ..., x + n - 1
+        int n = 2;
+        while (x + n - 1 < p.blocks - 1 && (on[(x + n - 1) >> 5] >> ((x + n - 1) & 31) & 1u)) ++n;
+        n = min(n, p.blocks - x);
+        const Open u = p.open[x];
+        auto at = [&](int j) { return ((int64_t)(x + j) * 2 + (j == 0 ? 1 : 0)) * p.part_rows + row; };
+        // maxima and sums of all, a lane one (or several) of them
+        float m = -INFINITY, l = 0.f;
         for (int j = lane; j < n; j += 32) {
             const float2 ml = p.part_ml[at(j)];
-            l += exp2_of(ml.x - base) * ml.y;
+            const float top = fmaxf(m, ml.x), base = top == -INFINITY ? 0.f : top;
+            l = l * exp2_of(m - base) + ml.y * exp2_of(ml.x - base);
+            m = top;
         }
+        float all = m;
 #pragma unroll
-    for (int o = 16; o; o >>= 1) l += __shfl_xor_sync(~0u, l, o);
-    float o[kVecs][kVec];
+        for (int s = 16; s; s >>= 1) all = fmaxf(all, __shfl_xor_sync(~0u, all, s));
+        const float base = all == -INFINITY ? 0.f : all;
+        l *= exp2_of(m - base);
 #pragma unroll
-    for (int v = 0; v < kVecs; ++v)
+        for (int s = 16; s; s >>= 1) l += __shfl_xor_sync(~0u, l, s);
+        float o[kVecs][kVec];
 #pragma unroll
-        for (int i = 0; i < kVec; ++i) o[v][i] = 0.f;
-    if (is) {
+        for (int v = 0; v < kVecs; ++v)
+#pragma unroll
+            for (int i = 0; i < kVec; ++i) o[v][i] = 0.f;
 #pragma unroll 4
-        for (int j = share; j < n; j += 4) {
+        for (int j = together ? warp : 0; j < n; j += step) {
             const float f = exp2_of(p.part_ml[at(j)].x - base);
             const float *src = p.part_o + at(j) * D + lane * kVec;
 #pragma unroll
@@ -858,29 +911,38 @@ __global__ void __launch_bounds__(256) kv_tree_join_kernel(const __grid_constant
                 for (int i = 0; i < kVec; ++i) o[v][i] = fmaf(f, y[i], o[v][i]);
             }
         }
-    }
+        if (together) {   // (one row a block: this is its only one)
 #pragma unroll
-    for (int v = 0; v < kVecs; ++v)
+            for (int v = 0; v < kVecs; ++v)
 #pragma unroll
-        for (int i = 0; i < kVec; ++i) sums[warp >> 2][share][v * 128 + lane * kVec + i] = o[v][i];
-    __syncthreads();
-    if (!is || share) return;
-    const int at_row = u.row0 + row, node = (int)div_by(p.by_group, (uint32_t)at_row);
-    const int h = u.head * p.group + at_row - node * p.group;
-    const float inv = l == 0.f ? 0.f : 1.f / l;
-    T *dst = reinterpret_cast<T *>(p.out) + (int64_t)(u.node0 + node) * p.out_stride_token + h * p.out_stride_head;
-    for (int c = 2 * lane; c < D; c += 64) {
-        float y[2];
+                for (int i = 0; i < kVec; ++i) sums[warp][v * 128 + lane * kVec + i] = o[v][i];
+            __syncthreads();
+            if (warp) return;
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const float(*s)[D] = sums[warp >> 2];
-            y[i] = ((s[0][c + i] + s[1][c + i]) + (s[2][c + i] + s[3][c + i])) * inv;
+            for (int v = 0; v < kVecs; ++v)
+#pragma unroll
+                for (int i = 0; i < kVec; ++i) {
+                    float y = 0.f;
+#pragma unroll
+                    for (int w = 0; w < 8; ++w) y += sums[w][v * 128 + lane * kVec + i];
+                    o[v][i] = y;
+                }
         }
-        *reinterpret_cast<uint32_t *>(dst + c) = pack2<T>(y[0], y[1]);
+        const int at_row = u.row0 + row, node = (int)div_by(p.by_group, (uint32_t)at_row);
+        const int h = u.head * p.group + at_row - node * p.group;
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+        T *dst = reinterpret_cast<T *>(p.out) + (int64_t)(u.node0 + node) * p.out_stride_token + h * p.out_stride_head + lane * kVec;
+#pragma unroll
+        for (int v = 0; v < kVecs; ++v) {
+            if constexpr (kVec == 4)
+                *reinterpret_cast<uint2 *>(dst + v * 128) =
+                    make_uint2(pack2<T>(o[v][0] * inv, o[v][1] * inv), pack2<T>(o[v][2] * inv, o[v][3] * inv));
+            else *reinterpret_cast<uint32_t *>(dst) = pack2<T>(o[v][0] * inv, o[v][1] * inv);
+        }
+        if (p.lse && lane == 0)
+            p.lse[(int64_t)(u.node0 + node) * (p.n_kv_heads * p.group) + h] =
+                l == 0.f ? -INFINITY : 0.6931471805599453f * (all - kLift) + logf(l);
     }
-    if (p.lse && lane == 0)
-        p.lse[(int64_t)(u.node0 + node) * (p.n_kv_heads * p.group) + h] =
-            l == 0.f ? -INFINITY : 0.6931471805599453f * (m - kLift) + logf(l);
 }
 
 int64_t round256(int64_t x) { return (x + 255) & ~(int64_t)255; }
@@ -898,7 +960,7 @@ int32_t launch(const KvTreeParams &p, int sms, cudaStream_t stream) {
     if (e == cudaSuccess)
         e = launch_after_producer(kv_tree_kernel<T, D>, dim3(sms), dim3(kThreads), Shape<D>::kSmem, stream, p);
     if (e == cudaSuccess)
-        e = launch_after_producer(kv_tree_join_kernel<T, D>, dim3(sms, (p.part_rows + 1) / 2), dim3(256), 0, stream, p);
+        e = launch_after_producer(kv_tree_join_kernel<T, D>, dim3(sms * 4), dim3(256), 0, stream, p);
     if (e != cudaSuccess) {
         set_last_cuda_error(e);
         return STOM_ERR_CUDA;
@@ -991,6 +1053,7 @@ extern "C" int32_t stom_kv_attend_tree(const stom_kv_pool *pool, const stom_kv_s
     p.out_stride_token = out_stride_token;
     p.out_stride_head = out_stride_head;
     p.lse = lse;
+    p.blocks = sms;
     p.part_rows = (int32_t)part_rows(n_tokens, p.group);
     const int64_t rows = (int64_t)kMaxBlocks * 2 * p.part_rows;
     char *ws = static_cast<char *>(workspace);
