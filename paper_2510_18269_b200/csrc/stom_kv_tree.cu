@@ -288,7 +288,9 @@ __global__ void __launch_bounds__(kThreads, 1) kv_tree_kernel(const __grid_const
             units_before[b0 + j] += ahead_units;
         }
         __syncthreads();
-        const uint64_t per = max((uint64_t)1, (total + gridDim.x - 1) / gridDim.x);
+        // (divisions of 64 bits are slow, and the line is rarely that long)
+        const uint64_t up = total + gridDim.x - 1;
+        const uint64_t per = max((uint64_t)1, up >> 32 ? up / gridDim.x : (uint64_t)((uint32_t)up / gridDim.x));
         if (warp < 2) {
             // warp 0 looks for the stretch's first place, warp 1 for the first behind it: tiles before it, and where it is
             const uint64_t f = min(total, ((uint64_t)blockIdx.x + warp) * per);
@@ -317,7 +319,8 @@ __global__ void __launch_bounds__(kThreads, 1) kv_tree_kernel(const __grid_const
                     const uint32_t here = __ballot_sync(~0u, in < sum);
                     if (here) {
                         if (lane == __ffs(here) - 1) {
-                            const uint64_t rest = in - (sum - n), each = n / p.n_kv_heads, head = rest / each;
+                            const uint64_t rest = in - (sum - n), each = places_of(s, t0 + lane);
+                            const uint64_t head = rest >> 32 ? rest / each : (uint64_t)((uint32_t)rest / (uint32_t)each);
                             const int place = (int)(rest - head * each), tile = max(0, place - kUnitCost);
                             if (warp == 0) {
                                 sh.start_seq = low;
@@ -839,6 +842,7 @@ __global__ void __launch_bounds__(256) kv_tree_join_kernel(const __grid_constant
     constexpr float kLift = std::is_same<T, __half>::value ? 7.f : 0.f;
     static_assert(kMaxBlocks == 256, "a thread for each block of the kernel above");
     __shared__ float sums[8][D];
+    __shared__ float2 warp_ml[8];
     __shared__ int before[kMaxBlocks + 1], warp_rows[8];   // rows before each block's unit
     __shared__ uint32_t on[kMaxBlocks / 32];               // blocks behind which the unit that came in goes on
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -863,8 +867,7 @@ __global__ void __launch_bounds__(256) kv_tree_join_kernel(const __grid_constant
     }
     const int total = before[kMaxBlocks];
     const bool together = total <= (int)gridDim.x;
-    const int step = together ? 8 : 1;
-    const int items = gridDim.x * (together ? 1 : 8);
+    const int step = together ? 8 : 1, items = gridDim.x * (together ? 1 : 8);
     for (int item = together ? blockIdx.x : blockIdx.x * 8 + warp; item < total; item += items) {
         // its unit: the last block whose rows begin there or before
         int x = 0;
@@ -872,43 +875,57 @@ __global__ void __launch_bounds__(256) kv_tree_join_kernel(const __grid_constant
         for (int s = kMaxBlocks / 2; s; s >>= 1)
             if (before[x + s] <= item) x += s;
         const int row = item - before[x];
-        // the blocks it goes through: x, x + 1, ..., x + n - 1
-        int n = 2;
-        while (x + n - 1 < p.blocks - 1 && (on[(x + n - 1) >> 5] >> ((x + n - 1) & 31) & 1u)) ++n;
-        n = min(n, p.blocks - x);
         const Open u = p.open[x];
+        // the blocks it goes through: x, x + 1, ..., x + n - 1, the last of them the first behind x that it does not go on behind
+        const uint32_t rest = lane < kMaxBlocks / 32 ? ~on[lane] & (lane == (x + 1) >> 5 ? ~0u << ((x + 1) & 31) : lane > (x + 1) >> 5 ? ~0u : 0u) : 0u;
+        const uint32_t words = __ballot_sync(~0u, rest != 0);
+        const int word = words ? __ffs(words) - 1 : 0, bit = __ffs(__shfl_sync(~0u, rest, word)) - 1;
+        const int n = (words ? min(word * 32 + bit + 1, p.blocks) : p.blocks) - x;
         auto at = [&](int j) { return ((int64_t)(x + j) * 2 + (j == 0 ? 1 : 0)) * p.part_rows + row; };
-        // maxima and sums of all, a lane one (or several) of them
+        // this warp's partial results, four at a time, relative to the largest maximum so far
         float m = -INFINITY, l = 0.f;
-        for (int j = lane; j < n; j += 32) {
-            const float2 ml = p.part_ml[at(j)];
-            const float top = fmaxf(m, ml.x), base = top == -INFINITY ? 0.f : top;
-            l = l * exp2_of(m - base) + ml.y * exp2_of(ml.x - base);
-            m = top;
-        }
-        float all = m;
-#pragma unroll
-        for (int s = 16; s; s >>= 1) all = fmaxf(all, __shfl_xor_sync(~0u, all, s));
-        const float base = all == -INFINITY ? 0.f : all;
-        l *= exp2_of(m - base);
-#pragma unroll
-        for (int s = 16; s; s >>= 1) l += __shfl_xor_sync(~0u, l, s);
         float o[kVecs][kVec];
 #pragma unroll
         for (int v = 0; v < kVecs; ++v)
 #pragma unroll
             for (int i = 0; i < kVec; ++i) o[v][i] = 0.f;
-#pragma unroll 4
-        for (int j = together ? warp : 0; j < n; j += step) {
-            const float f = exp2_of(p.part_ml[at(j)].x - base);
-            const float *src = p.part_o + at(j) * D + lane * kVec;
+        constexpr int kBatch = 4;
+        for (int j0 = together ? warp : 0; j0 < n; j0 += kBatch * step) {
+            float2 ml[kBatch];
+            float y[kBatch][kVecs][kVec];
 #pragma unroll
-            for (int v = 0; v < kVecs; ++v) {
-                float y[kVec];
-                if constexpr (kVec == 4) *reinterpret_cast<float4 *>(y) = *reinterpret_cast<const float4 *>(src + v * 128);
-                else *reinterpret_cast<float2 *>(y) = *reinterpret_cast<const float2 *>(src);
+            for (int b = 0; b < kBatch; ++b) {
+                const int j = j0 + b * step;
+                ml[b] = make_float2(-INFINITY, 0.f);
+                if (j < n) {
+                    ml[b] = p.part_ml[at(j)];
+                    const float *src = p.part_o + at(j) * D + lane * kVec;
 #pragma unroll
-                for (int i = 0; i < kVec; ++i) o[v][i] = fmaf(f, y[i], o[v][i]);
+                    for (int v = 0; v < kVecs; ++v) {
+                        if constexpr (kVec == 4) *reinterpret_cast<float4 *>(y[b][v]) = *reinterpret_cast<const float4 *>(src + v * 128);
+                        else *reinterpret_cast<float2 *>(y[b][v]) = *reinterpret_cast<const float2 *>(src);
+                    }
+                }
+            }
+            float top = m;
+#pragma unroll
+            for (int b = 0; b < kBatch; ++b) top = fmaxf(top, ml[b].x);
+            const float base = top == -INFINITY ? 0.f : top, f = exp2_of(m - base);
+            m = top;
+            l *= f;
+#pragma unroll
+            for (int v = 0; v < kVecs; ++v)
+#pragma unroll
+                for (int i = 0; i < kVec; ++i) o[v][i] *= f;
+#pragma unroll
+            for (int b = 0; b < kBatch; ++b) {
+                if (j0 + b * step >= n) continue;
+                const float g = exp2_of(ml[b].x - base);
+                l = fmaf(g, ml[b].y, l);
+#pragma unroll
+                for (int v = 0; v < kVecs; ++v)
+#pragma unroll
+                    for (int i = 0; i < kVec; ++i) o[v][i] = fmaf(g, y[b][v][i], o[v][i]);
             }
         }
         if (together) {   // (one row a block: this is its only one)
@@ -916,17 +933,26 @@ __global__ void __launch_bounds__(256) kv_tree_join_kernel(const __grid_constant
             for (int v = 0; v < kVecs; ++v)
 #pragma unroll
                 for (int i = 0; i < kVec; ++i) sums[warp][v * 128 + lane * kVec + i] = o[v][i];
+            if (lane == 0) warp_ml[warp] = make_float2(m, l);
             __syncthreads();
             if (warp) return;
+            m = -INFINITY, l = 0.f;
+#pragma unroll
+            for (int w = 0; w < 8; ++w) m = fmaxf(m, warp_ml[w].x);
+            const float base = m == -INFINITY ? 0.f : m;
 #pragma unroll
             for (int v = 0; v < kVecs; ++v)
 #pragma unroll
-                for (int i = 0; i < kVec; ++i) {
-                    float y = 0.f;
+                for (int i = 0; i < kVec; ++i) o[v][i] = 0.f;
 #pragma unroll
-                    for (int w = 0; w < 8; ++w) y += sums[w][v * 128 + lane * kVec + i];
-                    o[v][i] = y;
-                }
+            for (int w = 0; w < 8; ++w) {
+                const float f = exp2_of(warp_ml[w].x - base);
+                l = fmaf(f, warp_ml[w].y, l);
+#pragma unroll
+                for (int v = 0; v < kVecs; ++v)
+#pragma unroll
+                    for (int i = 0; i < kVec; ++i) o[v][i] = fmaf(f, sums[w][v * 128 + lane * kVec + i], o[v][i]);
+            }
         }
         const int at_row = u.row0 + row, node = (int)div_by(p.by_group, (uint32_t)at_row);
         const int h = u.head * p.group + at_row - node * p.group;
@@ -941,7 +967,7 @@ __global__ void __launch_bounds__(256) kv_tree_join_kernel(const __grid_constant
         }
         if (p.lse && lane == 0)
             p.lse[(int64_t)(u.node0 + node) * (p.n_kv_heads * p.group) + h] =
-                l == 0.f ? -INFINITY : 0.6931471805599453f * (all - kLift) + logf(l);
+                l == 0.f ? -INFINITY : 0.6931471805599453f * (m - kLift) + logf(l);
     }
 }
 
