@@ -6,11 +6,11 @@
 // of the right operand as they lie in shared memory, 128-byte-swizzled, and a factor and a sum for each token and group.
 //
 // A block has 128 rows of the matrix, N tokens and a part of the columns, a STAGE of 128 of them at a time.  Codes arrive by
-// 16-byte asynchronous copies, 256 columns at a time, several ahead.  Sixteen warps unpack: a thread has one row and a quarter of a
-// stage's columns, 4 words that become 4 chunks of 16 bytes in the left operand (K-major, 128-byte swizzle; two stages of it).  One
-// thread issues the products, each group into accumulators of their own in tensor memory, since scales differ from
-// group to group; the sixteen warps fold those of the stage before into their sums while the products of this one run: a
-// thread has a row again, and a quarter of the tokens.
+// 16-byte asynchronous copies, 256 columns at a time, several ahead.  Eight warps unpack: a thread has one row and half of a
+// stage's columns, 8 words that become 8 chunks of 16 bytes in the left operand (K-major, 128-byte swizzle; two stages of it).
+// One thread issues the products, each group into accumulators of its own in tensor memory, since scales differ from group to
+// group.  Eight more warps fold those of the stage before into sums while the products of this one run: a thread has a row
+// again, and half of the tokens.
 // Blocks that share out the columns of the same rows form a cluster (up to 8, so many that all multiprocessors have a
 // block), whose sums are joined over distributed shared memory.
 #include "stom_tensor.cuh"
@@ -21,7 +21,8 @@ namespace stom {
 namespace {
 
 constexpr int kRows = 128, kStageCols = 128;
-constexpr int kWorkWarps = 16, kSides = kWorkWarps / 4, kWorkThreads = kWorkWarps * 32, kThreads = kWorkThreads + 4 * 32;
+constexpr int kUnpackWarps = 8, kFoldWarps = 8, kWorkWarps = kUnpackWarps + kFoldWarps;
+constexpr int kUnpackThreads = kUnpackWarps * 32, kFoldThreads = kFoldWarps * 32, kThreads = (kWorkWarps + 4) * 32;
 constexpr int kChunkCols = 256, kChunks = 4;              // columns of a copy, copies in the ring
 constexpr int kPitch = kChunkCols / 2 + 16, kChunkBytes = kRows * kPitch;   // an odd number of 16 bytes: a row a thread without conflicts
 constexpr int kAStage = kRows * kStageCols * 2, kBStages = 3;
@@ -93,7 +94,7 @@ struct Many {
 template <typename T, int GROUP, int N>
 __global__ void __launch_bounds__(kThreads, 1) w4_many_kernel(const __grid_constant__ ManyParams p) {
     using S = Many<GROUP, N>;
-    constexpr int kGroups = S::kGroups, kBStage = S::kBStage, kOwn = N / kSides;   // tokens of a thread
+    constexpr int kGroups = S::kGroups, kBStage = S::kBStage, kOwn = N / 2;   // tokens of a thread that folds
     extern __shared__ uint8_t raw_smem[];
     __shared__ uint64_t c_full[kChunks], c_empty[kChunks], b_full[kBStages], b_empty[kBStages], a_full[2], done[2], folded[2], drained;
     __shared__ uint32_t tmem_word, abort_word, never_word;   // never_word stays 0
@@ -106,12 +107,12 @@ __global__ void __launch_bounds__(kThreads, 1) w4_many_kernel(const __grid_const
     const int col0 = s0 * kStageCols, n_chunks = (n_stages + 1) / 2;
     volatile uint32_t *abort_flag = &abort_word;
     if (tid == 0) {
-        for (int i = 0; i < kChunks; ++i) mbar_init(smem_u32(&c_full[i]), 64), mbar_init(smem_u32(&c_empty[i]), kWorkWarps);
-        for (int i = 0; i < kBStages; ++i) mbar_init(smem_u32(&b_full[i]), 1), mbar_init(smem_u32(&b_empty[i]), 1 + kWorkWarps);
+        for (int i = 0; i < kChunks; ++i) mbar_init(smem_u32(&c_full[i]), 64), mbar_init(smem_u32(&c_empty[i]), kUnpackWarps);
+        for (int i = 0; i < kBStages; ++i) mbar_init(smem_u32(&b_full[i]), 1), mbar_init(smem_u32(&b_empty[i]), 1 + kFoldWarps);
         for (int i = 0; i < 2; ++i) {
-            mbar_init(smem_u32(&a_full[i]), kWorkThreads);
+            mbar_init(smem_u32(&a_full[i]), kUnpackThreads);
             mbar_init(smem_u32(&done[i]), 1);
-            mbar_init(smem_u32(&folded[i]), kWorkThreads);
+            mbar_init(smem_u32(&folded[i]), kFoldThreads);
         }
         mbar_init(smem_u32(&drained), 1);
         abort_word = never_word = 0;
@@ -127,10 +128,7 @@ __global__ void __launch_bounds__(kThreads, 1) w4_many_kernel(const __grid_const
         if (!ok) *abort_flag = 1;
         return ok;
     };
-    float acc[kOwn];
-#pragma unroll
-    for (int i = 0; i < kOwn; ++i) acc[i] = 0.f;
-    const int quarter = warp & 3, side = warp >> 2, row = quarter * 32 + lane;   // of a working thread
+    const int quarter = warp & 3, side = warp >> 2 & 1, row = quarter * 32 + lane;   // of a thread that unpacks or folds
 
     if (warp == kWorkWarps || warp == kWorkWarps + 3) {
         // ---- codes: two warps with half of the rows each, 16 bytes a lane, 4 rows at a time (rows behind the last: the last,
@@ -189,19 +187,54 @@ __global__ void __launch_bounds__(kThreads, 1) w4_many_kernel(const __grid_const
             umma_commit(smem_u32(&drained));   // before tensor memory is given back
             if (!mbar_wait_bounded(smem_u32(&drained), 0, &never_word, kWaitLimitNs)) *abort_flag = 1;
         }
+    } else if (warp < kUnpackWarps) {
+        // ---- unpacking
+        uint8_t *to = smem + side * (kRows * 128) + row * 128;
+        const uint8_t *from = smem + S::kOffCodes + row * kPitch + side * 32;
+        int slot = 0;
+        uint32_t round = 0;
+        for (int s = 0; s < n_stages; ++s) {
+            const int b = s & 1;
+            if (!b) wait(c_full[slot], round);
+            if (s > 1) wait(done[b], (s - 2) >> 1);   // its products have read the operand that was there
+            __syncwarp();
+            const uint4 v[2] = {*reinterpret_cast<const uint4 *>(from + slot * kChunkBytes + b * 64),
+                                *reinterpret_cast<const uint4 *>(from + slot * kChunkBytes + b * 64 + 16)};
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const uint32_t u = w[j] >> 8;
+                    *reinterpret_cast<uint4 *>(to + b * kAStage + (((i * 4 + j) ^ (row & 7)) << 4)) =
+                        make_uint4(w[j] & 0x000f000fu, w[j] & 0x00f000f0u, u & 0x000f000fu, u & 0x00f000f0u);
+                }
+            }
+            fence_proxy_async();
+            mbar_arrive(smem_u32(&a_full[b]));
+            if (b || s + 1 == n_stages) {
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&c_empty[slot]));
+                if (++slot == kChunks) {
+                    slot = 0;
+                    round ^= 1u;
+                }
+            }
+        }
     } else {
-        // ---- unpacking and folding.  Scales of a chunk's groups go to shared memory as pairs; a thread brings kPairs of them,
-        // a chunk ahead in registers, into one of three buffers (the one before the last may still be read).
-        constexpr int kChunkGroups = kChunkCols / GROUP, kAll = kChunkGroups * kRows, kPairs = (kAll + kWorkThreads - 1) / kWorkThreads;
+        // ---- folding.  Scales of a chunk's groups go to shared memory as pairs; a thread brings kPairs of them, a chunk ahead in
+        // registers, into one of three buffers (the one before the last may still be read).
+        constexpr int kChunkGroups = kChunkCols / GROUP, kPairs = kChunkGroups * kRows / kFoldThreads;
         const bool wide = p.w.meta_dtype == STOM_FP32, narrow_bf = p.w.meta_dtype == STOM_BF16;
+        const int ft = tid - kUnpackThreads, r0 = ft / kChunkGroups, q0 = ft % kChunkGroups;   // of a thread's first pair
         uint32_t rs[kPairs], rz[kPairs];
         auto load_meta = [&](int c) {
+            const int gr = (col0 + c * kChunkCols) / GROUP + q0;
 #pragma unroll
             for (int i = 0; i < kPairs; ++i) {
-                const int e = i * kWorkThreads + tid, r = e / kChunkGroups, gr = (col0 + c * kChunkCols) / GROUP + e % kChunkGroups;
                 rs[i] = rz[i] = 0;
-                if ((kAll % kWorkThreads && e >= kAll) || c >= n_chunks || gr >= p.w.groups) continue;
-                const int64_t at = min(row0 + r, p.w.n - 1) * p.w.meta_stride + gr;
+                if (c >= n_chunks || gr >= p.w.groups) continue;
+                const int64_t at = min(row0 + r0 + i * (kFoldThreads / kChunkGroups), p.w.n - 1) * p.w.meta_stride + gr;
                 if (wide) {
                     rs[i] = __ldg(static_cast<const uint32_t *>(p.w.scale) + at);
                     if (p.w.zero) rz[i] = __ldg(static_cast<const uint32_t *>(p.w.zero) + at);
@@ -214,14 +247,30 @@ __global__ void __launch_bounds__(kThreads, 1) w4_many_kernel(const __grid_const
         auto number = [&](uint32_t bits) {
             return wide ? __uint_as_float(bits) : narrow_bf ? __uint_as_float(bits << 16) : __half2float(__ushort_as_half((unsigned short)bits));
         };
-        auto fold = [&](int s) {
+        uint64_t acc[kOwn / 2];   // two tokens each
+#pragma unroll
+        for (int i = 0; i < kOwn / 2; ++i) acc[i] = 0;
+        load_meta(0);
+        int b_slot = 0, m_slot = 0;
+        uint32_t b_round = 0;
+        for (int s = 0; s < n_stages; ++s) {
             const int b = s & 1;
-            wait(b_full[s % kBStages], s / kBStages);
+            if (!b) {
+                float2 *meta = reinterpret_cast<float2 *>(smem + S::kOffMeta + m_slot * S::kMeta) + q0 * kRows + r0;
+#pragma unroll
+                for (int i = 0; i < kPairs; ++i) {
+                    const float scale = number(rs[i]);
+                    meta[i * (kFoldThreads / kChunkGroups)] = make_float2(kCodeUnit * scale, p.w.zero ? number(rz[i]) : -8.f * scale);
+                }
+                load_meta((s >> 1) + 1);
+                named_sync(1, kFoldThreads);
+            }
+            wait(b_full[b_slot], b_round);
             wait(done[b], s >> 1);   // (a wait that has failed: what is there is used, and the call flagged)
             __syncwarp();
             tc_fence_after_sync();
-            const float2 *meta = reinterpret_cast<const float2 *>(smem + S::kOffMeta + (s >> 1) % 3 * S::kMeta) +
-                                 (s & 1) * kGroups * kRows + row;
+            const float2 *meta = reinterpret_cast<const float2 *>(smem + S::kOffMeta + m_slot * S::kMeta) + b * kGroups * kRows + row;
+            const ulonglong2 *fx = reinterpret_cast<const ulonglong2 *>(smem + S::kOffB + b_slot * kBStage + N * kStageCols * 2 + side * kOwn * 4);
 #pragma unroll
             for (int q = 0; q < kGroups; ++q) {
                 float d[kOwn];
@@ -231,64 +280,31 @@ __global__ void __launch_bounds__(kThreads, 1) w4_many_kernel(const __grid_const
                     mbar_arrive(smem_u32(&folded[b]));
                 }
                 const float2 f = meta[q * kRows];
-                const float4 *fx = reinterpret_cast<const float4 *>(smem + S::kOffB + s % kBStages * kBStage + N * kStageCols * 2) +
-                                   (q * N + side * kOwn) / 4;
-                const float4 *sx = fx + kGroups * N / 4;
+                const uint64_t fs = pair_of(f.x, f.x), fz = pair_of(f.y, f.y);
 #pragma unroll
                 for (int i = 0; i < kOwn; i += 4) {
-                    const float4 x = fx[i / 4], y = sx[i / 4];
-                    acc[i] = fmaf(f.y, y.x, fmaf(f.x, d[i] * x.x, acc[i]));
-                    acc[i + 1] = fmaf(f.y, y.y, fmaf(f.x, d[i + 1] * x.y, acc[i + 1]));
-                    acc[i + 2] = fmaf(f.y, y.z, fmaf(f.x, d[i + 2] * x.z, acc[i + 2]));
-                    acc[i + 3] = fmaf(f.y, y.w, fmaf(f.x, d[i + 3] * x.w, acc[i + 3]));
+                    const ulonglong2 x = fx[(q * N + i) / 4], y = fx[((kGroups + q) * N + i) / 4];   // factors, sums of four tokens
+                    acc[i / 2] = fma_pair(fz, y.x, fma_pair(fs, mul_pair(pair_of(d[i], d[i + 1]), x.x), acc[i / 2]));
+                    acc[i / 2 + 1] = fma_pair(fz, y.y, fma_pair(fs, mul_pair(pair_of(d[i + 2], d[i + 3]), x.y), acc[i / 2 + 1]));
                 }
             }
             __syncwarp();
-            if (lane == 0) mbar_arrive(smem_u32(&b_empty[s % kBStages]));
-        };
-        load_meta(0);
-        for (int c = 0; c < n_chunks; ++c) {
-            float2 *meta = reinterpret_cast<float2 *>(smem + S::kOffMeta + c % 3 * S::kMeta);
-#pragma unroll
-            for (int i = 0; i < kPairs; ++i) {
-                const int e = i * kWorkThreads + tid, r = e / kChunkGroups, q = e % kChunkGroups;
-                const float s = number(rs[i]);
-                if (kAll % kWorkThreads && e >= kAll) continue;
-                meta[q * kRows + r] = make_float2(kCodeUnit * s, p.w.zero ? number(rz[i]) : -8.f * s);
+            if (lane == 0) mbar_arrive(smem_u32(&b_empty[b_slot]));
+            if (++b_slot == kBStages) {
+                b_slot = 0;
+                b_round ^= 1u;
             }
-            load_meta(c + 1);
-            named_sync(1, kWorkThreads);
-            wait(c_full[c % kChunks], c / kChunks);
-            __syncwarp();
-#pragma unroll 1
-            for (int h = 0; h < 2; ++h) {
-                const int s = 2 * c + h, b = s & 1;
-                if (s >= n_stages) break;
-                // (the products of stage s - 2 are done: this thread has folded them)
-                const uint4 *from = reinterpret_cast<const uint4 *>(smem + S::kOffCodes + c % kChunks * kChunkBytes + row * kPitch + h * 64 + side * 16);
-                uint8_t *to = smem + b * kAStage + (side >> 1) * (kRows * 128) + row * 128;
-                const uint4 v = *from;
-                const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const uint32_t u = w[j] >> 8;
-                    *reinterpret_cast<uint4 *>(to + ((((side & 1) * 4 + j) ^ (row & 7)) << 4)) =
-                        make_uint4(w[j] & 0x000f000fu, w[j] & 0x00f000f0u, u & 0x000f000fu, u & 0x00f000f0u);
-                }
-                fence_proxy_async();
-                mbar_arrive(smem_u32(&a_full[b]));
-                if (h == 1 || s + 1 == n_stages) {
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(smem_u32(&c_empty[c % kChunks]));
-                }
-                if (s > 0) fold(s - 1);
-            }
+            if (b && ++m_slot == 3) m_slot = 0;
         }
-        fold(n_stages - 1);
         // sums to where the left operand was: its products are done
         float *out = reinterpret_cast<float *>(smem);
 #pragma unroll
-        for (int i = 0; i < kOwn; ++i) out[(side * kOwn + i) * S::kPitchOut + row] = acc[i];
+        for (int i = 0; i < kOwn / 2; ++i) {
+            float u, v;
+            parts_of(acc[i], u, v);
+            out[(side * kOwn + 2 * i) * S::kPitchOut + row] = u;
+            out[(side * kOwn + 2 * i + 1) * S::kPitchOut + row] = v;
+        }
     }
     __syncthreads();
     if (tid == 0 && *abort_flag && p.w.flags) atomicOr(p.w.flags, STOM_FLAG_TIMEOUT);
@@ -297,7 +313,8 @@ __global__ void __launch_bounds__(kThreads, 1) w4_many_kernel(const __grid_const
     cluster_sync();   // every block's sums are there
     // a block of the cluster joins every split-th token
     const float *out = reinterpret_cast<const float *>(smem);
-    if (tid < kWorkThreads) {
+    constexpr int kSides = kWorkWarps / 4;
+    if (tid < kWorkWarps * 32) {
         const int r = tid & (kRows - 1), at_row = row0 + r;
         for (int i = rank + (tid >> 7) * p.split; i < N; i += kSides * p.split) {
             const int tok = tile * N + i;
