@@ -468,6 +468,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_tree_kernel(const __grid_const
         // ================================================================ products
         if (lane == 0) {
             const uint32_t idesc_s = umma_idesc(kFmt, kTok), idesc_o = umma_idesc(kFmt, D) | kUmmaRightMn;
+            const uint32_t q_low = umma_low_k128(q_u), k_low = umma_low_k128(ring_u), v_low = umma_low_mn128(ring_u, kBlock);
             uint32_t unit = 0, in_unit = 0, unit_tiles = 0, fresh = 0;   // of the first products; fresh: bit c & 31, a unit begins
             bool live = true;
             auto scores = [&](uint32_t c) {
@@ -485,11 +486,12 @@ __global__ void __launch_bounds__(kThreads, 1) kv_tree_kernel(const __grid_const
                 if (!wait(sh.full[slot], k / kSlots)) return false;
                 fence_proxy_async();
                 tc_fence_after_sync();
-                const uint32_t qb = q_u + ((unit - 1) % kQBufs) * S::kQ, kb = ring_u + slot * kHalf;
+                const uint32_t ql = q_low + ((unit - 1) % kQBufs) * (S::kQ / 16), kl = k_low + slot * (kHalf / 16);
+                const uint32_t to = tmem + S::kSAt + c % kSBufs * kTok;
 #pragma unroll
                 for (int ks = 0; ks < D / 16; ++ks)
-                    umma_ss(tmem + S::kSAt + c % kSBufs * kTok, umma_desc_k128(qb + (ks >> 2) * (kRows * 128) + (ks & 3) * 32),
-                            umma_desc_k128(kb + (ks >> 2) * kBlock + (ks & 3) * 32), idesc_s, ks != 0);
+                    umma_ss_low(to, ql + (ks >> 2) * (kRows * 8) + (ks & 3) * 2, kl + (ks >> 2) * (kBlock / 16) + (ks & 3) * 2, idesc_s,
+                                ks != 0);
                 umma_commit(bar(sh.empty[slot]));
                 umma_commit(bar(sh.s_full[c % kSBufs]));
                 if (in_unit == unit_tiles) umma_commit(bar(sh.q_empty[(unit - 1) % kQBufs]));
@@ -502,12 +504,10 @@ __global__ void __launch_bounds__(kThreads, 1) kv_tree_kernel(const __grid_const
                 if (!live) break;
                 fence_proxy_async();
                 tc_fence_after_sync();
-                const uint32_t vb = ring_u + slot * kHalf;
+                const uint32_t vl = v_low + slot * (kHalf / 16), pl = tmem + S::kSAt + c % kSBufs * kTok;
                 const uint32_t more = !(fresh >> (c & 31) & 1u);
 #pragma unroll
-                for (int ks = 0; ks < kTok / 16; ++ks)
-                    umma_ts(tmem, tmem + S::kSAt + c % kSBufs * kTok + ks * 8, umma_desc_mn128(vb + ks * 2048, kBlock), idesc_o,
-                            more | (ks != 0));
+                for (int ks = 0; ks < kTok / 16; ++ks) umma_ts_low(tmem, pl + ks * 8, vl + ks * 128, idesc_o, more | (ks != 0));
                 umma_commit(bar(sh.empty[slot]));
                 umma_commit(bar(sh.pv_done[c & 1]));
                 if (c + kSBufs < n_tiles) live = wait(sh.pv_done[c & 1], c >> 1) && scores(c + kSBufs);   // its S takes P's place

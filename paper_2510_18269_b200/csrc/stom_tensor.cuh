@@ -42,21 +42,33 @@ __device__ __forceinline__ void umma_ss(uint32_t d_tmem, uint64_t a_desc, uint64
 __device__ __forceinline__ void umma_commit(uint32_t bar) {
     asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
-// Matrix descriptor of an operand whose rows are its columns of the product (MN-major) in the same layout: a row of 128
-// bytes holds 64 adjacent entries of the outer axis, groups of 8 rows (steps of the summed axis) are 1024 bytes apart, the
-// next 64 entries of the outer axis `block` bytes away.
-__device__ __forceinline__ uint64_t umma_desc_mn128(uint32_t addr, uint32_t block) {
-    return (uint64_t)((addr & 0x3FFFFu) >> 4) | ((uint64_t)(block >> 4) << 16) | ((uint64_t)(1024 >> 4) << 32) | (1ull << 46) |
-           (2ull << 61);
-}
 constexpr uint32_t kUmmaRightMn = 1u << 16;   // of an instruction descriptor: the right operand is MN-major
-// D[tmem] (+)= A[tmem] . B[smem]^T, issued by one thread; A: a row a lane, two 16-bit entries a column
-__device__ __forceinline__ void umma_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+// The same products with the descriptors' low halves only, for loops that step through an operand by adding to them (a step of
+// n bytes is n / 16; their high halves are all alike): one thread issues them, and every instruction between two counts
+constexpr uint32_t kUmmaHigh = (1024u >> 4) | (1u << 14) | (2u << 29);
+__device__ __forceinline__ uint32_t umma_low_k128(uint32_t addr) { return ((addr & 0x3FFFFu) >> 4) | (1u << 16); }
+// An operand whose rows are its columns of the product (MN-major) in the same layout: a row of 128 bytes holds 64 adjacent
+// entries of the outer axis, groups of 8 rows (steps of the summed axis) are 1024 bytes apart, the next 64 entries of the outer
+// axis `block` bytes away.
+__device__ __forceinline__ uint32_t umma_low_mn128(uint32_t addr, uint32_t block) { return ((addr & 0x3FFFFu) >> 4) | ((block >> 4) << 16); }
+__device__ __forceinline__ void umma_ss_low(uint32_t d_tmem, uint32_t a, uint32_t b, uint32_t idesc, uint32_t accumulate) {
     asm volatile(
-        "{\n\t.reg .pred p;\n\t"
+        "{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\t"
         "setp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
-        ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate)
+        "mov.b64 da, {%1, %5};\n\t"
+        "mov.b64 db, {%2, %5};\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %3, p;\n\t}"
+        ::"r"(d_tmem), "r"(a), "r"(b), "r"(idesc), "r"(accumulate), "r"(kUmmaHigh)
+        : "memory");
+}
+// A in tensor memory: a row a lane, two 16-bit entries a column
+__device__ __forceinline__ void umma_ts_low(uint32_t d_tmem, uint32_t a_tmem, uint32_t b, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t.reg .b64 db;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "mov.b64 db, {%2, %5};\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %3, p;\n\t}"
+        ::"r"(d_tmem), "r"(a_tmem), "r"(b), "r"(idesc), "r"(accumulate), "r"(kUmmaHigh)
         : "memory");
 }
 // Consecutive columns of this thread's lane of tensor memory; a load waits for its values, stores are waited for below

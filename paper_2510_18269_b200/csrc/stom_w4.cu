@@ -267,7 +267,7 @@ cudaError_t launch_few(const W4Params &p, int sms, cudaStream_t s) {
 
 template <typename T, int GROUP>
 cudaError_t by_tokens(const W4Params &p, int sms, void *workspace, cudaStream_t s) {
-    if (!is_few(p.k, p.groups, p.tokens)) return w4_many<T>(p, GROUP, workspace, s);
+    if (!is_few(p.k, p.groups, p.tokens)) return w4_many<T>(p, GROUP, sms, workspace, s);
     return depth_of<1>(p.k, p.groups, p.tokens) == 4 ? launch_few<T, GROUP, 1, 4>(p, sms, s) : launch_few<T, GROUP, 1, 3>(p, sms, s);
 }
 

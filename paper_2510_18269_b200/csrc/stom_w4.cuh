@@ -68,7 +68,7 @@ __device__ __forceinline__ uint4 token_operand(const uint4 &v, float before) {
 
 // Many tokens (stom_w4_many.cu)
 template <typename T>
-cudaError_t w4_many(const W4Params &p, int group, void *workspace, cudaStream_t s);
+cudaError_t w4_many(const W4Params &p, int group, int sms, void *workspace, cudaStream_t s);
 int64_t w4_many_workspace(int32_t k, int32_t group, int32_t tokens);
 
 }  // namespace stom

@@ -11,8 +11,10 @@
 // One thread issues the products, each group into accumulators of its own in tensor memory, since scales differ from group to
 // group.  Eight more warps fold those of the stage before into sums while the products of this one run: a thread has a row
 // again, and half of the tokens.
-// Blocks that share out the columns of the same rows form a cluster (up to 8, so many that all multiprocessors have a
-// block), whose sums are joined over distributed shared memory.
+//
+// Split.  The work is one line of stages, tile by tile (128 rows, N tokens), and every block, one a multiprocessor, takes an
+// equal, contiguous stretch of it.  The sums of a tile that is cut by a stretch's end go to the workspace, and a third small
+// kernel joins them.
 #include "stom_tensor.cuh"
 #include "stom_w4.cuh"
 
@@ -23,9 +25,10 @@ namespace {
 constexpr int kRows = 128, kStageCols = 128;
 constexpr int kUnpackWarps = 8, kFoldWarps = 8, kWorkWarps = kUnpackWarps + kFoldWarps;
 constexpr int kUnpackThreads = kUnpackWarps * 32, kFoldThreads = kFoldWarps * 32, kThreads = (kWorkWarps + 4) * 32;
-constexpr int kChunkCols = 256, kChunks = 4;              // columns of a copy, copies in the ring
+constexpr int kChunkCols = 256;                           // columns of a copy
 constexpr int kPitch = kChunkCols / 2 + 16, kChunkBytes = kRows * kPitch;   // an odd number of 16 bytes: a row a thread without conflicts
 constexpr int kAStage = kRows * kStageCols * 2, kBStages = 3;
+constexpr int kMaxBlocks = 256;                            // blocks of the grid the workspace has room for
 constexpr unsigned long long kWaitLimitNs = 1000000000ull;   // a wait that has taken 1 s ends the block
 
 // Bytes of a stage's operand of the tokens, factors and sums
@@ -34,7 +37,10 @@ __host__ __device__ constexpr int stage_bytes(int group, int n) { return n * kSt
 struct ManyParams {
     W4Params w;
     uint8_t *image;        // [token tile][stage]: operand [2][N][128 bytes], factors [group][N], sums [group][N]
-    int32_t stages, split; // of 128 columns; blocks of a cluster
+    float *part;           // [block][2][N][128]: sums of the tile that came in from the block before, and of the one that goes on
+    int32_t stages;        // of 128 columns, of a tile
+    int32_t row_tiles, blocks;
+    int64_t per, total;    // stages of a block, of all
 };
 
 __device__ __forceinline__ void named_sync(int id, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
@@ -83,33 +89,66 @@ struct Many {
     static constexpr int kGroups = kStageCols / GROUP;         // of a stage
     static constexpr int kBStage = (stage_bytes(GROUP, N) + 1023) / 1024 * 1024;
     static constexpr int kMeta = kChunkCols / GROUP * kRows * 8;
-    static constexpr int kCols = 2 * kGroups * N < 32 ? 32 : 2 * kGroups * N;   // of tensor memory, a power of two
-    static constexpr int kOffB = 2 * kAStage, kOffCodes = kOffB + kBStages * kBStage, kOffMeta = kOffCodes + kChunks * kChunkBytes;
+    // stages of the left operand and of accumulators: three where they fit into shared and tensor memory
+    static constexpr int kBufs = 3 * kGroups * N <= 512 ? 3 : 2, kChunks = kBufs == 3 && N == 64 ? 3 : 4;
+    static constexpr int kCols = kBufs * kGroups * N <= 64 ? 64 : kBufs * kGroups * N <= 128 ? 128 : kBufs * kGroups * N <= 256 ? 256 : 512;
+    static constexpr int kOffB = kBufs * kAStage, kOffCodes = kOffB + kBStages * kBStage, kOffMeta = kOffCodes + kChunks * kChunkBytes;
     static constexpr int kSmem = 1024 + kOffMeta + 3 * kMeta;
-    static constexpr int kPitchOut = kRows + 4;                // floats from token to token of the sums that a cluster joins
-    static_assert(kSmem <= 226 * 1024 && kCols <= 512, "room");
-    static_assert(N * kPitchOut * 4 <= 2 * kAStage, "the sums take the left operand's place");
+    static_assert(kSmem <= 226 * 1024, "room");
 };
+
+// A part of a block's stretch: stages first ... first + n - 1 of a tile
+struct Part {
+    int32_t tile, row0, first, n;
+    bool whole;
+};
+__device__ __forceinline__ Part part_at(const ManyParams &p, int64_t at, int64_t end) {
+    const int64_t tile = at / p.stages;
+    Part r;
+    r.first = (int32_t)(at - tile * p.stages);
+    r.n = (int32_t)min((int64_t)(p.stages - r.first), end - at);
+    r.whole = r.n == p.stages;
+    r.tile = (int32_t)(tile / p.row_tiles);                       // of tokens
+    r.row0 = (int32_t)(tile - (int64_t)r.tile * p.row_tiles) * kRows;
+    return r;
+}
+// Slots of a ring and the parity of the round
+struct Ring {
+    int slot = 0;
+    uint32_t round = 0;
+    __device__ __forceinline__ void next(int slots) {
+        if (++slot == slots) {
+            slot = 0;
+            round ^= 1u;
+        }
+    }
+};
+
+template <typename T>
+__device__ __forceinline__ void put(const W4Params &w, int tok, int row, float y) {
+    if (w.bias) y += to_float(static_cast<const T *>(w.bias)[row]);
+    if (w.add) y += to_float(static_cast<const T *>(w.add)[tok * w.add_stride + row]);
+    static_cast<T *>(w.y)[tok * w.y_stride + row] = from_float<T>(y);
+}
 
 template <typename T, int GROUP, int N>
 __global__ void __launch_bounds__(kThreads, 1) w4_many_kernel(const __grid_constant__ ManyParams p) {
     using S = Many<GROUP, N>;
     constexpr int kGroups = S::kGroups, kBStage = S::kBStage, kOwn = N / 2;   // tokens of a thread that folds
+    constexpr int kBufs = S::kBufs, kChunks = S::kChunks;
     extern __shared__ uint8_t raw_smem[];
-    __shared__ uint64_t c_full[kChunks], c_empty[kChunks], b_full[kBStages], b_empty[kBStages], a_full[2], done[2], folded[2], drained;
+    __shared__ uint64_t c_full[kChunks], c_empty[kChunks], b_full[kBStages], b_empty[kBStages], a_full[kBufs], done[kBufs],
+        folded[kBufs], drained;
     __shared__ uint32_t tmem_word, abort_word, never_word;   // never_word stays 0
     uint8_t *smem = raw_smem + ((1024u - (smem_u32(raw_smem) & 1023u)) & 1023u);   // the swizzle goes by addresses
     const uint32_t smem_at = smem_u32(smem);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int rank = blockIdx.x, row0 = blockIdx.y * kRows, tile = blockIdx.z;
-    // the block's stages, as equal shares as they can be
-    const int s0 = (int)((int64_t)p.stages * rank / p.split), n_stages = (int)((int64_t)p.stages * (rank + 1) / p.split) - s0;
-    const int col0 = s0 * kStageCols, n_chunks = (n_stages + 1) / 2;
+    const int64_t begin = min(p.total, blockIdx.x * p.per), end = min(p.total, begin + p.per);
     volatile uint32_t *abort_flag = &abort_word;
     if (tid == 0) {
         for (int i = 0; i < kChunks; ++i) mbar_init(smem_u32(&c_full[i]), 64), mbar_init(smem_u32(&c_empty[i]), kUnpackWarps);
         for (int i = 0; i < kBStages; ++i) mbar_init(smem_u32(&b_full[i]), 1), mbar_init(smem_u32(&b_empty[i]), 1 + kFoldWarps);
-        for (int i = 0; i < 2; ++i) {
+        for (int i = 0; i < kBufs; ++i) {
             mbar_init(smem_u32(&a_full[i]), kUnpackThreads);
             mbar_init(smem_u32(&done[i]), 1);
             mbar_init(smem_u32(&folded[i]), kFoldThreads);
@@ -124,7 +163,7 @@ __global__ void __launch_bounds__(kThreads, 1) w4_many_kernel(const __grid_const
     tc_fence_after_sync();
     const uint32_t tmem = tmem_word;
     auto wait = [&](uint64_t &b, uint32_t parity) {
-        const bool ok = mbar_wait_bounded(smem_u32(&b), parity & 1u, abort_flag, kWaitLimitNs);
+        const bool ok = mbar_wait_bounded(smem_u32(&b), parity, abort_flag, kWaitLimitNs);
         if (!ok) *abort_flag = 1;
         return ok;
     };
@@ -134,55 +173,75 @@ __global__ void __launch_bounds__(kThreads, 1) w4_many_kernel(const __grid_const
         // ---- codes: two warps with half of the rows each, 16 bytes a lane, 4 rows at a time (rows behind the last: the last,
         // never written).  Weights are read before the tokens' kernel is waited for: it began when all before it had ended.
         // (Bulk copies of a row's 128 bytes each would take as long as 60 clocks apiece.)
-        const int half = (warp - kWorkWarps) / 3 * 64, mine = row0 + half + (lane >> 3);
-        const uint8_t *from = p.w.codes + col0 / 2 + (lane & 7) * 16;
-        uint32_t to = smem_at + S::kOffCodes + (half + (lane >> 3)) * kPitch + (lane & 7) * 16;
-        for (int c = 0; c < n_chunks; ++c) {
-            const int slot = c % kChunks;
-            if (c >= kChunks && !__all_sync(~0u, wait(c_empty[slot], c / kChunks - 1))) break;
-            if (col0 + c * kChunkCols + (lane & 7) * 32 < p.w.k) {   // (of columns behind the last any codes will do)
-                const uint8_t *src = from + c * (kChunkCols / 2);
-                const uint32_t dst = to + slot * kChunkBytes;
-                if (row0 + kRows <= p.w.n) {
-                    src += mine * p.w.code_stride;
+        const int mine = (warp - kWorkWarps) / 3 * 64 + (lane >> 3);
+        const uint32_t to = smem_at + S::kOffCodes + mine * kPitch + (lane & 7) * 16;
+        Ring c;
+        bool again = false, live = true;
+        for (int64_t at = begin; at < end && live;) {
+            const Part part = part_at(p, at, end);
+            at += part.n;
+            const bool full_rows = part.row0 + kRows <= p.w.n;
+            const uint8_t *from = p.w.codes + (part.row0 + mine) * p.w.code_stride + (lane & 7) * 16;
+            for (int s = 0; s < part.n; s += 2) {
+                if (again && !(live = __all_sync(~0u, wait(c_empty[c.slot], c.round ^ 1u)))) break;
+                const int col = (part.first + s) * kStageCols;
+                if (col + (lane & 7) * 32 < p.w.k && (s + 1 < part.n || (lane & 7) < 4)) {   // (behind the last any codes will do)
+                    const uint32_t dst = to + c.slot * kChunkBytes;
+                    if (full_rows) {
+                        const uint8_t *src = from + col / 2;
 #pragma unroll
-                    for (int r = 0; r < 16; ++r, src += 4 * p.w.code_stride) copy16_async(dst + r * 4 * kPitch, src, 16);
-                } else {
+                        for (int r = 0; r < 16; ++r, src += 4 * p.w.code_stride) copy16_async(dst + r * 4 * kPitch, src, 16);
+                    } else {
 #pragma unroll 4
-                    for (int r = 0; r < 16; ++r)
-                        copy16_async(dst + r * 4 * kPitch, src + min(mine + 4 * r, p.w.n - 1) * p.w.code_stride, 16);
+                        for (int r = 0; r < 16; ++r)
+                            copy16_async(dst + r * 4 * kPitch,
+                                         p.w.codes + min(part.row0 + mine + 4 * r, p.w.n - 1) * p.w.code_stride + (lane & 7) * 16 + col / 2, 16);
+                    }
                 }
+                asm volatile("cp.async.mbarrier.arrive.noinc.shared.b64 [%0];" ::"r"(smem_u32(&c_full[c.slot])) : "memory");
+                c.next(kChunks);
+                again |= c.slot == 0;
             }
-            asm volatile("cp.async.mbarrier.arrive.noinc.shared.b64 [%0];" ::"r"(smem_u32(&c_full[slot])) : "memory");
         }
         asm volatile("cp.async.wait_all;" ::: "memory");
     } else if (warp == kWorkWarps + 2) {
         // ---- operands of the tokens
         grid_dependency_wait();
-        if (lane == 0)
-            for (int s = 0; s < n_stages; ++s) {
-                const int slot = s % kBStages;
-                if (s >= kBStages && !wait(b_empty[slot], s / kBStages - 1)) break;
+        if (lane == 0) {
+            Ring b;
+            bool again = false, live = true;
+            for (int64_t at = begin; at < end && live;) {
+                const Part part = part_at(p, at, end);
+                at += part.n;
                 constexpr int kBytes = stage_bytes(GROUP, N);
-                mbar_expect_tx(smem_u32(&b_full[slot]), kBytes);
-                bulk_load(smem_at + S::kOffB + slot * kBStage, p.image + ((int64_t)tile * p.stages + s0 + s) * kBytes, kBytes,
-                          smem_u32(&b_full[slot]));
+                const uint8_t *from = p.image + ((int64_t)part.tile * p.stages + part.first) * kBytes;
+                for (int s = 0; s < part.n; ++s, from += kBytes) {
+                    if (again && !(live = wait(b_empty[b.slot], b.round ^ 1u))) break;
+                    mbar_expect_tx(smem_u32(&b_full[b.slot]), kBytes);
+                    bulk_load(smem_at + S::kOffB + b.slot * kBStage, from, kBytes, smem_u32(&b_full[b.slot]));
+                    b.next(kBStages);
+                    again |= b.slot == 0;
+                }
             }
+        }
     } else if (warp == kWorkWarps + 1) {
         // ---- products
         if (lane == 0) {
-            const uint32_t idesc = umma_idesc(0, N);
-            for (int s = 0; s < n_stages; ++s) {
-                const int b = s & 1, slot = s % kBStages;
-                if (!(wait(b_full[slot], s / kBStages) && wait(a_full[b], s >> 1) && (s < 2 || wait(folded[b], (s >> 1) - 1)))) break;
+            const uint32_t idesc = umma_idesc(0, N), a_low = umma_low_k128(smem_at), b_low = umma_low_k128(smem_at + S::kOffB);
+            Ring a, b;
+            for (int64_t s = begin; s < end; ++s) {
+                if (!(wait(b_full[b.slot], b.round) && wait(a_full[a.slot], a.round) &&
+                      (s < begin + kBufs || wait(folded[a.slot], a.round ^ 1u)))) break;
                 tc_fence_after_sync();
-                const uint32_t as = smem_at + b * kAStage, bs = smem_at + S::kOffB + slot * kBStage;
+                const uint32_t al = a_low + a.slot * (kAStage / 16), bl = b_low + b.slot * (kBStage / 16), to = tmem + a.slot * (kGroups * N);
 #pragma unroll
                 for (int ks = 0; ks < kStageCols / 16; ++ks)
-                    umma_ss(tmem + (b * kGroups + ks * 16 / GROUP) * N, umma_desc_k128(as + (ks >> 2) * (kRows * 128) + (ks & 3) * 32),
-                            umma_desc_k128(bs + (ks >> 2) * (N * 128) + (ks & 3) * 32), idesc, ks * 16 % GROUP != 0);
-                umma_commit(smem_u32(&b_empty[slot]));
-                umma_commit(smem_u32(&done[b]));
+                    umma_ss_low(to + ks * 16 / GROUP * N, al + (ks >> 2) * (kRows * 8) + (ks & 3) * 2, bl + (ks >> 2) * (N * 8) + (ks & 3) * 2,
+                                idesc, ks * 16 % GROUP != 0);
+                umma_commit(smem_u32(&b_empty[b.slot]));
+                umma_commit(smem_u32(&done[a.slot]));
+                a.next(kBufs);
+                b.next(kBStages);
             }
             umma_commit(smem_u32(&drained));   // before tensor memory is given back
             if (!mbar_wait_bounded(smem_u32(&drained), 0, &never_word, kWaitLimitNs)) *abort_flag = 1;
@@ -191,33 +250,36 @@ __global__ void __launch_bounds__(kThreads, 1) w4_many_kernel(const __grid_const
         // ---- unpacking
         uint8_t *to = smem + side * (kRows * 128) + row * 128;
         const uint8_t *from = smem + S::kOffCodes + row * kPitch + side * 32;
-        int slot = 0;
-        uint32_t round = 0;
-        for (int s = 0; s < n_stages; ++s) {
-            const int b = s & 1;
-            if (!b) wait(c_full[slot], round);
-            if (s > 1) wait(done[b], (s - 2) >> 1);   // its products have read the operand that was there
-            __syncwarp();
-            const uint4 v[2] = {*reinterpret_cast<const uint4 *>(from + slot * kChunkBytes + b * 64),
-                                *reinterpret_cast<const uint4 *>(from + slot * kChunkBytes + b * 64 + 16)};
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const uint32_t u = w[j] >> 8;
-                    *reinterpret_cast<uint4 *>(to + b * kAStage + (((i * 4 + j) ^ (row & 7)) << 4)) =
-                        make_uint4(w[j] & 0x000f000fu, w[j] & 0x00f000f0u, u & 0x000f000fu, u & 0x00f000f0u);
-                }
-            }
-            fence_proxy_async();
-            mbar_arrive(smem_u32(&a_full[b]));
-            if (b || s + 1 == n_stages) {
+        Ring a, c;
+        bool again = false;
+        for (int64_t at = begin; at < end;) {
+            const int n = part_at(p, at, end).n;
+            at += n;
+            for (int s = 0; s < n; ++s) {
+                if (!(s & 1)) wait(c_full[c.slot], c.round);
+                if (again) wait(done[a.slot], a.round ^ 1u);   // its products have read the operand that was there
                 __syncwarp();
-                if (lane == 0) mbar_arrive(smem_u32(&c_empty[slot]));
-                if (++slot == kChunks) {
-                    slot = 0;
-                    round ^= 1u;
+                const uint8_t *src = from + c.slot * kChunkBytes + (s & 1) * 64;
+                uint8_t *dst = to + a.slot * kAStage;
+                const uint4 v[2] = {*reinterpret_cast<const uint4 *>(src), *reinterpret_cast<const uint4 *>(src + 16)};
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const uint32_t u = w[j] >> 8;
+                        *reinterpret_cast<uint4 *>(dst + (((i * 4 + j) ^ (row & 7)) << 4)) =
+                            make_uint4(w[j] & 0x000f000fu, w[j] & 0x00f000f0u, u & 0x000f000fu, u & 0x00f000f0u);
+                    }
+                }
+                fence_proxy_async();
+                mbar_arrive(smem_u32(&a_full[a.slot]));
+                a.next(kBufs);
+                again |= a.slot == 0;
+                if ((s & 1) || s + 1 == n) {
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(smem_u32(&c_empty[c.slot]));
+                    c.next(kChunks);
                 }
             }
         }
@@ -228,13 +290,13 @@ __global__ void __launch_bounds__(kThreads, 1) w4_many_kernel(const __grid_const
         const bool wide = p.w.meta_dtype == STOM_FP32, narrow_bf = p.w.meta_dtype == STOM_BF16;
         const int ft = tid - kUnpackThreads, r0 = ft / kChunkGroups, q0 = ft % kChunkGroups;   // of a thread's first pair
         uint32_t rs[kPairs], rz[kPairs];
-        auto load_meta = [&](int c) {
-            const int gr = (col0 + c * kChunkCols) / GROUP + q0;
+        auto load_meta = [&](const Part &part, int s) {
+            const int gr = (part.first + s) * kGroups + q0;
 #pragma unroll
             for (int i = 0; i < kPairs; ++i) {
                 rs[i] = rz[i] = 0;
-                if (c >= n_chunks || gr >= p.w.groups) continue;
-                const int64_t at = min(row0 + r0 + i * (kFoldThreads / kChunkGroups), p.w.n - 1) * p.w.meta_stride + gr;
+                if (gr >= p.w.groups) continue;
+                const int64_t at = min(part.row0 + r0 + i * (kFoldThreads / kChunkGroups), p.w.n - 1) * p.w.meta_stride + gr;
                 if (wide) {
                     rs[i] = __ldg(static_cast<const uint32_t *>(p.w.scale) + at);
                     if (p.w.zero) rz[i] = __ldg(static_cast<const uint32_t *>(p.w.zero) + at);
@@ -247,170 +309,156 @@ __global__ void __launch_bounds__(kThreads, 1) w4_many_kernel(const __grid_const
         auto number = [&](uint32_t bits) {
             return wide ? __uint_as_float(bits) : narrow_bf ? __uint_as_float(bits << 16) : __half2float(__ushort_as_half((unsigned short)bits));
         };
-        uint64_t acc[kOwn / 2];   // two tokens each
+        Ring a, b;
+        int m_slot = 0;
+        Part next = part_at(p, begin, end);
+        if (begin < end) load_meta(next, 0);
+        for (int64_t at = begin; at < end;) {
+            const Part part = next;
+            at += part.n;
+            if (at < end) next = part_at(p, at, end);
+            uint64_t acc[kOwn / 2];   // two tokens each
 #pragma unroll
-        for (int i = 0; i < kOwn / 2; ++i) acc[i] = 0;
-        load_meta(0);
-        int b_slot = 0, m_slot = 0;
-        uint32_t b_round = 0;
-        for (int s = 0; s < n_stages; ++s) {
-            const int b = s & 1;
-            if (!b) {
-                float2 *meta = reinterpret_cast<float2 *>(smem + S::kOffMeta + m_slot * S::kMeta) + q0 * kRows + r0;
+            for (int i = 0; i < kOwn / 2; ++i) acc[i] = 0;
+            for (int s = 0; s < part.n; ++s) {
+                if (!(s & 1)) {
+                    float2 *meta = reinterpret_cast<float2 *>(smem + S::kOffMeta + m_slot * S::kMeta) + q0 * kRows + r0;
 #pragma unroll
-                for (int i = 0; i < kPairs; ++i) {
-                    const float scale = number(rs[i]);
-                    meta[i * (kFoldThreads / kChunkGroups)] = make_float2(kCodeUnit * scale, p.w.zero ? number(rz[i]) : -8.f * scale);
+                    for (int i = 0; i < kPairs; ++i) {
+                        const float scale = number(rs[i]);
+                        meta[i * (kFoldThreads / kChunkGroups)] = make_float2(kCodeUnit * scale, p.w.zero ? number(rz[i]) : -8.f * scale);
+                    }
+                    if (s + 2 < part.n) load_meta(part, s + 2);
+                    else if (at < end) load_meta(next, 0);
+                    named_sync(1, kFoldThreads);
                 }
-                load_meta((s >> 1) + 1);
-                named_sync(1, kFoldThreads);
-            }
-            wait(b_full[b_slot], b_round);
-            wait(done[b], s >> 1);   // (a wait that has failed: what is there is used, and the call flagged)
-            __syncwarp();
-            tc_fence_after_sync();
-            const float2 *meta = reinterpret_cast<const float2 *>(smem + S::kOffMeta + m_slot * S::kMeta) + b * kGroups * kRows + row;
-            const ulonglong2 *fx = reinterpret_cast<const ulonglong2 *>(smem + S::kOffB + b_slot * kBStage + N * kStageCols * 2 + side * kOwn * 4);
+                wait(b_full[b.slot], b.round);
+                wait(done[a.slot], a.round);   // (a wait that has failed: what is there is used, and the call flagged)
+                __syncwarp();
+                tc_fence_after_sync();
+                const float2 *meta = reinterpret_cast<const float2 *>(smem + S::kOffMeta + m_slot * S::kMeta) + (s & 1) * kGroups * kRows + row;
+                const ulonglong2 *fx = reinterpret_cast<const ulonglong2 *>(smem + S::kOffB + b.slot * kBStage + N * kStageCols * 2 + side * kOwn * 4);
 #pragma unroll
-            for (int q = 0; q < kGroups; ++q) {
-                float d[kOwn];
-                tmem_load(tmem + ((uint32_t)(32 * quarter) << 16) + (b * kGroups + q) * N + side * kOwn, d);
-                if (q == kGroups - 1) {
-                    tc_fence_before_sync();
-                    mbar_arrive(smem_u32(&folded[b]));
+                for (int q = 0; q < kGroups; ++q) {
+                    float d[kOwn];
+                    tmem_load(tmem + ((uint32_t)(32 * quarter) << 16) + (a.slot * kGroups + q) * N + side * kOwn, d);
+                    if (q == kGroups - 1) {
+                        tc_fence_before_sync();
+                        mbar_arrive(smem_u32(&folded[a.slot]));
+                    }
+                    const float2 f = meta[q * kRows];
+                    const uint64_t fs = pair_of(f.x, f.x), fz = pair_of(f.y, f.y);
+#pragma unroll
+                    for (int i = 0; i < kOwn; i += 4) {
+                        const ulonglong2 x = fx[(q * N + i) / 4], y = fx[((kGroups + q) * N + i) / 4];   // factors, sums of four tokens
+                        acc[i / 2] = fma_pair(fz, y.x, fma_pair(fs, mul_pair(pair_of(d[i], d[i + 1]), x.x), acc[i / 2]));
+                        acc[i / 2 + 1] = fma_pair(fz, y.y, fma_pair(fs, mul_pair(pair_of(d[i + 2], d[i + 3]), x.y), acc[i / 2 + 1]));
+                    }
                 }
-                const float2 f = meta[q * kRows];
-                const uint64_t fs = pair_of(f.x, f.x), fz = pair_of(f.y, f.y);
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&b_empty[b.slot]));
+                a.next(kBufs);
+                b.next(kBStages);
+                if (((s & 1) || s + 1 == part.n) && ++m_slot == 3) m_slot = 0;
+            }
+            grid_dependency_wait();   // (kernels before may read what is written here)
+            if (part.whole) {
+                if (part.row0 + row < p.w.n)
 #pragma unroll
-                for (int i = 0; i < kOwn; i += 4) {
-                    const ulonglong2 x = fx[(q * N + i) / 4], y = fx[((kGroups + q) * N + i) / 4];   // factors, sums of four tokens
-                    acc[i / 2] = fma_pair(fz, y.x, fma_pair(fs, mul_pair(pair_of(d[i], d[i + 1]), x.x), acc[i / 2]));
-                    acc[i / 2 + 1] = fma_pair(fz, y.y, fma_pair(fs, mul_pair(pair_of(d[i + 2], d[i + 3]), x.y), acc[i / 2 + 1]));
+                    for (int i = 0; i < kOwn / 2; ++i) {
+                        float u, v;
+                        parts_of(acc[i], u, v);
+                        const int tok = part.tile * N + side * kOwn + 2 * i;
+                        if (tok < p.w.tokens) put<T>(p.w, tok, part.row0 + row, u);
+                        if (tok + 1 < p.w.tokens) put<T>(p.w, tok + 1, part.row0 + row, v);
+                    }
+            } else {
+                float *to = p.part + (((int64_t)blockIdx.x * 2 + (part.first == 0 ? 1 : 0)) * N + side * kOwn) * kRows + row;
+#pragma unroll
+                for (int i = 0; i < kOwn / 2; ++i) {
+                    float u, v;
+                    parts_of(acc[i], u, v);
+                    to[2 * i * kRows] = u;
+                    to[(2 * i + 1) * kRows] = v;
                 }
             }
-            __syncwarp();
-            if (lane == 0) mbar_arrive(smem_u32(&b_empty[b_slot]));
-            if (++b_slot == kBStages) {
-                b_slot = 0;
-                b_round ^= 1u;
-            }
-            if (b && ++m_slot == 3) m_slot = 0;
-        }
-        // sums to where the left operand was: its products are done
-        float *out = reinterpret_cast<float *>(smem);
-#pragma unroll
-        for (int i = 0; i < kOwn / 2; ++i) {
-            float u, v;
-            parts_of(acc[i], u, v);
-            out[(side * kOwn + 2 * i) * S::kPitchOut + row] = u;
-            out[(side * kOwn + 2 * i + 1) * S::kPitchOut + row] = v;
         }
     }
     __syncthreads();
     if (tid == 0 && *abort_flag && p.w.flags) atomicOr(p.w.flags, STOM_FLAG_TIMEOUT);
     if (warp == kWorkWarps + 1) tmem_dealloc(tmem, S::kCols);
+}
+
+// Joins the sums of the tiles that are cut: block (i, j) those of the tile in which stretch i + 1 begins, if it is the first to
+// begin within it, for 8 tokens; a thread has a row and every second of them.
+template <typename T, int N>
+__global__ void __launch_bounds__(256) w4_join_kernel(const __grid_constant__ ManyParams p) {
     grid_dependency_wait();
-    cluster_sync();   // every block's sums are there
-    // a block of the cluster joins every split-th token
-    const float *out = reinterpret_cast<const float *>(smem);
-    constexpr int kSides = kWorkWarps / 4;
-    if (tid < kWorkWarps * 32) {
-        const int r = tid & (kRows - 1), at_row = row0 + r;
-        for (int i = rank + (tid >> 7) * p.split; i < N; i += kSides * p.split) {
-            const int tok = tile * N + i;
-            if (tok >= p.w.tokens || at_row >= p.w.n) continue;
-            float y = 0.f;
-            for (int b = 0; b < p.split; ++b) y += ld_cluster_f(out + i * S::kPitchOut + r, b);
-            if (p.w.bias) y += to_float(static_cast<const T *>(p.w.bias)[at_row]);
-            if (p.w.add) y += to_float(static_cast<const T *>(p.w.add)[tok * p.w.add_stride + at_row]);
-            static_cast<T *>(p.w.y)[tok * p.w.y_stride + at_row] = from_float<T>(y);
-        }
+    const int64_t cut = (blockIdx.x + 1) * p.per;
+    if (cut >= p.total) return;
+    const int64_t tile = cut / p.stages, begin = tile * p.stages, end = begin + p.stages;
+    if (cut == begin || cut - p.per > begin) return;   // not cut there, or before as well
+    const int tok0 = (int)(tile / p.row_tiles) * N, row0 = (int)(tile % p.row_tiles) * kRows;
+    const int r = threadIdx.x & (kRows - 1), first = blockIdx.x, last = (int)((end - 1) / p.per);
+    if (row0 + r >= p.w.n) return;
+    for (int i = blockIdx.y * 8 + (threadIdx.x >> 7); i < blockIdx.y * 8 + 8 && tok0 + i < p.w.tokens; i += 2) {
+        float y = 0.f;
+#pragma unroll 4
+        for (int b = first; b <= last; ++b) y += p.part[(((int64_t)b * 2 + (b == first ? 1 : 0)) * N + i) * kRows + r];
+        put<T>(p.w, tok0 + i, row0 + r, y);
     }
-    cluster_sync();   // nobody reads this block's sums any more
 }
 
 int tokens_of_tile(int tokens) { return tokens <= 16 ? 16 : tokens <= 32 ? 32 : 64; }
 
-// Blocks that share out the columns: the number for which the longest-working multiprocessor has the fewest stages to go
-// through (a block's beginning and end count for about six).  room[i]: clusters of i + 1 blocks that the device holds at once
-// (fewer than its multiprocessors would do: a cluster lies within one of its parts).
-int split_of(int stages, int64_t tiles, const int (&room)[8]) {
-    int best = 1;
-    int64_t least = INT64_MAX;
-    for (int split = 1; split <= 8 && split <= stages; ++split) {
-        if (room[split - 1] < 1) continue;
-        const int64_t rounds = (tiles + room[split - 1] - 1) / room[split - 1], cost = rounds * ((stages + split - 1) / split + 6);
-        if (cost < least) {
-            least = cost;
-            best = split;
-        }
-    }
-    return best;
-}
-
 template <typename T, int GROUP, int N>
-cudaError_t launch(ManyParams &p, cudaStream_t s) {
-    const int row_tiles = (p.w.n + kRows - 1) / kRows, tiles = (p.w.tokens + N - 1) / N;
+cudaError_t launch(ManyParams &p, int sms, cudaStream_t s) {
+    const int tiles = (p.w.tokens + N - 1) / N;
+    p.row_tiles = (p.w.n + kRows - 1) / kRows;
+    p.total = (int64_t)p.row_tiles * tiles * p.stages;
+    // (a stretch of fewer than four stages would be all beginning and end)
+    p.per = (p.total + sms - 1) / sms;
+    if (p.per < 4) p.per = 4;
+    p.blocks = (int32_t)((p.total + p.per - 1) / p.per);
     static std::atomic<uint64_t> allowed{0};
     cudaError_t e = allow_shared(reinterpret_cast<const void *>(w4_many_kernel<T, GROUP, N>), Many<GROUP, N>::kSmem, allowed);
-    if (e != cudaSuccess) return e;
-    cudaLaunchConfig_t lc = {};
-    lc.blockDim = dim3(kThreads);
-    lc.dynamicSmemBytes = Many<GROUP, N>::kSmem;
-    lc.stream = s;
-    cudaLaunchAttribute at[2];
-    at[0].id = cudaLaunchAttributeClusterDimension;
-    at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
-    at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at[1].val.programmaticStreamSerializationAllowed = 1;
-    lc.attrs = at;
-    // what a device holds does not change: asked for once
-    static std::atomic<int> known[64][8];
-    int dev = 0, room[8];
-    e = cudaGetDevice(&dev);
-    for (int i = 0; i < 8 && e == cudaSuccess; ++i) {
-        room[i] = dev < 64 ? known[dev][i].load(std::memory_order_relaxed) : 0;
-        if (room[i]) continue;
-        at[0].val.clusterDim.x = i + 1;
-        lc.gridDim = dim3(i + 1);
-        lc.numAttrs = 1;
-        e = cudaOccupancyMaxActiveClusters(&room[i], w4_many_kernel<T, GROUP, N>, &lc);
-        if (room[i] < 1) room[i] = -1;
-        if (dev < 64) known[dev][i].store(room[i], std::memory_order_relaxed);
-    }
-    if (e != cudaSuccess) return e;
-    p.split = split_of(p.stages, (int64_t)row_tiles * tiles, room);
     const int warps = tiles * N * ((p.stages + 1) / 2);
-    e = launch_after_producer(w4_tokens_kernel<T, GROUP, N>, dim3((warps + 7) / 8), dim3(256), 0, s, p);
-    if (e != cudaSuccess) return e;
-    lc.gridDim = dim3(p.split, row_tiles, tiles);
-    at[0].val.clusterDim.x = p.split;
-    lc.numAttrs = 2;
-    return cudaLaunchKernelEx(&lc, w4_many_kernel<T, GROUP, N>, p);
+    if (e == cudaSuccess) e = launch_after_producer(w4_tokens_kernel<T, GROUP, N>, dim3((warps + 7) / 8), dim3(256), 0, s, p);
+    if (e == cudaSuccess)
+        e = launch_after_producer(w4_many_kernel<T, GROUP, N>, dim3(p.blocks), dim3(kThreads), Many<GROUP, N>::kSmem, s, p);
+    if (e == cudaSuccess && p.per % p.stages && p.blocks > 1)
+        e = launch_after_producer(w4_join_kernel<T, N>, dim3(p.blocks - 1, N / 8), dim3(256), 0, s, p);
+    return e;
 }
 
 template <typename T, int GROUP>
-cudaError_t by_tokens(ManyParams &p, cudaStream_t s) {
+cudaError_t by_tokens(ManyParams &p, int sms, cudaStream_t s) {
     const int n = tokens_of_tile(p.w.tokens);
-    return n == 16 ? launch<T, GROUP, 16>(p, s) : n == 32 ? launch<T, GROUP, 32>(p, s) : launch<T, GROUP, 64>(p, s);
+    return n == 16 ? launch<T, GROUP, 16>(p, sms, s) : n == 32 ? launch<T, GROUP, 32>(p, sms, s) : launch<T, GROUP, 64>(p, sms, s);
 }
 
 }  // namespace
 
+static int64_t image_bytes(int32_t k, int32_t group, int32_t tokens) {
+    const int64_t n = tokens_of_tile(tokens), bytes = (tokens + n - 1) / n * ((k + kStageCols - 1) / kStageCols) * stage_bytes(group, (int)n);
+    return (bytes + 255) / 256 * 256;
+}
+
 int64_t w4_many_workspace(int32_t k, int32_t group, int32_t tokens) {
-    const int64_t n = tokens_of_tile(tokens);
-    return (tokens + n - 1) / n * ((k + kStageCols - 1) / kStageCols) * stage_bytes(group, (int)n);
+    return image_bytes(k, group, tokens) + (int64_t)kMaxBlocks * 2 * tokens_of_tile(tokens) * kRows * 4;
 }
 
 template <typename T>
-cudaError_t w4_many(const W4Params &w, int group, void *workspace, cudaStream_t s) {
+cudaError_t w4_many(const W4Params &w, int group, int sms, void *workspace, cudaStream_t s) {
     ManyParams p = {};
     p.w = w;
     p.stages = (w.k + kStageCols - 1) / kStageCols;
     p.image = static_cast<uint8_t *>(workspace);
-    return group == 32 ? by_tokens<T, 32>(p, s) : group == 64 ? by_tokens<T, 64>(p, s) : by_tokens<T, 128>(p, s);
+    p.part = reinterpret_cast<float *>(p.image + image_bytes(w.k, group, w.tokens));
+    if (sms > kMaxBlocks) sms = kMaxBlocks;
+    return group == 32 ? by_tokens<T, 32>(p, sms, s) : group == 64 ? by_tokens<T, 64>(p, sms, s) : by_tokens<T, 128>(p, sms, s);
 }
-template cudaError_t w4_many<__nv_bfloat16>(const W4Params &, int, void *, cudaStream_t);
-template cudaError_t w4_many<__half>(const W4Params &, int, void *, cudaStream_t);
+template cudaError_t w4_many<__nv_bfloat16>(const W4Params &, int, int, void *, cudaStream_t);
+template cudaError_t w4_many<__half>(const W4Params &, int, int, void *, cudaStream_t);
 
 }  // namespace stom
