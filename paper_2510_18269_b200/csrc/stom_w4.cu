@@ -57,7 +57,8 @@ __global__ void __launch_bounds__(kThreads, 1) w4_few_kernel(const __grid_consta
     constexpr int kTok = 8 * NT;
     extern __shared__ __align__(16) uint8_t smem[];
     __shared__ float2 meta_s[kWarps][2][kGroups][kRows];
-    const FewLayout<NT> at(p.k, p.groups, p.tokens, DEPTH);
+    const int tok0 = blockIdx.y * (8 * NT), tokens = min(8 * NT, p.tokens - tok0);   // of the block
+    const FewLayout<NT> at(p.k, p.groups, tokens, DEPTH);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, team = warp / kTeamWarps, tw = warp % kTeamWarps;
     const int g = lane >> 2, t = lane & 3;
     const int units = (p.k + kUnitCols - 1) / kUnitCols, slabs = (p.n + kRows - 1) / kRows;
@@ -126,10 +127,10 @@ __global__ void __launch_bounds__(kThreads, 1) w4_few_kernel(const __grid_consta
     // ---- tokens: a warp takes 256 columns of one at a time, a lane 8 of them; the lanes of a group find its largest value and
     // its sum
     float2 *factor = reinterpret_cast<float2 *>(smem + at.factor);   // [group][kTok / 2][factors, sums]
-    for (int i = warp; i < units * p.tokens; i += kWarps) {
+    for (int i = warp; i < units * tokens; i += kWarps) {
         const int tok = i / units, col = (i - tok * units) * kUnitCols + lane * 8;
         uint4 v = make_uint4(0, 0, 0, 0);
-        if (col < p.k) v = *reinterpret_cast<const uint4 *>(static_cast<const T *>(p.x) + tok * p.x_stride + col);
+        if (col < p.k) v = *reinterpret_cast<const uint4 *>(static_cast<const T *>(p.x) + (tok0 + tok) * p.x_stride + col);
         float a[8];
         unpack2<T>(v.x, a[0], a[1]);
         unpack2<T>(v.y, a[2], a[3]);
@@ -145,7 +146,7 @@ __global__ void __launch_bounds__(kThreads, 1) w4_few_kernel(const __grid_consta
         }
         float before, after;
         factors_of<T>(m, before, after);
-        *reinterpret_cast<uint4 *>(smem + ((int64_t)(col / 32 * p.tokens + tok) * 4 + (lane & 3)) * 16) = token_operand<T>(v, before);
+        *reinterpret_cast<uint4 *>(smem + ((int64_t)(col / 32 * tokens + tok) * 4 + (lane & 3)) * 16) = token_operand<T>(v, before);
         if (lane % (GROUP / 8) == 0) {
             float *to = reinterpret_cast<float *>(factor + (col / GROUP * (kTok / 2) + (tok >> 1)) * 2) + (tok & 1);
             to[0] = after;
@@ -157,7 +158,7 @@ __global__ void __launch_bounds__(kThreads, 1) w4_few_kernel(const __grid_consta
     // ---- products (a lane of a token that there is not reads the last one's: its columns of the product are not used)
     const uint8_t *own_x[NT];
 #pragma unroll
-    for (int c = 0; c < NT; ++c) own_x[c] = smem + (min(c * 8 + g, p.tokens - 1) * 4 + t) * 16;
+    for (int c = 0; c < NT; ++c) own_x[c] = smem + (min(c * 8 + g, tokens - 1) * 4 + t) * 16;
     int slot = 0, turn = 0;
 #pragma unroll 1
     for (int sl = 0; sl < mine; ++sl) {
@@ -187,7 +188,7 @@ __global__ void __launch_bounds__(kThreads, 1) w4_few_kernel(const __grid_consta
             const uint8_t *cs = ring + slot * kUnitBytes + g * kPitch + t * 4;
             slot = slot + 1 == DEPTH ? 0 : slot + 1;
             float d[NT][4];
-            const uint32_t x_at = u * (kUnitCols / 32) * (p.tokens * 64);
+            const uint32_t x_at = u * (kUnitCols / 32) * (tokens * 64);
             const float4 *fx = reinterpret_cast<const float4 *>(factor) + u * kGroups * (kTok / 2) + t;
 #pragma unroll
             for (int j = 0; j < kUnitCols / 32; ++j) {
@@ -202,7 +203,7 @@ __global__ void __launch_bounds__(kThreads, 1) w4_few_kernel(const __grid_consta
                 }
 #pragma unroll
                 for (int c = 0; c < NT; ++c) {
-                    const uint4 b = *reinterpret_cast<const uint4 *>(own_x[c] + x_at + j * (p.tokens * 64));
+                    const uint4 b = *reinterpret_cast<const uint4 *>(own_x[c] + x_at + j * (tokens * 64));
                     if (j * 32 % GROUP == 0) mma16x8x16_first(d[c], a[0], b.x, b.y);
                     else mma16x8x16<__half>(d[c], a[0], b.x, b.y);
                     mma16x8x16<__half>(d[c], a[1], b.z, b.w);
@@ -232,13 +233,13 @@ __global__ void __launch_bounds__(kThreads, 1) w4_few_kernel(const __grid_consta
 #pragma unroll
         for (int h = 0; h < (NT + 1) / 2; ++h) {
             const int c = h * 16 + tw * 2 + (lane >> 4);
-            if (row < p.n && c < p.tokens) {
+            if (row < p.n && c < tokens) {
                 float y = 0.f;
 #pragma unroll
                 for (int w = 0; w < kTeamWarps; ++w) y += part[w][lane & 15][c];
                 if (p.bias) y += to_float(static_cast<const T *>(p.bias)[row]);
-                if (p.add) y += to_float(static_cast<const T *>(p.add)[c * p.add_stride + row]);
-                static_cast<T *>(p.y)[c * p.y_stride + row] = from_float<T>(y);
+                if (p.add) y += to_float(static_cast<const T *>(p.add)[(tok0 + c) * p.add_stride + row]);
+                static_cast<T *>(p.y)[(tok0 + c) * p.y_stride + row] = from_float<T>(y);
             }
         }
     }
@@ -252,23 +253,27 @@ int depth_of(int k, int groups, int tokens) {
         if (FewLayout<NT>(k, groups, tokens, depth).total <= kMostShared) return depth;
     return 0;
 }
-// The few-tokens kernel where there are at most 8 and they fit into shared memory
-bool is_few(int k, int groups, int tokens) { return tokens <= 8 && depth_of<1>(k, groups, tokens) > 0; }
+// The few-tokens kernel takes up to 16, as twice 8 where they are more (the second reads the codes from L2), if 8 of them fit
+// into shared memory.  Measured against the kernel for many, columns from memory, 3 584 of them: 8 tokens, 4 608 rows 8.3 us
+// against 14.9, 28 672 rows 22 against 44, 151 001 rows 85 against 184; 16 tokens, twice as long against the same; at 32 the
+// other is ahead everywhere.
+bool is_few(int k, int groups, int tokens) { return tokens <= 16 && depth_of<1>(k, groups, tokens < 8 ? tokens : 8) > 0; }
 
 template <typename T, int GROUP, int NT, int DEPTH>
 cudaError_t launch_few(const W4Params &p, int sms, cudaStream_t s) {
-    const FewLayout<NT> l(p.k, p.groups, p.tokens, DEPTH);
+    const int tokens = p.tokens < 8 * NT ? p.tokens : 8 * NT;
+    const FewLayout<NT> l(p.k, p.groups, tokens, DEPTH);
     static std::atomic<uint64_t> allowed{0};
     const cudaError_t e = allow_shared(reinterpret_cast<const void *>(w4_few_kernel<T, GROUP, NT, DEPTH>), kMostShared, allowed);
     if (e != cudaSuccess) return e;
     const int slabs = (p.n + kRows - 1) / kRows;
-    return launch_after_producer(w4_few_kernel<T, GROUP, NT, DEPTH>, dim3(slabs < sms ? slabs : sms), dim3(kThreads), (size_t)l.total, s, p);
+    return launch_after_producer(w4_few_kernel<T, GROUP, NT, DEPTH>, dim3(slabs < sms ? slabs : sms, (p.tokens + tokens - 1) / tokens), dim3(kThreads), (size_t)l.total, s, p);
 }
 
 template <typename T, int GROUP>
 cudaError_t by_tokens(const W4Params &p, int sms, void *workspace, cudaStream_t s) {
     if (!is_few(p.k, p.groups, p.tokens)) return w4_many<T>(p, GROUP, sms, workspace, s);
-    return depth_of<1>(p.k, p.groups, p.tokens) == 4 ? launch_few<T, GROUP, 1, 4>(p, sms, s) : launch_few<T, GROUP, 1, 3>(p, sms, s);
+    return depth_of<1>(p.k, p.groups, p.tokens < 8 ? p.tokens : 8) == 4 ? launch_few<T, GROUP, 1, 4>(p, sms, s) : launch_few<T, GROUP, 1, 3>(p, sms, s);
 }
 
 template <typename T>

@@ -147,7 +147,7 @@ __global__ void __launch_bounds__(kThreads, 1) w4_many_kernel(const __grid_const
     volatile uint32_t *abort_flag = &abort_word;
     if (tid == 0) {
         for (int i = 0; i < kChunks; ++i) mbar_init(smem_u32(&c_full[i]), 64), mbar_init(smem_u32(&c_empty[i]), kUnpackWarps);
-        for (int i = 0; i < kBStages; ++i) mbar_init(smem_u32(&b_full[i]), 1), mbar_init(smem_u32(&b_empty[i]), 1 + kFoldWarps);
+        for (int i = 0; i < kBStages; ++i) mbar_init(smem_u32(&b_full[i]), 1), mbar_init(smem_u32(&b_empty[i]), kFoldWarps);
         for (int i = 0; i < kBufs; ++i) {
             mbar_init(smem_u32(&a_full[i]), kUnpackThreads);
             mbar_init(smem_u32(&done[i]), 1);
@@ -238,7 +238,6 @@ __global__ void __launch_bounds__(kThreads, 1) w4_many_kernel(const __grid_const
                 for (int ks = 0; ks < kStageCols / 16; ++ks)
                     umma_ss_low(to + ks * 16 / GROUP * N, al + (ks >> 2) * (kRows * 8) + (ks & 3) * 2, bl + (ks >> 2) * (N * 8) + (ks & 3) * 2,
                                 idesc, ks * 16 % GROUP != 0);
-                umma_commit(smem_u32(&b_empty[b.slot]));
                 umma_commit(smem_u32(&done[a.slot]));
                 a.next(kBufs);
                 b.next(kBStages);
@@ -356,7 +355,7 @@ __global__ void __launch_bounds__(kThreads, 1) w4_many_kernel(const __grid_const
                     }
                 }
                 __syncwarp();
-                if (lane == 0) mbar_arrive(smem_u32(&b_empty[b.slot]));
+                if (lane == 0) mbar_arrive(smem_u32(&b_empty[b.slot]));   // (its products are done, too)
                 a.next(kBufs);
                 b.next(kBStages);
                 if (((s & 1) || s + 1 == part.n) && ++m_slot == 3) m_slot = 0;
