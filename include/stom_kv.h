@@ -184,8 +184,9 @@ int32_t stom_kv_attend(const stom_kv_pool *pool, const stom_kv_seqs *seqs, int32
  * pool's type: off by 2^-8 of itself (bf16), or by 2^-11 of itself or 2^-32 of
  * the row's largest weight, whichever is more (fp16).
  * q, out (pool->dtype): element (row, h, c) at row*stride_token +
- * h*stride_head + c.  lse: binary32 [n_tokens][n_q_heads], or NULL.  Other
- * limits are those of stom_kv_attend, and n_tokens * n_q_heads < 2^31.
+ * h*stride_head + c.  lse: binary32 [n_tokens][n_q_heads], or NULL.  The
+ * limits are those of stom_kv_attend for softmax_scale, softcap, heads and
+ * n_seqs; max_pages * page_tokens < 2^31 - 256, n_tokens * n_q_heads < 2^31 - 128.
  * Errors as for stom_kv_attend. */
 #define STOM_KV_MAX_TREE 256
 int64_t stom_kv_attend_tree_workspace_bytes(const stom_kv_pool *pool, const stom_kv_seqs *seqs, int32_t n_tokens,

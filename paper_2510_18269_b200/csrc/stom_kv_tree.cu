@@ -1016,7 +1016,7 @@ extern "C" int32_t stom_kv_attend_tree(const stom_kv_pool *pool, const stom_kv_s
     if (n_q_heads % pool->n_kv_heads || n_q_heads / pool->n_kv_heads > 64) return STOM_ERR_SHAPE;
     if (seqs->n_seqs > STOM_KV_MAX_SEQS || (int64_t)n_tokens * n_q_heads > INT32_MAX - kRows) return STOM_ERR_SHAPE;
     const int64_t most = (int64_t)seqs->max_pages * pool->page_tokens;
-    if (most > INT32_MAX - 32) return STOM_ERR_SHAPE;
+    if (most > INT32_MAX - 256) return STOM_ERR_SHAPE;   // (tokens of a row's last tile are counted in 32 bits)
     if (seqs->n_seqs == 0 || n_tokens == 0) return STOM_OK;
     if (!first || !q || !out) return STOM_ERR_INVALID_ARG;
     if ((reinterpret_cast<uintptr_t>(first) | reinterpret_cast<uintptr_t>(parent) | reinterpret_cast<uintptr_t>(lse)) & 3u)

@@ -72,17 +72,6 @@ __device__ __forceinline__ void umma_ts_low(uint32_t d_tmem, uint32_t a_tmem, ui
         : "memory");
 }
 // Consecutive columns of this thread's lane of tensor memory; a load waits for its values, stores are waited for below
-__device__ __forceinline__ void tmem_load(uint32_t taddr, float (&v)[4]) {
-    uint32_t r[4];
-    asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x4.b32 {%0, %1, %2, %3}, [%4];\n\t"
-        "tcgen05.wait::ld.sync.aligned;"
-        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
-        : "r"(taddr)
-        : "memory");
-#pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = __uint_as_float(r[i]);
-}
 __device__ __forceinline__ void tmem_load(uint32_t taddr, float (&v)[8]) {
     uint32_t r[8];
     asm volatile(
@@ -143,13 +132,6 @@ __device__ __forceinline__ void tmem_load(uint32_t taddr, float (&v)[64]) {
         : "memory");
 #pragma unroll
     for (int i = 0; i < 64; ++i) v[i] = __uint_as_float(r[i]);
-}
-__device__ __forceinline__ void tmem_store(uint32_t taddr, const uint32_t (&r)[16]) {
-    asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
-        ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]),
-          "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
-        : "memory");
 }
 __device__ __forceinline__ void tmem_store(uint32_t taddr, const uint32_t (&r)[32]) {
     asm volatile(

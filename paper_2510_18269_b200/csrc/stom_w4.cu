@@ -17,6 +17,7 @@ namespace stom {
 namespace {
 
 constexpr int kRows = 16;     // of the matrix, per slab
+constexpr int kTok = 8;       // most tokens of a block
 constexpr int kTeams = 2, kTeamWarps = 8, kWarps = kTeams * kTeamWarps, kThreads = kWarps * 32;   // of a block
 constexpr int kUnitCols = 256;                // columns of a unit
 constexpr int kPitch = kUnitCols / 2 + 16;    // bytes from row to row in shared memory: 8 rows' words of 4 lanes lie in 32 banks
@@ -33,32 +34,30 @@ __device__ __forceinline__ void mma16x8x16_first(float (&c)[4], const uint32_t (
 }
 
 // Bytes of shared memory: the tokens' operands, a factor and a sum for each token and group, the warps' results, the rings
-template <int NT>
 struct FewLayout {
     int64_t factor, sums, rings, total;
     __host__ __device__ FewLayout(int k, int groups, int tokens, int depth) {
         const int64_t units = (k + kUnitCols - 1) / kUnitCols, group = k / groups;   // (columns behind the last: zeros)
         factor = units * (kUnitCols / 32) * tokens * 64;
-        sums = factor + units * (kUnitCols / group) * (8 * NT) * 8;
-        rings = sums + kTeams * 2 * kTeamWarps * kRows * (8 * NT + 1) * 4;
+        sums = factor + units * (kUnitCols / group) * kTok * 8;
+        rings = sums + kTeams * 2 * kTeamWarps * kRows * (kTok + 1) * 4;
         total = rings + kWarps * depth * kUnitBytes;
     }
 };
 
-// Up to 8 NT tokens; GROUP columns a group; a ring of DEPTH units.
+// Up to 8 tokens of those from 8 * blockIdx.y on; GROUP columns a group; a ring of DEPTH units.
 // A block, one a multiprocessor, has two teams of eight warps.  A team goes through slabs of 16 rows, whose UNITS of 256
 // columns its warps take in turn (and go on in turn with the next slab's, so that none has more of them).  A warp is alone
 // with its units: its own ring in shared memory, filled by 16-byte asynchronous copies DEPTH - 1 units ahead, the rows' scales
 // a unit ahead in registers.  At a slab's end the warps' sums are joined in shared memory, with one barrier of the team.
 // Tokens stay in shared memory, in the order of the fragments.
-template <typename T, int GROUP, int NT, int DEPTH>
+template <typename T, int GROUP, int DEPTH>
 __global__ void __launch_bounds__(kThreads, 1) w4_few_kernel(const __grid_constant__ W4Params p) {
     constexpr int kGroups = kUnitCols / GROUP;   // of a unit
-    constexpr int kTok = 8 * NT;
     extern __shared__ __align__(16) uint8_t smem[];
     __shared__ float2 meta_s[kWarps][2][kGroups][kRows];
-    const int tok0 = blockIdx.y * (8 * NT), tokens = min(8 * NT, p.tokens - tok0);   // of the block
-    const FewLayout<NT> at(p.k, p.groups, tokens, DEPTH);
+    const int tok0 = blockIdx.y * kTok, tokens = min(kTok, p.tokens - tok0);   // of the block
+    const FewLayout at(p.k, p.groups, tokens, DEPTH);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, team = warp / kTeamWarps, tw = warp % kTeamWarps;
     const int g = lane >> 2, t = lane & 3;
     const int units = (p.k + kUnitCols - 1) / kUnitCols, slabs = (p.n + kRows - 1) / kRows;
@@ -156,17 +155,11 @@ __global__ void __launch_bounds__(kThreads, 1) w4_few_kernel(const __grid_consta
     __syncthreads();
 
     // ---- products (a lane of a token that there is not reads the last one's: its columns of the product are not used)
-    const uint8_t *own_x[NT];
-#pragma unroll
-    for (int c = 0; c < NT; ++c) own_x[c] = smem + (min(c * 8 + g, tokens - 1) * 4 + t) * 16;
+    const uint8_t *own_x = smem + (min(g, tokens - 1) * 4 + t) * 16;
     int slot = 0, turn = 0;
 #pragma unroll 1
     for (int sl = 0; sl < mine; ++sl) {
-        float acc[NT][4];
-#pragma unroll
-        for (int c = 0; c < NT; ++c)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) acc[c][e] = 0.f;
+        float acc[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 1
         for (int u = first_unit(sl); u < units; u += kTeamWarps) {
             float2(*meta)[kRows] = meta_s[warp][turn & 1];
@@ -187,7 +180,7 @@ __global__ void __launch_bounds__(kThreads, 1) w4_few_kernel(const __grid_consta
             copy_unit();   // into the slot that the unit before this one has left
             const uint8_t *cs = ring + slot * kUnitBytes + g * kPitch + t * 4;
             slot = slot + 1 == DEPTH ? 0 : slot + 1;
-            float d[NT][4];
+            float d[4];
             const uint32_t x_at = u * (kUnitCols / 32) * (tokens * 64);
             const float4 *fx = reinterpret_cast<const float4 *>(factor) + u * kGroups * (kTok / 2) + t;
 #pragma unroll
@@ -201,79 +194,68 @@ __global__ void __launch_bounds__(kThreads, 1) w4_few_kernel(const __grid_consta
                     a[1][h] = w & 0x000f000fu;
                     a[1][2 + h] = w & 0x00f000f0u;
                 }
-#pragma unroll
-                for (int c = 0; c < NT; ++c) {
-                    const uint4 b = *reinterpret_cast<const uint4 *>(own_x[c] + x_at + j * (tokens * 64));
-                    if (j * 32 % GROUP == 0) mma16x8x16_first(d[c], a[0], b.x, b.y);
-                    else mma16x8x16<__half>(d[c], a[0], b.x, b.y);
-                    mma16x8x16<__half>(d[c], a[1], b.z, b.w);
-                }
+                const uint4 b = *reinterpret_cast<const uint4 *>(own_x + x_at + j * (tokens * 64));
+                if (j * 32 % GROUP == 0) mma16x8x16_first(d, a[0], b.x, b.y);
+                else mma16x8x16<__half>(d, a[0], b.x, b.y);
+                mma16x8x16<__half>(d, a[1], b.z, b.w);
                 if ((j + 1) * 32 % GROUP == 0) {
                     const int q = j * 32 / GROUP;
                     const float2 f0 = meta[q][g], f1 = meta[q][g + 8];
-#pragma unroll
-                    for (int c = 0; c < NT; ++c) {
-                        const float4 x = fx[q * (kTok / 2) + c * 4];   // factors and sums of tokens 2 t, 2 t + 1
-                        acc[c][0] = fmaf(f0.y, x.z, fmaf(f0.x, d[c][0] * x.x, acc[c][0]));
-                        acc[c][1] = fmaf(f0.y, x.w, fmaf(f0.x, d[c][1] * x.y, acc[c][1]));
-                        acc[c][2] = fmaf(f1.y, x.z, fmaf(f1.x, d[c][2] * x.x, acc[c][2]));
-                        acc[c][3] = fmaf(f1.y, x.w, fmaf(f1.x, d[c][3] * x.y, acc[c][3]));
-                    }
+                    const float4 x = fx[q * (kTok / 2)];   // factors and sums of tokens 2 t, 2 t + 1
+                    acc[0] = fmaf(f0.y, x.z, fmaf(f0.x, d[0] * x.x, acc[0]));
+                    acc[1] = fmaf(f0.y, x.w, fmaf(f0.x, d[1] * x.y, acc[1]));
+                    acc[2] = fmaf(f1.y, x.z, fmaf(f1.x, d[2] * x.x, acc[2]));
+                    acc[3] = fmaf(f1.y, x.w, fmaf(f1.x, d[3] * x.y, acc[3]));
                 }
             }
         }
         float(*part)[kRows][kTok + 1] =
             reinterpret_cast<float(*)[kRows][kTok + 1]>(smem + at.sums) + (team * 2 + (sl & 1)) * kTeamWarps;
 #pragma unroll
-        for (int c = 0; c < NT; ++c)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) part[tw][(e >> 1) * 8 + g][c * 8 + t * 2 + (e & 1)] = acc[c][e];
+        for (int e = 0; e < 4; ++e) part[tw][(e >> 1) * 8 + g][t * 2 + (e & 1)] = acc[e];
         named_sync(1 + team, kTeamWarps * 32);   // (the slab after the next waits here before it writes to this part again)
-        const int row = (slab0 + sl * slab_step) * kRows + (lane & 15);
+        const int row = (slab0 + sl * slab_step) * kRows + (lane & 15), c = tw * 2 + (lane >> 4);
+        if (row < p.n && c < tokens) {
+            float y = 0.f;
 #pragma unroll
-        for (int h = 0; h < (NT + 1) / 2; ++h) {
-            const int c = h * 16 + tw * 2 + (lane >> 4);
-            if (row < p.n && c < tokens) {
-                float y = 0.f;
-#pragma unroll
-                for (int w = 0; w < kTeamWarps; ++w) y += part[w][lane & 15][c];
-                if (p.bias) y += to_float(static_cast<const T *>(p.bias)[row]);
-                if (p.add) y += to_float(static_cast<const T *>(p.add)[(tok0 + c) * p.add_stride + row]);
-                static_cast<T *>(p.y)[(tok0 + c) * p.y_stride + row] = from_float<T>(y);
-            }
+            for (int w = 0; w < kTeamWarps; ++w) y += part[w][lane & 15][c];
+            if (p.bias) y += to_float(static_cast<const T *>(p.bias)[row]);
+            if (p.add) y += to_float(static_cast<const T *>(p.add)[(tok0 + c) * p.add_stride + row]);
+            static_cast<T *>(p.y)[(tok0 + c) * p.y_stride + row] = from_float<T>(y);
         }
     }
     copy_wait<0>();
 }
 
 // Units of a warp's ring with which the few-tokens kernel fits into shared memory, or 0
-template <int NT>
 int depth_of(int k, int groups, int tokens) {
     for (int depth = 4; depth >= 3; --depth)
-        if (FewLayout<NT>(k, groups, tokens, depth).total <= kMostShared) return depth;
+        if (FewLayout(k, groups, tokens < kTok ? tokens : kTok, depth).total <= kMostShared) return depth;
     return 0;
 }
-// The few-tokens kernel takes up to 16, as twice 8 where they are more (the second reads the codes from L2), if 8 of them fit
-// into shared memory.  Measured against the kernel for many, columns from memory, 3 584 of them: 8 tokens, 4 608 rows 8.3 us
-// against 14.9, 28 672 rows 22 against 44, 151 001 rows 85 against 184; 16 tokens, twice as long against the same; at 32 the
-// other is ahead everywhere.
-bool is_few(int k, int groups, int tokens) { return tokens <= 16 && depth_of<1>(k, groups, tokens < 8 ? tokens : 8) > 0; }
+// The few-tokens kernel takes up to 16, as twice 8 where they are more (the second reads the codes from L2), if they fit into
+// shared memory.  Measured against the kernel for many, codes from memory, 3 584 columns, us: 8 tokens of 512 rows 6.6 against
+// 12.1, of 4 608 rows 8.3 against 14.9, of 28 672 rows 22 against 44, of 151 001 rows 85 against 184; 16 tokens of 4 608 rows
+// 15.7 against 15.2, of 28 672 rows 41 against 45, of 151 001 rows 160 against 185.  A third pass would lose: 24 tokens are
+// three times the time of 8, and the other kernel takes 14.9, 42 and 174 us for 32.
+bool is_few(int k, int groups, int tokens) { return tokens <= 2 * kTok && depth_of(k, groups, tokens) > 0; }
 
-template <typename T, int GROUP, int NT, int DEPTH>
+template <typename T, int GROUP, int DEPTH>
 cudaError_t launch_few(const W4Params &p, int sms, cudaStream_t s) {
-    const int tokens = p.tokens < 8 * NT ? p.tokens : 8 * NT;
-    const FewLayout<NT> l(p.k, p.groups, tokens, DEPTH);
+    const int tokens = p.tokens < kTok ? p.tokens : kTok;
+    const FewLayout l(p.k, p.groups, tokens, DEPTH);
     static std::atomic<uint64_t> allowed{0};
-    const cudaError_t e = allow_shared(reinterpret_cast<const void *>(w4_few_kernel<T, GROUP, NT, DEPTH>), kMostShared, allowed);
+    const cudaError_t e = allow_shared(reinterpret_cast<const void *>(w4_few_kernel<T, GROUP, DEPTH>), kMostShared, allowed);
     if (e != cudaSuccess) return e;
     const int slabs = (p.n + kRows - 1) / kRows;
-    return launch_after_producer(w4_few_kernel<T, GROUP, NT, DEPTH>, dim3(slabs < sms ? slabs : sms, (p.tokens + tokens - 1) / tokens), dim3(kThreads), (size_t)l.total, s, p);
+    const dim3 grid(slabs < sms ? slabs : sms, (p.tokens + tokens - 1) / tokens);
+    return launch_after_producer(w4_few_kernel<T, GROUP, DEPTH>, grid, dim3(kThreads), (size_t)l.total, s, p);
 }
 
 template <typename T, int GROUP>
 cudaError_t by_tokens(const W4Params &p, int sms, void *workspace, cudaStream_t s) {
     if (!is_few(p.k, p.groups, p.tokens)) return w4_many<T>(p, GROUP, sms, workspace, s);
-    return depth_of<1>(p.k, p.groups, p.tokens < 8 ? p.tokens : 8) == 4 ? launch_few<T, GROUP, 1, 4>(p, sms, s) : launch_few<T, GROUP, 1, 3>(p, sms, s);
+    return depth_of(p.k, p.groups, p.tokens) == 4 ? launch_few<T, GROUP, 4>(p, sms, s) : launch_few<T, GROUP, 3>(p, sms, s);
 }
 
 template <typename T>

@@ -421,7 +421,7 @@ cudaError_t launch(ManyParams &p, int sms, cudaStream_t s) {
     p.blocks = (int32_t)((p.total + p.per - 1) / p.per);
     static std::atomic<uint64_t> allowed{0};
     cudaError_t e = allow_shared(reinterpret_cast<const void *>(w4_many_kernel<T, GROUP, N>), Many<GROUP, N>::kSmem, allowed);
-    const int warps = tiles * N * ((p.stages + 1) / 2);
+    const int warps = tiles * N * ((p.stages + 1) / 2);   // (fewer than 2^31: the workspace has 512 bytes for each)
     if (e == cudaSuccess) e = launch_after_producer(w4_tokens_kernel<T, GROUP, N>, dim3((warps + 7) / 8), dim3(256), 0, s, p);
     if (e == cudaSuccess)
         e = launch_after_producer(w4_many_kernel<T, GROUP, N>, dim3(p.blocks), dim3(kThreads), Many<GROUP, N>::kSmem, s, p);

@@ -56,6 +56,12 @@ def test_tree_refuses_more_sequences_or_longer_rows_than_it_counts(oqm):  # noqa
     assert tree(oqm, seqs=long) == -2 and accept(oqm, seqs=long) == -2
 
 
+def test_tree_refuses_rows_whose_last_tile_would_pass_32_bits(oqm):  # noqa: F811
+    """Token numbers of a tile are 32 bits wide, also behind a row's end."""
+    pages = (2 ** 31 - 64) // pool_of(oqm).page_tokens
+    assert tree(oqm, seqs=seqs_of(oqm, n_seqs=1, max_pages=pages, table_stride=pages)) == -2
+
+
 def test_calls_of_nothing_need_no_arrays(oqm):  # noqa: F811
     none = seqs_of(oqm, table=None, len=None, n_seqs=0)
     assert tree(oqm, seqs=none, n=0, first=None, parent=None, q=None, out=None) == 0
