@@ -602,17 +602,18 @@ __global__ void __launch_bounds__(kThreads, 1) kv_tree_kernel(const __grid_const
                     if (falls)
 #pragma unroll
                         for (int i = 0; i < 64; ++i) x[i] = -x[i];
-                    if (masked)
+                    if (masked) {
+                        const uint32_t low = ch ? there[kTok / 32 - 2] : there[0], high = ch ? there[kTok / 32 - 1] : there[1];
 #pragma unroll
-                        for (int i = 0; i < 64; ++i) x[i] = there[ch * 2 + (i >> 5)] >> (i & 31) & 1u ? x[i] : -INFINITY;
+                        for (int i = 0; i < 64; ++i) x[i] = (i < 32 ? low : high) >> (i & 31) & 1u ? x[i] : -INFINITY;
+                    }
                 };
                 float top = -INFINITY;
                 if (some) {
 #pragma unroll 1
                     for (int ch = 0; ch < kTok / 64; ++ch) {
                         float x[64];
-                        if (kTok > 64 && ch) load_scores(1, x);
-                        else load_scores(0, x);
+                        load_scores(ch, x);
                         float tops[4] = {x[0], x[1], x[2], x[3]};
 #pragma unroll
                         for (int i = 4; i < 64; ++i) tops[i & 3] = fmaxf(tops[i & 3], x[i]);
@@ -677,8 +678,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_tree_kernel(const __grid_const
 #pragma unroll 1
                     for (int ch = 0; ch < kTok / 64; ++ch) {
                         float x[64];
-                        if (kTok > 64 && ch) load_scores(1, x);
-                        else load_scores(0, x);
+                        load_scores(ch, x);
                         if (!all_fused) {
 #pragma unroll
                             for (int i = 0; i < 64; ++i)
