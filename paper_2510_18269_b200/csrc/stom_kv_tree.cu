@@ -171,7 +171,7 @@ __device__ __forceinline__ uint32_t not_finite(uint32_t w) {
     return ((w & 0x7fff7fffu) + (std::is_same<T, __nv_bfloat16>::value ? 0x00800080u : 0x04000400u)) & 0x80008000u;
 }
 
-template <typename T, int D>
+template <typename T, int D, bool CAP>
 __global__ void __launch_bounds__(kThreads, 1) kv_tree_kernel(const __grid_constant__ KvTreeParams p) {
     using S = Shape<D>;
     constexpr int kTok = S::kTok, kHalf = S::kHalf, kBlock = S::kBlock, kSlots = S::kSlots, kQBufs = S::kQBufs;
@@ -522,7 +522,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_tree_kernel(const __grid_const
         const int quarter = warp & 3, group = warp >> 2, row = quarter * 32 + lane;
         const uint32_t lane_base = tmem + ((uint32_t)(32 * quarter) << 16), o_at = lane_base;
         const float log2e = 1.4426950408889634f;
-        const float s1 = p.cap > 0.f ? p.scale / p.cap : p.scale * log2e, s2 = p.cap * log2e;
+        const float s1 = CAP ? p.scale / p.cap : p.scale * log2e, s2 = p.cap * log2e;
         // A wait that fails (the block has given up) is not a reason to leave the others alone at a barrier: the unit goes on
         // with what is there, and all leave together where the next one begins.
         auto wait_on = [&](const uint64_t &b, uint32_t parity) {
@@ -532,8 +532,8 @@ __global__ void __launch_bounds__(kThreads, 1) kv_tree_kernel(const __grid_const
         };
         // Without a cap and with a positive scale the scores stay unscaled until the exponent, where scaling and the step to
         // the reference are one multiply-add.
-        const bool plain = !(p.cap > 0.f) && s1 > 0.f, falls = s1 < 0.f;
-        auto scaled = [&](float x) { return p.cap > 0.f ? s2 * tanhf(x * s1) : x * s1; };
+        const bool plain = !CAP && s1 > 0.f, falls = s1 < 0.f;   // falls: load_scores gives them with the other sign
+        const float s1_abs = fabsf(s1);
         uint32_t c = 0;
         int paths_of_seq = -1, paths_of_row = -1, depth = 0;   // whose paths are in shared memory
         for (uint32_t unit = 0; c < n_tiles; ++unit) {
@@ -619,7 +619,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_tree_kernel(const __grid_const
                         for (int i = 4; i < 64; ++i) tops[i & 3] = fmaxf(tops[i & 3], x[i]);
                         top = fmaxf(top, fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])));
                     }
-                    if (top > -INFINITY) top = scaled(falls ? -top : top);
+                    if (top > -INFINITY) top = CAP ? s2 * tanhf(top * s1_abs) : top * s1_abs;
                 }
                 // values that are no numbers, in tiles where rows differ in what they see
                 bool dirty = false;
@@ -679,10 +679,16 @@ __global__ void __launch_bounds__(kThreads, 1) kv_tree_kernel(const __grid_const
                     for (int ch = 0; ch < kTok / 64; ++ch) {
                         float x[64];
                         load_scores(ch, x);
-                        if (!all_fused) {
+                        // (without branches of their own: 64 of those took 5.5 us a tile)
+                        if constexpr (CAP) {
 #pragma unroll
-                            for (int i = 0; i < 64; ++i)
-                                if (!fused && x[i] > -INFINITY) x[i] = scaled(falls ? -x[i] : x[i]);
+                            for (int i = 0; i < 64; ++i) {
+                                const float y = s2 * tanhf(x[i] * s1_abs);
+                                x[i] = x[i] > -INFINITY ? y : x[i];
+                            }
+                        } else if (!all_fused) {   // (with a cap in a kernel of its own, whose code the others' would have to pass)
+#pragma unroll
+                            for (int i = 0; i < 64; ++i) x[i] = !fused && x[i] > -INFINITY ? x[i] * s1_abs : x[i];
                         }
                         uint32_t w[32];
 #pragma unroll
@@ -962,12 +968,12 @@ int64_t part_rows(int32_t n_tokens, int32_t group) {
     return rows < kRows ? rows : kRows;
 }
 
-template <typename T, int D>
-int32_t launch(const KvTreeParams &p, int sms, cudaStream_t stream) {
+template <typename T, int D, bool CAP>
+int32_t launch_kernels(const KvTreeParams &p, int sms, cudaStream_t stream) {
     static std::atomic<uint64_t> allowed{0};
-    cudaError_t e = allow_shared(reinterpret_cast<const void *>(kv_tree_kernel<T, D>), Shape<D>::kSmem, allowed);
+    cudaError_t e = allow_shared(reinterpret_cast<const void *>(kv_tree_kernel<T, D, CAP>), Shape<D>::kSmem, allowed);
     if (e == cudaSuccess)
-        e = launch_after_producer(kv_tree_kernel<T, D>, dim3(sms), dim3(kThreads), Shape<D>::kSmem, stream, p);
+        e = launch_after_producer(kv_tree_kernel<T, D, CAP>, dim3(sms), dim3(kThreads), Shape<D>::kSmem, stream, p);
     if (e == cudaSuccess)
         e = launch_after_producer(kv_tree_join_kernel<T, D>, dim3(sms * 4), dim3(256), 0, stream, p);
     if (e != cudaSuccess) {
@@ -975,6 +981,11 @@ int32_t launch(const KvTreeParams &p, int sms, cudaStream_t stream) {
         return STOM_ERR_CUDA;
     }
     return finish_launch();
+}
+
+template <typename T, int D>
+int32_t launch(const KvTreeParams &p, int sms, cudaStream_t s) {
+    return p.cap > 0.f ? launch_kernels<T, D, true>(p, sms, s) : launch_kernels<T, D, false>(p, sms, s);
 }
 
 template <typename T>
