@@ -1,5 +1,6 @@
 """Thin Python binding of libstom_oqm.so (argument marshalling only): ctypes, and for the calls of the paged cache, the
-next token and the 4-bit products, which are made once per token, _stom_bind.so (written against torch's C++ tensors; only those calls need it).
+next token and the 4-bit products, which are made once per token, _stom_bind.so (written against torch's C++ tensors; only
+those calls need it).
 
 Every step of the path runs in the library's CUDA kernels; PyTorch is used for
 device memory and streams.  There is no CPU fallback: if the library is not

@@ -2,15 +2,13 @@
 
 Tolerance of y, element by element, with u the type's half step (2^-8 bf16, 2^-11 fp16) and k columns:
     u |y|                                  the one rounding of the result
-  + 2^-24 * sum over groups of             binary32 sums within a group (D of sum (1 + c/16) x and X of sum x: at most 128
-      (160 s M + 130 |z'| M), M = sum|x|    additions each, every one off by 2^-24 of at most 2 M resp. M; then 16 s D and
-                                            (z - 16 s) X, z' = z - 16 s rounded once) -- errors of a sum are bounded by the
-                                            number of its additions; 16 s * 2 M * (128 + 2) = 4160 s M is the worst case,
-                                            which random signs never come near: a root of it, sqrt(128) ~ 11.3 for the
-                                            additions, times 16 * 2 is 362, taken with a factor 2: 724
-  + 2^-24 * sqrt(groups) * 4 * |terms|     the sum over groups and the four to eight warps' parts
-  + 2^-24 (fp16)                           where the result is subnormal
-The bound below takes 2^-24 * 1000 * sum_g M_g (16 s + |z|) / 16 for all of it: products are exact."""
+  + 2^-24 * 1000 * sum over groups of M_g (16 s + |z|) / 16, M_g = sum of the group's |x|
+                                           the sums of a group: products of codes and tokens are exact; sums of codes times
+                                            x, at most 15 M, and of x, at most M, are off by 2^-24 of their size for each of at
+                                            most 128 additions.  The worst case, 130 * (15 s + |z|) M, is twice the bound;
+                                            random signs come nowhere near it (a root: sqrt(128) ~ 11.3 for 128 additions)
+  + 2^-23 |y|                              the sums over groups and over warps
+  + 2^-24 (fp16)                           where the result is subnormal"""
 import numpy as np
 import pytest
 import torch
