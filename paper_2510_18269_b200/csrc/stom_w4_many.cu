@@ -92,7 +92,10 @@ template <int GROUP, int N>
 struct Many {
     static constexpr int kGroups = kStageCols / GROUP;         // of a stage
     static constexpr int kBStage = (stage_bytes(GROUP, N) + 1023) / 1024 * 1024;
-    static constexpr int kMeta = kChunkCols / GROUP * kRows * 8;
+    // scales and offsets of a chunk's groups as pairs, a row of kRows for each group and kMetaPad more, with which the pairs that
+    // half a warp stores (of adjacent groups and rows) lie in banks of their own
+    static constexpr int kChunkGroups = kChunkCols / GROUP, kMetaPad = 16 / kChunkGroups, kMetaRow = kRows + kMetaPad;
+    static constexpr int kMeta = kChunkGroups * kMetaRow * 8;
     // stages of the left operand and of accumulators: three where they fit into shared and tensor memory
     static constexpr int kBufs = 3 * kGroups * N <= 512 ? 3 : 2, kChunks = kBufs == 3 && N == 64 ? 3 : 4;
     static constexpr int kCols = kBufs * kGroups * N <= 64 ? 64 : kBufs * kGroups * N <= 128 ? 128 : kBufs * kGroups * N <= 256 ? 256 : 512;
@@ -289,28 +292,30 @@ __global__ void __launch_bounds__(kThreads, 1) w4_many_kernel(const __grid_const
     } else {
         // ---- folding.  Scales of a chunk's groups go to shared memory as pairs; a thread brings kPairs of them, a chunk ahead in
         // registers, into one of three buffers (the one before the last may still be read).
-        constexpr int kChunkGroups = kChunkCols / GROUP, kPairs = kChunkGroups * kRows / kFoldThreads;
-        const bool wide = p.w.meta_dtype == STOM_FP32, narrow_bf = p.w.meta_dtype == STOM_BF16;
+        constexpr int kChunkGroups = S::kChunkGroups, kPairs = kChunkGroups * kRows / kFoldThreads, kPairRows = kFoldThreads / kChunkGroups;
+        const bool wide = p.w.meta_dtype == STOM_FP32, half = p.w.meta_dtype == STOM_FP16, offsets = p.w.zero != nullptr;
+        const void *zero = offsets ? p.w.zero : p.w.scale;
         const int ft = tid - kUnpackThreads, r0 = ft / kChunkGroups, q0 = ft % kChunkGroups;   // of a thread's first pair
         uint32_t rs[kPairs], rz[kPairs];
         auto load_meta = [&](const Part &part, int s) {
             const int gr = (part.first + s) * kGroups + q0;
+            const bool is = gr < p.w.groups;
+            int64_t at[kPairs];
 #pragma unroll
-            for (int i = 0; i < kPairs; ++i) {
-                rs[i] = rz[i] = 0;
-                if (gr >= p.w.groups) continue;
-                const int64_t at = min(part.row0 + r0 + i * (kFoldThreads / kChunkGroups), p.w.n - 1) * p.w.meta_stride + gr;
-                if (wide) {
-                    rs[i] = __ldg(static_cast<const uint32_t *>(p.w.scale) + at);
-                    if (p.w.zero) rz[i] = __ldg(static_cast<const uint32_t *>(p.w.zero) + at);
-                } else {
-                    rs[i] = __ldg(static_cast<const uint16_t *>(p.w.scale) + at);
-                    if (p.w.zero) rz[i] = __ldg(static_cast<const uint16_t *>(p.w.zero) + at);
+            for (int i = 0; i < kPairs; ++i) at[i] = min(part.row0 + r0 + i * kPairRows, p.w.n - 1) * p.w.meta_stride + gr;
+            if (wide) {
+#pragma unroll
+                for (int i = 0; i < kPairs; ++i) {
+                    rs[i] = is ? __ldg(static_cast<const uint32_t *>(p.w.scale) + at[i]) : 0u;
+                    rz[i] = is ? __ldg(static_cast<const uint32_t *>(zero) + at[i]) : 0u;
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < kPairs; ++i) {
+                    rs[i] = is ? __ldg(static_cast<const uint16_t *>(p.w.scale) + at[i]) : 0u;
+                    rz[i] = is ? __ldg(static_cast<const uint16_t *>(zero) + at[i]) : 0u;
                 }
             }
-        };
-        auto number = [&](uint32_t bits) {
-            return wide ? __uint_as_float(bits) : narrow_bf ? __uint_as_float(bits << 16) : __half2float(__ushort_as_half((unsigned short)bits));
         };
         Ring a, b;
         int m_slot = 0;
@@ -325,12 +330,20 @@ __global__ void __launch_bounds__(kThreads, 1) w4_many_kernel(const __grid_const
             for (int i = 0; i < kOwn / 2; ++i) acc[i] = 0;
             for (int s = 0; s < part.n; ++s) {
                 if (!(s & 1)) {
-                    float2 *meta = reinterpret_cast<float2 *>(smem + S::kOffMeta + m_slot * S::kMeta) + q0 * kRows + r0;
+                    float2 *meta = reinterpret_cast<float2 *>(smem + S::kOffMeta + m_slot * S::kMeta) + q0 * S::kMetaRow + r0;
+                    float2 v[kPairs];
+                    if (half) {
 #pragma unroll
-                    for (int i = 0; i < kPairs; ++i) {
-                        const float scale = number(rs[i]);
-                        meta[i * (kFoldThreads / kChunkGroups)] = make_float2(kCodeUnit * scale, p.w.zero ? number(rz[i]) : -8.f * scale);
+                        for (int i = 0; i < kPairs; ++i)
+                            v[i] = make_float2(__half2float(__ushort_as_half((unsigned short)rs[i])), __half2float(__ushort_as_half((unsigned short)rz[i])));
+                    } else {
+                        const int up = wide ? 0 : 16;
+#pragma unroll
+                        for (int i = 0; i < kPairs; ++i) v[i] = make_float2(__uint_as_float(rs[i] << up), __uint_as_float(rz[i] << up));
                     }
+#pragma unroll
+                    for (int i = 0; i < kPairs; ++i)
+                        meta[i * kPairRows] = make_float2(kCodeUnit * v[i].x, offsets ? v[i].y : -8.f * v[i].x);
                     if (s + 2 < part.n) load_meta(part, s + 2);
                     else if (at < end) load_meta(next, 0);
                     named_sync(1, kFoldThreads);
@@ -339,7 +352,7 @@ __global__ void __launch_bounds__(kThreads, 1) w4_many_kernel(const __grid_const
                 wait(done[a.slot], a.round);   // (a wait that has failed: what is there is used, and the call flagged)
                 __syncwarp();
                 tc_fence_after_sync();
-                const float2 *meta = reinterpret_cast<const float2 *>(smem + S::kOffMeta + m_slot * S::kMeta) + (s & 1) * kGroups * kRows + row;
+                const float2 *meta = reinterpret_cast<const float2 *>(smem + S::kOffMeta + m_slot * S::kMeta) + (s & 1) * kGroups * S::kMetaRow + row;
                 const ulonglong2 *fx = reinterpret_cast<const ulonglong2 *>(smem + S::kOffB + b.slot * kBStage + N * kStageCols * 2 + side * kOwn * 4);
 #pragma unroll
                 for (int q = 0; q < kGroups; ++q) {
@@ -349,7 +362,7 @@ __global__ void __launch_bounds__(kThreads, 1) w4_many_kernel(const __grid_const
                         tc_fence_before_sync();
                         mbar_arrive(smem_u32(&folded[a.slot]));
                     }
-                    const float2 f = meta[q * kRows];
+                    const float2 f = meta[q * S::kMetaRow];
                     const uint64_t fs = pair_of(f.x, f.x), fz = pair_of(f.y, f.y);
 #pragma unroll
                     for (int i = 0; i < kOwn; i += 4) {
