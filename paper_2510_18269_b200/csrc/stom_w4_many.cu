@@ -31,7 +31,8 @@ constexpr int kUnpackWarps = 8, kFoldWarps = 8, kWorkWarps = kUnpackWarps + kFol
 constexpr int kUnpackThreads = kUnpackWarps * 32, kFoldThreads = kFoldWarps * 32, kThreads = (kWorkWarps + 4) * 32;
 constexpr int kChunkCols = 256;                           // columns of a copy
 constexpr int kPitch = kChunkCols / 2 + 16, kChunkBytes = kRows * kPitch;   // an odd number of 16 bytes: a row a thread without conflicts
-constexpr int kAStage = kRows * kStageCols * 2, kBStages = 3;
+constexpr int kAStage = kRows * kStageCols * 2, kMostBStages = 6;
+constexpr int kMostShared = 226 * 1024;                   // dynamic shared memory of a block
 constexpr int kMaxBlocks = 256;                            // blocks of the grid the workspace has room for
 constexpr unsigned long long kWaitLimitNs = 1000000000ull;   // a wait that has taken 1 s ends the block
 
@@ -97,11 +98,15 @@ struct Many {
     static constexpr int kChunkGroups = kChunkCols / GROUP, kMetaPad = 16 / kChunkGroups, kMetaRow = kRows + kMetaPad;
     static constexpr int kMeta = kChunkGroups * kMetaRow * 8;
     // stages of the left operand and of accumulators: three where they fit into shared and tensor memory
-    static constexpr int kBufs = 3 * kGroups * N <= 512 ? 3 : 2, kChunks = kBufs == 3 && N == 64 ? 3 : 4;
+    static constexpr int kBufs = 3 * kGroups * N <= 512 ? 3 : 2, kChunks = N == 64 ? 3 : 4;
     static constexpr int kCols = kBufs * kGroups * N <= 64 ? 64 : kBufs * kGroups * N <= 128 ? 128 : kBufs * kGroups * N <= 256 ? 256 : 512;
+    static constexpr int kFixed = 1024 + kBufs * kAStage + kChunks * kChunkBytes + 3 * kMeta;
+    // of the right operand as many as fit: they are given back only when the sums have been folded, and come again from L2 (64
+    // tokens, groups of 128: BSTFIG)
+    static constexpr int kFit = (kMostShared - kFixed) / kBStage, kBStages = kFit < kMostBStages ? kFit : kMostBStages;
     static constexpr int kOffB = kBufs * kAStage, kOffCodes = kOffB + kBStages * kBStage, kOffMeta = kOffCodes + kChunks * kChunkBytes;
-    static constexpr int kSmem = 1024 + kOffMeta + 3 * kMeta;
-    static_assert(kSmem <= 226 * 1024, "room");
+    static constexpr int kSmem = kFixed + kBStages * kBStage;
+    static_assert(kBStages >= 3 && kSmem <= kMostShared, "room");
 };
 
 // A part of a block's stretch: stages first ... first + n - 1 of a tile
@@ -142,7 +147,7 @@ template <typename T, int GROUP, int N>
 __global__ void __launch_bounds__(kThreads, 1) w4_many_kernel(const __grid_constant__ ManyParams p) {
     using S = Many<GROUP, N>;
     constexpr int kGroups = S::kGroups, kBStage = S::kBStage, kOwn = N / 2;   // tokens of a thread that folds
-    constexpr int kBufs = S::kBufs, kChunks = S::kChunks;
+    constexpr int kBufs = S::kBufs, kChunks = S::kChunks, kBStages = S::kBStages;
     extern __shared__ uint8_t raw_smem[];
     __shared__ uint64_t c_full[kChunks], c_empty[kChunks], b_full[kBStages], b_empty[kBStages], a_full[kBufs], done[kBufs],
         folded[kBufs], drained;
