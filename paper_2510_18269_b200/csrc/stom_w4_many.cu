@@ -31,7 +31,7 @@ constexpr int kUnpackWarps = 8, kFoldWarps = 8, kWorkWarps = kUnpackWarps + kFol
 constexpr int kUnpackThreads = kUnpackWarps * 32, kFoldThreads = kFoldWarps * 32, kThreads = (kWorkWarps + 4) * 32;
 constexpr int kChunkCols = 256;                           // columns of a copy
 constexpr int kPitch = kChunkCols / 2 + 16, kChunkBytes = kRows * kPitch;   // an odd number of 16 bytes: a row a thread without conflicts
-constexpr int kAStage = kRows * kStageCols * 2, kMostBStages = 6;
+constexpr int kAStage = kRows * kStageCols * 2, kLeftCols = kStageCols / 2, kMostBStages = 6;
 constexpr int kMostShared = 226 * 1024;                   // dynamic shared memory of a block
 constexpr int kMaxBlocks = 256;                            // blocks of the grid the workspace has room for
 constexpr unsigned long long kWaitLimitNs = 1000000000ull;   // a wait that has taken 1 s ends the block
@@ -97,14 +97,17 @@ struct Many {
     // half a warp stores (of adjacent groups and rows) lie in banks of their own
     static constexpr int kChunkGroups = kChunkCols / GROUP, kMetaPad = 16 / kChunkGroups, kMetaRow = kRows + kMetaPad;
     static constexpr int kMeta = kChunkGroups * kMetaRow * 8;
-    // stages of the left operand and of accumulators: three where they fit into shared and tensor memory
-    static constexpr int kBufs = 3 * kGroups * N <= 512 ? 3 : 2, kChunks = N == 64 ? 3 : 4;
-    static constexpr int kCols = kBufs * kGroups * N <= 64 ? 64 : kBufs * kGroups * N <= 128 ? 128 : kBufs * kGroups * N <= 256 ? 256 : 512;
-    static constexpr int kFixed = 1024 + kBufs * kAStage + kChunks * kChunkBytes + 3 * kMeta;
+    // the left operand, 64 columns a stage, lies in tensor memory beside the accumulators where it has room for two stages of both
+    static constexpr bool kLeftInTmem = 2 * (kGroups * N + kLeftCols) <= 512;
+    static constexpr int kStageTmem = kGroups * N + (kLeftInTmem ? kLeftCols : 0);
+    static constexpr int kBufs = 3 * kStageTmem <= 512 ? 3 : 2, kChunks = N == 64 && !kLeftInTmem ? 3 : 4;
+    static constexpr int kCols = kBufs * kStageTmem <= 256 ? 256 : 512;   // (a power of two of them; there is one block a multiprocessor)
+    static constexpr int kLeftAt = kBufs * kGroups * N, kLeftShared = kLeftInTmem ? 0 : kBufs * kAStage;
+    static constexpr int kFixed = 1024 + kLeftShared + kChunks * kChunkBytes + 3 * kMeta;
     // of the right operand as many as fit: they are given back only when the sums have been folded, and come again from L2 (64
     // tokens, groups of 128: BSTFIG)
     static constexpr int kFit = (kMostShared - kFixed) / kBStage, kBStages = kFit < kMostBStages ? kFit : kMostBStages;
-    static constexpr int kOffB = kBufs * kAStage, kOffCodes = kOffB + kBStages * kBStage, kOffMeta = kOffCodes + kChunks * kChunkBytes;
+    static constexpr int kOffB = kLeftShared, kOffCodes = kOffB + kBStages * kBStage, kOffMeta = kOffCodes + kChunks * kChunkBytes;
     static constexpr int kSmem = kFixed + kBStages * kBStage;
     static_assert(kBStages >= 3 && kSmem <= kMostShared, "room");
 };
@@ -245,11 +248,15 @@ __global__ void __launch_bounds__(kThreads, 1) w4_many_kernel(const __grid_const
                 if (!(wait(b_full[b.slot], b.round) && wait(a_full[a.slot], a.round) &&
                       (s < begin + kBufs || wait(folded[a.slot], a.round ^ 1u)))) break;
                 tc_fence_after_sync();
-                const uint32_t al = a_low + a.slot * (kAStage / 16), bl = b_low + b.slot * (kBStage / 16), to = tmem + a.slot * (kGroups * N);
+                const uint32_t al = a_low + a.slot * (kAStage / 16), bl = b_low + b.slot * (kBStage / 16), to = tmem + a.slot * (kGroups * N),
+                               at = tmem + S::kLeftAt + a.slot * kLeftCols;
 #pragma unroll
                 for (int ks = 0; ks < kStageCols / 16; ++ks)
-                    umma_ss_low(to + ks * 16 / GROUP * N, al + (ks >> 2) * (kRows * 8) + (ks & 3) * 2, bl + (ks >> 2) * (N * 8) + (ks & 3) * 2,
-                                idesc, ks * 16 % GROUP != 0);
+                    if constexpr (S::kLeftInTmem)
+                        umma_ts_low(to + ks * 16 / GROUP * N, at + ks * 8, bl + (ks >> 2) * (N * 8) + (ks & 3) * 2, idesc, ks * 16 % GROUP != 0);
+                    else
+                        umma_ss_low(to + ks * 16 / GROUP * N, al + (ks >> 2) * (kRows * 8) + (ks & 3) * 2,
+                                    bl + (ks >> 2) * (N * 8) + (ks & 3) * 2, idesc, ks * 16 % GROUP != 0);
                 umma_commit(smem_u32(&done[a.slot]));
                 a.next(kBufs);
                 b.next(kBStages);
@@ -272,18 +279,28 @@ __global__ void __launch_bounds__(kThreads, 1) w4_many_kernel(const __grid_const
                 __syncwarp();
                 const uint8_t *src = from + c.slot * kChunkBytes + (s & 1) * 64;
                 uint8_t *dst = to + a.slot * kAStage;
-                const uint4 v[2] = {*reinterpret_cast<const uint4 *>(src), *reinterpret_cast<const uint4 *>(src + 16)};
+                uint32_t w[8], o[32];
+                *reinterpret_cast<uint4 *>(w) = *reinterpret_cast<const uint4 *>(src);
+                *reinterpret_cast<uint4 *>(w + 4) = *reinterpret_cast<const uint4 *>(src + 16);
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const uint32_t u = w[j] >> 8;
-                        *reinterpret_cast<uint4 *>(dst + (((i * 4 + j) ^ (row & 7)) << 4)) =
-                            make_uint4(w[j] & 0x000f000fu, w[j] & 0x00f000f0u, u & 0x000f000fu, u & 0x00f000f0u);
-                    }
+                for (int j = 0; j < 8; ++j) {
+                    const uint32_t u = w[j] >> 8;
+                    o[j * 4] = w[j] & 0x000f000fu;
+                    o[j * 4 + 1] = w[j] & 0x00f000f0u;
+                    o[j * 4 + 2] = u & 0x000f000fu;
+                    o[j * 4 + 3] = u & 0x00f000f0u;
                 }
-                fence_proxy_async();
+                if constexpr (S::kLeftInTmem) {
+                    tc_fence_after_sync();
+                    tmem_store(tmem + ((uint32_t)(32 * quarter) << 16) + S::kLeftAt + a.slot * kLeftCols + side * 32, o);
+                    tmem_wait_store();
+                    tc_fence_before_sync();
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        *reinterpret_cast<uint4 *>(dst + ((j ^ (row & 7)) << 4)) = make_uint4(o[j * 4], o[j * 4 + 1], o[j * 4 + 2], o[j * 4 + 3]);
+                    fence_proxy_async();
+                }
                 mbar_arrive(smem_u32(&a_full[a.slot]));
                 a.next(kBufs);
                 again |= a.slot == 0;
