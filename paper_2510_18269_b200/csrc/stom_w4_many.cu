@@ -152,8 +152,8 @@ __global__ void __launch_bounds__(kThreads, 1) w4_many_kernel(const __grid_const
     constexpr int kGroups = S::kGroups, kBStage = S::kBStage, kOwn = N / 2;   // tokens of a thread that folds
     constexpr int kBufs = S::kBufs, kChunks = S::kChunks, kBStages = S::kBStages;
     extern __shared__ uint8_t raw_smem[];
-    __shared__ uint64_t c_full[kChunks], c_empty[kChunks], b_full[kBStages], b_empty[kBStages], a_full[kBufs], done[kBufs],
-        folded[kBufs], drained;
+    // ready: a stage's left operand is there, and the accumulators' sums of the stage before in that place have been read
+    __shared__ uint64_t c_full[kChunks], c_empty[kChunks], b_full[kBStages], b_empty[kBStages], ready[kBufs], done[kBufs], drained;
     __shared__ uint32_t tmem_word, abort_word, never_word;   // never_word stays 0
     uint8_t *smem = raw_smem + ((1024u - (smem_u32(raw_smem) & 1023u)) & 1023u);   // the swizzle goes by addresses
     const uint32_t smem_at = smem_u32(smem);
@@ -164,9 +164,8 @@ __global__ void __launch_bounds__(kThreads, 1) w4_many_kernel(const __grid_const
         for (int i = 0; i < kChunks; ++i) mbar_init(smem_u32(&c_full[i]), 64), mbar_init(smem_u32(&c_empty[i]), kUnpackWarps);
         for (int i = 0; i < kBStages; ++i) mbar_init(smem_u32(&b_full[i]), 1), mbar_init(smem_u32(&b_empty[i]), kFoldWarps);
         for (int i = 0; i < kBufs; ++i) {
-            mbar_init(smem_u32(&a_full[i]), kUnpackThreads);
+            mbar_init(smem_u32(&ready[i]), kUnpackWarps + kFoldWarps);
             mbar_init(smem_u32(&done[i]), 1);
-            mbar_init(smem_u32(&folded[i]), kFoldThreads);
         }
         mbar_init(smem_u32(&drained), 1);
         abort_word = never_word = 0;
@@ -245,8 +244,7 @@ __global__ void __launch_bounds__(kThreads, 1) w4_many_kernel(const __grid_const
             const uint32_t idesc = umma_idesc(0, N), a_low = umma_low_k128(smem_at), b_low = umma_low_k128(smem_at + S::kOffB);
             Ring a, b;
             for (int64_t s = begin; s < end; ++s) {
-                if (!(wait(b_full[b.slot], b.round) && wait(a_full[a.slot], a.round) &&
-                      (s < begin + kBufs || wait(folded[a.slot], a.round ^ 1u)))) break;
+                if (!(wait(b_full[b.slot], b.round) && wait(ready[a.slot], a.round))) break;
                 tc_fence_after_sync();
                 const uint32_t al = a_low + a.slot * (kAStage / 16), bl = b_low + b.slot * (kBStage / 16), to = tmem + a.slot * (kGroups * N),
                                at = tmem + S::kLeftAt + a.slot * kLeftCols;
@@ -301,7 +299,8 @@ __global__ void __launch_bounds__(kThreads, 1) w4_many_kernel(const __grid_const
                         *reinterpret_cast<uint4 *>(dst + ((j ^ (row & 7)) << 4)) = make_uint4(o[j * 4], o[j * 4 + 1], o[j * 4 + 2], o[j * 4 + 3]);
                     fence_proxy_async();
                 }
-                mbar_arrive(smem_u32(&a_full[a.slot]));
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&ready[a.slot]));
                 a.next(kBufs);
                 again |= a.slot == 0;
                 if ((s & 1) || s + 1 == n) {
@@ -339,6 +338,8 @@ __global__ void __launch_bounds__(kThreads, 1) w4_many_kernel(const __grid_const
                 }
             }
         };
+        if (lane == 0)
+            for (int i = 0; i < kBufs; ++i) mbar_arrive(smem_u32(&ready[i]));   // no sums are there at first
         Ring a, b;
         int m_slot = 0;
         Part next = part_at(p, begin, end);
@@ -382,7 +383,8 @@ __global__ void __launch_bounds__(kThreads, 1) w4_many_kernel(const __grid_const
                     tmem_load(tmem + ((uint32_t)(32 * quarter) << 16) + (a.slot * kGroups + q) * N + side * kOwn, d);
                     if (q == kGroups - 1) {
                         tc_fence_before_sync();
-                        mbar_arrive(smem_u32(&folded[a.slot]));
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(smem_u32(&ready[a.slot]));
                     }
                     const float2 f = meta[q * S::kMetaRow];
                     const uint64_t fs = pair_of(f.x, f.x), fz = pair_of(f.y, f.y);
