@@ -238,12 +238,14 @@ int depth_of(int k, int groups, int tokens) {
         if (FewLayout(k, groups, tokens < kTok ? tokens : kTok, depth).total <= kMostShared) return depth;
     return 0;
 }
-// The few-tokens kernel takes up to 16, as twice 8 where they are more (the second reads the codes from L2), if they fit into
-// shared memory.  Measured against the kernel for many, codes from memory, 3 584 columns, us: 8 tokens of 512 rows 6.6 against
-// 12.1, of 4 608 rows 8.3 against 14.9, of 28 672 rows 22 against 44, of 151 001 rows 85 against 184; 16 tokens of 4 608 rows
-// 15.7 against 15.2, of 28 672 rows 41 against 45, of 151 001 rows 160 against 185.  A third pass would lose: 24 tokens are
-// three times the time of 8, and the other kernel takes 14.9, 42 and 174 us for 32.
-bool is_few(int k, int groups, int tokens) { return tokens <= 2 * kTok && depth_of(k, groups, tokens) > 0; }
+// The few-tokens kernel takes up to 8, if they fit into shared memory, and up to 16 as twice 8 where the matrix has so few rows
+// that the blocks of both have a multiprocessor each (74 of 148).  Measured against the kernel for many, codes from memory, 3 584
+// columns, us: 8 tokens of 512 rows 6.7 against 13.5, of 4 608 rows 8.3 against 13.8, of 28 672 rows 22 against 36, of 151 001
+// rows 82 against 139; 9 to 16 tokens of 512 rows 6.6 to 6.9 against 13, of 4 608 rows 12.6 to 15.6 against 13.9, of 28 672 rows
+// 38 to 41 against 36, of 151 001 rows 160 against 140.
+bool is_few(int n, int k, int groups, int tokens) {
+    return tokens <= (n <= 74 * kRows ? 2 * kTok : kTok) && depth_of(k, groups, tokens) > 0;
+}
 
 template <typename T, int GROUP, int DEPTH>
 cudaError_t launch_few(const W4Params &p, int sms, cudaStream_t s) {
@@ -259,7 +261,7 @@ cudaError_t launch_few(const W4Params &p, int sms, cudaStream_t s) {
 
 template <typename T, int GROUP>
 cudaError_t by_tokens(const W4Params &p, int sms, void *workspace, cudaStream_t s) {
-    if (!is_few(p.k, p.groups, p.tokens)) return w4_many<T>(p, GROUP, sms, workspace, s);
+    if (!is_few(p.n, p.k, p.groups, p.tokens)) return w4_many<T>(p, GROUP, sms, workspace, s);
     return depth_of(p.k, p.groups, p.tokens) == 4 ? launch_few<T, GROUP, 4>(p, sms, s) : launch_few<T, GROUP, 3>(p, sms, s);
 }
 
@@ -289,7 +291,7 @@ static int32_t check_matrix(const stom_w4_matrix *w, int32_t rows) {
 extern "C" int64_t stom_w4_workspace_bytes(const stom_w4_matrix *w, int32_t rows) {
     const int32_t rc = check_matrix(w, rows);
     if (rc) return rc;
-    return rows == 0 || is_few(w->k, w->k / w->group, rows) ? 0 : w4_many_workspace(w->k, w->group, rows);
+    return rows == 0 || is_few(w->n, w->k, w->k / w->group, rows) ? 0 : w4_many_workspace(w->k, w->group, rows);
 }
 
 extern "C" int32_t stom_w4_linear(const stom_w4_matrix *w, int32_t dtype, int32_t rows, const void *x, int64_t x_stride,

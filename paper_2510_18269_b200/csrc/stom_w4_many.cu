@@ -7,18 +7,21 @@
 //
 // A block has 128 rows of the matrix, N tokens and a part of the columns, a STAGE of 128 of them at a time.  Codes arrive by
 // 16-byte asynchronous copies, 256 columns at a time, several ahead.  Eight warps unpack: a thread has one row and half of a
-// stage's columns, 8 words that become 8 chunks of 16 bytes in the left operand (K-major, 128-byte swizzle; two stages of it).
-// One thread issues the products, each group into accumulators of its own in tensor memory, since scales differ from group to
-// group.  Eight more warps fold those of the stage before into sums while the products of this one run: a thread has a row
-// again, and half of the tokens.
+// stage's columns, 8 words that become 32 registers of the left operand, in tensor memory where the accumulators leave room for
+// it (all but 64 tokens with groups of 32: there in shared memory, K-major, 128-byte swizzle).  Shared memory's bandwidth is
+// then left to codes and tokens.  One thread issues the products, each group into accumulators of its own in tensor memory,
+// since scales differ from group to group.  Eight more warps fold those of the stage before into sums while the products of this
+// one run: a thread has a row again, and half of the tokens.
 //
 // Split.  The work is one line of stages, tile by tile (128 rows, N tokens), and every block, one a multiprocessor, takes an
 // equal, contiguous stretch of it.  The sums of a tile that is cut by a stretch's end go to the workspace, and a third small
 // kernel joins them.
 //
-// Measured on one B200, us: 64 tokens of 3 584 x 14 336 33 (0.2 PFLOP/s, 0.9 TB/s), 13 of 10 007 x 8 192 in groups of 32 46.  8 to 9
-// of them are the small kernels and launches; a stage takes 1 700 cycles at 64 tokens, of which the folding warps work 1 440, the
-// others 930.  Codes by the units of a row's 128 bytes as bulk copies: 58 cycles each, 7 400 a stage.
+// Measured on one B200, us: 64 tokens of 3 584 x 14 336 31 (0.2 PFLOP/s, 1 TB/s), 13 of 10 007 x 8 192 in groups of 32 38.  8 to 9
+// of them are the small kernels and launches.  A stage takes about 1 400 cycles, which the issuing thread (1 200) and the folding
+// warps (1 400: 700 of them the sums, 80 their way out of tensor memory, the rest waits and scales) share.  The left operand in
+// shared memory: 33 and 43 us; sixteen folding warps: 31.6 and 38.4.  Codes as bulk copies of a row's 128 bytes: 58 cycles each,
+// 7 400 a stage.
 #include "stom_tensor.cuh"
 #include "stom_w4.cuh"
 
@@ -104,8 +107,8 @@ struct Many {
     static constexpr int kCols = kBufs * kStageTmem <= 256 ? 256 : 512;   // (a power of two of them; there is one block a multiprocessor)
     static constexpr int kLeftAt = kBufs * kGroups * N, kLeftShared = kLeftInTmem ? 0 : kBufs * kAStage;
     static constexpr int kFixed = 1024 + kLeftShared + kChunks * kChunkBytes + 3 * kMeta;
-    // of the right operand as many as fit: they are given back only when the sums have been folded, and come again from L2 (64
-    // tokens, groups of 128: BSTFIG)
+    // of the right operand as many as fit: they are given back only when the sums have been folded, and come again from L2 (13 tokens,
+    // 8 192 columns, groups of 32: 42.7 us instead of 43.4 with three)
     static constexpr int kFit = (kMostShared - kFixed) / kBStage, kBStages = kFit < kMostBStages ? kFit : kMostBStages;
     static constexpr int kOffB = kLeftShared, kOffCodes = kOffB + kBStages * kBStage, kOffMeta = kOffCodes + kChunks * kChunkBytes;
     static constexpr int kSmem = kFixed + kBStages * kBStage;
