@@ -129,6 +129,14 @@ def test_windows_and_caps(kind, window, cap, d, dtype):
     _check(s, *_call(s, cap=cap, window=window), cap=cap, window=window)
 
 
+@pytest.mark.parametrize("cap", [0.0, 4.0, 30.0])
+@pytest.mark.parametrize("scale,d,dtype", [(-0.09, 128, BF), (0.2, 64, HF), (1e-20, 256, HF), (-0.06, 256, BF)])
+def test_scales_of_either_sign(scale, cap, d, dtype):
+    s = _make([250, 0, 130, 3], [20, 9, 1, 40], 8, 2, d, 16, dtype, "tree", seed=d)
+    for window in (0, 40):
+        _check(s, *_call(s, scale=scale, cap=cap, window=window), scale=scale, cap=cap, window=window)
+
+
 def test_a_chain_without_parents_equals_one_with():
     s = _make([777, 5], [30, 100], 8, 2, 128, 16, BF, "path")
     a = _call(s)

@@ -93,6 +93,13 @@ def test_sizes(n, k, group, rows):
     _check(s, _call(s))
 
 
+@pytest.mark.parametrize("n", [1184, 1185])
+@pytest.mark.parametrize("rows", [8, 9, 16, 17])
+def test_where_one_kernel_takes_over_from_the_other(n, rows):
+    s = _make(rows, n, 1152, 64, seed=rows)
+    _check(s, _call(s))
+
+
 @pytest.mark.parametrize("rows", [1, 12, 50, 130])
 def test_with_and_without_bias_and_addend(rows):
     s = _make(rows, 77, 512, 64)
