@@ -11,10 +11,11 @@
 // tokens agree: lane (g, t) of a fragment takes the t-th word (8 codes) of a row's 32 columns, two products' worth.  All of
 // a product's columns lie in one group.
 //
-// Measured on one B200, us: one token of 4 608 x 3 584 5.0, of 28 672 x 3 584 23 (2.5 of 6.5 TB/s), five of 151 001 x 3 584 83
-// (3.5 TB/s).  What bounds it now is the issue of instructions, 104 a warp for 1 024 weights (a scheduler issues every second
-// cycle; the tensor cores are busy for a fifth of the time).  A ring of its own for every warp took one token from 74 to 30 us;
-// codes as subnormal numbers instead of unpacked ones, with offsets, five tokens' logits from 93 to 84.
+// Measured on one B200, us: one token of 4 608 x 3 584 5.0, of 28 672 x 3 584 in groups of 64 21 (2.7 of 6.5 TB/s), five of
+// 151 001 x 3 584 69 (4.2 TB/s).  What bounds it now is the issue of instructions, 120 that read, unpack and multiply for 4 096
+// weights and about as many for copies, scales and folding.  A ring of its own for every warp took one token from 74 to 30 us;
+// codes as subnormal numbers instead of unpacked ones, with offsets, five tokens' logits from 93 to 84; smaller teams from 84
+// to 69.
 #include "stom_w4.cuh"
 
 namespace stom {
@@ -23,7 +24,7 @@ namespace {
 
 constexpr int kRows = 16;     // of the matrix, per slab
 constexpr int kTok = 8;       // most tokens of a block
-constexpr int kTeams = 2, kTeamWarps = 8, kWarps = kTeams * kTeamWarps, kThreads = kWarps * 32;   // of a block
+constexpr int kWarps = 16, kThreads = kWarps * 32;   // of a block
 constexpr int kUnitCols = 256;                // columns of a unit
 constexpr int kPitch = kUnitCols / 2 + 16;    // bytes from row to row in shared memory: 8 rows' words of 4 lanes lie in 32 banks
 constexpr int kUnitBytes = kRows * kPitch;
@@ -45,20 +46,21 @@ struct FewLayout {
         const int64_t units = (k + kUnitCols - 1) / kUnitCols, group = k / groups;   // (columns behind the last: zeros)
         factor = units * (kUnitCols / 32) * tokens * 64;
         sums = factor + units * (kUnitCols / group) * kTok * 8;
-        rings = sums + kTeams * 2 * kTeamWarps * kRows * (kTok + 1) * 4;
+        rings = sums + 2 * kWarps * kRows * (kTok + 1) * 4;
         total = rings + kWarps * depth * kUnitBytes;
     }
 };
 
 // Up to 8 tokens of those from 8 * blockIdx.y on; GROUP columns a group; a ring of DEPTH units.
-// A block, one a multiprocessor, has two teams of eight warps.  A team goes through slabs of 16 rows, whose UNITS of 256
+// A block, one a multiprocessor, has TEAMS teams of warps, sixteen together.  A team goes through slabs of 16 rows, whose UNITS of 256
 // columns its warps take in turn (and go on in turn with the next slab's, so that none has more of them).  A warp is alone
 // with its units: its own ring in shared memory, filled by 16-byte asynchronous copies DEPTH - 1 units ahead, the rows' scales
 // a unit ahead in registers.  At a slab's end the warps' sums are joined in shared memory, with one barrier of the team.
 // Tokens stay in shared memory, in the order of the fragments.
-template <typename T, int GROUP, int DEPTH>
+template <typename T, int GROUP, int DEPTH, int TEAMS>
 __global__ void __launch_bounds__(kThreads, 1) w4_few_kernel(const __grid_constant__ W4Params p) {
     constexpr int kGroups = kUnitCols / GROUP;   // of a unit
+    constexpr int kTeams = TEAMS, kTeamWarps = kWarps / TEAMS;
     extern __shared__ __align__(16) uint8_t smem[];
     __shared__ float2 meta_s[kWarps][2][kGroups][kRows];
     const int tok0 = blockIdx.y * kTok, tokens = min(kTok, p.tokens - tok0);   // of the block
@@ -219,14 +221,18 @@ __global__ void __launch_bounds__(kThreads, 1) w4_few_kernel(const __grid_consta
 #pragma unroll
         for (int e = 0; e < 4; ++e) part[tw][(e >> 1) * 8 + g][t * 2 + (e & 1)] = acc[e];
         named_sync(1 + team, kTeamWarps * 32);   // (the slab after the next waits here before it writes to this part again)
-        const int row = (slab0 + sl * slab_step) * kRows + (lane & 15), c = tw * 2 + (lane >> 4);
-        if (row < p.n && c < tokens) {
-            float y = 0.f;
+        const int row = (slab0 + sl * slab_step) * kRows + (lane & 15);
 #pragma unroll
-            for (int w = 0; w < kTeamWarps; ++w) y += part[w][lane & 15][c];
-            if (p.bias) y += to_float(static_cast<const T *>(p.bias)[row]);
-            if (p.add) y += to_float(static_cast<const T *>(p.add)[(tok0 + c) * p.add_stride + row]);
-            static_cast<T *>(p.y)[(tok0 + c) * p.y_stride + row] = from_float<T>(y);
+        for (int c0 = 0; c0 < kTok; c0 += 2 * kTeamWarps) {
+            const int c = c0 + tw * 2 + (lane >> 4);
+            if (row < p.n && c < tokens) {
+                float y = 0.f;
+#pragma unroll
+                for (int w = 0; w < kTeamWarps; ++w) y += part[w][lane & 15][c];
+                if (p.bias) y += to_float(static_cast<const T *>(p.bias)[row]);
+                if (p.add) y += to_float(static_cast<const T *>(p.add)[(tok0 + c) * p.add_stride + row]);
+                static_cast<T *>(p.y)[(tok0 + c) * p.y_stride + row] = from_float<T>(y);
+            }
         }
     }
     copy_wait<0>();
@@ -247,22 +253,30 @@ bool is_few(int n, int k, int groups, int tokens) {
     return tokens <= (n <= 74 * kRows ? 2 * kTok : kTok) && depth_of(k, groups, tokens) > 0;
 }
 
-template <typename T, int GROUP, int DEPTH>
+template <typename T, int GROUP, int DEPTH, int TEAMS>
 cudaError_t launch_few(const W4Params &p, int sms, cudaStream_t s) {
     const int tokens = p.tokens < kTok ? p.tokens : kTok;
     const FewLayout l(p.k, p.groups, tokens, DEPTH);
     static std::atomic<uint64_t> allowed{0};
-    const cudaError_t e = allow_shared(reinterpret_cast<const void *>(w4_few_kernel<T, GROUP, DEPTH>), kMostShared, allowed);
+    const cudaError_t e = allow_shared(reinterpret_cast<const void *>(w4_few_kernel<T, GROUP, DEPTH, TEAMS>), kMostShared, allowed);
     if (e != cudaSuccess) return e;
     const int slabs = (p.n + kRows - 1) / kRows;
     const dim3 grid(slabs < sms ? slabs : sms, (p.tokens + tokens - 1) / tokens);
-    return launch_after_producer(w4_few_kernel<T, GROUP, DEPTH>, grid, dim3(kThreads), (size_t)l.total, s, p);
+    return launch_after_producer(w4_few_kernel<T, GROUP, DEPTH, TEAMS>, grid, dim3(kThreads), (size_t)l.total, s, p);
+}
+// Two teams of eight warps where a block has up to three slabs, so that each is done sooner, and eight of two where it has more:
+// the joins at a slab's end then come after four times as many units of a warp.  Two against eight, one and eight tokens, us:
+// 3 584 x 14 336 14.0 against 16.9 (8 take the other kernel), 4 608 x 3 584 5.9 and 8.3 against 5.9 and 8.7, 9 472 x 3 584 8.8 and
+// 11.1 against 7.8 and 10.4, 28 672 x 3 584 18.8 and 21.5 against 16.7 and 18.9, 151 001 x 3 584 77 and 82 against 57 and 60.
+template <typename T, int GROUP, int DEPTH>
+cudaError_t by_teams(const W4Params &p, int sms, cudaStream_t s) {
+    return (p.n + kRows - 1) / kRows <= 3 * sms ? launch_few<T, GROUP, DEPTH, 2>(p, sms, s) : launch_few<T, GROUP, DEPTH, 8>(p, sms, s);
 }
 
 template <typename T, int GROUP>
 cudaError_t by_tokens(const W4Params &p, int sms, void *workspace, cudaStream_t s) {
     if (!is_few(p.n, p.k, p.groups, p.tokens)) return w4_many<T>(p, GROUP, sms, workspace, s);
-    return depth_of(p.k, p.groups, p.tokens) == 4 ? launch_few<T, GROUP, 4>(p, sms, s) : launch_few<T, GROUP, 3>(p, sms, s);
+    return depth_of(p.k, p.groups, p.tokens) == 4 ? by_teams<T, GROUP, 4>(p, sms, s) : by_teams<T, GROUP, 3>(p, sms, s);
 }
 
 template <typename T>

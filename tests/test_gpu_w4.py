@@ -93,6 +93,13 @@ def test_sizes(n, k, group, rows):
     _check(s, _call(s))
 
 
+@pytest.mark.parametrize("n,k,group", [(9472, 512, 32), (9473, 640, 128), (12001, 3584, 64), (30011, 384, 128)])
+@pytest.mark.parametrize("rows", [1, 3, 8])
+def test_matrices_of_many_rows(n, k, group, rows):
+    s = _make(rows, n, k, group, seed=rows + n)
+    _check(s, _call(s))
+
+
 @pytest.mark.parametrize("n", [1184, 1185])
 @pytest.mark.parametrize("rows", [8, 9, 16, 17])
 def test_where_one_kernel_takes_over_from_the_other(n, rows):
