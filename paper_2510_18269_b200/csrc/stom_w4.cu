@@ -245,12 +245,13 @@ int depth_of(int k, int groups, int tokens) {
     return 0;
 }
 // The few-tokens kernel takes up to 8, if they fit into shared memory, and up to 16 as twice 8 where the matrix has so few rows
-// that the blocks of both have a multiprocessor each (74 of 148).  Measured against the kernel for many, codes from memory, 3 584
-// columns, us: 8 tokens of 512 rows 6.7 against 13.5, of 4 608 rows 8.3 against 13.8, of 28 672 rows 22 against 36, of 151 001
-// rows 82 against 139; 9 to 16 tokens of 512 rows 6.6 to 6.9 against 13, of 4 608 rows 12.6 to 15.6 against 13.9, of 28 672 rows
-// 38 to 41 against 36, of 151 001 rows 160 against 140.
+// that the blocks of both have a multiprocessor each (74 of 148), or more than 12 slabs a block.  Measured against the kernel for
+// many, codes from memory, 3 584 columns, us: 8 tokens of 512 rows 6.7 against 13, of 4 608 rows 8.4 against 13.7, of 28 672 rows
+// 19 against 36, of 151 001 rows 60 against 139; 9 to 16 tokens of 512 rows 6.7 against 13, of 4 608 rows 12.6 to 15.6 against 13.9,
+// of 18 944 rows 23 to 26 against 22, of 28 672 rows 32 to 36 against 36, of 151 001 rows 113 to 117 against 140.
 bool is_few(int n, int k, int groups, int tokens) {
-    return tokens <= (n <= 74 * kRows ? 2 * kTok : kTok) && depth_of(k, groups, tokens) > 0;
+    const bool twice = n <= 74 * kRows || n > 12 * 148 * kRows;
+    return tokens <= (twice ? 2 * kTok : kTok) && depth_of(k, groups, tokens) > 0;
 }
 
 template <typename T, int GROUP, int DEPTH, int TEAMS>

@@ -94,7 +94,7 @@ def test_sizes(n, k, group, rows):
 
 
 @pytest.mark.parametrize("n,k,group", [(9472, 512, 32), (9473, 640, 128), (12001, 3584, 64), (30011, 384, 128)])
-@pytest.mark.parametrize("rows", [1, 3, 8])
+@pytest.mark.parametrize("rows", [1, 3, 8, 13, 16])
 def test_matrices_of_many_rows(n, k, group, rows):
     s = _make(rows, n, k, group, seed=rows + n)
     _check(s, _call(s))
