@@ -180,9 +180,10 @@ int32_t stom_kv_attend(const stom_kv_pool *pool, const stom_kv_seqs *seqs, int32
  * are none) gives zeros and -inf.
  * Keys and values of a token that a node does not see have no effect on it,
  * also where they are no finite numbers.  Products of 16-bit operands are
- * summed in binary32; a softmax weight enters the second product rounded to the
- * pool's type: off by 2^-8 of itself (bf16), or by 2^-11 of itself or 2^-32 of
- * the row's largest weight, whichever is more (fp16).
+ * summed in binary32; a softmax weight enters the second product as a high and a
+ * low part of the pool's type, as in stom_kv_attend: off by 2^-16 of itself (bf16),
+ * or by 2^-22 of itself or 2^-32 of the row's largest weight, whichever is more
+ * (fp16).
  * q, out (pool->dtype): element (row, h, c) at row*stride_token +
  * h*stride_head + c.  lse: binary32 [n_tokens][n_q_heads], or NULL.  The
  * limits are those of stom_kv_attend for softmax_scale, softcap, heads and

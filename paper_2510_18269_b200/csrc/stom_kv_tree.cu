@@ -16,12 +16,18 @@
 // values, each of them in the 128-byte-swizzled layout in which keys are a K-major operand (rows: tokens) and values an
 // MN-major one (rows: the summed axis).  One thread issues the products: S = Q K^T of tile t + 3 when the values' product
 // of tile t is done, O += P V from tensor memory.  Eight warps do the softmax, two groups in turn with the tiles, a thread with
-// one row: while one group waits, the other's exponentials run.  P takes the place of S in tensor memory, in 16 bits.
+// one row: while one group waits, the other's exponentials run.  P takes the place of S in tensor memory, as two 16-bit parts.
 //
 // The running maximum moves only when a row's scores rise by more than 2^8 above it: the weights then are at most 2^8 (no
 // loss: they are floating-point numbers, and bf16 has binary32's exponents; in fp16 the reference weight is 2^7, so that
 // they end at 2^15 and begin at 2^-24, 2^-31 of it), and the accumulators in tensor memory are rescaled once or twice a unit
-// instead of once a tile.  Weights are rounded once to the pool's type for the second product; their sum is taken before.
+// instead of once a tile.
+//
+// Weights enter the second product as a high and a low part of the pool's type (2^-16 of themselves off in bf16, 2^-22 in fp16
+// as long as the low part is above 2^-24): one part alone adds an error of the size of the output's own rounding (0.0023 of the
+// output's norm off instead of 0.0017 in bf16, 0.00026 instead of 0.00021 in fp16), and a step of several tokens would answer
+// less exactly than one of a single token over the same cache.  The parts of 32 tokens take their scores' 32 columns.  It costs
+// the second product again: one tree of 64 nodes 38.4 -> 40.2 us, 48 streams 188 -> 193 to 207, questions 317 to 340 -> 385 to 430.
 //
 // Masks.  Only tiles that reach the nodes, or a window's edge, are masked: 32 bits a row and 32 columns, from the range of
 // the context that the row sees and the bits of its path, which a row walks once per unit.  A product multiplies what a row
@@ -516,7 +522,11 @@ __global__ void __launch_bounds__(kThreads, 1) kv_tree_kernel(const __grid_const
                 const uint32_t vl = v_low + slot * (kHalf / 16), pl = tmem + S::kSAt + c % kSBufs * kTok;
                 const uint32_t more = !(fresh >> (c & 31) & 1u);
 #pragma unroll
-                for (int ks = 0; ks < kTok / 16; ++ks) umma_ts_low(tmem, pl + ks * 8, vl + ks * 128, idesc_o, more | (ks != 0));
+                for (int ks = 0; ks < kTok / 16; ++ks) {   // (high parts of 32 tokens' weights lie before their low ones)
+                    const uint32_t w = pl + (ks >> 1) * 32 + (ks & 1) * 8;
+                    umma_ts_low(tmem, w, vl + ks * 128, idesc_o, more | (ks != 0));
+                    umma_ts_low(tmem, w + 16, vl + ks * 128, idesc_o, 1);
+                }
                 umma_commit(bar(sh.empty[slot]));
                 umma_commit(bar(sh.pv_done[c & 1]));
                 if (c + kSBufs < n_tiles) live = wait(sh.pv_done[c & 1], c >> 1) && scores(c + kSBufs);   // its S takes P's place
@@ -605,16 +615,25 @@ __global__ void __launch_bounds__(kThreads, 1) kv_tree_kernel(const __grid_const
                         there[w] = mask & sh.tokens[c & 7][w];
                     }
                 }
-                // 64 columns of S, what is not seen as what never is the largest
-                auto load_scores = [&](int ch, float (&x)[64]) {
-                    tmem_load(s_at + ch * 64, x);
+                // 64 columns of S, or 32, what is not seen as what never is the largest
+                auto load_scores = [&](int ch, auto &x) {
+                    constexpr int n = sizeof(x) / 4;
+                    tmem_load(s_at + ch * n, x);
                     if (falls)
 #pragma unroll
-                        for (int i = 0; i < 64; ++i) x[i] = -x[i];
+                        for (int i = 0; i < n; ++i) x[i] = -x[i];
                     if (masked) {
-                        const uint32_t low = ch ? there[kTok / 32 - 2] : there[0], high = ch ? there[kTok / 32 - 1] : there[1];
+                        uint32_t see[2];
+                        if constexpr (n == 64) {
+                            see[0] = ch ? there[kTok / 32 - 2] : there[0];
+                            see[1] = ch ? there[kTok / 32 - 1] : there[1];
+                        } else {
+                            see[0] = there[0];
 #pragma unroll
-                        for (int i = 0; i < 64; ++i) x[i] = (i < 32 ? low : high) >> (i & 31) & 1u ? x[i] : -INFINITY;
+                            for (int w = 1; w < kTok / 32; ++w) see[0] = ch == w ? there[w] : see[0];
+                        }
+#pragma unroll
+                        for (int i = 0; i < n; ++i) x[i] = see[i / 32] >> (i & 31) & 1u ? x[i] : -INFINITY;
                     }
                 };
                 float top = -INFINITY;
@@ -682,35 +701,40 @@ __global__ void __launch_bounds__(kThreads, 1) kv_tree_kernel(const __grid_const
                     const bool fused = plain && fabsf(m_ref) < 65536.f;
                     const float by_one = fused ? s1 : 1.f;
                     const bool all_fused = __all_sync(~0u, fused || m_ref == -INFINITY) && plain;
-                    const uint64_t by = pair_of(by_one, by_one), less = pair_of(-one, -one);
+                    const uint64_t by = pair_of(by_one, by_one), less = pair_of(-one, -one), minus_one = pair_of(-1.f, -1.f);
                     uint64_t sum = 0, sum1 = 0;   // two numbers each
+                    // (32 columns at a time: for 64 there are too few registers, one tree of 64 nodes took 43.8 us instead of 40.2)
 #pragma unroll 1
-                    for (int ch = 0; ch < kTok / 64; ++ch) {
-                        float x[64];
+                    for (int ch = 0; ch < kTok / 32; ++ch) {
+                        float x[32];
                         load_scores(ch, x);
                         // (without branches of their own: 64 of those took 5.5 us a tile)
                         if constexpr (CAP) {
 #pragma unroll
-                            for (int i = 0; i < 64; ++i) {
+                            for (int i = 0; i < 32; ++i) {
                                 const float y = s2 * tanhf(x[i] * s1_abs);
                                 x[i] = x[i] > -INFINITY ? y : x[i];
                             }
                         } else if (!all_fused) {   // (with a cap in a kernel of its own, whose code the others' would have to pass)
 #pragma unroll
-                            for (int i = 0; i < 64; ++i) x[i] = !fused && x[i] > -INFINITY ? x[i] * s1_abs : x[i];
+                            for (int i = 0; i < 32; ++i) x[i] = !fused && x[i] > -INFINITY ? x[i] * s1_abs : x[i];
                         }
-                        uint32_t w[32];
+                        uint32_t w[16], rest[16];
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) {
-                            float a, b;
+                        for (int i = 0; i < 16; ++i) {
+                            float a, b, ha, hb;
                             parts_of(fma_pair(pair_of(x[2 * i], x[2 * i + 1]), by, less), a, b);
                             a = exp2_of(a);
                             b = exp2_of(b);
                             uint64_t &to = i & 1 ? sum1 : sum;
                             to = add_pair(to, pair_of(a, b));
                             w[i] = pack2<T>(a, b);
+                            unpack2<T>(w[i], ha, hb);
+                            parts_of(fma_pair(pair_of(ha, hb), minus_one, pair_of(a, b)), a, b);   // (exact)
+                            rest[i] = pack2<T>(a, b);
                         }
-                        tmem_store(s_at + ch * 32, w);   // (over columns that have been read: of this half, or of the first)
+                        tmem_store(s_at + ch * 32, w);   // over columns that have been read
+                        tmem_store(s_at + ch * 32 + 16, rest);
                     }
                     float la, lb;
                     parts_of(add_pair(sum, sum1), la, lb);
