@@ -21,7 +21,9 @@
 // The running maximum moves only when a row's scores rise by more than 2^8 above it: the weights then are at most 2^8 (no
 // loss: they are floating-point numbers, and bf16 has binary32's exponents; in fp16 the reference weight is 2^7, so that
 // they end at 2^15 and begin at 2^-24, 2^-31 of it), and the accumulators in tensor memory are rescaled once or twice a unit
-// instead of once a tile.
+// instead of once a tile.  In fp16 it follows falls of more than 2^8, too (down to 2^-48 of the row's largest, so that nothing
+// overflows): relative to the largest, weights would vanish where thousands of tokens count only in sum, beside one that stands
+// 15 nats above them.  So a weight's error is 2^-32 of the row's largest and 2^-24 of its own tile's at most.
 //
 // Weights enter the second product as a high and a low part of the pool's type (2^-16 of themselves off in bf16, 2^-22 in fp16
 // as long as the low part is above 2^-24): one part alone adds an error of the size of the output's own rounding (0.0023 of the
@@ -61,6 +63,8 @@ constexpr int kSBufs = 3;            // buffers of scores: one is multiplied, on
 constexpr int kUnits = 8;            // descriptions of units that are kept
 constexpr int kUnitCost = 2;          // what a unit's beginning and end take, in tiles
 constexpr float kSlack = 8.f;         // log2 of what weights may exceed 1 by
+constexpr float kFall = 8.f;          // fp16: log2 of what a tile's largest may be below the reference
+constexpr float kReach = 48.f;        // and of what the reference may be below the row's largest so far
 constexpr unsigned long long kWaitLimitNs = 1000000000ull;   // a wait that has taken 1 s ends the block
 
 // Of a unit that crosses a block's end, for the joining kernel
@@ -130,6 +134,7 @@ struct Shared {                       // beside the operands
     uint32_t tokens[8][4];            // per tile: which rows are tokens
     uint32_t dirty[2][4];             // per group: tokens of the tile with values that are no numbers
     float ref[2][kRows];              // per group: its last tile's reference
+    float most[2][kRows];             // and (fp16) the row's largest score up to there
     float sum[2][kRows];
     uint32_t path[kRows][kPathWords];
     int16_t parent[kUnits][STOM_KV_MAX_TREE];
@@ -688,8 +693,16 @@ __global__ void __launch_bounds__(kThreads, 1) kv_tree_kernel(const __grid_const
                 // the reference so far, from the group of the tile before; this tile's, to the group of the next
                 if (c > 0) sync_some(8 + group, kSoftThreads);
                 const float m_before = t > 0 ? sh.ref[group ^ 1][row] : -INFINITY;
-                const bool moves = top > m_before + kSlack || (m_before == -INFINITY && top > -INFINITY);
-                const float m_ref = moves ? top : m_before;
+                bool moves = top > m_before + kSlack || (m_before == -INFINITY && top > -INFINITY);
+                float m_ref = moves ? top : m_before;
+                if constexpr (kHalfType) {
+                    const float most = t > 0 ? fmaxf(top, sh.most[group ^ 1][row]) : top, low = fmaxf(top, most - kReach);
+                    sh.most[group][row] = most;
+                    if (top > -INFINITY && low < m_before - kFall) {
+                        moves = true;
+                        m_ref = low;
+                    }
+                }
                 sh.ref[group][row] = m_ref;
                 if (!dirty && c + 1 < n_tiles) arrive_some(8 + (group ^ 1), kSoftThreads);
                 if (m_own != m_ref) l *= exp2_of(m_own - m_ref);
