@@ -65,7 +65,8 @@ constexpr int kUnitCost = 2;          // what a unit's beginning and end take, i
 constexpr float kSlack = 8.f;         // log2 of what weights may exceed 1 by
 constexpr float kFall = 8.f;          // fp16: log2 of what a tile's largest may be below the reference
 constexpr float kReach = 48.f;        // and of what the reference may be below the row's largest so far
-constexpr unsigned long long kWaitLimitNs = 1000000000ull;   // a wait that has taken 1 s ends the block
+constexpr unsigned long long kWaitLimitNs = 1000000000ull;   // a wait that has taken 1 s fails, and with
+// it all later ones of the block: loads and products end there, the softmax goes on to its unit's end without waiting
 
 // Of a unit that crosses a block's end, for the joining kernel
 struct Open {
@@ -168,18 +169,6 @@ __device__ __forceinline__ void arrive_when_copied(uint32_t bar) {
 }
 __device__ __forceinline__ void sync_some(int id, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
 __device__ __forceinline__ void arrive_some(int id, int threads) { asm volatile("bar.arrive %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
-__device__ __forceinline__ bool any_of_some(int id, int threads, bool mine) {
-    uint32_t r;
-    asm volatile(
-        "{\n\t.reg .pred p, q;\n\t"
-        "setp.ne.b32 p, %1, 0;\n\t"
-        "bar.red.or.pred q, %2, %3, p;\n\t"
-        "selp.u32 %0, 1, 0, q;\n\t}"
-        : "=r"(r)
-        : "r"((uint32_t)mine), "r"(id), "r"(threads)
-        : "memory");
-    return r != 0;
-}
 __device__ __forceinline__ float exp2_of(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -789,7 +778,9 @@ __global__ void __launch_bounds__(kThreads, 1) kv_tree_kernel(const __grid_const
                                 for (uint32_t bits = sh.dirty[group][g] & sh.tokens[c & 7][g]; bits; bits &= bits - 1) {
                                     const int b = __ffs(bits) - 1, tok = t0 + g * 32 + b;
                                     const uint32_t pg = div_by(p.page, (uint32_t)tok);
-                                    const int id = p.table[u.seq * p.table_stride + pg];
+                                    // (behind the unit's end, or none: a block that has given up, whose bits are another tile's)
+                                    const int id = tok < u.end ? p.table[u.seq * p.table_stride + pg] : -1;
+                                    if ((uint32_t)id >= (uint32_t)p.n_pages) continue;
                                     const T *src = reinterpret_cast<const T *>(p.v) + id * p.stride_page +
                                                    (int64_t)(tok - (int)(pg * p.page.d)) * p.stride_token + u.head * p.stride_head + o;
 #pragma unroll

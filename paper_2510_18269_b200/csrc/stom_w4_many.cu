@@ -37,7 +37,8 @@ constexpr int kPitch = kChunkCols / 2 + 16, kChunkBytes = kRows * kPitch;   // a
 constexpr int kAStage = kRows * kStageCols * 2, kLeftCols = kStageCols / 2, kMostBStages = 6;
 constexpr int kMostShared = 226 * 1024;                   // dynamic shared memory of a block
 constexpr int kMaxBlocks = 256;                            // blocks of the grid the workspace has room for
-constexpr unsigned long long kWaitLimitNs = 1000000000ull;   // a wait that has taken 1 s ends the block
+constexpr unsigned long long kWaitLimitNs = 1000000000ull;   // a wait that has taken 1 s fails, and with it
+// all later ones of the block, which ends; sums go on to the end of their part without waiting
 
 // Bytes of a stage's operand of the tokens, factors and sums
 __host__ __device__ constexpr int stage_bytes(int group, int n) { return n * kStageCols * 2 + kStageCols / group * n * 8; }
@@ -240,6 +241,11 @@ __global__ void __launch_bounds__(kThreads, 1) w4_many_kernel(const __grid_const
                     again |= b.slot == 0;
                 }
             }
+            // copies on their way arrive before the block ends: each slot's last, of this round or of the one before
+            for (int i = 0; i < kBStages; ++i)
+                if ((i < b.slot || again) &&
+                    !mbar_wait_bounded(smem_u32(&b_full[i]), i < b.slot ? b.round : b.round ^ 1u, &never_word, kWaitLimitNs))
+                    *abort_flag = 1;
         }
     } else if (warp == kWorkWarps + 1) {
         // ---- products
@@ -271,13 +277,14 @@ __global__ void __launch_bounds__(kThreads, 1) w4_many_kernel(const __grid_const
         const uint8_t *from = smem + S::kOffCodes + row * kPitch + side * 32;
         Ring a, c;
         bool again = false;
-        for (int64_t at = begin; at < end;) {
+        bool live = true;
+        for (int64_t at = begin; at < end && live;) {
             const int n = part_at(p, at, end).n;
             at += n;
             for (int s = 0; s < n; ++s) {
-                if (!(s & 1)) wait(c_full[c.slot], c.round);
-                if (again) wait(done[a.slot], a.round ^ 1u);   // its products have read the operand that was there
-                __syncwarp();
+                const bool there = (s & 1) || wait(c_full[c.slot], c.round);
+                const bool left = !again || wait(done[a.slot], a.round ^ 1u);   // its products have read the operand that was there
+                if (!(live = __all_sync(~0u, there && left))) break;
                 const uint8_t *src = from + c.slot * kChunkBytes + (s & 1) * 64;
                 uint8_t *dst = to + a.slot * kAStage;
                 uint32_t w[8], o[32];
@@ -348,6 +355,7 @@ __global__ void __launch_bounds__(kThreads, 1) w4_many_kernel(const __grid_const
         Part next = part_at(p, begin, end);
         if (begin < end) load_meta(next, 0);
         for (int64_t at = begin; at < end;) {
+            if (any_of_some(1, kFoldThreads, *abort_flag != 0)) break;   // all leave together
             const Part part = next;
             at += part.n;
             if (at < end) next = part_at(p, at, end);
@@ -375,7 +383,7 @@ __global__ void __launch_bounds__(kThreads, 1) w4_many_kernel(const __grid_const
                     named_sync(1, kFoldThreads);
                 }
                 wait(b_full[b.slot], b.round);
-                wait(done[a.slot], a.round);   // (a wait that has failed: what is there is used, and the call flagged)
+                wait(done[a.slot], a.round);   // (one that has failed: what is there is used until the part's end, and the call flagged)
                 __syncwarp();
                 tc_fence_after_sync();
                 const float2 *meta = reinterpret_cast<const float2 *>(smem + S::kOffMeta + m_slot * S::kMeta) + (s & 1) * kGroups * S::kMetaRow + row;
