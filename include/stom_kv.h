@@ -213,7 +213,8 @@ int32_t stom_kv_attend_tree(const stom_kv_pool *pool, const stom_kv_seqs *seqs, 
  * A sequence without nodes keeps what it has: n_accepted 0, next -1; so does one
  * that stom_kv_attend_tree would skip, or (without parents too) with more than
  * STOM_KV_MAX_TREE nodes or tokens than its row has, and sets
- * STOM_FLAG_BAD_INDEX.  Page ids outside [0, n_pages) are skipped and set it too.
+ * STOM_FLAG_BAD_INDEX.  Page ids outside [0, n_pages) are skipped and set it too,
+ * and so does a parent outside -1 .. j - 1, which counts as -1.
  * Pages that nodes lie in must not be shared.  path, n_accepted and next may be
  * NULL.  Errors: INVALID_ARG, SHAPE, UNSUPPORTED, ALIGNMENT, CUDA. */
 int32_t stom_kv_accept(const stom_kv_pool *pool, const stom_kv_seqs *seqs, int32_t n_tokens, const int32_t *first,

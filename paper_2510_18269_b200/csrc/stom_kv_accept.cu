@@ -75,7 +75,8 @@ __global__ void __launch_bounds__(kThreads) kv_accept_kernel(const __grid_consta
         if (!good && p.flags && tid == 0) atomicOr(p.flags, STOM_FLAG_BAD_INDEX);
         if (tid < nodes) {
             if (p.path) p.path[a + tid] = tid < count ? kept[tid] : -1;
-            if (row_of[tid] < 0 && p.flags) atomicOr(p.flags, STOM_FLAG_BAD_INDEX);
+            // (a parent that is none counts as the context: the walk never finds it)
+            if ((row_of[tid] < 0 || parent[tid] < -1 || parent[tid] >= tid) && p.flags) atomicOr(p.flags, STOM_FLAG_BAD_INDEX);
         }
         if (tid == 0) {
             if (p.n_accepted) p.n_accepted[i] = count;
