@@ -24,7 +24,6 @@ struct AcceptParams {
     int32_t n_layers, n_pages, n_kv_heads, chunk_bits;   // 2^chunk_bits 16-byte chunks make a row
     FastDiv by_page, by_head;
     int32_t *table, *len, *refs;
-    int32_t max_pages;
     int64_t table_stride, room;
     int32_t n_tokens;
     const int32_t *first, *parent, *draft, *chosen;
@@ -169,7 +168,6 @@ extern "C" int32_t stom_kv_accept(const stom_kv_pool *pool, const stom_kv_seqs *
     p.table = seqs->table;
     p.len = seqs->len;
     p.refs = seqs->refs;
-    p.max_pages = seqs->max_pages;
     p.table_stride = seqs->table_stride;
     p.room = room;
     p.n_tokens = n_tokens;
