@@ -42,9 +42,12 @@ typedef struct stom_w4_matrix {
  * bias [n] (dtype) and add may be NULL; add may be y; x and y do not overlap.
  * STOM_FLAG_TIMEOUT in the optional dev_flags: a bounded wait inside a kernel
  * ran out, y is not to be used.
- * workspace: 128-byte aligned, of at least stom_w4_workspace_bytes() bytes (none
- * for few tokens); its contents do not matter, and it may be used by one call at
- * a time.  k <= 2^24, n < 2^23 - 127, rows <= 524 280.
+ * workspace: 128-byte aligned, of at least stom_w4_workspace_bytes() bytes, asked
+ * for with the same device current; its contents do not matter, and it may be used
+ * by one call at a time.  None is needed for few tokens, whose operands of all
+ * columns fit into a multiprocessor's shared memory: up to 8 (16 of the smallest
+ * and largest matrices) of 3 840 columns, 5 of 5 632, one of 17 408 in groups of
+ * 32, and of 4 096, 6 400 and 27 648 in groups of 128.  k <= 2^24, n < 2^23 - 127, rows <= 524 280.
  * Errors: INVALID_ARG, SHAPE, UNSUPPORTED, ALIGNMENT, WORKSPACE, CUDA. */
 int64_t stom_w4_workspace_bytes(const stom_w4_matrix *w, int32_t rows);
 int32_t stom_w4_linear(const stom_w4_matrix *w, int32_t dtype, int32_t rows, const void *x, int64_t x_stride,

@@ -245,12 +245,14 @@ int depth_of(int k, int groups, int tokens) {
     return 0;
 }
 // The few-tokens kernel takes up to 8, if they fit into shared memory, and up to 16 as twice 8 where the matrix has so few rows
-// that the blocks of both have a multiprocessor each (74 of 148), or more than 12 slabs a block.  Measured against the kernel for
+// that the blocks of both have a multiprocessor each, or more than 12 slabs a block (`sms` of them; 0: no device is known, and 8
+// is all that is sure).  Measured against the kernel for
 // many, codes from memory, 3 584 columns, us: 8 tokens of 512 rows 6.7 against 13, of 4 608 rows 8.4 against 13.7, of 28 672 rows
 // 19 against 36, of 151 001 rows 60 against 139; 9 to 16 tokens of 512 rows 6.7 against 13, of 4 608 rows 12.6 to 15.6 against 13.9,
 // of 18 944 rows 23 to 26 against 22, of 28 672 rows 32 to 36 against 36, of 151 001 rows 113 to 117 against 140.
-bool is_few(int n, int k, int groups, int tokens) {
-    const bool twice = n <= 74 * kRows || n > 12 * 148 * kRows;
+bool is_few(int n, int k, int groups, int tokens, int sms) {
+    const int slabs = (n + kRows - 1) / kRows;
+    const bool twice = sms > 0 && (slabs <= sms / 2 || slabs > 12 * sms);
     return tokens <= (twice ? 2 * kTok : kTok) && depth_of(k, groups, tokens) > 0;
 }
 
@@ -276,7 +278,7 @@ cudaError_t by_teams(const W4Params &p, int sms, cudaStream_t s) {
 
 template <typename T, int GROUP>
 cudaError_t by_tokens(const W4Params &p, int sms, void *workspace, cudaStream_t s) {
-    if (!is_few(p.n, p.k, p.groups, p.tokens)) return w4_many<T>(p, GROUP, sms, workspace, s);
+    if (!is_few(p.n, p.k, p.groups, p.tokens, sms)) return w4_many<T>(p, GROUP, sms, workspace, s);
     return depth_of(p.k, p.groups, p.tokens) == 4 ? by_teams<T, GROUP, 4>(p, sms, s) : by_teams<T, GROUP, 3>(p, sms, s);
 }
 
@@ -306,7 +308,7 @@ static int32_t check_matrix(const stom_w4_matrix *w, int32_t rows) {
 extern "C" int64_t stom_w4_workspace_bytes(const stom_w4_matrix *w, int32_t rows) {
     const int32_t rc = check_matrix(w, rows);
     if (rc) return rc;
-    return rows == 0 || is_few(w->n, w->k, w->k / w->group, rows) ? 0 : w4_many_workspace(w->k, w->group, rows);
+    return rows == 0 || is_few(w->n, w->k, w->k / w->group, rows, sm_count()) ? 0 : w4_many_workspace(w->k, w->group, rows);
 }
 
 extern "C" int32_t stom_w4_linear(const stom_w4_matrix *w, int32_t dtype, int32_t rows, const void *x, int64_t x_stride,

@@ -628,7 +628,8 @@ class W4Matrix:
 
 
 def stom_w4_workspace_bytes(w: W4Matrix, rows: int) -> int:
-    n = lib().stom_w4_workspace_bytes(w.ref, rows)
+    with torch.cuda.device(w.dev):   # (what is needed goes by the device's size)
+        n = lib().stom_w4_workspace_bytes(w.ref, rows)
     if n < 0:
         _check(int(n), "stom_w4_workspace_bytes")
     return int(n)
