@@ -36,8 +36,8 @@ typedef struct stom_w4_matrix {
  * rounded once to dtype.
  * x, add, y (dtype: STOM_BF16 | STOM_FP16): element (t, i) at t*stride + i; x
  * and its stride 16-byte aligned, the others any alignment of an element.
- * x values below 2^-22 (fp16) or 2^-25 (bf16) of the largest of their token and
- * group lose bits, 2^-36 of that at most; a token with a value that is no finite
+ * x values below 2^-24 (fp16) or 2^-27 (bf16) of the largest of their token and
+ * group may lose bits, 2^-35 of that at most; a token with a value that is no finite
  * number gives no finite numbers.
  * bias [n] (dtype) and add may be NULL; add may be y; x and y do not overlap.
  * STOM_FLAG_TIMEOUT in the optional dev_flags: a bounded wait inside a kernel

@@ -4,8 +4,9 @@
 // four bits higher up it is c * 2^-20, of equal spacing still.  So a word of 8 codes becomes four operand registers of two
 // codes each by one shift and four ANDs, without any offset that would have to be taken out of the sums again.
 // The tokens' values meet them in the same type: multiplied by the power of two that brings the largest of their group to
-// 2^14 .. 2^15, where codes stand higher by 2^-4 of it.  bf16 values keep all their bits, unless they are below 2^-25 of the
-// largest (their error is then at most 2^-39 of it), and fp16 values down to 2^-22 of it.  Products are exact, sums binary32.
+// 2^14 .. 2^15, where codes stand higher (every second column) by 2^-4 of it, so that it is at 2^10 at least.  A value keeps its
+// 8 (bf16) or 11 bits as long as the last of them is 2^-24, the smallest number, or more: down to 2^-27 or 2^-24 of the largest
+// (2^-31 and 2^-28 in the other columns).  Below, it is off by 2^-25, 2^-35 of the largest (2^-39), at most.  Products are exact, sums binary32.
 #pragma once
 
 #include "stom_internal.cuh"
