@@ -179,7 +179,8 @@ int32_t stom_kv_attend(const stom_kv_pool *pool, const stom_kv_seqs *seqs, int32
  * and what stom_kv_attend flags.  A node that sees nothing (all of its pages
  * are none) gives zeros and -inf.
  * Keys and values of a token that a node does not see have no effect on it,
- * also where they are no finite numbers.  Products of 16-bit operands are
+ * also where they are no finite numbers; a value that is none makes none of the
+ * same channel of what sees it.  Products of 16-bit operands are
  * summed in binary32; a softmax weight enters the second product as a high and a
  * low part of the pool's type, as in stom_kv_attend: off by 2^-16 of itself (bf16),
  * or by 2^-22 of itself or, where that is less, by 2^-32 of the row's largest
