@@ -183,8 +183,9 @@ int32_t stom_kv_attend(const stom_kv_pool *pool, const stom_kv_seqs *seqs, int32
  * same channel of what sees it.  Products of 16-bit operands are
  * summed in binary32; a softmax weight enters the second product as a high and a
  * low part of the pool's type, as in stom_kv_attend: off by 2^-16 of itself (bf16),
- * or by 2^-22 of itself or, where that is less, by 2^-32 of the row's largest
- * weight and 2^-24 of the largest among the 127 tokens on either side (fp16).
+ * or by 2^-22 of itself or the lesser of 2^-32 of the row's largest weight and
+ * 2^-24 of the largest among the 127 tokens on either side (but for 2^-80 of the
+ * row's), whichever is more (fp16).
  * q, out (pool->dtype): element (row, h, c) at row*stride_token +
  * h*stride_head + c.  lse: binary32 [n_tokens][n_q_heads], or NULL.  The
  * limits are those of stom_kv_attend for softmax_scale, softcap, heads and

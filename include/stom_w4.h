@@ -2,8 +2,9 @@
  * stom_w4.h -- products with 4-bit weights, on NVIDIA B200 (sm_100a); part of
  * libstom_oqm.so.  Conventions as in stom_kv.h.
  *
- * A pass over one or a few tokens reads every weight once and does little else:
- * with 4 bits a weight it is almost four times as fast as with 16.
+ * A pass over one or a few tokens reads every weight once and does little else,
+ * and a weight of 4 bits is a quarter of one of 16.  More than 64 tokens are taken
+ * 64 at a time.
  */
 #ifndef STOM_W4_H
 #define STOM_W4_H

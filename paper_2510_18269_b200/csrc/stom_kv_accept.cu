@@ -7,8 +7,9 @@
 // that no store touches a later step's source and all of a batch's loads may run ahead of its stores.  Page ids are read
 // before a cluster barrier, behind which the first block writes length, table and counts.
 //
-// What bounds it: latency (length and range, then pages and tree, then rows).  Measured, 28 layers, 4 heads of 128: one stream
-// with a tree of 64 nodes 9 us, 40 streams of 33 nodes 12 us (1 us of it the copies' bytes).
+// What bounds it: latency (length and range, then pages and tree, then rows).  Measured together with the stom_kv_reserve that
+// makes room for the nodes, 28 layers, 4 heads of 128: one stream with a tree of 64 nodes 9 to 10 us, 40 streams of 33 nodes 12
+// us (1 us of it the copies' bytes).
 #include "stom_kv.cuh"
 
 namespace stom {

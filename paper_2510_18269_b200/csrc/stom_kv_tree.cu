@@ -5,8 +5,10 @@
 // The query heads of a kv head and the nodes of a sequence together are the ROWS of two products with the same keys and
 // values: row r is node r / group, head r % group.  Rows are cut into tiles of 128, the height of a tcgen05 product, and a
 // UNIT is one (sequence, row tile, kv head).  What bounds it: a tile of 128 rows does 4 * 128 flops for every pair of a
-// key's and a value's elements that it reads, 256 flops a byte, about as many as the device has; up to one tile it is the
-// cache's bytes, beyond (many heads times nodes, a question's prefill) the products, and the exponentials beside them.
+// key's and a value's elements that it reads, 128 flops a byte, half of what the device's products take for a byte from memory
+// (1 640 TFLOP/s over 6.5 TB/s).  One tile of a kv head is bound by the cache's bytes; where several read the same keys (many
+// heads times nodes, a question's prefill), they come from L2, and the copies from there, the products and the exponentials share
+// the time.
 //
 // Split.  As for one new token, the work is one line of TILES of tokens (128, or 64 where head_dim is 256): sequence by
 // sequence, row tile by row tile, head by head.  Each block, one a multiprocessor, takes an equal, contiguous stretch of it;
@@ -29,20 +31,21 @@
 // as long as the low part is above 2^-24): one part alone adds an error of the size of the output's own rounding (0.0023 of the
 // output's norm off instead of 0.0017 in bf16, 0.00026 instead of 0.00021 in fp16), and a step of several tokens would answer
 // less exactly than one of a single token over the same cache.  The parts of 32 tokens take their scores' 32 columns.  It costs
-// the second product again: one tree of 64 nodes 38.4 -> 40.2 us, 48 streams 188 -> 193 to 207, questions 317 to 340 -> 385 to 430.
+// the second product again: one tree of 64 nodes 38.4 -> 40.2 us, 48 streams 188 -> 193 to 215, questions 317 to 350 -> 385 to 470.
 //
 // Masks.  Only tiles that reach the nodes, or a window's edge, are masked: 32 bits a row and 32 columns, from the range of
 // the context that the row sees and the bits of its path, which a row walks once per unit.  A product multiplies what a row
 // does not see by zero, which is not enough where it is no number: in such tiles the values are looked through, what is no
 // number is taken out, and put back afterwards in the rows that see it.
 //
-// Measured on one B200.  28 + 4 heads of 128, bf16, 12 583 tokens: five nodes 19 us, 64 nodes 38 us; 48 streams of 17 to 8 011
-// tokens with up to 33 nodes, 64 + 8 heads, fp16: 182 us (3.1 of 6.5 TB/s); questions of 201 to 1 201 tokens over three caches:
-// 350 to 375 us (0.65 PFLOP/s; the copies of keys and values, which every row tile reads again from L2, alone take 306).
-// Of the 38 us, 3 go to finding the place, 2.5 to page ids, tree and rows of q, 2 to the first keys' way, 1.3 to each of 11
-// tiles, 3 to the partial result, and the rest to launches and the second kernel.  A softmax group takes 2.6 us for a tile of its
-// own (0.4 until the scores are there, 0.6 for the maximum, 1.3 for the exponentials, 0.3 until the product before is done), of
-// which the exponentials' units are busy for 0.54; with one group instead of two the call took 48 us instead of 42.
+// Measured on one B200.  28 + 4 heads of 128, bf16, 12 583 tokens: five nodes 19.6 us, 64 nodes 40 us; 48 streams of 17 to 8 011
+// tokens with up to 33 nodes, 64 + 8 heads, fp16: 193 us, 205 to 215 when the device nears its power limit (2.6 to 2.9 of 6.5
+// TB/s); questions of 201 to 1 201 tokens over three caches: 385 to 470 us, likewise (0.5 to 0.6 PFLOP/s; the copies of keys and
+// values, which every row tile reads again from L2, alone take 306).  Of the 40 us, 3 go to finding the place, 2.5 to page ids,
+// tree and rows of q, 2 to the first keys' way, 1.45 to each of 11 tiles, 3 to the partial result, and the rest to launches and
+// the second kernel.  With weights of one part a softmax group took 2.6 us for a tile of its own (0.4 until the scores are there,
+// 0.6 for the maximum, 1.3 for the exponentials, 0.3 until the product before is done), of which the exponentials' units are busy
+// for 0.54; the second part adds 0.3.  With one group instead of two the call took 48 us instead of 42, then.
 #include "stom_kv.cuh"
 #include "stom_tensor.cuh"
 

@@ -11,8 +11,10 @@
 // tokens agree: lane (g, t) of a fragment takes the t-th word (8 codes) of a row's 32 columns, two products' worth.  All of
 // a product's columns lie in one group.
 //
-// Measured on one B200, us: one token of 4 608 x 3 584 5.0, of 28 672 x 3 584 in groups of 64 21 (2.7 of 6.5 TB/s), five of
-// 151 001 x 3 584 69 (4.2 TB/s).  What bounds it now is the issue of instructions, 120 that read, unpack and multiply for 4 096
+// Measured on one B200, us, called from Python with a few sets of inputs in turn (perf/more_operators.py; the smallest matrices
+// then come from L2): one token of 4 608 x 3 584 5.0, of 28 672 x 3 584 in groups of 64 21.5 (2.7 of 6.5 TB/s), five of
+// 151 001 x 3 584 67 to 70 (4.2 TB/s).  The comparisons below are of calls queued ahead on the device, codes from memory, groups
+// of 128 with offsets, bf16; there the same three take 5.7, 17.1 and 58.  What bounds it now is the issue of instructions, 120 that read, unpack and multiply for 4 096
 // weights and about as many for copies, scales and folding.  A ring of its own for every warp took one token from 74 to 30 us;
 // codes as subnormal numbers instead of unpacked ones, with offsets, five tokens' logits from 93 to 84; smaller teams from 84
 // to 69.
@@ -246,10 +248,15 @@ int depth_of(int k, int groups, int tokens) {
 }
 // The few-tokens kernel takes up to 8, if they fit into shared memory, and up to 16 as twice 8 where the matrix has so few rows
 // that the blocks of both have a multiprocessor each, or more than 12 slabs a block (`sms` of them; 0: no device is known, and 8
-// is all that is sure).  Measured against the kernel for
-// many, codes from memory, 3 584 columns, us: 8 tokens of 512 rows 6.7 against 13, of 4 608 rows 8.4 against 13.7, of 28 672 rows
-// 19 against 36, of 151 001 rows 60 against 139; 9 to 16 tokens of 512 rows 6.7 against 13, of 4 608 rows 12.6 to 15.6 against 13.9,
-// of 18 944 rows 23 to 26 against 22, of 28 672 rows 32 to 36 against 36, of 151 001 rows 113 to 117 against 140.
+// is all that is sure).  Measured against the kernel for many, us:
+//   rows            512          4 608            18 944           28 672           151 001
+//   3 584 columns: 8 tokens 6.6 / 12.7, 9.4 / 14.3, 15.1 / 23.1, 20.3 / 36.8, 61 / 142; 9 and 16 tokens
+//                   6.8, 6.7 / 12.7, 13.8, 17.4 / 14.4, 24.4, 28.5 / 23.2, 33.6, 37.8 / 37, 116, 125 / 143
+//   2 048 columns: 4.5 / 10.3, 6.2 / 11.6, 10.4 / 15.7, 13.5 / 25.0, 40 / 84;
+//                   4.5, 4.5 / 10.3, 9.5, 11.5 / 11.6, 17.0, 19.3 / 15.7, 22.6, 24.9 / 25.0, 74, 76 / 84
+//   1 024 columns: 3.4 / 10.1, 4.1 / 10.6, 6.6 / 10.9, 8.8 / 18.0, 25 / 46;
+//                   3.4, 3.4 / 10.1, 6.8, 7.6 / 10.6, 11.2, 12.1 / 10.9, 14.7, 15.7 / 18.0, 45, 46 / 46
+// (So with few columns twice 8 would also be ahead by up to 4 us in between.)
 bool is_few(int n, int k, int groups, int tokens, int sms) {
     const int slabs = (n + kRows - 1) / kRows;
     const bool twice = sms > 0 && (slabs <= sms / 2 || slabs > 12 * sms);
@@ -269,8 +276,8 @@ cudaError_t launch_few(const W4Params &p, int sms, cudaStream_t s) {
 }
 // Two teams of eight warps where a block has up to three slabs, so that each is done sooner, and eight of two where it has more:
 // the joins at a slab's end then come after four times as many units of a warp.  Two against eight, one and eight tokens, us:
-// 3 584 x 14 336 14.0 against 16.9 (8 take the other kernel), 4 608 x 3 584 5.9 and 8.3 against 5.9 and 8.7, 9 472 x 3 584 8.8 and
-// 11.1 against 7.8 and 10.4, 28 672 x 3 584 18.8 and 21.5 against 16.7 and 18.9, 151 001 x 3 584 77 and 82 against 57 and 60.
+// 3 584 x 14 336 14.1 against 17.4 (8 take the other kernel), 4 608 x 3 584 5.7 and 9.4 against 5.9 and 10.0, 9 472 x 3 584 8.8 and
+// 12.2 against 7.9 and 11.5, 28 672 x 3 584 18.9 and 22.9 against 17.0 and 20.3, 151 001 x 3 584 78 and 83 against 57 and 61.
 template <typename T, int GROUP, int DEPTH>
 cudaError_t by_teams(const W4Params &p, int sms, cudaStream_t s) {
     return (p.n + kRows - 1) / kRows <= 3 * sms ? launch_few<T, GROUP, DEPTH, 2>(p, sms, s) : launch_few<T, GROUP, DEPTH, 8>(p, sms, s);
