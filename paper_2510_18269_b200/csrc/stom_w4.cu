@@ -248,14 +248,17 @@ int depth_of(int k, int groups, int tokens) {
 }
 // The few-tokens kernel takes up to 8, if they fit into shared memory, and up to 16 as twice 8 where the matrix has so few rows
 // that the blocks of both have a multiprocessor each, or more than 12 slabs a block (`sms` of them; 0: no device is known, and 8
-// is all that is sure).  Measured against the kernel for many, us:
-//   rows            512          4 608            18 944           28 672           151 001
-//   3 584 columns: 8 tokens 6.6 / 12.7, 9.4 / 14.3, 15.1 / 23.1, 20.3 / 36.8, 61 / 142; 9 and 16 tokens
-//                   6.8, 6.7 / 12.7, 13.8, 17.4 / 14.4, 24.4, 28.5 / 23.2, 33.6, 37.8 / 37, 116, 125 / 143
-//   2 048 columns: 4.5 / 10.3, 6.2 / 11.6, 10.4 / 15.7, 13.5 / 25.0, 40 / 84;
-//                   4.5, 4.5 / 10.3, 9.5, 11.5 / 11.6, 17.0, 19.3 / 15.7, 22.6, 24.9 / 25.0, 74, 76 / 84
-//   1 024 columns: 3.4 / 10.1, 4.1 / 10.6, 6.6 / 10.9, 8.8 / 18.0, 25 / 46;
-//                   3.4, 3.4 / 10.1, 6.8, 7.6 / 10.6, 11.2, 12.1 / 10.9, 14.7, 15.7 / 18.0, 45, 46 / 46
+// is all that is sure).  Measured in us, this kernel (9 and 16 tokens: as twice 8 everywhere) and then the one for many:
+//   columns  tokens       512 rows         4 608        18 944        28 672       151 001
+//     3 584       8     6.6 / 12.7    9.4 / 14.3   15.1 / 23.1   20.3 / 36.8      61 / 142
+//     3 584       9     6.8 / 12.7   13.8 / 14.4   24.4 / 23.2   33.6 / 36.8     116 / 143
+//     3 584      16     6.7 / 12.7   17.4 / 14.5   28.5 / 23.3   37.8 / 37.1     125 / 143
+//     2 048       8     4.5 / 10.3    6.2 / 11.6   10.4 / 15.7   13.5 / 25.0       40 / 84
+//     2 048       9     4.5 / 10.3    9.5 / 11.6   17.0 / 15.7   22.6 / 25.0       74 / 85
+//     2 048      16     4.5 / 10.3   11.5 / 11.7   19.3 / 15.8   24.9 / 25.5       76 / 85
+//     1 024       8     3.4 / 10.1    4.1 / 10.6    6.6 / 10.9    8.8 / 18.0       25 / 46
+//     1 024       9     3.4 / 10.1    6.8 / 10.6   11.2 / 10.9   14.7 / 18.0       45 / 46
+//     1 024      16     3.4 / 10.2    7.6 / 10.9   12.1 / 11.0   15.7 / 18.4       46 / 47
 // (So with few columns twice 8 would also be ahead by up to 4 us in between.)
 bool is_few(int n, int k, int groups, int tokens, int sms) {
     const int slabs = (n + kRows - 1) / kRows;

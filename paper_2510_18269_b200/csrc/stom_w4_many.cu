@@ -241,7 +241,7 @@ __global__ void __launch_bounds__(kThreads, 1) w4_many_kernel(const __grid_const
                     again |= b.slot == 0;
                 }
             }
-            // copies on their way arrive before the block ends: each slot's last, of this round or of the one before
+            // copies on their way arrive before the block ends: each slot's last, of this turn of the ring or of the one before
             for (int i = 0; i < kBStages; ++i)
                 if ((i < b.slot || again) &&
                     !mbar_wait_bounded(smem_u32(&b_full[i]), i < b.slot ? b.round : b.round ^ 1u, &never_word, kWaitLimitNs))
